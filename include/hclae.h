@@ -359,6 +359,74 @@ int hclae_reorder_by_variance(hclae_ctx *ctx, int64_t N, int D, float *C, int M,
 int hclae_code_stats(hclae_ctx *ctx, const uint8_t *codes, int64_t N, int M, int K,
                      int64_t *hist, int a, int b, int64_t *joint);
 
+/* ---- vectors of a language model as codes: a cache of H heads, and rows of a table ---------------- */
+
+#define HCLAE_F32  0       /* type of caller's rows: float                                         */
+#define HCLAE_F16  1       /* IEEE half                                                            */
+#define HCLAE_BF16 2       /* bfloat16                                                             */
+
+#define HCLAE_MAX_H       1024                 /* heads of a cache                                    */
+#define HCLAE_CACHE_MAX_D 256                  /* longest row of a cache                              */
+#define HCLAE_MAX_SLOTS   ((int64_t)1 << 40)   /* rows of a code array: slots of a cache, rows of a table */
+
+/*
+ * A cache of keys and values kept as codes: every head has M dictionaries of its own, a row of a head is M bytes
+ * (and, if the caller keeps scales, one float).  hclae_cache_begin lays the dictionaries out for the calls below and
+ * keeps a copy of them in the ctx (2 H M K D floats, K rounded up to 64, 128 or 256 in one of the two; allocated by the first call and
+ * by one with more heads than any before, which may therefore not be recorded into a HIP graph).  After a change to C it is called again.
+ *   C: DEVICE float[H][M][K][D].  D <= HCLAE_CACHE_MAX_D.
+ * Layout of the cache (DEVICE, caller-owned): codes uint8[n_slots][H][M], scale float[n_slots][H].
+ */
+int hclae_cache_begin(hclae_ctx *ctx, const float *C, int H, int M, int K, int D);
+
+/*
+ * Quantises n new rows per head as they are written.  Row i of head h are the D elements of `type` from
+ * X + i * row_stride + h * head_stride (elements; multiples of 4, as X's alignment is of 4 elements).
+ * It goes to slot slots[i] (DEVICE int64[n]); a slot outside [0, n_slots) means that the row is not kept.  Slots of one
+ * call are distinct: where two rows name one slot its bytes are theirs in any mixture.  With g = max |x|:
+ *   u = x / g (x where scale is NULL; 0 where g is 0);  r <- u;
+ *   for m = 0..M-1:  codes[slot][h][m] = argmin_k ||r - C[h][m][k]||^2,  r <- r - c;   scale[slot][h] = g.
+ * The arithmetic is that of hclae_encode: r is held in fp32, distances are decided in their direct form in 64 bits,
+ * the lowest index of equals.  A row with a NaN or an infinity is kept as a row of zeros with scale NaN, and reads back as NaN
+ * (without scales as a row of zeros).  Slots that no row names are left as they are.  n <= N_max of hclae_create.  Only enqueues; uses no scratch.
+ */
+int hclae_cache_write(hclae_ctx *ctx, const void *X, int type, int64_t n, int64_t row_stride, int64_t head_stride,
+                      const int64_t *slots, int64_t n_slots, uint8_t *codes, float *scale);
+
+/*
+ * Reads rows of a cache back.  The cache is in pages of `page` slots (n_slots / page of them); sequence b of B has its rows
+ * in the pages tables[b][0], tables[b][1], ... (DEVICE int32[B][max_pages]) and gets rows starts[b] .. starts[b + 1] - 1 of
+ * out (DEVICE int32[B + 1], ascending from 0): row starts[b] + t of head h is
+ *   scale[s][h] * sum_m C[h][m][codes[s][h][m]],   s = tables[b][t / page] * page + t % page      (scale NULL: 1)
+ * summed in fp32 and rounded once to `type`.  A row whose page is not in the table or not in the cache is zero; rows of out
+ * before starts[0] and from starts[B] on are left as they are.  Codes of K or more are read as K - 1.  out's rows lie apart; strides as in
+ * hclae_cache_write.  n, the rows of out, <= N_max.  Only enqueues; uses no scratch.
+ */
+int hclae_cache_read(hclae_ctx *ctx, const uint8_t *codes, const float *scale, int64_t n_slots, const int32_t *tables, int B, int max_pages, int page,
+                     const int32_t *starts, int64_t n, void *out, int type, int64_t row_stride, int64_t head_stride);
+
+/*
+ * Rows of a table that is kept as codes (DEVICE uint8[V][M]), scaled: an embedding lookup, or with rows == NULL the decoding of
+ * rows 0 .. T-1 (then T <= V):
+ *   out[t] = factor * sum_m C[m][codes[rows[t]][m]]                      rows: DEVICE int64[T]
+ * summed in fp32 and rounded once to `type`.  A row number outside [0, V) stands for no row: its output is zero.  Codes of K or more
+ * are read as K - 1.  out: DEVICE, T rows of D elements, row_stride elements apart (>= D, a multiple of 4).  T <= N_max.
+ */
+int hclae_lookup(hclae_ctx *ctx, const int64_t *rows, int64_t T, const uint8_t *codes, int64_t V, float factor, const float *C, int M, int K, int D,
+                 void *out, int type, int64_t row_stride);
+
+/*
+ * The gradient of hclae_lookup with respect to the dictionaries, from that of its output (grad: DEVICE, T rows of D elements of
+ * `type`, row_stride elements apart):
+ *   dC[m][k] = factor * sum over the t with codes[rows[t]][m] == k of grad[t]          dC: DEVICE float[M][K][D]
+ * Every element of dC is written, with zero where no row has the codeword.  Row numbers outside [0, V) take no part.  Sums are in
+ * fp32 in an order fixed by the sizes and codes alone: equal calls give equal bits.  Beyond 4096 rows the first call allocates
+ * scratch for N_max rows (4 M N_max bytes and 4 KB per row of dC at most), which the ctx keeps, and may not be recorded into a HIP graph;
+ * two recorded calls of one ctx share that scratch and must not run at the same time.
+ */
+int hclae_lookup_grad(hclae_ctx *ctx, const int64_t *rows, int64_t T, const uint8_t *codes, int64_t V, float factor, const void *grad, int type,
+                      int64_t row_stride, int M, int K, int D, float *dC);
+
 /* ---- measurement: work done, and per-kernel durations from HIP events on the ctx's stream ------------- */
 
 /* Work since hclae_create or the last reset, counted on the device: out[0] = nearest-codeword assignments run

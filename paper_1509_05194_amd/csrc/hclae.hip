@@ -21,6 +21,9 @@
 #include "eigen.hpp"
 #include "stats.hpp"
 #include "beam.hpp"
+#include "cache_write.hpp"
+#include "decode.hpp"
+#include "lookup_grad.hpp"
 #include <algorithm>
 #include <vector>
 
@@ -156,6 +159,12 @@ struct hclae_ctx {
     float *beam_rows[2];     // [beam_cap][beam_L][D] residuals, ping-pong
     uint8_t *beam_pre[2];    // [beam_cap][beam_L][M] code prefixes
     BeamMask *beam_mask;     // [beam_cap][beam_L]
+    // coded cache: the dictionaries of its heads (hclae_cache_begin)
+    int cache_H;             // 0: none yet
+    float *cache_C;          // [H][M][K][D]
+    float4 *cache_T;         // [H][M][D / 4][few_columns(K)]
+    // sorted rows of hclae_lookup_grad (allocated on first use)
+    char *grad_buf;
     // optional per-kernel timing (HIP events on ctx->stream)
     uint32_t t_mask;
     int t_used;
@@ -1075,7 +1084,7 @@ int hclae_destroy(hclae_ctx *ctx)
                    ctx->r16_rows, ctx->r16_norm, ctx->r16_img, ctx->r16_sums, ctx->r16_negmu, ctx->r16_consts, ctx->r16_ref, ctx->r16_words,
                    ctx->carry_u, ctx->carry_l, ctx->carry_path, ctx->carry_snap, ctx->carry_Centry, ctx->carry_T, ctx->carry_amax,
                    ctx->beam_rows[0], ctx->beam_rows[1],
-                   ctx->beam_pre[0], ctx->beam_pre[1], ctx->beam_mask};
+                   ctx->beam_pre[0], ctx->beam_pre[1], ctx->beam_mask, ctx->cache_C, ctx->cache_T, ctx->grad_buf};
     for (void *p : dev)
         if (p) (void)hipFree(p);
     if (ctx->rec_host) (void)hipHostFree(ctx->rec_host);
@@ -1531,7 +1540,7 @@ int hclae_online_chunk(hclae_ctx *ctx, const uint8_t *Xu8, int64_t n, int D, flo
 static void beam_release(hclae_ctx *ctx)
 {
     void *dev[] = {ctx->beam_rows[0], ctx->beam_rows[1],
-                   ctx->beam_pre[0], ctx->beam_pre[1], ctx->beam_mask};
+                   ctx->beam_pre[0], ctx->beam_pre[1], ctx->beam_mask, ctx->cache_C, ctx->cache_T, ctx->grad_buf};
     for (void *p : dev)
         if (p) (void)hipFree(p);
     ctx->beam_rows[0] = ctx->beam_rows[1] = nullptr;
@@ -2091,6 +2100,244 @@ int hclae_code_stats(hclae_ctx *ctx, const uint8_t *codes, int64_t N, int M, int
     if (e == hipSuccess) e = hipStreamSynchronize(ctx->stream);
     if (e != hipSuccess) return fail(ctx, HCLAE_EHIP, "code statistics", e);
     return HCLAE_OK;
+}
+
+// ---- vectors of a language model as codes: a cache, and rows of a table -------------------------
+
+// The context's device while an entry point runs, whichever is the caller's.
+struct OnDevice {
+    int caller = -1;
+    hipError_t e;
+    explicit OnDevice(const hclae_ctx *ctx)
+    {
+        e = hipGetDevice(&caller);
+        if (e == hipSuccess && caller != ctx->device) e = hipSetDevice(ctx->device);
+        else caller = -1;
+    }
+    ~OnDevice()
+    {
+        if (caller >= 0) (void)hipSetDevice(caller);
+    }
+};
+#define ON_DEVICE(ctx)          \
+    const OnDevice device_(ctx); \
+    HIP_TRY(ctx, device_.e)
+
+// Rows of `type` in a caller's array: four elements at a time.
+static bool bad_rows(const void *p, int type, int64_t row_stride, int64_t head_stride)
+{
+    if (type != HCLAE_F32 && type != HCLAE_F16 && type != HCLAE_BF16) return true;
+    const uintptr_t align = type == HCLAE_F32 ? 16 : 8;
+    return reinterpret_cast<uintptr_t>(p) % align != 0 || row_stride < 0 || head_stride < 0 || row_stride % 4 != 0 || head_stride % 4 != 0;
+}
+
+// Whether rows of D elements, n of them for each of H heads, lie apart: heads inside a row or rows inside a head.
+static bool apart(int64_t n, int H, int D, int64_t row_stride, int64_t head_stride)
+{
+    if (n <= 1 && H <= 1) return true;
+    if (H <= 1) return row_stride >= D;
+    if (n <= 1) return head_stride >= D;
+    if (row_stride < D || head_stride < D) return false;
+    return (row_stride - D) / (H - 1) >= head_stride || (head_stride - D) / (n - 1) >= row_stride;
+}
+
+int hclae_cache_begin(hclae_ctx *ctx, const float *C, int H, int M, int K, int D)
+{
+    int rc = check_call(ctx, 0, D, M, K);
+    if (rc != HCLAE_OK) return rc;
+    if (!C || H < 1 || H > HCLAE_MAX_H) return fail(ctx, HCLAE_EINVAL, "hclae_cache_begin: bad argument");
+    if (D > HCLAE_CACHE_MAX_D) return fail(ctx, HCLAE_EINVAL, "hclae_cache_begin: D exceeds HCLAE_CACHE_MAX_D");
+    if (misaligned(C)) return fail(ctx, HCLAE_EINVAL, "hclae_cache_begin: C must be 16-byte aligned");
+    ON_DEVICE(ctx);
+    const size_t sets = (size_t)H * M;
+    const int columns = few_columns(K), d4 = D / 4;
+    if (H > ctx->cache_H) {
+        float *copy = nullptr;
+        float4 *T = nullptr;
+        hipError_t e = hipMalloc((void **)&copy, sets * K * D * sizeof(float));
+        if (e == hipSuccess) e = hipMalloc((void **)&T, sets * d4 * columns * sizeof(float4));
+        if (e != hipSuccess) {
+            if (copy) (void)hipFree(copy);
+            return fail(ctx, e == hipErrorOutOfMemory ? HCLAE_ENOMEM : HCLAE_EHIP, "hipMalloc (cache dictionaries)", e);
+        }
+        if (ctx->cache_C) (void)hipFree(ctx->cache_C);
+        if (ctx->cache_T) (void)hipFree(ctx->cache_T);
+        ctx->cache_C = copy;
+        ctx->cache_T = T;
+    }
+    ctx->cache_H = H;
+    hipLaunchKernelGGL(k_cache_lay, dim3((unsigned)sets, (unsigned)((d4 + 15) / 16)), dim3(256), 0, ctx->stream, C, K, D, columns, ctx->cache_C, ctx->cache_T);
+    HIP_TRY(ctx, hipGetLastError());
+    return HCLAE_OK;
+}
+
+extern "C++" {
+template <int COLS, int P, int R>
+static int launch_cache_write_few(hclae_ctx *ctx, const CacheRowsIn &a)
+{
+    const int64_t jobs = (a.n + R - 1) / R * a.H;
+    const int64_t blocks = jobs < (1 << 20) ? jobs : (1 << 20);
+    hipLaunchKernelGGL((k_cache_write_few<COLS, P, R>), dim3((unsigned)blocks), dim3(kFewThreads), 0, ctx->stream, a, ctx->cache_T);
+    HIP_TRY(ctx, hipGetLastError());
+    return HCLAE_OK;
+}
+template <int COLS, int P>
+static int launch_cache_write_rows(hclae_ctx *ctx, const CacheRowsIn &a)
+{
+    const int64_t items = a.n * a.H;
+    return items <= ctx->cus ? launch_cache_write_few<COLS, P, 1>(ctx, a) : launch_cache_write_few<COLS, P, 4>(ctx, a);
+}
+}  // extern "C++"
+
+int hclae_cache_write(hclae_ctx *ctx, const void *X, int type, int64_t n, int64_t row_stride, int64_t head_stride,
+                      const int64_t *slots, int64_t n_slots, uint8_t *codes, float *scale)
+{
+    if (!ctx) return HCLAE_EINVAL;
+    int rc = check_call(ctx, n, ctx->D, ctx->M, ctx->K);
+    if (rc != HCLAE_OK) return rc;
+    if (!ctx->cache_H) return fail(ctx, HCLAE_ESTATE, "hclae_cache_write before hclae_cache_begin");
+    if (n_slots < 0 || n_slots > HCLAE_MAX_SLOTS) return fail(ctx, HCLAE_EINVAL, "hclae_cache_write: n_slots out of range");
+    if (n == 0 || n_slots == 0) return HCLAE_OK;
+    if (!X || !slots || !codes) return fail(ctx, HCLAE_EINVAL, "hclae_cache_write: bad argument");
+    if (bad_rows(X, type, row_stride, head_stride)) return fail(ctx, HCLAE_EINVAL, "hclae_cache_write: type, alignment or strides of X");
+    ON_DEVICE(ctx);
+    const CacheRowsIn a = {X, type, row_stride, head_stride, slots, n, n_slots, codes, scale, ctx->cache_H, ctx->M, ctx->K, ctx->D};
+    const int D = ctx->D;
+    switch (few_columns(ctx->K)) {
+    case 64: return D <= 128 ? launch_cache_write_rows<64, 2>(ctx, a) : launch_cache_write_rows<64, 4>(ctx, a);
+    case 128: return D <= 128 ? launch_cache_write_rows<128, 4>(ctx, a) : launch_cache_write_rows<128, 8>(ctx, a);
+    default: return D <= 64 ? launch_cache_write_rows<256, 4>(ctx, a) : D <= 128 ? launch_cache_write_rows<256, 8>(ctx, a) : launch_cache_write_rows<256, 16>(ctx, a);
+    }
+}
+
+extern "C++" {
+template <typename T, typename Rows>
+static int launch_decode(hclae_ctx *ctx, const DecodeArgs &a, const Rows &rows)
+{
+    int lanes = 1;
+    while (lanes < a.D / 4 && lanes < kDecodeThreads) lanes *= 2;
+    const int per = kDecodeThreads / lanes;
+    const int64_t need = (a.n * a.H + per - 1) / per;
+    const unsigned parts = (unsigned)((a.D / 4 + kDecodeThreads - 1) / kDecodeThreads);
+    hipLaunchKernelGGL((k_decode_rows<T, Rows>), dim3((unsigned)(need < (1 << 20) ? need : (1 << 20)), parts), dim3(kDecodeThreads), 0, ctx->stream, a, rows, lanes);
+    HIP_TRY(ctx, hipGetLastError());
+    return HCLAE_OK;
+}
+template <typename Rows>
+static int launch_decode_type(hclae_ctx *ctx, int type, const DecodeArgs &a, const Rows &rows)
+{
+    return type == HCLAE_F32 ? launch_decode<F32>(ctx, a, rows) : type == HCLAE_F16 ? launch_decode<F16>(ctx, a, rows) : launch_decode<Bf16>(ctx, a, rows);
+}
+}  // extern "C++"
+
+int hclae_cache_read(hclae_ctx *ctx, const uint8_t *codes, const float *scale, int64_t n_slots, const int32_t *tables, int B, int max_pages, int page,
+                     const int32_t *starts, int64_t n, void *out, int type, int64_t row_stride, int64_t head_stride)
+{
+    if (!ctx) return HCLAE_EINVAL;
+    int rc = check_call(ctx, n, ctx->D, ctx->M, ctx->K);
+    if (rc != HCLAE_OK) return rc;
+    if (!ctx->cache_H) return fail(ctx, HCLAE_ESTATE, "hclae_cache_read before hclae_cache_begin");
+    if (n_slots < 0 || n_slots > HCLAE_MAX_SLOTS || B < 0 || max_pages < 0 || page < 1)
+        return fail(ctx, HCLAE_EINVAL, "hclae_cache_read: n_slots, B, max_pages or page out of range");
+    if (n == 0 || B == 0) return HCLAE_OK;
+    if (!starts || !out || (max_pages > 0 && !tables) || (n_slots > 0 && !codes)) return fail(ctx, HCLAE_EINVAL, "hclae_cache_read: bad argument");
+    if (bad_rows(out, type, row_stride, head_stride)) return fail(ctx, HCLAE_EINVAL, "hclae_cache_read: type, alignment or strides of out");
+    if (!apart(n, ctx->cache_H, ctx->D, row_stride, head_stride)) return fail(ctx, HCLAE_EINVAL, "hclae_cache_read: rows of out overlap");
+    ON_DEVICE(ctx);
+    const DecodeArgs a = {codes, scale, 1.f, ctx->cache_C, ctx->cache_H, ctx->M, ctx->K, ctx->D, n, out, row_stride, head_stride};
+    return launch_decode_type(ctx, type, a, CacheRows{tables, starts, B, max_pages, page, n_slots / page});
+}
+
+// What hclae_lookup and hclae_lookup_grad ask of their arguments alike.
+static int check_lookup(hclae_ctx *ctx, const char *name, const int64_t *rows, int64_t T, const uint8_t *codes, int64_t V, int M, int K, int D,
+                        const float *C, const void *x, int type, int64_t row_stride)
+{
+    int rc = check_call(ctx, T, D, M, K);
+    if (rc != HCLAE_OK) return rc;
+    if (V < 0 || V > HCLAE_MAX_SLOTS || (!rows && V < T)) return fail(ctx, HCLAE_EINVAL, name);
+    if (!C || misaligned(C)) return fail(ctx, HCLAE_EINVAL, name);
+    if (T == 0) return HCLAE_OK;
+    if (!x || (V > 0 && !codes) || bad_rows(x, type, row_stride, 0)) return fail(ctx, HCLAE_EINVAL, name);
+    return HCLAE_OK;
+}
+
+int hclae_lookup(hclae_ctx *ctx, const int64_t *rows, int64_t T, const uint8_t *codes, int64_t V, float factor, const float *C, int M, int K, int D,
+                 void *out, int type, int64_t row_stride)
+{
+    if (!ctx) return HCLAE_EINVAL;
+    if (T == 0) return check_call(ctx, T, D, M, K);
+    int rc = check_lookup(ctx, "hclae_lookup: bad argument (null, misaligned, type, stride, or fewer rows of codes than T)", rows, T, codes, V, M, K, D, C, out,
+                          type, row_stride);
+    if (rc != HCLAE_OK) return rc;
+    if (!apart(T, 1, D, row_stride, 0)) return fail(ctx, HCLAE_EINVAL, "hclae_lookup: rows of out overlap");
+    ON_DEVICE(ctx);
+    const DecodeArgs a = {codes, nullptr, factor, C, 1, M, K, D, T, out, row_stride, 0};
+    return launch_decode_type(ctx, type, a, TableRows{rows, V});
+}
+
+// Rows of one item of a sorted gradient: 128, or so many that a dictionary has about 512 items of several-item codewords.
+static int grad_chunk(int64_t T) { return (int)std::max<int64_t>(128, (T / 512 + kWave - 1) / kWave * kWave); }
+
+extern "C++" {
+template <typename T>
+static int launch_lookup_grad(hclae_ctx *ctx, const GradArgs &a)
+{
+    const int pieces = (a.D + Piece<T>::dims - 1) / Piece<T>::dims;
+    if (a.T <= kGradFew) {
+        int lanes = 1;
+        while (lanes < pieces && lanes < kWave) lanes *= 2;
+        const int parts = std::min(8, (pieces + kWave - 1) / kWave);
+        hipLaunchKernelGGL(k_grad_few<T>, dim3((unsigned)(a.M * a.K * parts)), dim3(kGradThreads), 0, ctx->stream, a, lanes, parts);
+        HIP_TRY(ctx, hipGetLastError());
+        return HCLAE_OK;
+    }
+    const size_t M = a.M, K = a.K, N = ctx->N_max;
+    const size_t ranges_max = (N + kSortRange - 1) / kSortRange, items_max = K + 512, parts_max = 1026;
+    const size_t counts_b = M * ranges_max * K * sizeof(unsigned), list_b = M * N * sizeof(int), items_b = M * items_max * sizeof(GradItem),
+                 buckets_b = M * K * sizeof(GradBucket), partial_b = M * parts_max * a.D * sizeof(float);
+    auto up = [](size_t b) { return (b + 255) / 256 * 256; };
+    if (!ctx->grad_buf) {
+        const hipError_t e = hipMalloc((void **)&ctx->grad_buf, up(counts_b) + up(list_b) + up(items_b) + up(buckets_b) + up(partial_b));
+        if (e != hipSuccess) return fail(ctx, e == hipErrorOutOfMemory ? HCLAE_ENOMEM : HCLAE_EHIP, "hipMalloc (sorted rows)", e);
+    }
+    SortArgs s;
+    char *p = ctx->grad_buf;
+    s.counts = reinterpret_cast<unsigned *>(p);
+    s.list = reinterpret_cast<int *>(p += up(counts_b));
+    s.items = reinterpret_cast<GradItem *>(p += up(list_b));
+    s.buckets = reinterpret_cast<GradBucket *>(p += up(items_b));
+    s.partial = reinterpret_cast<float *>(p += up(buckets_b));
+    s.ranges = (int)((a.T + kSortRange - 1) / kSortRange);
+    s.chunk = grad_chunk(a.T);
+    s.max_items = a.K + (int)(a.T / s.chunk);
+    s.max_parts = 2 * (int)(a.T / s.chunk) + 2;
+    const dim3 sort_grid((unsigned)s.ranges, (unsigned)((a.M + kSortGroup - 1) / kSortGroup));
+    hipLaunchKernelGGL(k_grad_count, sort_grid, dim3(kSortThreads), 0, ctx->stream, a, s);
+    HIP_TRY(ctx, hipGetLastError());
+    hipLaunchKernelGGL(k_grad_items, dim3((unsigned)a.M), dim3(256), 0, ctx->stream, a, s);
+    HIP_TRY(ctx, hipGetLastError());
+    hipLaunchKernelGGL(k_grad_place, sort_grid, dim3(kSortThreads), 0, ctx->stream, a, s);
+    HIP_TRY(ctx, hipGetLastError());
+    const int slices = (pieces + 7) / 8, side = std::min(slices, 8), waves = kGradThreads / kWave;
+    const int blocks = (a.M * s.max_items + waves - 1) / waves, rounds = (slices + side - 1) / side;
+    hipLaunchKernelGGL(k_grad_sums<T>, dim3((unsigned)(rounds * side * blocks)), dim3(kGradThreads), 0, ctx->stream, a, s, slices, blocks);
+    HIP_TRY(ctx, hipGetLastError());
+    hipLaunchKernelGGL(k_grad_join, dim3((unsigned)(a.M * a.K), (unsigned)((a.D / 4 + kGradThreads - 1) / kGradThreads)), dim3(kGradThreads), 0, ctx->stream, a, s);
+    HIP_TRY(ctx, hipGetLastError());
+    return HCLAE_OK;
+}
+}  // extern "C++"
+
+int hclae_lookup_grad(hclae_ctx *ctx, const int64_t *rows, int64_t T, const uint8_t *codes, int64_t V, float factor, const void *grad, int type,
+                      int64_t row_stride, int M, int K, int D, float *dC)
+{
+    if (!ctx) return HCLAE_EINVAL;
+    int rc = check_lookup(ctx, "hclae_lookup_grad: bad argument (null, misaligned, type, stride, or fewer rows of codes than T)", rows, T, codes, V, M, K, D, dC,
+                          grad, type, row_stride);
+    if (rc != HCLAE_OK) return rc;
+    ON_DEVICE(ctx);
+    const GradArgs a = {grad, row_stride, codes, {rows, V}, factor, M, K, D, T, dC};
+    return type == HCLAE_F16 ? launch_lookup_grad<F16>(ctx, a) : type == HCLAE_BF16 ? launch_lookup_grad<Bf16>(ctx, a) : launch_lookup_grad<F32>(ctx, a);
 }
 
 int hclae_timing_enable(hclae_ctx *ctx, uint32_t class_mask)

@@ -25,6 +25,7 @@ EXPORTS = (
     "hclae_covariance", "hclae_pca_axes", "hclae_symmetric_eigen", "hclae_rotate", "hclae_assign_prefix", "hclae_anneal_stage_pca", "hclae_dimension_schedule", "hclae_set_cooldown",
     "hclae_reorder_by_variance", "hclae_code_stats",
     "hclae_beam_step", "hclae_encode_beam", "hclae_set_beam_width", "hclae_set_contraction", "hclae_set_pruning",
+    "hclae_cache_begin", "hclae_cache_write", "hclae_cache_read", "hclae_lookup", "hclae_lookup_grad",
 )
 
 KERNEL_CLASSES = ("heat", "cool", "assign", "refine", "accumulate", "merge", "norms", "error", "transition",
@@ -104,6 +105,12 @@ def lib():
     L.hclae_set_beam_width.argtypes = [vp, i32]
     L.hclae_set_contraction.argtypes = [vp, i32]
     L.hclae_set_pruning.argtypes = [vp, i32]
+    f32 = ctypes.c_float
+    L.hclae_cache_begin.argtypes = [vp, vp, i32, i32, i32, i32]
+    L.hclae_cache_write.argtypes = [vp, vp, i32, i64, i64, i64, vp, i64, vp, vp]
+    L.hclae_cache_read.argtypes = [vp, vp, vp, i64, vp, i32, i32, i32, vp, i64, vp, i32, i64, i64]
+    L.hclae_lookup.argtypes = [vp, vp, i64, vp, i64, f32, vp, i32, i32, i32, vp, i32, i64]
+    L.hclae_lookup_grad.argtypes = [vp, vp, i64, vp, i64, f32, vp, i32, i64, i32, i32, i32, vp]
     L.hclae_timing_enable.argtypes = [vp, ctypes.c_uint32]
     L.hclae_timing_read.argtypes = [vp, ctypes.POINTER(KernelTimes)]
     for name in EXPORTS:
@@ -158,12 +165,25 @@ def _ptr(t, dtype_name, shape=None):
     if t is None:
         return None
     import torch
-    want = {"f32": torch.float32, "u8": torch.uint8, "i32": torch.int32, "f64": torch.float64}[dtype_name]
+    want = {"f32": torch.float32, "u8": torch.uint8, "i32": torch.int32, "f64": torch.float64, "i64": torch.int64}[dtype_name]
     if not (t.is_cuda and t.dtype == want and t.is_contiguous()):
         raise TypeError("expected a contiguous CUDA %s tensor" % dtype_name)
     if shape is not None and tuple(t.shape) != tuple(shape):
         raise ValueError("tensor shape %s, expected %s" % (tuple(t.shape), tuple(shape)))
     return ctypes.c_void_p(t.data_ptr())
+
+
+def _rows(t, shape):
+    """(device pointer, type, strides in elements) of rows of float32, float16 or bfloat16 whose elements lie side by side."""
+    import torch
+    kind = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}.get(t.dtype)
+    if not t.is_cuda or kind is None:
+        raise TypeError("expected a CUDA float32, float16 or bfloat16 tensor")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("tensor shape %s, expected %s" % (tuple(t.shape), tuple(shape)))
+    if t.numel() and t.stride(-1) != 1:
+        raise ValueError("the elements of a row must lie side by side")
+    return ctypes.c_void_p(t.data_ptr()), kind, t.stride()
 
 
 class Context:
@@ -394,6 +414,47 @@ class Context:
             idx.ctypes.data_as(ctypes.c_void_p) if idx is not None else None,
             ctypes.byref(stats) if want_stats else None))
         return stats.as_dict() if want_stats else None
+
+    # ---- vectors of a language model as codes ---------------------------------------------
+    def cache_begin(self, C):
+        """Lays out the dictionaries of a cache, C float32 [H][M][K][D]; called again after a change to them."""
+        H = C.shape[0]
+        self._chk(lib().hclae_cache_begin(self._h, _ptr(C, "f32", (H, self.M, self.K, self.D)), H, self.M, self.K, self.D))
+        self._H = H
+
+    def cache_write(self, X, slots, codes, scale=None):
+        """Quantises the rows X [n][H][D] (float32, float16 or bfloat16; rows and heads at any distance) into slots int64 [n] of
+        codes uint8 [n_slots][H][M] and scale float32 [n_slots][H] (None: rows are quantised as they are); a slot outside
+        [0, n_slots) keeps nothing."""
+        n, n_slots, H = X.shape[0], codes.shape[0], getattr(self, "_H", codes.shape[1])
+        p, kind, st = _rows(X, (n, H, self.D))
+        self._chk(lib().hclae_cache_write(self._h, p, kind, n, st[0], st[1], _ptr(slots, "i64", (n,)), n_slots,
+                                          _ptr(codes, "u8", (n_slots, H, self.M)), _ptr(scale, "f32", (n_slots, H))))
+
+    def cache_read(self, codes, scale, tables, starts, page, out):
+        """Reads the rows of B sequences back: pages tables int32 [B][max_pages], sequence b into rows starts[b]..starts[b + 1]
+        of out [n][H][D] (float32, float16 or bfloat16), starts int32 [B + 1]; other rows of out are left as they are."""
+        n, n_slots, H = out.shape[0], codes.shape[0], getattr(self, "_H", codes.shape[1])
+        B, max_pages = tables.shape
+        p, kind, st = _rows(out, (n, H, self.D))
+        self._chk(lib().hclae_cache_read(self._h, _ptr(codes, "u8", (n_slots, H, self.M)), _ptr(scale, "f32", (n_slots, H)),
+                                         n_slots, _ptr(tables, "i32"), B, max_pages, page, _ptr(starts, "i32", (B + 1,)), n, p, kind,
+                                         st[0], st[1]))
+
+    def lookup(self, codes, C, out, rows=None, scale=1.0):
+        """out[t] = scale * sum_m C[m][codes[rows[t]][m]] for a table kept as codes uint8 [V][M]; rows int64 [T], or None: rows
+        0..T-1.  out [T][D] float32, float16 or bfloat16, rows at any distance."""
+        T, V = out.shape[0], codes.shape[0]
+        p, kind, st = _rows(out, (T, self.D))
+        self._chk(lib().hclae_lookup(self._h, _ptr(rows, "i64", (T,)), T, _ptr(codes, "u8", (V, self.M)), V, scale,
+                                     _ptr(C, "f32", (self.M, self.K, self.D)), self.M, self.K, self.D, p, kind, st[0]))
+
+    def lookup_grad(self, codes, grad, dC, rows=None, scale=1.0):
+        """dC float32 [M][K][D], the gradient of lookup with respect to C, from that of its output, grad [T][D]."""
+        T, V = grad.shape[0], codes.shape[0]
+        p, kind, st = _rows(grad, (T, self.D))
+        self._chk(lib().hclae_lookup_grad(self._h, _ptr(rows, "i64", (T,)), T, _ptr(codes, "u8", (V, self.M)), V, scale, p, kind,
+                                          st[0], self.M, self.K, self.D, _ptr(dC, "f32", (self.M, self.K, self.D))))
 
     # ---- dictionary order and code statistics ---------------------------------------------
     def reorder_by_variance(self, C, codes):
