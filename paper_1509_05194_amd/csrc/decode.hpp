@@ -125,4 +125,205 @@ __global__ __launch_bounds__(kDecodeThreads) void k_decode_rows(const DecodeArgs
     }
 }
 
+
+// Many rows: a block keeps one slice of coordinates of all codewords of a head in LDS and takes rows through it.
+//
+// A half line of 128 bytes holds, for one k, the slice of S = 32 / G coordinates of G dictionaries, those of step i being i G .. i G + G - 1;
+// a line, the K of a pair of steps, one step in each half.  Eight lanes read a row, each 16 bytes at a place of its own
+// within the half lines; even rows read the two steps of a pair in one order, odd rows in the other.  Whatever the codes are, sixteen lanes so meet none
+// of the 64 banks twice.  The lanes of one coordinate and different dictionaries add up at the end (DPP).  G is the least that lets
+// all of it fit LDS (M = 8, K = 256: two).  A wave takes 64 rows at a time: it looks for them two rounds ahead, fetches their codes one round ahead and keeps
+// them in LDS of its own, so that no barriers are needed once the slice is there.
+constexpr int kSliceThreads = 1024;
+constexpr int kSliceMaxM = 32;                      // codes of a row travel in eight registers
+
+struct SliceLds {
+    int pairs;                                      // of steps, ceil(M / G) of which a code has
+    int fours;                                      // of steps
+    int zero, codes, factors, total;                // byte offsets: a line of zeros, [wave][64 rows][G][fours] four offsets, [wave][64]
+};
+__host__ __device__ constexpr SliceLds slice_lds(int M, int K, int G)
+{
+    SliceLds l = {};
+    l.pairs = ((M + G - 1) / G + 1) / 2;
+    l.fours = (l.pairs + 1) / 2;
+    l.zero = l.pairs * K * 256;
+    l.codes = l.zero + 256;
+    l.factors = l.codes + kSliceThreads * G * l.fours * 8;
+    l.total = l.factors + kSliceThreads * 4;
+    return l;
+}
+// The G of a shape, 0 where nothing fits `budget` bytes.  No wider slices than the rows are.
+__host__ __device__ constexpr int slice_dictionaries(int M, int K, int D, int budget)
+{
+    if (M > kSliceMaxM) return 0;
+    int G = 1;
+    while (G < 8 && 16 / G >= D) G *= 2;
+    for (; G <= 8; G *= 2)
+        if (slice_lds(M, K, G).total <= budget) return G;
+    return 0;
+}
+
+template <int CTRL>
+__device__ __forceinline__ float4 dpp_add(const float4 &v)
+{
+    auto from = [](float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true)); };
+    return make_float4(v.x + from(v.x), v.y + from(v.y), v.z + from(v.z), v.w + from(v.w));
+}
+
+// splits: parts of the rows; blocks with neighbouring slices of one part, which write neighbouring pieces of its rows, are on one XCD
+// (blocks go round the eight XCDs in order).  words_aligned: every row's codes are whole, aligned words.  ONE: four steps a code at most.
+template <typename T, typename Rows, int G, bool ONE>
+__global__ __launch_bounds__(kSliceThreads) void k_decode_slices(const DecodeArgs a, const Rows rows, int slices, int splits, bool words_aligned)
+{
+    extern __shared__ float4 smem4[];
+    char *lds = reinterpret_cast<char *>(smem4);
+    constexpr int LQ = 8 / G, S = 4 * LQ;           // lanes and coordinates of a codeword's slice
+    constexpr int NW = ONE ? G : kSliceMaxM / 4;    // words of a row's codes
+    const SliceLds L = slice_lds(a.M, a.K, G);
+    const unsigned jobs = (unsigned)(a.H * slices * splits), per_xcd = (jobs + 7) / 8, job = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+    if ((blockIdx.x >> 3) >= per_xcd || job >= jobs) return;
+    const int slice = (int)(job % (unsigned)slices), part = (int)(job / (unsigned)slices), h = part % a.H, split = part / a.H;
+    const int lane = lane_id(), wave = threadIdx.x >> 6;
+
+    // this wave's rows: 64 at a time
+    const int64_t rounds = (a.n + kWave - 1) / kWave, first = rounds * split / splits, last = rounds * (split + 1) / splits;
+    constexpr int waves = kSliceThreads / kWave;
+    int64_t round = first + wave;
+    const int nw = (a.M + 3) >> 2;
+    auto find = [&](int64_t r) {
+        const int64_t t = r * kWave + lane;
+        return r < last && t < a.n ? rows.at(t) : kSkip;
+    };
+    unsigned code[NW];
+    float factor;
+    auto fetch = [&](int64_t at) {
+        factor = a.factor;
+        if (at < 0) return;
+        const uint8_t *p = a.codes + (at * a.H + h) * a.M;
+        if (words_aligned) {
+#pragma unroll
+            for (int j = 0; j < NW; ++j) code[j] = reinterpret_cast<const unsigned *>(p)[min(j, nw - 1)];
+        } else {
+#pragma unroll
+            for (int j = 0; j < NW; ++j) {
+                unsigned b[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) b[i] = p[min(4 * j + i, a.M - 1)];
+                code[j] = b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24;
+            }
+        }
+        if (a.scale) factor = a.scale[at * a.H + h] * a.factor;
+    };
+    int64_t at = find(round), next = find(round + waves);
+    fetch(at);
+
+    // the slice
+    {
+        const float *C = a.C + (size_t)h * a.M * a.K * a.D;
+        const int total = (L.pairs * a.K + 1) * 16, pos = threadIdx.x & 7, odd = (threadIdx.x >> 3) & 1, g = pos / LQ, d = slice * S + 4 * (pos % LQ);
+        for (int i0 = threadIdx.x; i0 < total; i0 += 8 * kSliceThreads) {
+            float4 v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int line = (i0 + u * kSliceThreads) >> 4, i = line / a.K, k = line - i * a.K, m = (2 * i + odd) * G + g;
+                v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (m < a.M && i < L.pairs && d < a.D) v[u] = *reinterpret_cast<const float4 *>(C + ((size_t)m * a.K + k) * a.D + d);
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (i0 + u * kSliceThreads < total) smem4[i0 + u * kSliceThreads] = v[u];
+        }
+    }
+    __syncthreads();
+
+    // a lane's place: the lanes 4..7 of a row run backwards, so that the half mirror adds equal coordinates
+    const int l8 = lane & 7, lm = G > 1 && l8 >= 4 ? 7 - l8 : l8;
+    const int q = lm % LQ, g = lm / LQ + (G > 1 && l8 >= 4 ? G / 2 : 0);
+    const int my = (g * LQ + q) * 16 + (lane & 8) * 16, other = my ^ 128;      // in a line's half of the row's first and second step
+    const int d = slice * S + 4 * q, fours = ONE ? 1 : L.fours, row_fours = G * fours;
+    uint2 *offs = reinterpret_cast<uint2 *>(lds + L.codes) + wave * kWave * row_fours;
+    float *factors = reinterpret_cast<float *>(lds + L.factors) + wave * kWave;
+    const bool writes = d < a.D && (G == 1 || (l8 < 4 && l8 < LQ));
+    auto off_of = [&](int m) {                      // of a codeword within its lines
+        const unsigned c = (code[min(m >> 2, NW - 1)] >> (8 * (m & 3))) & 255u;
+        return at >= 0 && m < a.M ? min(c, (unsigned)a.K - 1u) * 256u : 0u;
+    };
+    // four steps, those beyond the last pair being zeros
+    auto four = [&](const uint2 &c, int w, float4 (&v)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int pair = 2 * w + (i >> 1), base = (i & 1 ? other : my) + (pair < L.pairs ? pair * a.K * 256 : L.zero);
+            const unsigned both = i < 2 ? c.x : c.y, off = i & 1 ? both >> 16 : both & 0xffffu;
+            v[i] = *reinterpret_cast<const float4 *>(lds + (base + off));
+        }
+    };
+    auto plus = [](const float4 &x, const float4 &y) { return make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w); };
+    for (; round < last; round += waves) {
+        // offsets and factors of these rows into LDS
+#pragma unroll
+        for (int w = 0; w < (ONE ? 1 : kSliceMaxM / 4); ++w)
+            if (ONE || w < fours) {
+#pragma unroll
+                for (int i = 0; i < G; ++i) {
+                    const unsigned o0 = off_of(4 * w * G + i), o1 = off_of((4 * w + 1) * G + i), o2 = off_of((4 * w + 2) * G + i), o3 = off_of((4 * w + 3) * G + i);
+                    offs[(lane * G + i) * fours + w] = lane & 1 ? make_uint2(o1 | o0 << 16, o3 | o2 << 16) : make_uint2(o0 | o1 << 16, o2 | o3 << 16);
+                }
+            }
+        factors[lane] = at >= 0 ? factor : 0.f;
+        const bool skips = __ballot(at == kSkip) != 0ull;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const unsigned long long kept = __ballot(at != kSkip);
+        fetch(next);
+        const int64_t after = find(round + 2 * waves);
+        char *to = static_cast<char *>(a.out) + ((round * kWave + (lane >> 3)) * a.row_stride + h * a.head_stride + d) * T::bytes;
+        const int64_t step = 8 * a.row_stride * T::bytes;
+        const float *factor8 = factors + (lane >> 3);
+        const uint2 *off8 = offs + (lane >> 3) * row_fours + g * fours;
+        constexpr int U = 4;                        // rows in flight (two: 10 % slower)
+#pragma unroll
+        for (int j0 = 0; j0 < 8; j0 += U) {
+            float f[U];
+            uint2 c[U];
+            float4 v[U][4], s[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                c[u] = off8[8 * (j0 + u) * row_fours];
+                f[u] = factor8[8 * (j0 + u)];
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) four(c[u], 0, v[u]);
+#pragma unroll
+            for (int u = 0; u < U; ++u) s[u] = plus(plus(v[u][0], v[u][1]), plus(v[u][2], v[u][3]));
+            if (!ONE)
+                for (int w = 1; w < fours; ++w) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) four(off8[8 * (j0 + u) * row_fours + w], w, v[u]);
+#pragma unroll
+                    for (int u = 0; u < U; ++u) s[u] = plus(s[u], plus(plus(v[u][0], v[u][1]), plus(v[u][2], v[u][3])));
+                }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (G == 8) s[u] = dpp_add<0xB1>(s[u]);     // quad_perm 1 0 3 2
+                if (G >= 4) s[u] = dpp_add<0x4E>(s[u]);     // quad_perm 2 3 0 1
+                if (G >= 2) s[u] = dpp_add<0x141>(s[u]);    // row_half_mirror
+                // times zero plus zero: a row that is not there is +0
+                s[u] = make_float4(fmaf(s[u].x, f[u], 0.f), fmaf(s[u].y, f[u], 0.f), fmaf(s[u].z, f[u], 0.f), fmaf(s[u].w, f[u], 0.f));
+            }
+            if (!skips) {
+                if (writes)
+#pragma unroll
+                    for (int u = 0; u < U; ++u) T::store(to + (j0 + u) * step, 0, s[u]);
+            } else {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (writes && (kept >> (8 * (j0 + u) + (lane >> 3)) & 1ull)) T::store(to + (j0 + u) * step, 0, s[u]);
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        at = next;
+        next = after;
+    }
+}
+
 }  // namespace hclae

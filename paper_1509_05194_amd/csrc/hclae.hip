@@ -163,6 +163,8 @@ struct hclae_ctx {
     int cache_H;             // 0: none yet
     float *cache_C;          // [H][M][K][D]
     float4 *cache_T;         // [H][M][D / 4][few_columns(K)]
+    char *cache_buf;         // sorted, as fp16 images and tables (CacheTables)
+    CacheTables cache_tab;
     // sorted rows of hclae_lookup_grad (allocated on first use)
     char *grad_buf;
     // optional per-kernel timing (HIP events on ctx->stream)
@@ -1084,7 +1086,7 @@ int hclae_destroy(hclae_ctx *ctx)
                    ctx->r16_rows, ctx->r16_norm, ctx->r16_img, ctx->r16_sums, ctx->r16_negmu, ctx->r16_consts, ctx->r16_ref, ctx->r16_words,
                    ctx->carry_u, ctx->carry_l, ctx->carry_path, ctx->carry_snap, ctx->carry_Centry, ctx->carry_T, ctx->carry_amax,
                    ctx->beam_rows[0], ctx->beam_rows[1],
-                   ctx->beam_pre[0], ctx->beam_pre[1], ctx->beam_mask, ctx->cache_C, ctx->cache_T, ctx->grad_buf};
+                   ctx->beam_pre[0], ctx->beam_pre[1], ctx->beam_mask, ctx->cache_C, ctx->cache_T, ctx->cache_buf, ctx->grad_buf};
     for (void *p : dev)
         if (p) (void)hipFree(p);
     if (ctx->rec_host) (void)hipHostFree(ctx->rec_host);
@@ -1540,7 +1542,7 @@ int hclae_online_chunk(hclae_ctx *ctx, const uint8_t *Xu8, int64_t n, int D, flo
 static void beam_release(hclae_ctx *ctx)
 {
     void *dev[] = {ctx->beam_rows[0], ctx->beam_rows[1],
-                   ctx->beam_pre[0], ctx->beam_pre[1], ctx->beam_mask, ctx->cache_C, ctx->cache_T, ctx->grad_buf};
+                   ctx->beam_pre[0], ctx->beam_pre[1], ctx->beam_mask, ctx->cache_C, ctx->cache_T, ctx->cache_buf, ctx->grad_buf};
     for (void *p : dev)
         if (p) (void)hipFree(p);
     ctx->beam_rows[0] = ctx->beam_rows[1] = nullptr;
@@ -2141,6 +2143,11 @@ static bool apart(int64_t n, int H, int D, int64_t row_stride, int64_t head_stri
     return (row_stride - D) / (H - 1) >= head_stride || (head_stride - D) / (n - 1) >= row_stride;
 }
 
+// 64-dim chunks of a cache's rows: 1, 2 or 4.
+static int cache_chunks(int D) { return D <= 64 ? 1 : D <= 128 ? 2 : 4; }
+// Rows of all heads up to which k_cache_write_few takes them.
+constexpr int64_t kFewRows = 2048;
+
 int hclae_cache_begin(hclae_ctx *ctx, const float *C, int H, int M, int K, int D)
 {
     int rc = check_call(ctx, 0, D, M, K);
@@ -2150,23 +2157,49 @@ int hclae_cache_begin(hclae_ctx *ctx, const float *C, int H, int M, int K, int D
     if (misaligned(C)) return fail(ctx, HCLAE_EINVAL, "hclae_cache_begin: C must be 16-byte aligned");
     ON_DEVICE(ctx);
     const size_t sets = (size_t)H * M;
-    const int columns = few_columns(K), d4 = D / 4;
+    const int columns = few_columns(K), d4 = D / 4, kb = ctx->kb, nc = cache_chunks(D), kpad = 32 * kb;
+    auto up = [](size_t b) { return (b + 255) / 256 * 256; };
+    const size_t img_b = sets * nc * kb * 4096, per_codeword_b = up(sets * kpad * sizeof(float)), mu_b = up(sets * kChunkD * nc * sizeof(float)),
+                 consts_b = up(sets * kEncodeConsts * sizeof(float)), w_b = up(sets * kb * sizeof(float)), order_b = sets * 256, C_b = up(sets * K * D * sizeof(float));
     if (H > ctx->cache_H) {
         float *copy = nullptr;
         float4 *T = nullptr;
-        hipError_t e = hipMalloc((void **)&copy, sets * K * D * sizeof(float));
+        char *buf = nullptr;
+        hipError_t e = hipMalloc((void **)&copy, C_b);
         if (e == hipSuccess) e = hipMalloc((void **)&T, sets * d4 * columns * sizeof(float4));
+        if (e == hipSuccess) e = hipMalloc((void **)&buf, img_b + 2 * per_codeword_b + mu_b + consts_b + w_b + order_b + C_b + 256);
         if (e != hipSuccess) {
             if (copy) (void)hipFree(copy);
+            if (T) (void)hipFree(T);
             return fail(ctx, e == hipErrorOutOfMemory ? HCLAE_ENOMEM : HCLAE_EHIP, "hipMalloc (cache dictionaries)", e);
         }
         if (ctx->cache_C) (void)hipFree(ctx->cache_C);
         if (ctx->cache_T) (void)hipFree(ctx->cache_T);
+        if (ctx->cache_buf) (void)hipFree(ctx->cache_buf);
         ctx->cache_C = copy;
         ctx->cache_T = T;
+        ctx->cache_buf = buf;
     }
     ctx->cache_H = H;
+    char *p = ctx->cache_buf;
+    char *img = p;
+    float *hn = reinterpret_cast<float *>(p += img_b);
+    float *wtab = reinterpret_cast<float *>(p += per_codeword_b);
+    float *negmu = reinterpret_cast<float *>(p += per_codeword_b);
+    float *consts = reinterpret_cast<float *>(p += mu_b);
+    float *w = reinterpret_cast<float *>(p += consts_b);
+    uint8_t *order = reinterpret_cast<uint8_t *>(p += w_b);
+    float *sorted = reinterpret_cast<float *>(p += order_b);
+    unsigned *unused = reinterpret_cast<unsigned *>(p += C_b);
+    ctx->cache_tab = {img, hn, w, negmu, consts, sorted, order};
     hipLaunchKernelGGL(k_cache_lay, dim3((unsigned)sets, (unsigned)((d4 + 15) / 16)), dim3(256), 0, ctx->stream, C, K, D, columns, ctx->cache_C, ctx->cache_T);
+    HIP_TRY(ctx, hipGetLastError());
+    hipLaunchKernelGGL(k_cache_sort, dim3((unsigned)sets), dim3(256), 0, ctx->stream, C, K, D, sorted, order);
+    HIP_TRY(ctx, hipGetLastError());
+    hipLaunchKernelGGL(k_encode_prep<false>, dim3((unsigned)sets), dim3(kPrepThreads), 0, ctx->stream, sorted, K, D, kb, nc, img, hn, wtab, negmu, consts,
+                       (float *)nullptr, unused);
+    HIP_TRY(ctx, hipGetLastError());
+    hipLaunchKernelGGL(k_cache_block_w, dim3((unsigned)((sets * kb + 7) / 8)), dim3(256), 0, ctx->stream, wtab, (int64_t)(sets * kb), w);
     HIP_TRY(ctx, hipGetLastError());
     return HCLAE_OK;
 }
@@ -2187,6 +2220,20 @@ static int launch_cache_write_rows(hclae_ctx *ctx, const CacheRowsIn &a)
     const int64_t items = a.n * a.H;
     return items <= ctx->cus ? launch_cache_write_few<COLS, P, 1>(ctx, a) : launch_cache_write_few<COLS, P, 4>(ctx, a);
 }
+
+template <int KB, int NC>
+static int launch_cache_write_tiles(hclae_ctx *ctx, const CacheRowsIn &a)
+{
+    constexpr int UNITS = KB * NC > 16 ? 2 : 1, WAVES = NC == 4 ? 4 : 8;
+    constexpr size_t lds = (size_t)tile_lds(KB / UNITS, NC, WAVES).total;
+    static_assert(lds <= (size_t)kLdsBudget, "a part and the next fit LDS");
+    auto kern = &k_cache_write_tiles<KB, NC, UNITS, WAVES>;
+    HIP_TRY(ctx, hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBudget));
+    const int64_t groups = (a.n + kTileVec * WAVES - 1) / (kTileVec * WAVES), per_xcd = (groups * a.H + 7) / 8, most = std::max(1, ctx->cus / 8);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(8 * std::min(per_xcd, most))), dim3(64 * WAVES), lds, ctx->stream, a, ctx->cache_tab, (int)groups);
+    HIP_TRY(ctx, hipGetLastError());
+    return HCLAE_OK;
+}
 }  // extern "C++"
 
 int hclae_cache_write(hclae_ctx *ctx, const void *X, int type, int64_t n, int64_t row_stride, int64_t head_stride,
@@ -2203,6 +2250,20 @@ int hclae_cache_write(hclae_ctx *ctx, const void *X, int type, int64_t n, int64_
     ON_DEVICE(ctx);
     const CacheRowsIn a = {X, type, row_stride, head_stride, slots, n, n_slots, codes, scale, ctx->cache_H, ctx->M, ctx->K, ctx->D};
     const int D = ctx->D;
+    if (n * a.H > kFewRows && (n / kTileVec + 1) * a.H < (int64_t)1 << 30) switch (cache_chunks(D) * 16 + ctx->kb) {
+        case 16 + 1: return launch_cache_write_tiles<1, 1>(ctx, a);
+        case 16 + 2: return launch_cache_write_tiles<2, 1>(ctx, a);
+        case 16 + 4: return launch_cache_write_tiles<4, 1>(ctx, a);
+        case 16 + 8: return launch_cache_write_tiles<8, 1>(ctx, a);
+        case 32 + 1: return launch_cache_write_tiles<1, 2>(ctx, a);
+        case 32 + 2: return launch_cache_write_tiles<2, 2>(ctx, a);
+        case 32 + 4: return launch_cache_write_tiles<4, 2>(ctx, a);
+        case 32 + 8: return launch_cache_write_tiles<8, 2>(ctx, a);
+        case 64 + 1: return launch_cache_write_tiles<1, 4>(ctx, a);
+        case 64 + 2: return launch_cache_write_tiles<2, 4>(ctx, a);
+        case 64 + 4: return launch_cache_write_tiles<4, 4>(ctx, a);
+        default: return launch_cache_write_tiles<8, 4>(ctx, a);
+        }
     switch (few_columns(ctx->K)) {
     case 64: return D <= 128 ? launch_cache_write_rows<64, 2>(ctx, a) : launch_cache_write_rows<64, 4>(ctx, a);
     case 128: return D <= 128 ? launch_cache_write_rows<128, 4>(ctx, a) : launch_cache_write_rows<128, 8>(ctx, a);
@@ -2223,10 +2284,57 @@ static int launch_decode(hclae_ctx *ctx, const DecodeArgs &a, const Rows &rows)
     HIP_TRY(ctx, hipGetLastError());
     return HCLAE_OK;
 }
+// How many parts the rows of a sliced decode are cut into, and what it then takes in microseconds (an estimate): every round of blocks
+// fills LDS, which costs about 6 us, and takes 64 rows in about 0.2 us.
+struct SliceCut {
+    int slices, splits;
+    double us;
+};
+static SliceCut slice_cut(const hclae_ctx *ctx, const DecodeArgs &a, int G)
+{
+    const int S = 32 / G, slices = (a.D + S - 1) / S;
+    const int64_t jobs = (int64_t)a.H * slices, rows64 = (a.n + 63) / 64;
+    SliceCut best = {slices, 1, 1e30};
+    for (int splits = 1; splits <= 64 && splits <= rows64; ++splits) {
+        const int64_t rounds = (jobs * splits + ctx->cus - 1) / ctx->cus;
+        const double us = (double)rounds * (6.0 + 0.2 * (double)((rows64 + splits - 1) / splits));
+        if (us < best.us) best = {slices, splits, us};
+    }
+    return best;
+}
+template <typename T, typename Rows, int G>
+static int launch_decode_slices(hclae_ctx *ctx, const DecodeArgs &a, const Rows &rows, const SliceCut &cut)
+{
+    auto kern = a.M <= 4 * G ? &k_decode_slices<T, Rows, G, true> : &k_decode_slices<T, Rows, G, false>;
+    HIP_TRY(ctx, hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBudget));
+    const int64_t jobs = (int64_t)a.H * cut.slices * cut.splits;
+    const bool words = a.M % 4 == 0 && reinterpret_cast<uintptr_t>(a.codes) % 4 == 0;
+    hipLaunchKernelGGL(kern, dim3((unsigned)((jobs + 7) / 8 * 8)), dim3(kSliceThreads), (size_t)slice_lds(a.M, a.K, G).total, ctx->stream, a, rows, cut.slices,
+                       cut.splits, words);
+    HIP_TRY(ctx, hipGetLastError());
+    return HCLAE_OK;
+}
+template <typename T, typename Rows>
+static int launch_decode_any(hclae_ctx *ctx, const DecodeArgs &a, const Rows &rows)
+{
+    const int G = slice_dictionaries(a.M, a.K, a.D, kLdsBudget);
+    if (G) {
+        const SliceCut cut = slice_cut(ctx, a, G);
+        // codewords from L2 at about 12 TB/s
+        const double direct = 4.0 + (double)a.n * a.H * a.M * a.D * 4.0 / 12e6;
+        if (cut.us < direct) switch (G) {
+            case 1: return launch_decode_slices<T, Rows, 1>(ctx, a, rows, cut);
+            case 2: return launch_decode_slices<T, Rows, 2>(ctx, a, rows, cut);
+            case 4: return launch_decode_slices<T, Rows, 4>(ctx, a, rows, cut);
+            default: return launch_decode_slices<T, Rows, 8>(ctx, a, rows, cut);
+            }
+    }
+    return launch_decode<T>(ctx, a, rows);
+}
 template <typename Rows>
 static int launch_decode_type(hclae_ctx *ctx, int type, const DecodeArgs &a, const Rows &rows)
 {
-    return type == HCLAE_F32 ? launch_decode<F32>(ctx, a, rows) : type == HCLAE_F16 ? launch_decode<F16>(ctx, a, rows) : launch_decode<Bf16>(ctx, a, rows);
+    return type == HCLAE_F32 ? launch_decode_any<F32>(ctx, a, rows) : type == HCLAE_F16 ? launch_decode_any<F16>(ctx, a, rows) : launch_decode_any<Bf16>(ctx, a, rows);
 }
 }  // extern "C++"
 

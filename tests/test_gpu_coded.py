@@ -63,6 +63,12 @@ WRITE = [
     (3, 2, 256, 3, 256, "bf16", True, "wide"), (33, 5, 80, 5, 200, "fp32", False, "heads"), (70, 3, 36, 4, 20, "fp16", True, "wide"),
     (130, 2, 132, 2, 130, "bf16", False, "tight"), (300, 1, 128, 4, 256, "bf16", True, "wide"), (65, 4, 192, 2, 64, "fp32", True, "heads"),
     (257, 2, 64, 3, 256, "fp32", False, "wide"), (515, 1, 124, 2, 100, "fp16", True, "heads"), (40, 16, 20, 2, 33, "bf16", True, "tight"),
+    # more rows, every size of dictionary and row
+    (2100, 1, 64, 2, 20, "bf16", True, "wide"), (1101, 2, 60, 2, 60, "fp16", True, "heads"), (2200, 1, 36, 2, 100, "fp32", False, "tight"),
+    (700, 3, 64, 2, 256, "bf16", True, "wide"), (2500, 1, 128, 2, 30, "fp32", True, "tight"), (1200, 2, 100, 2, 64, "bf16", True, "heads"),
+    (2300, 1, 128, 2, 128, "fp16", True, "wide"), (3001, 1, 128, 3, 256, "bf16", False, "tight"), (2100, 1, 200, 2, 32, "bf16", True, "wide"),
+    (1100, 2, 256, 2, 64, "fp32", False, "heads"), (2100, 1, 160, 2, 120, "fp16", True, "tight"), (700, 4, 256, 2, 256, "bf16", True, "wide"),
+    (2089, 1, 196, 2, 201, "fp32", True, "heads"), (2060, 1, 4, 2, 1, "fp32", True, "tight"), (301, 9, 12, 3, 2, "fp32", False, "tight"),
 ]
 
 
@@ -105,7 +111,7 @@ def test_write(n, H, D, M, K, kind, scaled, layout):
 
 
 @pytest.mark.parametrize("spread", [1e-30, 1e-18, 1e15, 1e30])
-@pytest.mark.parametrize("n,K,D", [(5, 256, 64), (200, 90, 128)])
+@pytest.mark.parametrize("n,K,D", [(5, 256, 64), (200, 90, 128), (1100, 256, 128), (1200, 70, 132)])
 def test_write_unusual_magnitudes(spread, n, K, D):
     """Rows quantised as they are, whose squares leave the range of fp32."""
     from paper_1509_05194_amd import hclae
@@ -113,6 +119,27 @@ def test_write_unusual_magnitudes(spread, n, K, D):
     ctx = hclae.Context(n, D, 2, K)
     ctx.cache_begin(torch.from_numpy(C).cuda())
     codes = torch.zeros((n, 2, 2), dtype=torch.uint8, device="cuda")
+    ctx.cache_write(torch.from_numpy(x).cuda(), torch.arange(n, device="cuda"), codes)
+    for h in range(2):
+        assert np.array_equal(codes[:, h].cpu().numpy(), quantise(x[:, h].copy(), C[h], False)[0])
+    ctx.close()
+
+
+@pytest.mark.parametrize("n,K,D,what", [(1500, 256, 128, "far"), (1500, 256, 128, "equal"), (1100, 200, 64, "zeros"), (1100, 64, 200, "equal"),
+                                        (1300, 256, 256, "far"), (60, 256, 128, "far"), (60, 256, 128, "equal"), (60, 70, 64, "zeros")])
+def test_write_with_many_near_ties(n, K, D, what):
+    """Rows far from the origin compared with what tells them apart, dictionaries of equal codewords, and of zeros."""
+    from paper_1509_05194_amd import hclae
+    x, C = heads(n, 2, D, 3, K, 8)
+    if what == "far":
+        x, C[:, 0] = x + np.float32(300), C[:, 0] + np.float32(300)
+    elif what == "equal":
+        C[:, 1] = C[:, 1, np.random.default_rng(0).integers(0, 5, K)]
+    else:
+        C[:, 1:] = 0
+    ctx = hclae.Context(n, D, 3, K)
+    ctx.cache_begin(torch.from_numpy(C).cuda())
+    codes = torch.zeros((n, 2, 3), dtype=torch.uint8, device="cuda")
     ctx.cache_write(torch.from_numpy(x).cuda(), torch.arange(n, device="cuda"), codes)
     for h in range(2):
         assert np.array_equal(codes[:, h].cpu().numpy(), quantise(x[:, h].copy(), C[h], False)[0])
