@@ -4,7 +4,6 @@
 //   for m = 0..M-1:  i_m = argmin_k ||r - c_m(k)||^2 (the direct form in 64 bits, the lowest index of equals),  r = r - c_m(i_m) in 32 bits,
 // which is the greedy encoding of Eq. 3 with one path on a row brought to a largest magnitude of one.
 #pragma once
-#include <type_traits>
 #include "assign_half.hpp"
 #include "decode.hpp"
 #include "encode.hpp"
@@ -216,16 +215,23 @@ __global__ __launch_bounds__(kFewThreads) void k_cache_write_few(const CacheRows
 
 // Many rows a head: scores from the fp16 matrix cores, a wave per tile of 32 rows of one head, through all its dictionaries, the
 // rows staying in registers.  Scores, their bounds and the margins are those of assign_half.hpp: score k is off by at most
-// e w_k + h, so that with L the largest of (score - e w) - h a codeword is a candidate while score + e w + h >= L.
-// Here w is one for all 32 codewords of a block, the largest: the codewords are laid out by ascending norm (k_cache_sort), so that it
-// is nearly each one's own.  L runs along with the blocks: the candidates of a block are those that reach the L of that
-// time, and blocks whose best does not reach the last L drop out at the end.  No score is kept beyond its block.
+// e w_k + margin, so that with L the largest of (score - e w) a codeword is a candidate while score + e w_k >= L - 2 margin.
+// For L the largest w of a block of 32 codewords stands for each one's: the codewords are laid out by ascending norm (k_cache_sort), so that
+// it nearly is.  L runs along with the blocks: the candidates of two blocks are those that reach the L of that time, and blocks whose
+// best does not reach the last L drop out at the end, so that no score is kept beyond its blocks (64 registers less than keeping
+// all of them).  One candidate is the nearest codeword; two or more are decided in fp32 in their direct form, or in 64 bits.
+//
+// Coordinates are laid out so that a lane's eight of a matrix instruction lie side by side in memory: position 16 t + 4 i .. + 3
+// holds the coordinates 16 t + 4 j .. + 3 with j = 0, 2, 1, 3 for i = 0, 1, 2, 3.
 struct CacheTables {
     const char *img;                                // [H M] as k_encode_prep lays them out, of the sorted codewords
-    const float *hn, *w, *negmu, *consts;           // w: [H M][KB], the largest of each block's
-    const float *C;                                 // [H][M][K][D] sorted
+    const float *hn, *negmu, *consts;
+    const unsigned *pairs;                          // [H M][32 KB] fp16 {2^-10, w_k}
+    const float *w;                                 // [H M][KB] the largest w of a block
+    const float *C;                                 // [H M][K][Dp] sorted, positions in place of coordinates, zero beyond D
     const uint8_t *order;                           // [H M][256]: the codeword at a place
 };
+__host__ __device__ constexpr int cache_padded(int D) { return (D + 15) / 16 * 16; }
 
 // Codewords in ascending order of their distance from the mean of a few, equal ones by index.  A block per dictionary.
 __global__ __launch_bounds__(256) void k_cache_sort(const float *__restrict__ C, int K, int D, float *__restrict__ sorted, uint8_t *__restrict__ order)
@@ -233,12 +239,13 @@ __global__ __launch_bounds__(256) void k_cache_sort(const float *__restrict__ C,
     __shared__ float norm[256];
     __shared__ uint8_t at[256];
     const float *Cm = C + (size_t)blockIdx.x * K * D;
-    const int lane = lane_id(), wave = threadIdx.x >> 6, d4 = D >> 2;
+    const int lane = lane_id(), wave = threadIdx.x >> 6, tid = threadIdx.x;
     float4 mu = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int i = 0; i < kMuRows; ++i) {
         const float4 v = load_row_piece(Cm, (int)((unsigned)(i * K) / kMuRows), 4 * lane, K, D, D);
         mu = make_float4(mu.x + v.x / kMuRows, mu.y + v.y / kMuRows, mu.z + v.z / kMuRows, mu.w + v.w / kMuRows);
     }
+    at[tid] = 0;
     for (int k = wave; k < K; k += 4) {
         const float4 v = load_row_piece(Cm, k, 4 * lane, K, D, D);
         const float a = v.x - mu.x, b = v.y - mu.y, c = v.z - mu.z, d = v.w - mu.w;
@@ -248,73 +255,78 @@ __global__ __launch_bounds__(256) void k_cache_sort(const float *__restrict__ C,
         if (lane == 0) norm[k] = s;
     }
     __syncthreads();
-    if ((int)threadIdx.x < K) {
-        const float mine = norm[threadIdx.x];
+    if (tid < K) {
+        const float mine = norm[tid];
         int rank = 0;
-        for (int k = 0; k < K; ++k) rank += norm[k] < mine || (!(norm[k] > mine) && k < (int)threadIdx.x) ? 1 : 0;
-        rank = min(rank, K - 1);                    // codewords that are no numbers
-        at[rank] = (uint8_t)threadIdx.x;
+        for (int k = 0; k < K; ++k) rank += norm[k] < mine || (!(norm[k] > mine) && k < tid) ? 1 : 0;
+        at[min(rank, K - 1)] = (uint8_t)tid;        // the minimum for codewords that are no numbers
     }
     __syncthreads();
-    if ((int)threadIdx.x < 256) order[(size_t)blockIdx.x * 256 + threadIdx.x] = (int)threadIdx.x < K ? at[threadIdx.x] : 0;
-    for (int i = threadIdx.x; i < K * d4; i += 256) {
-        const int k = i / d4, p = i - k * d4;
-        reinterpret_cast<float4 *>(sorted + (size_t)blockIdx.x * K * D)[i] = reinterpret_cast<const float4 *>(Cm + (size_t)min((int)at[k], K - 1) * D)[p];
+    order[(size_t)blockIdx.x * 256 + tid] = at[tid];
+    const int Dp = cache_padded(D), d4 = Dp >> 2;
+    for (int i = tid; i < K * d4; i += 256) {
+        const int k = i / d4, p = i - k * d4, piece = (p & ~3) | (p & 1) << 1 | (p & 2) >> 1;
+        reinterpret_cast<float4 *>(sorted + (size_t)blockIdx.x * K * Dp)[i] = load_row_piece(Cm, at[k], 4 * piece, K, D, D);
     }
 }
 
-// The largest w of every block of 32 codewords (wtab: [blocks][32]).
-__global__ __launch_bounds__(256) void k_cache_block_w(const float *__restrict__ wtab, int64_t blocks, float *__restrict__ w)
+// From wtab [blocks][32]: the pairs, and the largest w of every block.
+__global__ __launch_bounds__(256) void k_cache_w(const float *__restrict__ wtab, int64_t blocks, unsigned *__restrict__ pairs, float *__restrict__ w)
 {
     const int64_t b = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     float v = b < blocks ? wtab[b * 32 + (threadIdx.x & 31)] : 0.f;
+    if (b < blocks) pairs[b * 32 + (threadIdx.x & 31)] = __builtin_bit_cast(unsigned, (halfx2){(_Float16)0.0009765625f, (_Float16)v});
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, kWave));
     if (b < blocks && (threadIdx.x & 31) == 0) w[b] = v;
 }
 
-// LDS of k_cache_write_tiles: a dictionary (or half of one) and the next, and what undecided rows are decided in.
+// LDS of k_cache_write_tiles: a dictionary (or half of one), and a stretch for every wave: four undecided rows, or a piece of 16 positions of the
+// codewords to subtract.
 constexpr int kTileBatch = 4;                       // undecided rows of a wave at a time, sixteen lanes each
 struct TileLds {
     int unit;                                       // bytes of an image
-    int img, hn, mu, w, rows, masks, total;  // byte offsets; all but the last two of them twice
+    int img, hn, pairs, mu, w, rows, masks, total;  // byte offsets
+    int stretch;
 };
 __host__ __device__ constexpr TileLds tile_lds(int kbu, int nc, int waves)
 {
     TileLds l = {};
     l.unit = kbu * nc * 4096;
+    l.stretch = nc == 4 ? 4096 : 2048;
     l.img = 0;
-    l.hn = 2 * l.unit;
-    l.mu = l.hn + 2 * 128 * kbu;
-    l.w = l.mu + 2 * 256 * nc;
-    l.rows = l.w + 2 * 32;
-    l.masks = l.rows + waves * kTileBatch * 256 * nc;
+    l.hn = l.unit;
+    l.pairs = l.hn + 128 * kbu;
+    l.mu = l.pairs + 128 * kbu;
+    l.w = l.mu + 256 * nc;
+    l.rows = l.w + 32;
+    l.masks = l.rows + waves * l.stretch;
     l.total = l.masks + waves * kTileBatch * 32;
     return l;
 }
 
+template <int CTRL>
+__device__ __forceinline__ float dpp_plus(float v)
+{
+    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
 // The sum over the sixteen lanes of a row, the same in all of them.
 __device__ __forceinline__ float sum16(float v)
 {
-    auto from = [](float x, auto c) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(c)::value, 0xf, 0xf, true)); };
-    v += from(v, std::integral_constant<int, 0xB1>());     // quad_perm 1 0 3 2
-    v += from(v, std::integral_constant<int, 0x4E>());     // quad_perm 2 3 0 1
-    v += from(v, std::integral_constant<int, 0x141>());    // row_half_mirror
-    v += from(v, std::integral_constant<int, 0x140>());    // row_mirror
-    return v;
+    return dpp_plus<0x140>(dpp_plus<0x141>(dpp_plus<0x4E>(dpp_plus<0xB1>(v))));     // quad_perm 1 0 3 2, 2 3 0 1, row_half_mirror, row_mirror
 }
 
-// KB: blocks of 32 codewords.  NC: 64-dim chunks (1, 2 or 4).  UNITS: parts in which a dictionary passes through LDS.
+// KB: blocks of 32 codewords.  NC: 64-position chunks (1, 2 or 4).  UNITS: parts in which a dictionary passes through LDS.
 template <int KB, int NC, int UNITS, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void k_cache_write_tiles(const CacheRowsIn a, const CacheTables tab, int groups)
+__global__ __launch_bounds__(64 * WAVES, NC == 4 ? 1 : 2) void k_cache_write_tiles(const CacheRowsIn a, const CacheTables tab, int groups)
 {
     extern __shared__ float4 smem4[];
     char *lds = reinterpret_cast<char *>(smem4);
-    constexpr int KBU = KB / UNITS, T = 4 * NC, S = 8 * NC;
+    constexpr int KBU = KB / UNITS, T = 4 * NC, S = 8 * NC, W = (KB + 1) / 2;
     constexpr TileLds L = tile_lds(KBU, NC, WAVES);
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5, r = lane & 31;
     const float inf = __builtin_inff();
-    const int D = a.D;
+    const int D = a.D, Dp = cache_padded(D);
     // blocks go round the XCDs: neighbouring groups of tiles, of one head, to one of them
     const int jobs = groups * a.H, per_xcd = (jobs + 7) / 8;
     const int stride = gridDim.x >> 3, mine0 = blockIdx.x >> 3;
@@ -323,43 +335,56 @@ __global__ __launch_bounds__(64 * WAVES) void k_cache_write_tiles(const CacheRow
         const int job = (int)(blockIdx.x & 7) * per_xcd + j;
         return j < per_xcd && job < jobs ? job : -1;
     };
-    // part u of dictionary `set` into a half of LDS, all waves together
-    auto stage = [&](int set, int u, int half) {
-        const char *from = tab.img + (size_t)set * UNITS * L.unit + 16 * lane;
-        char *to = lds + L.img + half * L.unit;
-        constexpr int pieces = L.unit / 1024;
-#pragma unroll
-        for (int i = 0; i < (pieces + WAVES - 1) / WAVES; ++i) {
-            const int at = i * WAVES + wave;        // kilobyte (t, b) of the part
-            if (pieces % WAVES == 0 || at < pieces) load_to_lds(from + ((at / KBU) * KB + u * KBU + at % KBU) * 1024, to + at * 1024);
-        }
+    // part u of dictionary `set` into LDS, all waves together
+    auto stage = [&](int set, int u) {
+        const char *from = tab.img + (size_t)set * UNITS * L.unit + u * KBU * 1024 + 16 * lane;
+        constexpr int pieces = L.unit / 1024;       // kilobytes (t, b)
+#pragma unroll 1
+        for (int at = wave; at < pieces; at += WAVES) load_to_lds(from + (at / KBU * KB + at % KBU) * 1024, lds + L.img + at * 1024);
         const int tid = threadIdx.x;
-        for (int i = tid; i < 32 * KBU; i += 64 * WAVES)
-            reinterpret_cast<float *>(lds + L.hn + half * 128 * KBU)[i] = tab.hn[(size_t)set * 32 * KB + u * 32 * KBU + i];
-        for (int i = tid; i < 64 * NC; i += 64 * WAVES) reinterpret_cast<float *>(lds + L.mu + half * 256 * NC)[i] = tab.negmu[(size_t)set * 64 * NC + i];
-        if (wave == WAVES - 1 && lane < KBU) reinterpret_cast<float *>(lds + L.w + half * 32)[lane] = tab.w[(size_t)set * KB + u * KBU + lane];
+        if (tid < 32 * KBU) {
+            reinterpret_cast<float *>(lds + L.hn)[tid] = tab.hn[(size_t)set * 32 * KB + u * 32 * KBU + tid];
+            reinterpret_cast<unsigned *>(lds + L.pairs)[tid] = tab.pairs[(size_t)set * 32 * KB + u * 32 * KBU + tid];
+        }
+        if (tid < 64 * NC) reinterpret_cast<float *>(lds + L.mu)[tid] = tab.negmu[(size_t)set * 64 * NC + tid];
+        if (tid < KBU) reinterpret_cast<float *>(lds + L.w)[tid] = tab.w[(size_t)set * KB + u * KBU + tid];
     };
+    static_assert(64 * WAVES >= 32 * KBU && 64 * WAVES >= 64 * NC, "a thread per entry");
     auto landed = [&]() {
         __builtin_amdgcn_s_waitcnt(0x0f70);         // vmcnt(0)
         __syncthreads();
     };
-    int half = 0, job = job_of(0);
+    char *stretch = lds + L.rows + wave * L.stretch;
+    int job = job_of(0);
     if (job < 0) return;                            // the whole block
-    stage(job / groups * a.M, 0, 0);
-    landed();
+    stage(job / groups * a.M, 0);
     for (int turn = 0; job >= 0; ++turn) {
         const int h = job / groups, after = job_of(turn + 1);
         const int64_t n0 = ((int64_t)(job - h * groups) * WAVES + wave) * kTileVec, n = n0 + r;
         const bool active = n0 < a.n;
         const int64_t slot = n < a.n ? a.slots[n] : -1;
         const bool live = slot >= 0 && slot < a.n_slots;
-        float4 x[S];
-#pragma unroll
-        for (int s = 0; s < S; ++s) {
-            x[s] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (live && 8 * s + 4 * hh < D) x[s] = load_in(a, n * a.row_stride + h * a.head_stride + 8 * s + 4 * hh);
-        }
+        float4 x[S];                                // x[2 t], x[2 t + 1]: coordinates 16 t + 8 hh .. + 7
         {
+            int end = D - 8 * hh;                   // coordinates of the lane's first eight on
+            asm volatile("" : "+v"(end));           // (what it decides is cheaper found again than kept: sixteen masks)
+            const int64_t at = (live ? n * a.row_stride + h * a.head_stride : 0) + 8 * hh;
+            auto from = [&](int s) { return at + min(16 * (s >> 1) + 4 * (s & 1), max(end - 4, -8 * hh)); };
+            // all loads are on their way before the first is used; rows that are not kept read the first one
+            if (a.type == kRowF32) {
+#pragma unroll
+                for (int s = 0; s < S; ++s) x[s] = F32::load(a.X, from(s));
+            } else {
+                uint2 raw[S];
+#pragma unroll
+                for (int s = 0; s < S; ++s) raw[s] = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(a.X) + from(s));
+                const bool half = a.type == kRowF16;
+#pragma unroll
+                for (int s = 0; s < S; ++s) x[s] = half ? F16::widen(raw[s]) : Bf16::widen(raw[s]);
+            }
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+                if (!live || 16 * (s >> 1) + 4 * (s & 1) >= end) x[s] = make_float4(0.f, 0.f, 0.f, 0.f);
             int top = 0;                            // magnitudes order as integers do, NaN above infinity
 #pragma unroll
             for (int s = 0; s < S; ++s)
@@ -367,14 +392,16 @@ __global__ __launch_bounds__(64 * WAVES) void k_cache_write_tiles(const CacheRow
             const uint2 both = both_halves((unsigned)top);
             top = (int)max(both.x, both.y);
             float g = __int_as_float(top);
-            const bool bad = top >= 0x7f800000;
-            if (bad) g = __builtin_nanf("");
-            if (bad) {
+            if (top >= 0x7f800000) {
+                g = __builtin_nanf("");
 #pragma unroll
                 for (int s = 0; s < S; ++s) x[s] = make_float4(0.f, 0.f, 0.f, 0.f);
             } else if (a.scale && top) {
+                // x / g as the product with 1 / g in 64 bits, off by 2^-52 of it: a quotient of two numbers of 24 bits is no
+                // nearer than 2^-49 of it to a point between two such numbers, so the rounding is that of the quotient
+                const double f = 1.0 / (double)g;
 #pragma unroll
-                for (int s = 0; s < S; ++s) x[s] = make_float4(x[s].x / g, x[s].y / g, x[s].z / g, x[s].w / g);
+                for (int s = 0; s < S; ++s) x[s] = make_float4((float)(x[s].x * f), (float)(x[s].y * f), (float)(x[s].z * f), (float)(x[s].w * f));
             }
             if (live && hh == 0 && a.scale) a.scale[slot * a.H + h] = g;
         }
@@ -389,17 +416,15 @@ __global__ __launch_bounds__(64 * WAVES) void k_cache_write_tiles(const CacheRow
             c.hx = cc[4];
             c.cmax = cc[5];
             halfx8 frag[T];
-            uint32_t mk[(KB + 1) / 2];
-            float top[KB];
+            uint32_t mk[W];                         // candidates: bit 16 b + v of word i is place 64 i + 32 b + 8 (v / 4) + 4 hh + v % 4
+            float top[W];                           // the largest of score + e w of a word's codewords, at most
             float x2 = 0.f, e = 0.f, margin = 0.f, best = -inf;
 #pragma unroll
             for (int u = 0; u < UNITS; ++u) {
-                // the next part travels while this one is contracted
-                const bool last = u == UNITS - 1 && m == a.M - 1;
-                if (!last || after >= 0) stage(last ? after / groups * a.M : u == UNITS - 1 ? set + 1 : set, u == UNITS - 1 ? 0 : u + 1, half ^ 1);
+                landed();
                 if (active) {
                     if (u == 0) {
-                        const float4 *mu4 = reinterpret_cast<const float4 *>(lds + L.mu + half * 256 * NC) + hh;
+                        const float4 *mu4 = reinterpret_cast<const float4 *>(lds + L.mu) + hh;
                         float xsq = 0.f, dsq = 0.f;
 #pragma unroll
                         for (int t = 0; t < T; ++t) {
@@ -414,12 +439,21 @@ __global__ __launch_bounds__(64 * WAVES) void k_cache_write_tiles(const CacheRow
                         // margin_half with the largest score there can be in place of the best
                         margin = margin_half(c, xn * c.cmax + 0.51f * c.cmax * c.cmax, xn, e);
                     }
-                    const char *base = lds + L.img + half * L.unit;
-                    const float *lds_h = reinterpret_cast<const float *>(lds + L.hn + half * 128 * KBU), *lds_w = reinterpret_cast<const float *>(lds + L.w + half * 32);
+                    const float *lds_h = reinterpret_cast<const float *>(lds + L.hn), *lds_w = reinterpret_cast<const float *>(lds + L.w);
+                    const unsigned *lds_pair = reinterpret_cast<const unsigned *>(lds + L.pairs);
                     const char *slot_of[4];
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) slot_of[t] = base + half_slot(t, hh, r);
+                    for (int t = 0; t < 4; ++t) slot_of[t] = lds + L.img + half_slot(t, hh, r);
                     constexpr int GB = KBU < 2 ? 1 : 2;             // blocks whose products run together
+                    // the dictionary's operands are read P products ahead, in an order that the scheduler may not change (contract_half)
+                    constexpr int N = KBU * T, P = N < 6 ? N : 6;
+                    auto operand = [&](int i) {
+                        const int t = i % (T * GB) / GB, b = i / (T * GB) * GB + i % GB;
+                        return *reinterpret_cast<const halfx8 *>(slot_of[t & 3] + (t * KBU + b) * 1024);
+                    };
+                    halfx8 ahead[P];
+#pragma unroll
+                    for (int i = 0; i < P; ++i) ahead[i] = operand(i);
 #pragma unroll
                     for (int b0 = 0; b0 < KBU; b0 += GB) {
                         floatx16 acc[GB];
@@ -427,76 +461,162 @@ __global__ __launch_bounds__(64 * WAVES) void k_cache_write_tiles(const CacheRow
 #pragma unroll
                         for (int t = 0; t < T; ++t)
 #pragma unroll
-                            for (int b = 0; b < GB; ++b)
-                                acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const halfx8 *>(slot_of[t & 3] + (t * KBU + b0 + b) * 1024), frag[t],
-                                                                                acc[b], 0, 0, 0);
+                            for (int b = 0; b < GB; ++b) {
+                                const int i = b0 * T + t * GB + b;
+                                acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ahead[i % P], frag[t], acc[b], 0, 0, 0);
+                                if (i + P < N) ahead[i % P] = operand(i + P);
+                                __builtin_amdgcn_sched_barrier(0x6);        // arithmetic may pass, products and memory not
+                            }
+                        const int i = (u * KBU + b0) / 2;
+                        float low = -inf;
+                        top[i] = -inf;
 #pragma unroll
                         for (int b = 0; b < GB; ++b) {
-                            const int blk = u * KBU + b0 + b;
-                            const float ew = e * lds_w[b0 + b];
-                            top[blk] = block_max(acc[b]) + ew;      // an upper bound but for h
-                            const uint2 t2 = both_halves(__float_as_uint(top[blk]));
-                            best = fmaxf(best, fmaxf(__uint_as_float(t2.x), __uint_as_float(t2.y)) - 2.f * ew);
-                            floatx16 one[1] = {acc[b]};
-                            subtract_half<1>(one, best - 2.f * margin - ew, hh);
-                            uint32_t below = 0u;
-#pragma unroll
-                            for (int v = 15; v >= 0; --v) below = __builtin_amdgcn_alignbit(below, __float_as_uint(one[0][v]), 31);
-                            const uint32_t bits = ~below & 0xffffu;
-                            if (blk & 1) mk[blk >> 1] |= bits << 16;
-                            else mk[blk >> 1] = bits;
+                            const float most = block_max(acc[b]), w = lds_w[b0 + b];
+                            low = __builtin_elementwise_maximum(low, fmaf(-e, w, most));
+                            top[i] = __builtin_elementwise_maximum(top[i], fmaf(e, w, most));
                         }
+                        const uint2 low2 = both_halves(__float_as_uint(low));
+                        best = __builtin_elementwise_maximum(__builtin_elementwise_maximum(best, __uint_as_float(low2.x)), __uint_as_float(low2.y));
+                        // score + e w - (best - 2 margin), one more product of four terms: the threshold in three fp16 pieces (subtract_half), and e w
+                        const float thr = fmaf(-2.f, margin, best);
+                        const _Float16 p0 = (_Float16)(thr * -0.0009765625f);
+                        const float rest = fmaf((float)p0, -1024.f, -thr);
+                        const _Float16 p1 = (_Float16)rest;
+                        halfx4 right = {p0, p1, (_Float16)((rest - (float)p1) * 1024.f), (_Float16)e};
+                        if (hh) right = (halfx4){(_Float16)0.f, (_Float16)0.f, (_Float16)0.f, (_Float16)0.f};
+                        uint32_t word = 0u;
+#pragma unroll
+                        for (int b = GB - 1; b >= 0; --b) {
+                            const uint2 left = make_uint2(__builtin_bit_cast(unsigned, (halfx2){(_Float16)1024.f, (_Float16)1.f}), lds_pair[32 * (b0 + b) + r]);
+                            acc[b] = __builtin_amdgcn_mfma_f32_32x32x8f16(__builtin_bit_cast(halfx4, left), right, acc[b], 0, 0, 0);
+#pragma unroll
+                            for (int v = 15; v >= 0; --v) word = __builtin_amdgcn_alignbit(word, __float_as_uint(acc[b][v]), 31);     // (word << 1) | sign
+                        }
+                        mk[i] = KB == 1 ? ~word & 0xffffu : ~word;
                     }
                 }
-                landed();                                           // the next part is there, this one is free
-                half ^= 1;
+                __syncthreads();                                    // this part is free; the next travels while rows are decided
+                const bool last = u == UNITS - 1 && m == a.M - 1;
+                if (!last || after >= 0) stage(last ? after / groups * a.M : u == UNITS - 1 ? set + 1 : set, u == UNITS - 1 ? 0 : u + 1);
             }
             if (!active) continue;
-            const bool big = !(x2 < kHalfMaxNorm * kHalfMaxNorm && fabsf(best) + 2.f * margin + 2.f * e * c.cmax < 0.5f * kHalfMaxThr);
-            unsigned mine = 0u;
-            int place = 256;
+            const float thr = fmaf(-2.f, margin, best);
+            const bool big = !(x2 < kHalfMaxNorm * kHalfMaxNorm && fabsf(best) + 2.f * margin < 0.5f * kHalfMaxThr);
 #pragma unroll
-            for (int b = KB - 1; b >= 0; --b) {
-                uint32_t bits = (mk[b >> 1] >> (16 * (b & 1))) & 0xffffu, real = 0xffffu;
-                if (!(top[b] >= best - 2.f * margin)) bits = 0u;
-                if (big) bits = 0xffffu;                            // may not fit fp16: all codewords that there are
-                if (32 * (b + 1) > a.K) {
+            for (int i = 0; i < W; ++i) mk[i] = top[i] >= thr ? mk[i] : 0u;
+            if (__ballot(big)) {                                    // may not fit fp16: all codewords that there are
 #pragma unroll
-                    for (int v = 0; v < 16; ++v)
-                        if (32 * b + 8 * (v >> 2) + 4 * hh + (v & 3) >= a.K) real &= ~(1u << v);
+                for (int i = 0; i < W; ++i) {
+                    uint32_t all = 0u;
+                    for (int v = 0; v < (KB == 1 ? 16 : 32); ++v)
+                        if (64 * i + 32 * (v >> 4) + 8 * ((v & 15) >> 2) + 4 * hh + (v & 3) < a.K) all |= 1u << v;
+                    mk[i] = big ? all : mk[i];
                 }
-                bits &= real;
-                mk[b >> 1] = b & 1 ? (mk[b >> 1] & 0xffffu) | bits << 16 : (mk[b >> 1] & 0xffff0000u) | bits;
-                mine += (unsigned)__popc(bits);
-                const int v = __ffs(bits) - 1;
-                if (bits) place = 32 * b + 8 * (v >> 2) + 4 * hh + (v & 3);
             }
-            const uint2 count = both_halves(mine), at2 = both_halves((unsigned)place);
-            place = (int)min(at2.x, at2.y);
-            place = place < a.K ? place : 0;
-            unsigned who = (unsigned)__ballot(live && count.x + count.y != 1u);
-            const float *Cm = tab.C + (size_t)set * a.K * D;
+            // how many, the first and the last
+            int place, other;
+            unsigned count;
+            {
+                unsigned mine = 0u;
+                uint32_t first = mk[W - 1], last = mk[0];
+                int fi = W - 1, li = 0;
+#pragma unroll
+                for (int i = 0; i < W; ++i) mine += (unsigned)__popc(mk[i]);
+#pragma unroll
+                for (int i = W - 2; i >= 0; --i)
+                    if (mk[i]) { first = mk[i]; fi = i; }
+#pragma unroll
+                for (int i = 1; i < W; ++i)
+                    if (mk[i]) { last = mk[i]; li = i; }
+                const int f = __ffs(first) - 1, l = 31 - __clz(last);
+                const uint2 n2 = both_halves(mine);
+                const uint2 f2 = both_halves(first ? (unsigned)(64 * fi + 8 * (f >> 2) + 4 * hh + (f & 3)) : 256u);
+                const uint2 l2 = both_halves(last ? (unsigned)(64 * li + 8 * (l >> 2) + 4 * hh + (l & 3)) : 0u);
+                count = n2.x + n2.y;
+                place = (int)min(f2.x, f2.y);
+                other = (int)max(l2.x, l2.y);
+                place = place < a.K ? place : 0;
+                other = other < a.K ? other : 0;
+            }
+            const float *Cm = tab.C + (size_t)set * a.K * Dp;
             const uint8_t *order = tab.order + (size_t)set * 256;
-            while (who) {
-                // up to four undecided rows, sixteen lanes each: fp32 direct form where the two best are further apart than its error
-                int v[kTileBatch];
+            const int g = lane >> 4, sub = lane & 15;
+            float *rows = reinterpret_cast<float *>(stretch);
+            unsigned two = (unsigned)__ballot(live && count == 2u), more = (unsigned)__ballot(live && count != 1u && count != 2u);
+            // four undecided rows at a time, sixteen lanes each, in fp32 where the two nearest are further apart than its error
+            int v[kTileBatch];
+            auto take_rows = [&](unsigned &from) {
 #pragma unroll
                 for (int j = 0; j < kTileBatch; ++j) {
-                    v[j] = who ? __ffs(who) - 1 : -1;
-                    who &= who - 1u;
+                    v[j] = from ? __ffs(from) - 1 : -1;
+                    from &= from - 1u;
                 }
-                float *rows = reinterpret_cast<float *>(lds + L.rows) + wave * kTileBatch * 64 * NC;
-                uint16_t *masks = reinterpret_cast<uint16_t *>(lds + L.masks) + wave * kTileBatch * 16;
                 const int to = r == v[0] ? 0 : r == v[1] ? 1 : r == v[2] ? 2 : r == v[3] ? 3 : -1;
                 if (to >= 0) {
 #pragma unroll
                     for (int s = 0; s < S; ++s) reinterpret_cast<float4 *>(rows + to * 64 * NC)[2 * s + hh] = x[s];
+                }
+                return to;
+            };
+            auto distances = [&](int k0, int k1, float &d0, float &d1) {    // of the lanes' row, codewords k0 and k1 (below 0: infinity)
+                const float4 *row = reinterpret_cast<const float4 *>(rows + g * 64 * NC);
+                float4 q[2][NC];
+#pragma unroll
+                for (int i = 0; i < NC; ++i) {
+                    const int p = sub + 16 * i;
+                    q[0][i] = q[1][i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (4 * p < Dp) {
+                        q[0][i] = *reinterpret_cast<const float4 *>(Cm + (unsigned)(max(k0, 0) * Dp + 4 * p));
+                        q[1][i] = *reinterpret_cast<const float4 *>(Cm + (unsigned)(max(k1, 0) * Dp + 4 * p));
+                    }
+                }
+                float d[2] = {0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < NC; ++i) {
+                    const float4 w = 4 * (sub + 16 * i) < Dp ? row[sub + 16 * i] : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const float e0 = w.x - q[j][i].x, e1 = w.y - q[j][i].y, e2 = w.z - q[j][i].z, e3 = w.w - q[j][i].w;
+                        d[j] = fmaf(e3, e3, fmaf(e2, e2, fmaf(e1, e1, fmaf(e0, e0, d[j]))));
+                    }
+                }
+                d0 = k0 >= 0 ? sum16(d[0]) : inf;
+                d1 = k1 >= 0 ? sum16(d[1]) : inf;
+            };
+            const float eta = (float)(4 * NC + 10) * 6.1e-8f;
+            unsigned hard = 0u;                                     // exact and nearly exact ties
+            while (two) {
+                (void)take_rows(two);
+                wave_lds_fence();
+                int k0 = -1, k1 = -1;
+#pragma unroll
+                for (int j = 0; j < kTileBatch; ++j) {
+                    const int at = max(v[j], 0), p0 = __builtin_amdgcn_readlane(place, at), p1 = __builtin_amdgcn_readlane(other, at);
+                    if (g == j) {
+                        k0 = p0;
+                        k1 = p1;
+                    }
+                }
+                float d0, d1;
+                distances(k0, k1, d0, d1);
+                const bool sure = fminf(d0, d1) * (1.f + eta) < fmaxf(d0, d1) * (1.f - eta) && fmaxf(d0, d1) > 1e-25f;
+                const unsigned long long unsure = __ballot(!sure), second = __ballot(d1 < d0);
+#pragma unroll
+                for (int j = 0; j < kTileBatch; ++j) {
+                    if (v[j] >= 0 && ((unsure >> (16 * j)) & 1ull)) hard |= 1u << v[j];
+                    if (r == v[j] && ((second >> (16 * j)) & 1ull)) place = other;
+                }
+                wave_lds_fence();
+            }
+            while (more) {
+                const int to = take_rows(more);
+                uint16_t *masks = reinterpret_cast<uint16_t *>(lds + L.masks) + wave * kTileBatch * 16;
+                if (to >= 0) {
 #pragma unroll
                     for (int b = 0; b < KB; ++b) masks[to * 16 + 2 * b + hh] = (uint16_t)(mk[b >> 1] >> (16 * (b & 1)));
                 }
                 wave_lds_fence();
-                const int g = lane >> 4, sub = lane & 15;
-                const float4 *row = reinterpret_cast<const float4 *>(rows + g * 64 * NC);
                 const unsigned *words = reinterpret_cast<const unsigned *>(masks + g * 16);
                 const bool have = (g == 0 ? v[0] : g == 1 ? v[1] : g == 2 ? v[2] : v[3]) >= 0;
                 int word = 0;
@@ -512,73 +632,90 @@ __global__ __launch_bounds__(64 * WAVES) void k_cache_write_tiles(const CacheRow
                 int at = 0;
                 for (int k0 = take(); __ballot(k0 >= 0); k0 = take()) {
                     const int k1 = take();
-                    float4 q[2][NC];
-#pragma unroll
-                    for (int i = 0; i < NC; ++i) {
-                        const int p = sub + 16 * i;
-                        q[0][i] = q[1][i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                        if (k0 >= 0 && 4 * p < D) q[0][i] = reinterpret_cast<const float4 *>(Cm + (size_t)k0 * D)[p];
-                        if (k1 >= 0 && 4 * p < D) q[1][i] = reinterpret_cast<const float4 *>(Cm + (size_t)k1 * D)[p];
-                    }
-                    float d[2] = {0.f, 0.f};
-#pragma unroll
-                    for (int i = 0; i < NC; ++i) {
-                        const float4 w = row[sub + 16 * i];
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const float e0 = w.x - q[j][i].x, e1 = w.y - q[j][i].y, e2 = w.z - q[j][i].z, e3 = w.w - q[j][i].w;
-                            d[j] = fmaf(e3, e3, fmaf(e2, e2, fmaf(e1, e1, fmaf(e0, e0, d[j]))));
-                        }
-                    }
-                    const float d0 = k0 >= 0 ? sum16(d[0]) : inf, d1 = k1 >= 0 ? sum16(d[1]) : inf;
+                    float d0, d1;
+                    distances(k0, k1, d0, d1);
                     second = d0 < least ? least : fminf(second, d0);
                     if (d0 < least) { least = d0; at = k0; }
                     second = d1 < least ? least : fminf(second, d1);
                     if (d1 < least) { least = d1; at = k1; }
                 }
-                const float eta = (float)(4 * NC + 10) * 6.1e-8f;
-                const bool sure = least * (1.f + eta) < second * (1.f - eta) && second > 1e-25f;
-                unsigned long long hard = __ballot(have && !sure && sub == 0);
-                while (hard) {                                      // exact and nearly exact ties, in 64 bits by the whole wave
-                    const int which = (__ffsll(hard) - 1) >> 4;
-                    hard &= hard - 1ull;
-                    const float *one = rows + which * 64 * NC;
-                    const unsigned *bits = reinterpret_cast<const unsigned *>(masks + which * 16);
-                    double db = __builtin_inf();
-                    int kb = 0x7fffffff, pb = 0;
-                    for (int p = lane; p < a.K; p += kWave) {
-                        const int i = p & 31, bit = 4 * (i >> 3) + (i & 3) + 16 * ((i >> 2) & 1);
-                        if (!((bits[p >> 5] >> bit) & 1u)) continue;
-                        const float *cw = Cm + (size_t)p * D;
-                        double t = 0.0;
-                        for (int d = 0; d < D; ++d) {
-                            const double u = (double)one[d] - (double)cw[d];
-                            t += u * u;
-                        }
-                        const int k = order[p];
-                        if (t < db || (t == db && k < kb)) { db = t; kb = k; pb = p; }
-                    }
-#pragma unroll
-                    for (int o = 32; o > 0; o >>= 1) {
-                        const double od = __shfl_xor(db, o, kWave);
-                        const int ok = __shfl_xor(kb, o, kWave), op = __shfl_xor(pb, o, kWave);
-                        if (od < db || (od == db && ok < kb)) { db = od; kb = ok; pb = op; }
-                    }
-                    if (g == which) at = pb;
-                }
+                const unsigned long long unsure = __ballot(!(least * (1.f + eta) < second * (1.f - eta) && second > 1e-25f));
 #pragma unroll
                 for (int j = 0; j < kTileBatch; ++j) {
                     const int decided = __builtin_amdgcn_readlane(at, 16 * j);
+                    if (v[j] >= 0 && ((unsure >> (16 * j)) & 1ull)) hard |= 1u << v[j];
                     if (r == v[j]) place = decided;
                 }
                 wave_lds_fence();
             }
-            if (live && hh == 0) a.codes[(slot * a.H + h) * a.M + m] = order[place];
+            while (hard) {                                          // one after another in 64 bits, by the whole wave
+                const int which = __ffs(hard) - 1;
+                hard &= hard - 1u;
+                if (r == which) {
 #pragma unroll
-            for (int s = 0; s < S; ++s) {
-                float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (8 * s + 4 * hh < D) q = reinterpret_cast<const float4 *>(Cm + (size_t)place * D)[2 * s + hh];
-                x[s] = make_float4(x[s].x - q.x, x[s].y - q.y, x[s].z - q.z, x[s].w - q.w);
+                    for (int s = 0; s < S; ++s) reinterpret_cast<float4 *>(rows)[2 * s + hh] = x[s];
+                }
+                wave_lds_fence();
+                uint32_t halves[2][W];
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    halves[0][i] = (uint32_t)__builtin_amdgcn_readlane((int)mk[i], which);
+                    halves[1][i] = (uint32_t)__builtin_amdgcn_readlane((int)mk[i], which + 32);
+                }
+                double db = __builtin_inf();
+                int kb = 0x7fffffff, pb = 0;
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    const int p = 64 * i + lane, bit = 16 * (lane >> 5) + 4 * ((lane & 31) >> 3) + (lane & 3);
+                    if (p >= a.K || !(((lane & 4 ? halves[1][i] : halves[0][i]) >> bit) & 1u)) continue;
+                    const float *cw = Cm + (size_t)p * Dp;
+                    double t = 0.0;
+                    for (int d = 0; d < Dp; ++d) {
+                        const double u = (double)rows[d] - (double)cw[d];
+                        t += u * u;
+                    }
+                    const int k = order[p];
+                    if (t < db || (t == db && k < kb)) { db = t; kb = k; pb = p; }
+                }
+#pragma unroll
+                for (int o = 32; o > 0; o >>= 1) {
+                    const double od = __shfl_xor(db, o, kWave);
+                    const int ok = __shfl_xor(kb, o, kWave), op = __shfl_xor(pb, o, kWave);
+                    if (od < db || (od == db && ok < kb)) { db = od; kb = ok; pb = op; }
+                }
+                if (r == which) place = pb;
+                wave_lds_fence();
+            }
+            if (live && hh == 0) a.codes[(slot * a.H + h) * a.M + m] = order[place];
+            // The codewords to subtract: four lanes read 64 bytes of one, and a piece of 16 positions of all rows goes round through LDS to
+            // the lanes that hold the rows.  (A lane that reads its own row's codeword touches a cache line of its own.)
+            {
+                const int row = lane >> 2, piece = lane & 3;
+                const int p0 = __shfl(place, row, kWave), p1 = __shfl(place, row + 16, kWave);
+                const unsigned o0 = (unsigned)(p0 * Dp + 4 * piece), o1 = (unsigned)(p1 * Dp + 4 * piece);
+                float4 q0[T], q1[T];
+#pragma unroll
+                for (int t = 0; t < T; ++t) {
+                    q0[t] = q1[t] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (16 * t < D) {
+                        q0[t] = *reinterpret_cast<const float4 *>(Cm + o0 + 16 * t);
+                        q1[t] = *reinterpret_cast<const float4 *>(Cm + o1 + 16 * t);
+                    }
+                }
+                float4 *around = reinterpret_cast<float4 *>(stretch);   // [32 rows][4 pieces], a piece at its number xor (row / 4) % 4
+                const int in = 4 * row + (piece ^ ((row >> 2) & 3)), out = 4 * r, turn_of = (r >> 2) & 3;
+#pragma unroll
+                for (int t = 0; t < T; ++t) {
+                    if (16 * t < D) {
+                        around[in] = q0[t];
+                        around[in + 64] = q1[t];
+                        wave_lds_fence();
+                        const float4 u = around[out + (hh ^ turn_of)], w = around[out + ((2 + hh) ^ turn_of)];
+                        x[2 * t] = make_float4(x[2 * t].x - u.x, x[2 * t].y - u.y, x[2 * t].z - u.z, x[2 * t].w - u.w);
+                        x[2 * t + 1] = make_float4(x[2 * t + 1].x - w.x, x[2 * t + 1].y - w.y, x[2 * t + 1].z - w.z, x[2 * t + 1].w - w.w);
+                        wave_lds_fence();
+                    }
+                }
             }
         }
         job = after;

@@ -17,11 +17,12 @@ struct F32 {
 struct F16 {
     static constexpr int bytes = 2;
     typedef _Float16 h4 __attribute__((ext_vector_type(4)));
-    __device__ static __forceinline__ float4 load(const void *p, int64_t at)
+    __device__ static __forceinline__ float4 widen(const uint2 &q)
     {
-        const h4 v = *reinterpret_cast<const h4 *>(static_cast<const _Float16 *>(p) + at);
+        const h4 v = __builtin_bit_cast(h4, q);
         return make_float4((float)v.x, (float)v.y, (float)v.z, (float)v.w);
     }
+    __device__ static __forceinline__ float4 load(const void *p, int64_t at) { return widen(*reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p) + at)); }
     __device__ static __forceinline__ void store(void *p, int64_t at, const float4 &v)
     {
         *reinterpret_cast<h4 *>(static_cast<_Float16 *>(p) + at) = (h4){(_Float16)v.x, (_Float16)v.y, (_Float16)v.z, (_Float16)v.w};
@@ -30,11 +31,11 @@ struct F16 {
 struct Bf16 {
     static constexpr int bytes = 2;
     typedef __bf16 b4 __attribute__((ext_vector_type(4)));
-    __device__ static __forceinline__ float4 load(const void *p, int64_t at)
+    __device__ static __forceinline__ float4 widen(const uint2 &v)
     {
-        const uint2 v = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p) + at);
         return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
     }
+    __device__ static __forceinline__ float4 load(const void *p, int64_t at) { return widen(*reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p) + at)); }
     __device__ static __forceinline__ void store(void *p, int64_t at, const float4 &v)
     {
         *reinterpret_cast<b4 *>(static_cast<uint16_t *>(p) + at) = (b4){(__bf16)v.x, (__bf16)v.y, (__bf16)v.z, (__bf16)v.w};
