@@ -231,7 +231,9 @@ struct CacheTables {
     const float *C;                                 // [H M][K][Dp] sorted, positions in place of coordinates, zero beyond D
     const uint8_t *order;                           // [H M][256]: the codeword at a place
 };
-__host__ __device__ constexpr int cache_padded(int D) { return (D + 15) / 16 * 16; }
+// 64-position chunks of a row: 1, 2 or 4.
+__host__ __device__ constexpr int cache_chunks(int D) { return D <= 64 ? 1 : D <= 128 ? 2 : 4; }
+__host__ __device__ constexpr int cache_padded(int D) { return 64 * cache_chunks(D); }
 
 // Codewords in ascending order of their distance from the mean of a few, equal ones by index.  A block per dictionary.
 __global__ __launch_bounds__(256) void k_cache_sort(const float *__restrict__ C, int K, int D, float *__restrict__ sorted, uint8_t *__restrict__ order)
@@ -281,12 +283,13 @@ __global__ __launch_bounds__(256) void k_cache_w(const float *__restrict__ wtab,
     if (b < blocks && (threadIdx.x & 31) == 0) w[b] = v;
 }
 
-// LDS of k_cache_write_tiles: a dictionary (or half of one), and a stretch for every wave: four undecided rows, or a piece of 16 positions of the
-// codewords to subtract.
+// LDS of k_cache_write_tiles: a dictionary (or half of one) and the next, and a stretch for every wave: four undecided rows, or a piece of 16
+// positions of the codewords to subtract.
 constexpr int kTileBatch = 4;                       // undecided rows of a wave at a time, sixteen lanes each
 struct TileLds {
-    int unit;                                       // bytes of an image
-    int img, hn, pairs, mu, w, rows, masks, total;  // byte offsets
+    int unit, half;                                 // bytes of an image, and of a half with its tables
+    int hn, pairs, mu, w, consts;                   // byte offsets in a half, behind the image
+    int rows, total;                                // byte offsets
     int stretch;
 };
 __host__ __device__ constexpr TileLds tile_lds(int kbu, int nc, int waves)
@@ -294,16 +297,18 @@ __host__ __device__ constexpr TileLds tile_lds(int kbu, int nc, int waves)
     TileLds l = {};
     l.unit = kbu * nc * 4096;
     l.stretch = nc == 4 ? 4096 : 2048;
-    l.img = 0;
     l.hn = l.unit;
     l.pairs = l.hn + 128 * kbu;
     l.mu = l.pairs + 128 * kbu;
     l.w = l.mu + 256 * nc;
-    l.rows = l.w + 32;
-    l.masks = l.rows + waves * l.stretch;
-    l.total = l.masks + waves * kTileBatch * 32;
+    l.consts = l.w + 32;
+    l.half = l.consts + 4 * kEncodeConsts;
+    l.rows = 2 * l.half;
+    l.total = l.rows + waves * l.stretch;
     return l;
 }
+
+typedef float floatv4 __attribute__((ext_vector_type(4)));
 
 template <int CTRL>
 __device__ __forceinline__ float dpp_plus(float v)
@@ -318,7 +323,7 @@ __device__ __forceinline__ float sum16(float v)
 
 // KB: blocks of 32 codewords.  NC: 64-position chunks (1, 2 or 4).  UNITS: parts in which a dictionary passes through LDS.
 template <int KB, int NC, int UNITS, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, NC == 4 ? 1 : 2) void k_cache_write_tiles(const CacheRowsIn a, const CacheTables tab, int groups)
+__global__ __launch_bounds__(64 * WAVES, WAVES / 4) void k_cache_write_tiles(const CacheRowsIn a, const CacheTables tab, int groups)
 {
     extern __shared__ float4 smem4[];
     char *lds = reinterpret_cast<char *>(smem4);
@@ -326,7 +331,8 @@ __global__ __launch_bounds__(64 * WAVES, NC == 4 ? 1 : 2) void k_cache_write_til
     constexpr TileLds L = tile_lds(KBU, NC, WAVES);
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5, r = lane & 31;
     const float inf = __builtin_inff();
-    const int D = a.D, Dp = cache_padded(D);
+    const int D = a.D;
+    constexpr int Dp = 64 * NC;
     // blocks go round the XCDs: neighbouring groups of tiles, of one head, to one of them
     const int jobs = groups * a.H, per_xcd = (jobs + 7) / 8;
     const int stride = gridDim.x >> 3, mine0 = blockIdx.x >> 3;
@@ -335,19 +341,21 @@ __global__ __launch_bounds__(64 * WAVES, NC == 4 ? 1 : 2) void k_cache_write_til
         const int job = (int)(blockIdx.x & 7) * per_xcd + j;
         return j < per_xcd && job < jobs ? job : -1;
     };
-    // part u of dictionary `set` into LDS, all waves together
-    auto stage = [&](int set, int u) {
+    // part u of dictionary `set` into a half of LDS, all waves together
+    auto stage = [&](int set, int u, int half) {
+        char *to = lds + half * L.half;
         const char *from = tab.img + (size_t)set * UNITS * L.unit + u * KBU * 1024 + 16 * lane;
         constexpr int pieces = L.unit / 1024;       // kilobytes (t, b)
 #pragma unroll 1
-        for (int at = wave; at < pieces; at += WAVES) load_to_lds(from + (at / KBU * KB + at % KBU) * 1024, lds + L.img + at * 1024);
+        for (int at = wave; at < pieces; at += WAVES) load_to_lds(from + (at / KBU * KB + at % KBU) * 1024, to + at * 1024);
         const int tid = threadIdx.x;
         if (tid < 32 * KBU) {
-            reinterpret_cast<float *>(lds + L.hn)[tid] = tab.hn[(size_t)set * 32 * KB + u * 32 * KBU + tid];
-            reinterpret_cast<unsigned *>(lds + L.pairs)[tid] = tab.pairs[(size_t)set * 32 * KB + u * 32 * KBU + tid];
+            reinterpret_cast<float *>(to + L.hn)[tid] = tab.hn[(size_t)set * 32 * KB + u * 32 * KBU + tid];
+            reinterpret_cast<unsigned *>(to + L.pairs)[tid] = tab.pairs[(size_t)set * 32 * KB + u * 32 * KBU + tid];
         }
-        if (tid < 64 * NC) reinterpret_cast<float *>(lds + L.mu)[tid] = tab.negmu[(size_t)set * 64 * NC + tid];
-        if (tid < KBU) reinterpret_cast<float *>(lds + L.w)[tid] = tab.w[(size_t)set * KB + u * KBU + tid];
+        if (tid < 64 * NC) reinterpret_cast<float *>(to + L.mu)[tid] = tab.negmu[(size_t)set * 64 * NC + tid];
+        if (tid < KBU) reinterpret_cast<float *>(to + L.w)[tid] = tab.w[(size_t)set * KB + u * KBU + tid];
+        if (tid >= 64 && tid < 64 + kEncodeConsts) reinterpret_cast<float *>(to + L.consts)[tid - 64] = tab.consts[(size_t)set * kEncodeConsts + tid - 64];
     };
     static_assert(64 * WAVES >= 32 * KBU && 64 * WAVES >= 64 * NC, "a thread per entry");
     auto landed = [&]() {
@@ -355,9 +363,9 @@ __global__ __launch_bounds__(64 * WAVES, NC == 4 ? 1 : 2) void k_cache_write_til
         __syncthreads();
     };
     char *stretch = lds + L.rows + wave * L.stretch;
-    int job = job_of(0);
+    int job = job_of(0), half = 1;
     if (job < 0) return;                            // the whole block
-    stage(job / groups * a.M, 0);
+    stage(job / groups * a.M, 0, 0);
     for (int turn = 0; job >= 0; ++turn) {
         const int h = job / groups, after = job_of(turn + 1);
         const int64_t n0 = ((int64_t)(job - h * groups) * WAVES + wave) * kTileVec, n = n0 + r;
@@ -407,24 +415,28 @@ __global__ __launch_bounds__(64 * WAVES, NC == 4 ? 1 : 2) void k_cache_write_til
         }
         for (int m = 0; m < a.M; ++m) {
             const int set = h * a.M + m;
-            const float *cc = tab.consts + (size_t)set * kEncodeConsts;
-            HalfConsts c;
-            c.scale = cc[0];
-            c.h = cc[1];
-            c.rho = cc[2];
-            c.acc = cc[3];
-            c.hx = cc[4];
-            c.cmax = cc[5];
             halfx8 frag[T];
             uint32_t mk[W];                         // candidates: bit 16 b + v of word i is place 64 i + 32 b + 8 (v / 4) + 4 hh + v % 4
             float top[W];                           // the largest of score + e w of a word's codewords, at most
             float x2 = 0.f, e = 0.f, margin = 0.f, best = -inf;
 #pragma unroll
             for (int u = 0; u < UNITS; ++u) {
-                landed();
+                landed();                                           // this part is there, and nobody needs the one before
+                half ^= 1;
+                const char *now = lds + half * L.half;
+                const bool last = u == UNITS - 1 && m == a.M - 1;
+                if (!last || after >= 0) stage(last ? after / groups * a.M : u == UNITS - 1 ? set + 1 : set, u == UNITS - 1 ? 0 : u + 1, half ^ 1);
                 if (active) {
                     if (u == 0) {
-                        const float4 *mu4 = reinterpret_cast<const float4 *>(lds + L.mu) + hh;
+                        const float *cc = reinterpret_cast<const float *>(now + L.consts);
+                        HalfConsts c;
+                        c.scale = cc[0];
+                        c.h = cc[1];
+                        c.rho = cc[2];
+                        c.acc = cc[3];
+                        c.hx = cc[4];
+                        c.cmax = cc[5];
+                        const float4 *mu4 = reinterpret_cast<const float4 *>(now + L.mu) + hh;
                         float xsq = 0.f, dsq = 0.f;
 #pragma unroll
                         for (int t = 0; t < T; ++t) {
@@ -439,11 +451,11 @@ __global__ __launch_bounds__(64 * WAVES, NC == 4 ? 1 : 2) void k_cache_write_til
                         // margin_half with the largest score there can be in place of the best
                         margin = margin_half(c, xn * c.cmax + 0.51f * c.cmax * c.cmax, xn, e);
                     }
-                    const float *lds_h = reinterpret_cast<const float *>(lds + L.hn), *lds_w = reinterpret_cast<const float *>(lds + L.w);
-                    const unsigned *lds_pair = reinterpret_cast<const unsigned *>(lds + L.pairs);
+                    const float *lds_h = reinterpret_cast<const float *>(now + L.hn), *lds_w = reinterpret_cast<const float *>(now + L.w);
+                    const unsigned *lds_pair = reinterpret_cast<const unsigned *>(now + L.pairs);
                     const char *slot_of[4];
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) slot_of[t] = lds + L.img + half_slot(t, hh, r);
+                    for (int t = 0; t < 4; ++t) slot_of[t] = now + half_slot(t, hh, r);
                     constexpr int GB = KBU < 2 ? 1 : 2;             // blocks whose products run together
                     // the dictionary's operands are read P products ahead, in an order that the scheduler may not change (contract_half)
                     constexpr int N = KBU * T, P = N < 6 ? N : 6;
@@ -496,9 +508,6 @@ __global__ __launch_bounds__(64 * WAVES, NC == 4 ? 1 : 2) void k_cache_write_til
                         mk[i] = KB == 1 ? ~word & 0xffffu : ~word;
                     }
                 }
-                __syncthreads();                                    // this part is free; the next travels while rows are decided
-                const bool last = u == UNITS - 1 && m == a.M - 1;
-                if (!last || after >= 0) stage(last ? after / groups * a.M : u == UNITS - 1 ? set + 1 : set, u == UNITS - 1 ? 0 : u + 1);
             }
             if (!active) continue;
             const float thr = fmaf(-2.f, margin, best);
@@ -514,208 +523,189 @@ __global__ __launch_bounds__(64 * WAVES, NC == 4 ? 1 : 2) void k_cache_write_til
                     mk[i] = big ? all : mk[i];
                 }
             }
-            // how many, the first and the last
-            int place, other;
-            unsigned count;
-            {
+            // the first and the last of the candidates left, the same in both lanes of the row; their number
+            auto ends = [&](const uint32_t (&w)[W], int &front, int &back) {
                 unsigned mine = 0u;
-                uint32_t first = mk[W - 1], last = mk[0];
+                uint32_t first = w[W - 1], last = w[0];
                 int fi = W - 1, li = 0;
 #pragma unroll
-                for (int i = 0; i < W; ++i) mine += (unsigned)__popc(mk[i]);
+                for (int i = 0; i < W; ++i) mine += (unsigned)__popc(w[i]);
 #pragma unroll
                 for (int i = W - 2; i >= 0; --i)
-                    if (mk[i]) { first = mk[i]; fi = i; }
+                    if (w[i]) { first = w[i]; fi = i; }
 #pragma unroll
                 for (int i = 1; i < W; ++i)
-                    if (mk[i]) { last = mk[i]; li = i; }
+                    if (w[i]) { last = w[i]; li = i; }
                 const int f = __ffs(first) - 1, l = 31 - __clz(last);
                 const uint2 n2 = both_halves(mine);
                 const uint2 f2 = both_halves(first ? (unsigned)(64 * fi + 8 * (f >> 2) + 4 * hh + (f & 3)) : 256u);
                 const uint2 l2 = both_halves(last ? (unsigned)(64 * li + 8 * (l >> 2) + 4 * hh + (l & 3)) : 0u);
-                count = n2.x + n2.y;
-                place = (int)min(f2.x, f2.y);
-                other = (int)max(l2.x, l2.y);
-                place = place < a.K ? place : 0;
-                other = other < a.K ? other : 0;
-            }
+                front = (int)min(f2.x, f2.y);
+                back = (int)max(l2.x, l2.y);
+                return n2.x + n2.y;
+            };
+            int front, back;
+            const unsigned count = ends(mk, front, back);
+            int place = front < a.K ? front : 0;
             const float *Cm = tab.C + (size_t)set * a.K * Dp;
             const uint8_t *order = tab.order + (size_t)set * 256;
+            // The first candidates' codewords are sent for at once, four lanes reading 64 bytes of one.  (A lane that reads its own row's codeword
+            // touches a cache line of its own.)
+            const int row4 = lane >> 2, piece4 = lane & 3;
+            int p0 = __shfl(place, row4, kWave), p1 = __shfl(place, row4 + 16, kWave);
+            floatv4 q0[T], q1[T];
+            auto codeword4 = [&](int p) { return reinterpret_cast<const floatv4 *>(Cm + (unsigned)(p * Dp + 4 * piece4)); };
+            {
+                const floatv4 *c0 = codeword4(p0), *c1 = codeword4(p1);
+#pragma unroll
+                for (int t = 0; t < T; ++t) {
+                    q0[t] = c0[4 * t];
+                    q1[t] = c1[4 * t];
+                }
+            }
+            // Undecided rows, four at a time, sixteen lanes each: two candidates a round in fp32, which decides where the two nearest are further
+            // apart than its error.
             const int g = lane >> 4, sub = lane & 15;
             float *rows = reinterpret_cast<float *>(stretch);
-            unsigned two = (unsigned)__ballot(live && count == 2u), more = (unsigned)__ballot(live && count != 1u && count != 2u);
-            // four undecided rows at a time, sixteen lanes each, in fp32 where the two nearest are further apart than its error
-            int v[kTileBatch];
-            auto take_rows = [&](unsigned &from) {
-#pragma unroll
-                for (int j = 0; j < kTileBatch; ++j) {
-                    v[j] = from ? __ffs(from) - 1 : -1;
-                    from &= from - 1u;
-                }
-                const int to = r == v[0] ? 0 : r == v[1] ? 1 : r == v[2] ? 2 : r == v[3] ? 3 : -1;
-                if (to >= 0) {
-#pragma unroll
-                    for (int s = 0; s < S; ++s) reinterpret_cast<float4 *>(rows + to * 64 * NC)[2 * s + hh] = x[s];
-                }
-                return to;
-            };
-            auto distances = [&](int k0, int k1, float &d0, float &d1) {    // of the lanes' row, codewords k0 and k1 (below 0: infinity)
-                const float4 *row = reinterpret_cast<const float4 *>(rows + g * 64 * NC);
-                float4 q[2][NC];
-#pragma unroll
-                for (int i = 0; i < NC; ++i) {
-                    const int p = sub + 16 * i;
-                    q[0][i] = q[1][i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (4 * p < Dp) {
-                        q[0][i] = *reinterpret_cast<const float4 *>(Cm + (unsigned)(max(k0, 0) * Dp + 4 * p));
-                        q[1][i] = *reinterpret_cast<const float4 *>(Cm + (unsigned)(max(k1, 0) * Dp + 4 * p));
-                    }
-                }
-                float d[2] = {0.f, 0.f};
-#pragma unroll
-                for (int i = 0; i < NC; ++i) {
-                    const float4 w = 4 * (sub + 16 * i) < Dp ? row[sub + 16 * i] : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const float e0 = w.x - q[j][i].x, e1 = w.y - q[j][i].y, e2 = w.z - q[j][i].z, e3 = w.w - q[j][i].w;
-                        d[j] = fmaf(e3, e3, fmaf(e2, e2, fmaf(e1, e1, fmaf(e0, e0, d[j]))));
-                    }
-                }
-                d0 = k0 >= 0 ? sum16(d[0]) : inf;
-                d1 = k1 >= 0 ? sum16(d[1]) : inf;
-            };
-            const float eta = (float)(4 * NC + 10) * 6.1e-8f;
-            unsigned hard = 0u;                                     // exact and nearly exact ties
-            while (two) {
-                (void)take_rows(two);
-                wave_lds_fence();
-                int k0 = -1, k1 = -1;
-#pragma unroll
-                for (int j = 0; j < kTileBatch; ++j) {
-                    const int at = max(v[j], 0), p0 = __builtin_amdgcn_readlane(place, at), p1 = __builtin_amdgcn_readlane(other, at);
-                    if (g == j) {
-                        k0 = p0;
-                        k1 = p1;
-                    }
-                }
-                float d0, d1;
-                distances(k0, k1, d0, d1);
-                const bool sure = fminf(d0, d1) * (1.f + eta) < fmaxf(d0, d1) * (1.f - eta) && fmaxf(d0, d1) > 1e-25f;
-                const unsigned long long unsure = __ballot(!sure), second = __ballot(d1 < d0);
-#pragma unroll
-                for (int j = 0; j < kTileBatch; ++j) {
-                    if (v[j] >= 0 && ((unsure >> (16 * j)) & 1ull)) hard |= 1u << v[j];
-                    if (r == v[j] && ((second >> (16 * j)) & 1ull)) place = other;
-                }
-                wave_lds_fence();
-            }
-            while (more) {
-                const int to = take_rows(more);
-                uint16_t *masks = reinterpret_cast<uint16_t *>(lds + L.masks) + wave * kTileBatch * 16;
-                if (to >= 0) {
-#pragma unroll
-                    for (int b = 0; b < KB; ++b) masks[to * 16 + 2 * b + hh] = (uint16_t)(mk[b >> 1] >> (16 * (b & 1)));
-                }
-                wave_lds_fence();
-                const unsigned *words = reinterpret_cast<const unsigned *>(masks + g * 16);
-                const bool have = (g == 0 ? v[0] : g == 1 ? v[1] : g == 2 ? v[2] : v[3]) >= 0;
-                int word = 0;
-                unsigned left = have ? words[0] : 0u;
-                auto take = [&]() {                                 // the next candidate, -1 beyond the last
-                    while (!left && have && word + 1 < KB) left = words[++word];
-                    if (!left) return -1;
-                    const int p = __ffs(left) - 1;
-                    left &= left - 1u;
-                    return 32 * word + 8 * ((p & 15) >> 2) + 4 * (p >> 4) + (p & 3);
-                };
+            unsigned open = (unsigned)__ballot(live && count != 1u);
+            if (open) {
+                uint32_t left[W];
                 float least = inf, second = inf;
-                int at = 0;
-                for (int k0 = take(); __ballot(k0 >= 0); k0 = take()) {
-                    const int k1 = take();
-                    float d0, d1;
-                    distances(k0, k1, d0, d1);
-                    second = d0 < least ? least : fminf(second, d0);
-                    if (d0 < least) { least = d0; at = k0; }
-                    second = d1 < least ? least : fminf(second, d1);
-                    if (d1 < least) { least = d1; at = k1; }
-                }
-                const unsigned long long unsure = __ballot(!(least * (1.f + eta) < second * (1.f - eta) && second > 1e-25f));
+                const bool amb = (open >> r) & 1u;
 #pragma unroll
-                for (int j = 0; j < kTileBatch; ++j) {
-                    const int decided = __builtin_amdgcn_readlane(at, 16 * j);
-                    if (v[j] >= 0 && ((unsure >> (16 * j)) & 1ull)) hard |= 1u << v[j];
-                    if (r == v[j]) place = decided;
-                }
-                wave_lds_fence();
-            }
-            while (hard) {                                          // one after another in 64 bits, by the whole wave
-                const int which = __ffs(hard) - 1;
-                hard &= hard - 1u;
-                if (r == which) {
+                for (int i = 0; i < W; ++i) left[i] = mk[i];
+                unsigned todo = open;
+                while (todo) {
+                    int v[kTileBatch];
+                    unsigned from = todo;
 #pragma unroll
-                    for (int s = 0; s < S; ++s) reinterpret_cast<float4 *>(rows)[2 * s + hh] = x[s];
-                }
-                wave_lds_fence();
-                uint32_t halves[2][W];
-#pragma unroll
-                for (int i = 0; i < W; ++i) {
-                    halves[0][i] = (uint32_t)__builtin_amdgcn_readlane((int)mk[i], which);
-                    halves[1][i] = (uint32_t)__builtin_amdgcn_readlane((int)mk[i], which + 32);
-                }
-                double db = __builtin_inf();
-                int kb = 0x7fffffff, pb = 0;
-#pragma unroll
-                for (int i = 0; i < W; ++i) {
-                    const int p = 64 * i + lane, bit = 16 * (lane >> 5) + 4 * ((lane & 31) >> 3) + (lane & 3);
-                    if (p >= a.K || !(((lane & 4 ? halves[1][i] : halves[0][i]) >> bit) & 1u)) continue;
-                    const float *cw = Cm + (size_t)p * Dp;
-                    double t = 0.0;
-                    for (int d = 0; d < Dp; ++d) {
-                        const double u = (double)rows[d] - (double)cw[d];
-                        t += u * u;
+                    for (int j = 0; j < kTileBatch; ++j) {
+                        v[j] = from ? __ffs(from) - 1 : -1;
+                        from &= from - 1u;
                     }
-                    const int k = order[p];
-                    if (t < db || (t == db && k < kb)) { db = t; kb = k; pb = p; }
-                }
+                    const int to = r == v[0] ? 0 : r == v[1] ? 1 : r == v[2] ? 2 : r == v[3] ? 3 : -1;
+                    if (to >= 0) {
 #pragma unroll
-                for (int o = 32; o > 0; o >>= 1) {
-                    const double od = __shfl_xor(db, o, kWave);
-                    const int ok = __shfl_xor(kb, o, kWave), op = __shfl_xor(pb, o, kWave);
-                    if (od < db || (od == db && ok < kb)) { db = od; kb = ok; pb = op; }
+                        for (int s = 0; s < S; ++s) reinterpret_cast<float4 *>(rows + to * 64 * NC)[2 * s + hh] = x[s];
+                    }
+                    wave_lds_fence();
+                    int k0 = 256, k1 = 256;
+#pragma unroll
+                    for (int j = 0; j < kTileBatch; ++j) {
+                        const int f = __builtin_amdgcn_readlane(front, max(v[j], 0)), l = __builtin_amdgcn_readlane(back, max(v[j], 0));
+                        if (g == j && v[j] >= 0) {
+                            k0 = f;
+                            k1 = l;
+                        }
+                    }
+                    const bool one = k0 < a.K, two = one && k1 != k0 && k1 < a.K;
+                    const unsigned o0 = (unsigned)((one ? k0 : 0) * Dp), o1 = (unsigned)((two ? k1 : 0) * Dp);
+                    float d0 = 0.f, d1 = 0.f;
+#pragma unroll
+                    for (int i = 0; i < NC; ++i) {
+                        const int p = sub + 16 * i;
+                        const float4 c0 = reinterpret_cast<const float4 *>(Cm + o0)[p], c1 = reinterpret_cast<const float4 *>(Cm + o1)[p];
+                        const float4 w = reinterpret_cast<const float4 *>(rows + g * 64 * NC)[p];
+                        const float e0 = w.x - c0.x, e1 = w.y - c0.y, e2 = w.z - c0.z, e3 = w.w - c0.w;
+                        const float f0 = w.x - c1.x, f1 = w.y - c1.y, f2 = w.z - c1.z, f3 = w.w - c1.w;
+                        d0 = fmaf(e3, e3, fmaf(e2, e2, fmaf(e1, e1, fmaf(e0, e0, d0))));
+                        d1 = fmaf(f3, f3, fmaf(f2, f2, fmaf(f1, f1, fmaf(f0, f0, d1))));
+                    }
+                    d0 = sum16(d0);
+                    d1 = sum16(d1);
+                    if (!one) d0 = inf;
+                    if (!two) d1 = inf;
+                    unsigned through = 0u;
+#pragma unroll
+                    for (int j = 0; j < kTileBatch; ++j) {
+                        const float t0 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(d0), 16 * j)), t1 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(d1), 16 * j));
+                        if (r == v[j]) {
+                            second = t0 < least ? least : fminf(second, t0);
+                            if (t0 < least) { least = t0; place = front; }
+                            second = t1 < least ? least : fminf(second, t1);
+                            if (t1 < least) { least = t1; place = back; }
+                        }
+                        if (v[j] >= 0) through |= 1u << v[j];
+                    }
+                    // the two are done with
+                    if (to >= 0) {
+#pragma unroll
+                        for (int i = 0; i < W; ++i) {
+                            const int f = front - 64 * i, l = back - 64 * i;
+                            if (f >= 0 && f < 64 && ((f >> 2) & 1) == hh) left[i] &= ~(1u << (4 * (f >> 3) + (f & 3)));
+                            if (l >= 0 && l < 64 && ((l >> 2) & 1) == hh) left[i] &= ~(1u << (4 * (l >> 3) + (l & 3)));
+                        }
+                    }
+                    const unsigned more = ends(left, front, back);
+                    todo &= ~through | (unsigned)__ballot(more != 0u);
+                    wave_lds_fence();
                 }
-                if (r == which) place = pb;
-                wave_lds_fence();
+                const float eta = (float)(4 * NC + 10) * 6.1e-8f;
+                unsigned hard = (unsigned)__ballot(amb && !(least * (1.f + eta) < second * (1.f - eta) && second > 1e-25f));
+                while (hard) {                                      // exact and nearly exact ties, one after another in 64 bits, by the whole wave
+                    const int which = __ffs(hard) - 1;
+                    hard &= hard - 1u;
+                    if (r == which) {
+#pragma unroll
+                        for (int s = 0; s < S; ++s) reinterpret_cast<float4 *>(rows)[2 * s + hh] = x[s];
+                    }
+                    wave_lds_fence();
+                    double db = __builtin_inf();
+                    int kb = 0x7fffffff, pb = 0;
+                    for (int i = 0; i < W; ++i) {
+                        const uint32_t low = (uint32_t)__builtin_amdgcn_readlane((int)mk[i], which), high = (uint32_t)__builtin_amdgcn_readlane((int)mk[i], which + 32);
+                        const int p = 64 * i + lane, bit = 4 * (lane >> 3) + (lane & 3);
+                        if (p >= a.K || !(((lane & 4 ? high : low) >> bit) & 1u)) continue;
+                        const float *cw = Cm + (size_t)p * Dp;
+                        double t = 0.0;
+                        for (int d = 0; d < Dp; ++d) {
+                            const double u = (double)rows[d] - (double)cw[d];
+                            t += u * u;
+                        }
+                        const int k = order[p];
+                        if (t < db || (t == db && k < kb)) { db = t; kb = k; pb = p; }
+                    }
+#pragma unroll
+                    for (int o = 32; o > 0; o >>= 1) {
+                        const double od = __shfl_xor(db, o, kWave);
+                        const int ok = __shfl_xor(kb, o, kWave), op = __shfl_xor(pb, o, kWave);
+                        if (od < db || (od == db && ok < kb)) { db = od; kb = ok; pb = op; }
+                    }
+                    if (r == which) place = pb;
+                    wave_lds_fence();
+                }
+                // rows whose nearest is not the first candidate: their codewords again
+                const int now0 = __shfl(place, row4, kWave), now1 = __shfl(place, row4 + 16, kWave);
+                const floatv4 *c0 = codeword4(now0), *c1 = codeword4(now1);
+                if (now0 != p0) {
+#pragma unroll
+                    for (int t = 0; t < T; ++t) q0[t] = c0[4 * t];
+                }
+                if (now1 != p1) {
+#pragma unroll
+                    for (int t = 0; t < T; ++t) q1[t] = c1[4 * t];
+                }
             }
             if (live && hh == 0) a.codes[(slot * a.H + h) * a.M + m] = order[place];
-            // The codewords to subtract: four lanes read 64 bytes of one, and a piece of 16 positions of all rows goes round through LDS to
-            // the lanes that hold the rows.  (A lane that reads its own row's codeword touches a cache line of its own.)
+            // a piece of 16 positions of all rows goes round through LDS to the lanes that hold the rows
             {
-                const int row = lane >> 2, piece = lane & 3;
-                const int p0 = __shfl(place, row, kWave), p1 = __shfl(place, row + 16, kWave);
-                const unsigned o0 = (unsigned)(p0 * Dp + 4 * piece), o1 = (unsigned)(p1 * Dp + 4 * piece);
-                float4 q0[T], q1[T];
+                floatv4 *around = reinterpret_cast<floatv4 *>(stretch);     // [32 rows][4 pieces], a piece at its number xor (row / 4) % 4
+                const int in = 4 * row4 + (piece4 ^ ((row4 >> 2) & 3)), out = 4 * r, turn_of = (r >> 2) & 3;
+                around[in] = q0[0];
+                around[in + 64] = q1[0];
 #pragma unroll
                 for (int t = 0; t < T; ++t) {
-                    q0[t] = q1[t] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (16 * t < D) {
-                        q0[t] = *reinterpret_cast<const float4 *>(Cm + o0 + 16 * t);
-                        q1[t] = *reinterpret_cast<const float4 *>(Cm + o1 + 16 * t);
+                    wave_lds_fence();
+                    const floatv4 u = around[out + (hh ^ turn_of)], w = around[out + ((2 + hh) ^ turn_of)];
+                    wave_lds_fence();
+                    if (t + 1 < T) {                                // behind the reads: a wave's LDS operations stay in order
+                        around[in] = q0[t + 1];
+                        around[in + 64] = q1[t + 1];
                     }
+                    x[2 * t] = make_float4(x[2 * t].x - u.x, x[2 * t].y - u.y, x[2 * t].z - u.z, x[2 * t].w - u.w);
+                    x[2 * t + 1] = make_float4(x[2 * t + 1].x - w.x, x[2 * t + 1].y - w.y, x[2 * t + 1].z - w.z, x[2 * t + 1].w - w.w);
                 }
-                float4 *around = reinterpret_cast<float4 *>(stretch);   // [32 rows][4 pieces], a piece at its number xor (row / 4) % 4
-                const int in = 4 * row + (piece ^ ((row >> 2) & 3)), out = 4 * r, turn_of = (r >> 2) & 3;
-#pragma unroll
-                for (int t = 0; t < T; ++t) {
-                    if (16 * t < D) {
-                        around[in] = q0[t];
-                        around[in + 64] = q1[t];
-                        wave_lds_fence();
-                        const float4 u = around[out + (hh ^ turn_of)], w = around[out + ((2 + hh) ^ turn_of)];
-                        x[2 * t] = make_float4(x[2 * t].x - u.x, x[2 * t].y - u.y, x[2 * t].z - u.z, x[2 * t].w - u.w);
-                        x[2 * t + 1] = make_float4(x[2 * t + 1].x - w.x, x[2 * t + 1].y - w.y, x[2 * t + 1].z - w.z, x[2 * t + 1].w - w.w);
-                        wave_lds_fence();
-                    }
-                }
+                wave_lds_fence();
             }
         }
         job = after;

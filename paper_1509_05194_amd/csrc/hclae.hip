@@ -2143,8 +2143,6 @@ static bool apart(int64_t n, int H, int D, int64_t row_stride, int64_t head_stri
     return (row_stride - D) / (H - 1) >= head_stride || (head_stride - D) / (n - 1) >= row_stride;
 }
 
-// 64-dim chunks of a cache's rows: 1, 2 or 4.
-static int cache_chunks(int D) { return D <= 64 ? 1 : D <= 128 ? 2 : 4; }
 // Rows of all heads up to which k_cache_write_few takes them.
 constexpr int64_t kFewRows = 2048;
 
@@ -2226,12 +2224,12 @@ static int launch_cache_write_rows(hclae_ctx *ctx, const CacheRowsIn &a)
 template <int KB, int NC>
 static int launch_cache_write_tiles(hclae_ctx *ctx, const CacheRowsIn &a)
 {
-    constexpr int UNITS = KB * NC > 16 ? 2 : 1, WAVES = 4;
+    constexpr int UNITS = KB * NC > 16 ? 2 : 1, WAVES = NC == 4 ? 4 : 8;
     constexpr size_t lds = (size_t)tile_lds(KB / UNITS, NC, WAVES).total;
-    static_assert(lds <= (size_t)kLdsBudget / (NC == 4 ? 1 : 2), "two blocks a CU where rows are short");
+    static_assert(lds <= (size_t)kLdsBudget, "a part and the next fit LDS");
     auto kern = &k_cache_write_tiles<KB, NC, UNITS, WAVES>;
     HIP_TRY(ctx, hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBudget));
-    const int64_t groups = (a.n + kTileVec * WAVES - 1) / (kTileVec * WAVES), per_xcd = (groups * a.H + 7) / 8, most = std::max(1, (NC == 4 ? 1 : 2) * ctx->cus / 8);
+    const int64_t groups = (a.n + kTileVec * WAVES - 1) / (kTileVec * WAVES), per_xcd = (groups * a.H + 7) / 8, most = std::max(1, ctx->cus / 8);
     hipLaunchKernelGGL(kern, dim3((unsigned)(8 * std::min(per_xcd, most))), dim3(64 * WAVES), lds, ctx->stream, a, ctx->cache_tab, (int)groups);
     HIP_TRY(ctx, hipGetLastError());
     return HCLAE_OK;
