@@ -224,13 +224,29 @@ __global__ __launch_bounds__(kFewThreads) void k_cache_write_few(const CacheRows
 // Coordinates are laid out so that a lane's eight of a matrix instruction lie side by side in memory: position 16 t + 4 i .. + 3
 // holds the coordinates 16 t + 4 j .. + 3 with j = 0, 2, 1, 3 for i = 0, 1, 2, 3.
 struct CacheTables {
-    const char *img;                                // [H M] as k_encode_prep lays them out, of the sorted codewords
-    const float *hn, *negmu, *consts;
-    const unsigned *pairs;                          // [H M][32 KB] fp16 {2^-10, w_k}
-    const float *w;                                 // [H M][KB] the largest w of a block
+    const char *parts;                              // [H M][UNITS]: what passes through LDS, as TilePart says
     const float *C;                                 // [H M][K][Dp] sorted, positions in place of coordinates, zero beyond D
     const uint8_t *order;                           // [H M][256]: the codeword at a place
 };
+
+// A part of a dictionary (all of it, or half of its blocks): the fp16 image, -||C||^2/2, fp16 {2^-10, w_k}, -mu, the largest w of each
+// block, the constants; whole kilobytes.
+struct TilePart {
+    int image, hn, pairs, mu, w, consts, bytes;     // byte offsets, but for the first and the last
+};
+__host__ __device__ constexpr TilePart tile_part(int kbu, int nc)
+{
+    TilePart p = {};
+    p.image = kbu * nc * 4096;
+    p.hn = p.image;
+    p.pairs = p.hn + 128 * kbu;
+    p.mu = p.pairs + 128 * kbu;
+    p.w = p.mu + 256 * nc;
+    p.consts = p.w + 32;
+    p.bytes = (p.consts + 4 * kEncodeConsts + 1023) / 1024 * 1024;
+    return p;
+}
+__host__ __device__ constexpr int tile_units(int kb, int nc) { return kb * nc > 16 ? 2 : 1; }
 // 64-position chunks of a row: 1, 2 or 4.
 __host__ __device__ constexpr int cache_chunks(int D) { return D <= 64 ? 1 : D <= 128 ? 2 : 4; }
 __host__ __device__ constexpr int cache_padded(int D) { return 64 * cache_chunks(D); }
@@ -272,41 +288,37 @@ __global__ __launch_bounds__(256) void k_cache_sort(const float *__restrict__ C,
     }
 }
 
-// From wtab [blocks][32]: the pairs, and the largest w of every block.
-__global__ __launch_bounds__(256) void k_cache_w(const float *__restrict__ wtab, int64_t blocks, unsigned *__restrict__ pairs, float *__restrict__ w)
+// The parts, from what k_encode_prep leaves.  A block per part.
+__global__ __launch_bounds__(256) void k_cache_pack(
+    const char *__restrict__ img, const float *__restrict__ hn, const float *__restrict__ wtab, const float *__restrict__ negmu,
+    const float *__restrict__ consts, int kb, int nc, int units, char *__restrict__ parts)
 {
-    const int64_t b = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    float v = b < blocks ? wtab[b * 32 + (threadIdx.x & 31)] : 0.f;
-    if (b < blocks) pairs[b * 32 + (threadIdx.x & 31)] = __builtin_bit_cast(unsigned, (halfx2){(_Float16)0.0009765625f, (_Float16)v});
+    const int set = blockIdx.x / units, u = blockIdx.x - set * units, kbu = kb / units, tid = threadIdx.x;
+    const TilePart p = tile_part(kbu, nc);
+    char *to = parts + (size_t)blockIdx.x * p.bytes;
+    for (int i = tid; i < p.image / 16; i += 256) {
+        const int at = i >> 6, t = at / kbu, b = at - t * kbu;      // kilobyte (t, b)
+        reinterpret_cast<uint4 *>(to)[i] = reinterpret_cast<const uint4 *>(img + ((size_t)set * 4 * nc * kb + t * kb + u * kbu + b) * 1024)[i & 63];
+    }
+    const size_t first = (size_t)set * 32 * kb + u * 32 * kbu;
+    if (tid < 32 * kbu) {
+        const float w = wtab[first + tid];
+        reinterpret_cast<float *>(to + p.hn)[tid] = hn[first + tid];
+        reinterpret_cast<unsigned *>(to + p.pairs)[tid] = __builtin_bit_cast(unsigned, (halfx2){(_Float16)0.0009765625f, (_Float16)w});
+        float most = w;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, kWave));
-    if (b < blocks && (threadIdx.x & 31) == 0) w[b] = v;
+        for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o, kWave));
+        if ((tid & 31) == 0) reinterpret_cast<float *>(to + p.w)[tid >> 5] = most;
+    }
+    if (tid < 64 * nc) reinterpret_cast<float *>(to + p.mu)[tid] = negmu[(size_t)set * 64 * nc + tid];
+    if (tid < kEncodeConsts) reinterpret_cast<float *>(to + p.consts)[tid] = consts[(size_t)set * kEncodeConsts + tid];
 }
 
-// LDS of k_cache_write_tiles: a dictionary (or half of one) and the next, and a stretch for every wave: four undecided rows, or a piece of 16
-// positions of the codewords to subtract.
+// LDS of k_cache_write_tiles: a part and the next, and a stretch for every wave: four undecided rows, or a piece of 16 positions of the
+// codewords to subtract.
 constexpr int kTileBatch = 4;                       // undecided rows of a wave at a time, sixteen lanes each
-struct TileLds {
-    int unit, half;                                 // bytes of an image, and of a half with its tables
-    int hn, pairs, mu, w, consts;                   // byte offsets in a half, behind the image
-    int rows, total;                                // byte offsets
-    int stretch;
-};
-__host__ __device__ constexpr TileLds tile_lds(int kbu, int nc, int waves)
-{
-    TileLds l = {};
-    l.unit = kbu * nc * 4096;
-    l.stretch = nc == 4 ? 4096 : 2048;
-    l.hn = l.unit;
-    l.pairs = l.hn + 128 * kbu;
-    l.mu = l.pairs + 128 * kbu;
-    l.w = l.mu + 256 * nc;
-    l.consts = l.w + 32;
-    l.half = l.consts + 4 * kEncodeConsts;
-    l.rows = 2 * l.half;
-    l.total = l.rows + waves * l.stretch;
-    return l;
-}
+__host__ __device__ constexpr int tile_stretch(int nc) { return nc == 4 ? 4096 : 2048; }
+__host__ __device__ constexpr int tile_lds(int kbu, int nc, int waves) { return 2 * tile_part(kbu, nc).bytes + waves * tile_stretch(nc); }
 
 typedef float floatv4 __attribute__((ext_vector_type(4)));
 
@@ -328,7 +340,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void k_cache_write_tiles(con
     extern __shared__ float4 smem4[];
     char *lds = reinterpret_cast<char *>(smem4);
     constexpr int KBU = KB / UNITS, T = 4 * NC, S = 8 * NC, W = (KB + 1) / 2;
-    constexpr TileLds L = tile_lds(KBU, NC, WAVES);
+    constexpr TilePart L = tile_part(KBU, NC);
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5, r = lane & 31;
     const float inf = __builtin_inff();
     const int D = a.D;
@@ -341,28 +353,18 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void k_cache_write_tiles(con
         const int job = (int)(blockIdx.x & 7) * per_xcd + j;
         return j < per_xcd && job < jobs ? job : -1;
     };
-    // part u of dictionary `set` into a half of LDS, all waves together
+    // part u of dictionary `set` into a half of LDS, a share for every wave
     auto stage = [&](int set, int u, int half) {
-        char *to = lds + half * L.half;
-        const char *from = tab.img + (size_t)set * UNITS * L.unit + u * KBU * 1024 + 16 * lane;
-        constexpr int pieces = L.unit / 1024;       // kilobytes (t, b)
+        const char *from = tab.parts + ((size_t)set * UNITS + u) * L.bytes + 16 * lane;
+        char *to = lds + half * L.bytes;
 #pragma unroll 1
-        for (int at = wave; at < pieces; at += WAVES) load_to_lds(from + (at / KBU * KB + at % KBU) * 1024, to + at * 1024);
-        const int tid = threadIdx.x;
-        if (tid < 32 * KBU) {
-            reinterpret_cast<float *>(to + L.hn)[tid] = tab.hn[(size_t)set * 32 * KB + u * 32 * KBU + tid];
-            reinterpret_cast<unsigned *>(to + L.pairs)[tid] = tab.pairs[(size_t)set * 32 * KB + u * 32 * KBU + tid];
-        }
-        if (tid < 64 * NC) reinterpret_cast<float *>(to + L.mu)[tid] = tab.negmu[(size_t)set * 64 * NC + tid];
-        if (tid < KBU) reinterpret_cast<float *>(to + L.w)[tid] = tab.w[(size_t)set * KB + u * KBU + tid];
-        if (tid >= 64 && tid < 64 + kEncodeConsts) reinterpret_cast<float *>(to + L.consts)[tid - 64] = tab.consts[(size_t)set * kEncodeConsts + tid - 64];
+        for (int at = wave * 1024; at < L.bytes; at += WAVES * 1024) load_to_lds(from + at, to + at);
     };
-    static_assert(64 * WAVES >= 32 * KBU && 64 * WAVES >= 64 * NC, "a thread per entry");
     auto landed = [&]() {
         __builtin_amdgcn_s_waitcnt(0x0f70);         // vmcnt(0)
         __syncthreads();
     };
-    char *stretch = lds + L.rows + wave * L.stretch;
+    char *stretch = lds + 2 * L.bytes + wave * tile_stretch(NC);
     int job = job_of(0), half = 1;
     if (job < 0) return;                            // the whole block
     stage(job / groups * a.M, 0, 0);
@@ -423,7 +425,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void k_cache_write_tiles(con
             for (int u = 0; u < UNITS; ++u) {
                 landed();                                           // this part is there, and nobody needs the one before
                 half ^= 1;
-                const char *now = lds + half * L.half;
+                const char *now = lds + half * L.bytes;
                 const bool last = u == UNITS - 1 && m == a.M - 1;
                 if (!last || after >= 0) stage(last ? after / groups * a.M : u == UNITS - 1 ? set + 1 : set, u == UNITS - 1 ? 0 : u + 1, half ^ 1);
                 if (active) {
@@ -436,13 +438,22 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void k_cache_write_tiles(con
                         c.acc = cc[3];
                         c.hx = cc[4];
                         c.cmax = cc[5];
-                        const float4 *mu4 = reinterpret_cast<const float4 *>(now + L.mu) + hh;
+                        const floatv4 *mu4 = reinterpret_cast<const floatv4 *>(now + L.mu) + hh;
                         float xsq = 0.f, dsq = 0.f;
 #pragma unroll
-                        for (int t = 0; t < T; ++t) {
-                            const halfx4 lo = half4(scaled(x[2 * t], c.scale, mu4[4 * t]), xsq, dsq);
-                            const halfx4 hi = half4(scaled(x[2 * t + 1], c.scale, mu4[4 * t + 2]), xsq, dsq);
-                            frag[t] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                        for (int t0 = 0; t0 < T; t0 += 4) {         // eight reads of LDS on their way at a time
+                            floatv4 mu[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) mu[i] = mu4[4 * t0 + 2 * i];
+                            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const int t = t0 + i;
+                                const floatv4 a = mu[2 * i], b = mu[2 * i + 1];
+                                const halfx4 lo = half4(scaled(x[2 * t], c.scale, make_float4(a.x, a.y, a.z, a.w)), xsq, dsq);
+                                const halfx4 hi = half4(scaled(x[2 * t + 1], c.scale, make_float4(b.x, b.y, b.z, b.w)), xsq, dsq);
+                                frag[t] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                            }
                         }
                         const uint2 s2 = both_halves(__float_as_uint(xsq)), d2 = both_halves(__float_as_uint(dsq));
                         x2 = __uint_as_float(s2.x) + __uint_as_float(s2.y);
@@ -458,7 +469,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void k_cache_write_tiles(con
                     for (int t = 0; t < 4; ++t) slot_of[t] = now + half_slot(t, hh, r);
                     constexpr int GB = KBU < 2 ? 1 : 2;             // blocks whose products run together
                     // the dictionary's operands are read P products ahead, in an order that the scheduler may not change (contract_half)
-                    constexpr int N = KBU * T, P = N < 6 ? N : 6;
+                    constexpr int N = KBU * T, P = N < 4 ? N : 4;
                     auto operand = [&](int i) {
                         const int t = i % (T * GB) / GB, b = i / (T * GB) * GB + i % GB;
                         return *reinterpret_cast<const halfx8 *>(slot_of[t & 3] + (t * KBU + b) * 1024);
@@ -466,25 +477,25 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void k_cache_write_tiles(con
                     halfx8 ahead[P];
 #pragma unroll
                     for (int i = 0; i < P; ++i) ahead[i] = operand(i);
+                    constexpr int PAIRS = KBU / GB;
+                    floatx16 acc[GB];
+                    halfx4 right;
+                    auto products = [&](int p) {
 #pragma unroll
-                    for (int b0 = 0; b0 < KBU; b0 += GB) {
-                        floatx16 acc[GB];
-                        init_acc<GB>(acc, lds_h + 32 * b0, hh);
-#pragma unroll
-                        for (int t = 0; t < T; ++t)
-#pragma unroll
-                            for (int b = 0; b < GB; ++b) {
-                                const int i = b0 * T + t * GB + b;
-                                acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ahead[i % P], frag[t], acc[b], 0, 0, 0);
-                                if (i + P < N) ahead[i % P] = operand(i + P);
-                                __builtin_amdgcn_sched_barrier(0x6);        // arithmetic may pass, products and memory not
-                            }
-                        const int i = (u * KBU + b0) / 2;
+                        for (int j = 0; j < T * GB; ++j) {
+                            const int i = p * T * GB + j, b = j % GB, t = j / GB;
+                            acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ahead[i % P], frag[t], acc[b], 0, 0, 0);
+                            if (i + P < N) ahead[i % P] = operand(i + P);
+                            __builtin_amdgcn_sched_barrier(0x6);            // arithmetic may pass, products and memory not
+                        }
+                    };
+                    auto threshold = [&](int p) {
+                        const int i = (u * KBU + p * GB) / 2;
                         float low = -inf;
                         top[i] = -inf;
 #pragma unroll
                         for (int b = 0; b < GB; ++b) {
-                            const float most = block_max(acc[b]), w = lds_w[b0 + b];
+                            const float most = block_max(acc[b]), w = lds_w[p * GB + b];
                             low = __builtin_elementwise_maximum(low, fmaf(-e, w, most));
                             top[i] = __builtin_elementwise_maximum(top[i], fmaf(e, w, most));
                         }
@@ -495,17 +506,32 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void k_cache_write_tiles(con
                         const _Float16 p0 = (_Float16)(thr * -0.0009765625f);
                         const float rest = fmaf((float)p0, -1024.f, -thr);
                         const _Float16 p1 = (_Float16)rest;
-                        halfx4 right = {p0, p1, (_Float16)((rest - (float)p1) * 1024.f), (_Float16)e};
+                        right = (halfx4){p0, p1, (_Float16)((rest - (float)p1) * 1024.f), (_Float16)e};
                         if (hh) right = (halfx4){(_Float16)0.f, (_Float16)0.f, (_Float16)0.f, (_Float16)0.f};
+                    };
+                    auto subtract = [&](int p) {
+#pragma unroll
+                        for (int b = 0; b < GB; ++b) {
+                            const uint2 left = make_uint2(__builtin_bit_cast(unsigned, (halfx2){(_Float16)1024.f, (_Float16)1.f}), lds_pair[32 * (p * GB + b) + r]);
+                            acc[b] = __builtin_amdgcn_mfma_f32_32x32x8f16(__builtin_bit_cast(halfx4, left), right, acc[b], 0, 0, 0);
+                        }
+                        __builtin_amdgcn_sched_barrier(0x6);
+                    };
+                    auto reached = [&](int p) {
                         uint32_t word = 0u;
 #pragma unroll
-                        for (int b = GB - 1; b >= 0; --b) {
-                            const uint2 left = make_uint2(__builtin_bit_cast(unsigned, (halfx2){(_Float16)1024.f, (_Float16)1.f}), lds_pair[32 * (b0 + b) + r]);
-                            acc[b] = __builtin_amdgcn_mfma_f32_32x32x8f16(__builtin_bit_cast(halfx4, left), right, acc[b], 0, 0, 0);
+                        for (int b = GB - 1; b >= 0; --b)
 #pragma unroll
-                            for (int v = 15; v >= 0; --v) word = __builtin_amdgcn_alignbit(word, __float_as_uint(acc[b][v]), 31);     // (word << 1) | sign
-                        }
-                        mk[i] = KB == 1 ? ~word & 0xffffu : ~word;
+                            for (int v = 15; v >= 0; --v) word = __builtin_amdgcn_alignbit(word, __float_as_uint(acc[b][v]), 31);  // (word << 1) | sign
+                        mk[(u * KBU + p * GB) / 2] = KB == 1 ? ~word & 0xffffu : ~word;
+                    };
+#pragma unroll
+                    for (int p = 0; p < PAIRS; ++p) {
+                        init_acc<GB>(acc, lds_h + 32 * GB * p, hh);
+                        products(p);
+                        threshold(p);
+                        subtract(p);
+                        reached(p);
                     }
                 }
             }
@@ -549,67 +575,74 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void k_cache_write_tiles(con
             int place = front < a.K ? front : 0;
             const float *Cm = tab.C + (size_t)set * a.K * Dp;
             const uint8_t *order = tab.order + (size_t)set * 256;
-            // The first candidates' codewords are sent for at once, four lanes reading 64 bytes of one.  (A lane that reads its own row's codeword
-            // touches a cache line of its own.)
+            // Undecided rows, four at a time, sixteen lanes each: two candidates a round in fp32, which decides where the two nearest are further
+            // apart than its error.  Their codewords are sent for before all others.
+            const int g = lane >> 4, sub = lane & 15;
+            float *rows = reinterpret_cast<float *>(stretch);
+            const unsigned open = (unsigned)__ballot(live && count != 1u);
+            int v[kTileBatch];                                      // the rows of a batch, -1: none
+            bool one = false, two = false;                          // the lanes' row has one candidate, two
+            floatv4 c0[NC], c1[NC];
+            auto batch = [&](unsigned todo) {
+#pragma unroll
+                for (int j = 0; j < kTileBatch; ++j) {
+                    v[j] = todo ? __ffs(todo) - 1 : -1;
+                    todo &= todo - 1u;
+                }
+                int k0 = 256, k1 = 256;
+#pragma unroll
+                for (int j = 0; j < kTileBatch; ++j) {
+                    const int f = __builtin_amdgcn_readlane(front, max(v[j], 0)), l = __builtin_amdgcn_readlane(back, max(v[j], 0));
+                    if (g == j && v[j] >= 0) {
+                        k0 = f;
+                        k1 = l;
+                    }
+                }
+                one = k0 < a.K;
+                two = one && k1 != k0 && k1 < a.K;
+                const floatv4 *at0 = reinterpret_cast<const floatv4 *>(Cm + (unsigned)((one ? k0 : 0) * Dp)) + sub;
+                const floatv4 *at1 = reinterpret_cast<const floatv4 *>(Cm + (unsigned)((two ? k1 : 0) * Dp)) + sub;
+#pragma unroll
+                for (int i = 0; i < NC; ++i) {
+                    c0[i] = at0[16 * i];
+                    c1[i] = at1[16 * i];
+                }
+            };
+            if (open) batch(open);
+            // The first candidates' codewords: four lanes read 64 bytes of one.  (A lane that reads its own row's codeword touches a cache
+            // line of its own.)
             const int row4 = lane >> 2, piece4 = lane & 3;
-            int p0 = __shfl(place, row4, kWave), p1 = __shfl(place, row4 + 16, kWave);
+            const int p0 = __shfl(place, row4, kWave), p1 = __shfl(place, row4 + 16, kWave);
             floatv4 q0[T], q1[T];
             auto codeword4 = [&](int p) { return reinterpret_cast<const floatv4 *>(Cm + (unsigned)(p * Dp + 4 * piece4)); };
             {
-                const floatv4 *c0 = codeword4(p0), *c1 = codeword4(p1);
+                const floatv4 *first0 = codeword4(p0), *first1 = codeword4(p1);
 #pragma unroll
                 for (int t = 0; t < T; ++t) {
-                    q0[t] = c0[4 * t];
-                    q1[t] = c1[4 * t];
+                    q0[t] = first0[4 * t];
+                    q1[t] = first1[4 * t];
                 }
             }
-            // Undecided rows, four at a time, sixteen lanes each: two candidates a round in fp32, which decides where the two nearest are further
-            // apart than its error.
-            const int g = lane >> 4, sub = lane & 15;
-            float *rows = reinterpret_cast<float *>(stretch);
-            unsigned open = (unsigned)__ballot(live && count != 1u);
             if (open) {
                 uint32_t left[W];
                 float least = inf, second = inf;
                 const bool amb = (open >> r) & 1u;
 #pragma unroll
                 for (int i = 0; i < W; ++i) left[i] = mk[i];
-                unsigned todo = open;
+                unsigned todo = open, more = count;
                 while (todo) {
-                    int v[kTileBatch];
-                    unsigned from = todo;
-#pragma unroll
-                    for (int j = 0; j < kTileBatch; ++j) {
-                        v[j] = from ? __ffs(from) - 1 : -1;
-                        from &= from - 1u;
-                    }
                     const int to = r == v[0] ? 0 : r == v[1] ? 1 : r == v[2] ? 2 : r == v[3] ? 3 : -1;
                     if (to >= 0) {
 #pragma unroll
                         for (int s = 0; s < S; ++s) reinterpret_cast<float4 *>(rows + to * 64 * NC)[2 * s + hh] = x[s];
                     }
                     wave_lds_fence();
-                    int k0 = 256, k1 = 256;
-#pragma unroll
-                    for (int j = 0; j < kTileBatch; ++j) {
-                        const int f = __builtin_amdgcn_readlane(front, max(v[j], 0)), l = __builtin_amdgcn_readlane(back, max(v[j], 0));
-                        if (g == j && v[j] >= 0) {
-                            k0 = f;
-                            k1 = l;
-                        }
-                    }
-                    const bool one = k0 < a.K, two = one && k1 != k0 && k1 < a.K;
-                    const unsigned o0 = (unsigned)((one ? k0 : 0) * Dp), o1 = (unsigned)((two ? k1 : 0) * Dp);
                     float d0 = 0.f, d1 = 0.f;
 #pragma unroll
                     for (int i = 0; i < NC; ++i) {
-                        const int p = sub + 16 * i;
-                        const float4 c0 = reinterpret_cast<const float4 *>(Cm + o0)[p], c1 = reinterpret_cast<const float4 *>(Cm + o1)[p];
-                        const float4 w = reinterpret_cast<const float4 *>(rows + g * 64 * NC)[p];
-                        const float e0 = w.x - c0.x, e1 = w.y - c0.y, e2 = w.z - c0.z, e3 = w.w - c0.w;
-                        const float f0 = w.x - c1.x, f1 = w.y - c1.y, f2 = w.z - c1.z, f3 = w.w - c1.w;
-                        d0 = fmaf(e3, e3, fmaf(e2, e2, fmaf(e1, e1, fmaf(e0, e0, d0))));
-                        d1 = fmaf(f3, f3, fmaf(f2, f2, fmaf(f1, f1, fmaf(f0, f0, d1))));
+                        const floatv4 w = reinterpret_cast<const floatv4 *>(rows + g * 64 * NC)[sub + 16 * i], e = w - c0[i], f = w - c1[i];
+                        d0 = fmaf(e.w, e.w, fmaf(e.z, e.z, fmaf(e.y, e.y, fmaf(e.x, e.x, d0))));
+                        d1 = fmaf(f.w, f.w, fmaf(f.z, f.z, fmaf(f.y, f.y, fmaf(f.x, f.x, d1))));
                     }
                     d0 = sum16(d0);
                     d1 = sum16(d1);
@@ -628,7 +661,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void k_cache_write_tiles(con
                         if (v[j] >= 0) through |= 1u << v[j];
                     }
                     // the two are done with
-                    if (to >= 0) {
+                    const bool all = !__ballot(to >= 0 && more > 2u);
+                    if (!all && to >= 0) {
 #pragma unroll
                         for (int i = 0; i < W; ++i) {
                             const int f = front - 64 * i, l = back - 64 * i;
@@ -636,8 +670,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void k_cache_write_tiles(con
                             if (l >= 0 && l < 64 && ((l >> 2) & 1) == hh) left[i] &= ~(1u << (4 * (l >> 3) + (l & 3)));
                         }
                     }
-                    const unsigned more = ends(left, front, back);
-                    todo &= ~through | (unsigned)__ballot(more != 0u);
+                    if (!all) more = ends(left, front, back);
+                    todo &= all ? ~through : ~through | (unsigned)__ballot(more != 0u);
+                    if (todo) batch(todo);
                     wave_lds_fence();
                 }
                 const float eta = (float)(4 * NC + 10) * 6.1e-8f;
@@ -676,14 +711,14 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void k_cache_write_tiles(con
                 }
                 // rows whose nearest is not the first candidate: their codewords again
                 const int now0 = __shfl(place, row4, kWave), now1 = __shfl(place, row4 + 16, kWave);
-                const floatv4 *c0 = codeword4(now0), *c1 = codeword4(now1);
+                const floatv4 *other0 = codeword4(now0), *other1 = codeword4(now1);
                 if (now0 != p0) {
 #pragma unroll
-                    for (int t = 0; t < T; ++t) q0[t] = c0[4 * t];
+                    for (int t = 0; t < T; ++t) q0[t] = other0[4 * t];
                 }
                 if (now1 != p1) {
 #pragma unroll
-                    for (int t = 0; t < T; ++t) q1[t] = c1[4 * t];
+                    for (int t = 0; t < T; ++t) q1[t] = other1[4 * t];
                 }
             }
             if (live && hh == 0) a.codes[(slot * a.H + h) * a.M + m] = order[place];

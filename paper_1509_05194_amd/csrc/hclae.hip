@@ -2157,16 +2157,18 @@ int hclae_cache_begin(hclae_ctx *ctx, const float *C, int H, int M, int K, int D
     const size_t sets = (size_t)H * M;
     const int columns = few_columns(K), d4 = D / 4, kb = ctx->kb, nc = cache_chunks(D), kpad = 32 * kb;
     auto up = [](size_t b) { return (b + 255) / 256 * 256; };
-    const size_t img_b = sets * nc * kb * 4096, per_codeword_b = up(sets * kpad * sizeof(float)), mu_b = up(sets * kChunkD * nc * sizeof(float)),
-                 consts_b = up(sets * kEncodeConsts * sizeof(float)), w_b = up(sets * kb * sizeof(float)), order_b = sets * 256, C_b = up(sets * K * D * sizeof(float)),
-                 sorted_b = up(sets * K * cache_padded(D) * sizeof(float));
+    const int units = tile_units(kb, nc);
+    const TilePart part = tile_part(kb / units, nc);
+    const size_t parts_b = sets * units * part.bytes, img_b = sets * nc * kb * 4096, per_codeword_b = up(sets * kpad * sizeof(float)),
+                 mu_b = up(sets * kChunkD * nc * sizeof(float)), consts_b = up(sets * kEncodeConsts * sizeof(float)), order_b = sets * 256,
+                 C_b = up(sets * K * D * sizeof(float)), sorted_b = up(sets * K * cache_padded(D) * sizeof(float));
     if (H > ctx->cache_H) {
         float *copy = nullptr;
         float4 *T = nullptr;
         char *buf = nullptr;
         hipError_t e = hipMalloc((void **)&copy, C_b);
         if (e == hipSuccess) e = hipMalloc((void **)&T, sets * d4 * columns * sizeof(float4));
-        if (e == hipSuccess) e = hipMalloc((void **)&buf, img_b + 3 * per_codeword_b + mu_b + consts_b + w_b + order_b + sorted_b + 256);
+        if (e == hipSuccess) e = hipMalloc((void **)&buf, parts_b + img_b + 2 * per_codeword_b + mu_b + consts_b + order_b + sorted_b + 256);
         if (e != hipSuccess) {
             if (copy) (void)hipFree(copy);
             if (T) (void)hipFree(T);
@@ -2181,17 +2183,16 @@ int hclae_cache_begin(hclae_ctx *ctx, const float *C, int H, int M, int K, int D
     }
     ctx->cache_H = H;
     char *p = ctx->cache_buf;
-    char *img = p;
+    char *parts = p;
+    char *img = p += parts_b;
     float *hn = reinterpret_cast<float *>(p += img_b);
     float *wtab = reinterpret_cast<float *>(p += per_codeword_b);
-    unsigned *pairs = reinterpret_cast<unsigned *>(p += per_codeword_b);
     float *negmu = reinterpret_cast<float *>(p += per_codeword_b);
     float *consts = reinterpret_cast<float *>(p += mu_b);
-    float *w = reinterpret_cast<float *>(p += consts_b);
-    uint8_t *order = reinterpret_cast<uint8_t *>(p += w_b);
+    uint8_t *order = reinterpret_cast<uint8_t *>(p += consts_b);
     float *sorted = reinterpret_cast<float *>(p += order_b);
     unsigned *unused = reinterpret_cast<unsigned *>(p += sorted_b);
-    ctx->cache_tab = {img, hn, negmu, consts, pairs, w, sorted, order};
+    ctx->cache_tab = {parts, sorted, order};
     hipLaunchKernelGGL(k_cache_lay, dim3((unsigned)sets, (unsigned)((d4 + 15) / 16)), dim3(256), 0, ctx->stream, C, K, D, columns, ctx->cache_C, ctx->cache_T);
     HIP_TRY(ctx, hipGetLastError());
     hipLaunchKernelGGL(k_cache_sort, dim3((unsigned)sets), dim3(256), 0, ctx->stream, C, K, D, sorted, order);
@@ -2199,7 +2200,7 @@ int hclae_cache_begin(hclae_ctx *ctx, const float *C, int H, int M, int K, int D
     hipLaunchKernelGGL(k_encode_prep<false>, dim3((unsigned)sets), dim3(kPrepThreads), 0, ctx->stream, sorted, K, cache_padded(D), kb, nc, img, hn, wtab, negmu, consts,
                        (float *)nullptr, unused);
     HIP_TRY(ctx, hipGetLastError());
-    hipLaunchKernelGGL(k_cache_w, dim3((unsigned)((sets * kb + 7) / 8)), dim3(256), 0, ctx->stream, wtab, (int64_t)(sets * kb), pairs, w);
+    hipLaunchKernelGGL(k_cache_pack, dim3((unsigned)(sets * units)), dim3(256), 0, ctx->stream, img, hn, wtab, negmu, consts, kb, nc, units, parts);
     HIP_TRY(ctx, hipGetLastError());
     return HCLAE_OK;
 }
@@ -2224,8 +2225,8 @@ static int launch_cache_write_rows(hclae_ctx *ctx, const CacheRowsIn &a)
 template <int KB, int NC>
 static int launch_cache_write_tiles(hclae_ctx *ctx, const CacheRowsIn &a)
 {
-    constexpr int UNITS = KB * NC > 16 ? 2 : 1, WAVES = NC == 4 ? 4 : 8;
-    constexpr size_t lds = (size_t)tile_lds(KB / UNITS, NC, WAVES).total;
+    constexpr int UNITS = tile_units(KB, NC), WAVES = NC == 4 ? 4 : 8;
+    constexpr size_t lds = (size_t)tile_lds(KB / UNITS, NC, WAVES);
     static_assert(lds <= (size_t)kLdsBudget, "a part and the next fit LDS");
     auto kern = &k_cache_write_tiles<KB, NC, UNITS, WAVES>;
     HIP_TRY(ctx, hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBudget));
