@@ -14,7 +14,7 @@ namespace hclae {
 constexpr int kCacheMaxD = 256;
 constexpr int kFewThreads = 1024;
 
-// Codewords a thread column of k_cache_write_few covers: 64, 128 or 256, and so the threads that share a codeword.
+// Codewords that a block's threads cover side by side: 64, 128 or 256.
 __host__ __device__ constexpr int few_columns(int K) { return K <= 64 ? 64 : K <= 128 ? 128 : 256; }
 
 struct CacheRowsIn {
@@ -33,13 +33,13 @@ __device__ __forceinline__ float4 load_in(const CacheRowsIn &a, int64_t at)
     return a.type == kRowF32 ? F32::load(a.X, at) : a.type == kRowF16 ? F16::load(a.X, at) : Bf16::load(a.X, at);
 }
 
-// The dictionaries as k_cache_write_few reads them: T[dictionary][piece of four coordinates][codeword], so that neighbouring lanes
-// read neighbouring codewords; and a copy as they are.  A block per dictionary and 16 pieces.
-__global__ __launch_bounds__(256) void k_cache_lay(const float *__restrict__ C, int K, int D, int columns, float *__restrict__ copy, float4 *__restrict__ T)
+// The dictionaries as k_cache_write_one and k_cache_write_some read them: T[dictionary][piece of four coordinates][codeword], so that neighbouring lanes
+// read neighbouring codewords, padded with zeros to `pieces`; and a copy as they are.  A block per dictionary and 16 pieces.
+__global__ __launch_bounds__(256) void k_cache_lay(const float *__restrict__ C, int K, int D, int columns, int pieces, float *__restrict__ copy, float4 *__restrict__ T)
 {
     const int d4 = D >> 2;
     const float4 *from = reinterpret_cast<const float4 *>(C + (size_t)blockIdx.x * K * D);
-    float4 *to = T + (size_t)blockIdx.x * d4 * columns;
+    float4 *to = T + (size_t)blockIdx.x * pieces * columns;
     float4 *same = reinterpret_cast<float4 *>(copy + (size_t)blockIdx.x * K * D);
     __shared__ float4 tile[16][17];
     const int i = threadIdx.x & 15, j = threadIdx.x >> 4;
@@ -52,166 +52,366 @@ __global__ __launch_bounds__(256) void k_cache_lay(const float *__restrict__ C, 
         }
         tile[i][j] = v;
         __syncthreads();
-        if (p0 + j < d4) to[(size_t)(p0 + j) * columns + k0 + i] = tile[j][i];
+        to[(size_t)(p0 + j) * columns + k0 + i] = tile[j][i];
         __syncthreads();
     }
 }
 
-// A few rows a head: a block takes R rows of one head through all dictionaries.  Every thread keeps a share of one codeword (its
-// pieces q, q + Q, ...) in registers, the next dictionary's on their way meanwhile; the rows are in LDS, where all lanes read the
-// same piece.  Distances in fp32, direct form, so a vector is hardly ever undecided (gap below some 1e-6); those are decided in 64
-// bits.  The threads that hold the chosen codeword subtract it: no gather, a dictionary is read once.
-template <int COLS, int P, int R>
-__global__ __launch_bounds__(kFewThreads) void k_cache_write_few(const CacheRowsIn a, const float4 *__restrict__ T)
+typedef float floatv4 __attribute__((ext_vector_type(4)));
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_plus(float v)
+{
+    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+// The sum over the sixteen lanes of a row, the same in all of them.
+__device__ __forceinline__ float sum16(float v)
+{
+    return dpp_plus<0x140>(dpp_plus<0x141>(dpp_plus<0x4E>(dpp_plus<0xB1>(v))));     // quad_perm 1 0 3 2, 2 3 0 1, row_half_mirror, row_mirror
+}
+
+// The least of 64 numbers that order as unsigned integers, the same in every lane (see wave_max_int).
+__device__ __forceinline__ unsigned wave_min_bits(unsigned v)
+{
+    v = min(v, (unsigned)__builtin_amdgcn_update_dpp(-1, (int)v, 0x111, 0xf, 0xf, false));   // row_shr:1
+    v = min(v, (unsigned)__builtin_amdgcn_update_dpp(-1, (int)v, 0x112, 0xf, 0xf, false));   // row_shr:2
+    v = min(v, (unsigned)__builtin_amdgcn_update_dpp(-1, (int)v, 0x114, 0xf, 0xf, false));   // row_shr:4
+    v = min(v, (unsigned)__builtin_amdgcn_update_dpp(-1, (int)v, 0x118, 0xf, 0xf, false));   // row_shr:8
+    v = min(v, (unsigned)__builtin_amdgcn_update_dpp(-1, (int)v, 0x142, 0xa, 0xf, false));   // row_bcast:15
+    v = min(v, (unsigned)__builtin_amdgcn_update_dpp(-1, (int)v, 0x143, 0xc, 0xf, false));   // row_bcast:31
+    return (unsigned)__builtin_amdgcn_readlane((int)v, kWave - 1);
+}
+
+// One row of the input into LDS, by a wave: divided by its largest magnitude where scales are kept, zero beyond D up to `padded`.
+__device__ __forceinline__ int64_t take_row(const CacheRowsIn &a, int64_t n, int h, float4 *row, int padded, int lane)
+{
+    const int64_t s = n < a.n ? a.slots[n] : -1;
+    const bool live = s >= 0 && s < a.n_slots;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (live && 4 * lane < a.D) v = load_in(a, n * a.row_stride + h * a.head_stride + 4 * lane);
+    // magnitudes order as integers do, NaN above infinity
+    int top = max(max(__float_as_int(fabsf(v.x)), __float_as_int(fabsf(v.y))), max(__float_as_int(fabsf(v.z)), __float_as_int(fabsf(v.w))));
+    top = wave_max_int(top);
+    float g = __int_as_float(top);
+    if (top >= 0x7f800000) {                        // not a number: kept as a row of zeros whose scale says so
+        v = make_float4(0.f, 0.f, 0.f, 0.f);
+        g = __builtin_nanf("");
+    } else if (a.scale && top) {
+        v = make_float4(v.x / g, v.y / g, v.z / g, v.w / g);
+    }
+    if (4 * lane < padded) row[lane] = v;
+    if (lane == 0 && live && a.scale) a.scale[s * a.H + h] = g;
+    return live ? s : -1;
+}
+
+// A row or few in all: a block takes one row of one head through all dictionaries.  Every thread keeps a share of one codeword (its
+// pieces q, q + Q, ...) in registers, the next dictionary's on their way meanwhile; the row is in LDS, where all lanes read the
+// same piece.  The threads that hold the chosen codeword subtract it: no gather, a dictionary is read once.
+template <int COLS, int P>
+__global__ __launch_bounds__(kFewThreads) void k_cache_write_one(const CacheRowsIn a, const float4 *__restrict__ T)
 {
     constexpr int Q = kFewThreads / COLS;           // threads that share a codeword
-    __shared__ float4 rows[R][kCacheMaxD / 4];
-    __shared__ float part[R][Q][COLS];
-    __shared__ int chosen[R];
-    __shared__ int64_t slot[R];
+    constexpr bool AHEAD = P <= 8;                  // room for the next dictionary's share
+    __shared__ float4 row[kCacheMaxD / 4];
+    __shared__ float part[Q][COLS];
+    __shared__ int chosen;
     const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
     const int k = tid % COLS, q = tid / COLS, d4 = a.D >> 2;
-    const int64_t jobs = (a.n + R - 1) / R * a.H;
+    constexpr size_t SET = (size_t)P * Q * COLS;    // of a dictionary
+    const int64_t jobs = a.n * a.H;
     for (int64_t job = blockIdx.x; job < jobs; job += gridDim.x) {
-    const int h = (int)(job % a.H);
-    const int64_t n0 = job / a.H * R;
-    const float4 *Th = T + (size_t)h * a.M * d4 * COLS;
-    float4 c[P];
-    auto fetch = [&](int m) {
+        const int h = (int)(job % a.H);
+        const float4 *Th = T + (size_t)h * a.M * SET;
+        float4 c[P], ahead[AHEAD ? P : 1];
+        auto fetch = [&](int m, float4 (&to)[P]) {
 #pragma unroll
-        for (int i = 0; i < P; ++i) {
-            const int p = q + i * Q;
-            c[i] = p < d4 ? Th[((size_t)m * d4 + p) * COLS + k] : make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-    };
-    fetch(0);
-    // the rows: a wave each
-    if (wave < R) {
-        const int64_t n = n0 + wave;
-        const int64_t s = n < a.n ? a.slots[n] : -1;
-        const bool live = s >= 0 && s < a.n_slots;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (live && lane < d4) v = load_in(a, n * a.row_stride + h * a.head_stride + 4 * lane);
-        // magnitudes order as integers do, NaN above infinity
-        int top = max(max(__float_as_int(fabsf(v.x)), __float_as_int(fabsf(v.y))), max(__float_as_int(fabsf(v.z)), __float_as_int(fabsf(v.w))));
-        top = wave_max_int(top);
-        float g = __int_as_float(top);
-        if (top >= 0x7f800000) {                    // not a number: kept as a row of zeros whose scale says so
-            v = make_float4(0.f, 0.f, 0.f, 0.f);
-            g = __builtin_nanf("");
-        } else if (a.scale && top) {
-            v = make_float4(v.x / g, v.y / g, v.z / g, v.w / g);
-        }
-        rows[wave][lane] = v;
-        if (lane == 0) {
-            slot[wave] = live ? s : -1;
-            if (live && a.scale) a.scale[s * a.H + h] = g;
-        }
-    }
-    __syncthreads();
-    for (int m = 0; m < a.M; ++m) {
-        float d[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) d[r] = 0.f;
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const float4 x = rows[r][min(q + i * Q, kCacheMaxD / 4 - 1)];
-                if (q + i * Q < d4) {
-                    const float e0 = x.x - c[i].x, e1 = x.y - c[i].y, e2 = x.z - c[i].z, e3 = x.w - c[i].w;
-                    d[r] = fmaf(e3, e3, fmaf(e2, e2, fmaf(e1, e1, fmaf(e0, e0, d[r]))));
-                }
-            }
-        }
-#pragma unroll
-        for (int r = 0; r < R; ++r) part[r][q][k] = d[r];
+            for (int i = 0; i < P; ++i) to[i] = (Th + m * SET + i * kFewThreads)[tid];       // piece q + i Q of codeword k
+        };
+        fetch(0, c);
+        int64_t slot = -1;
+        if (wave == 0) slot = take_row(a, job / a.H, h, row, kCacheMaxD, lane);
         __syncthreads();
-        if (wave < R) {                             // a wave per row
-            constexpr int N = COLS / kWave;
-            const float inf = __builtin_inff();
-            float s[N], best = inf, second = inf;
-            int at = 0x7fffffff;
+        for (int m = 0; m < a.M; ++m) {
+            if constexpr (AHEAD) fetch(min(m + 1, a.M - 1), ahead);
+            float d = 0.f;
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int kk = lane + kWave * i;
-                s[i] = 0.f;
-#pragma unroll
-                for (int j = 0; j < Q; ++j) s[i] += part[wave][j][kk];
-                if (kk >= a.K) s[i] = inf;
-                second = s[i] < best ? best : fminf(second, s[i]);
-                if (s[i] < best || at == 0x7fffffff) {
-                    if (kk < a.K) at = kk;
-                    best = fminf(best, s[i]);
-                }
+            for (int i = 0; i < P; ++i) {           // beyond D both are zero
+                const float4 x = row[q + i * Q];
+                const float e0 = x.x - c[i].x, e1 = x.y - c[i].y, e2 = x.z - c[i].z, e3 = x.w - c[i].w;
+                d = fmaf(e3, e3, fmaf(e2, e2, fmaf(e1, e1, fmaf(e0, e0, d))));
             }
-#pragma unroll
-            for (int o = 1; o < kWave; o <<= 1) {
-                const float ob = __shfl_xor(best, o, kWave), os = __shfl_xor(second, o, kWave);
-                const int oa = __shfl_xor(at, o, kWave);
-                second = fminf(fmaxf(best, ob), fminf(second, os));
-                if (ob < best || (ob == best && oa < at)) at = oa;
-                best = fminf(best, ob);
-            }
-            // relative error of a sum: 4 P additions of squares with one rounding each in the difference, twice in the square, and Q more
-            const float eta = (float)(4 * P + Q + 6) * 6.1e-8f;
-            if (!(best * (1.f + eta) < second * (1.f - eta) && second > 1e-25f)) {
-                // every codeword that may be the nearest, in 64 bits, ascending dimensions
-                const float limit = best * (1.f + 4.f * eta) + 1e-30f;
-                const float *row = reinterpret_cast<const float *>(rows[wave]);
-                double db = __builtin_inf();
-                int ka = 0x7fffffff;
+            part[q][k] = d;
+            __syncthreads();
+            if (wave == 0) {
+                constexpr int N = COLS / kWave;
+                float s[N];
+                unsigned best = ~0u, next = ~0u;    // distances are not negative: they order as integers, NaN last
+                int at = 0;
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const int kk = lane + kWave * i;
-                    if (kk >= a.K || !(s[i] <= limit || !(limit < inf))) continue;
-                    double t = 0.0;
-                    for (int p = 0; p < d4; ++p) {
-                        const float4 u = Th[((size_t)m * d4 + p) * COLS + kk];
-                        const double t0 = (double)row[4 * p] - (double)u.x, t1 = (double)row[4 * p + 1] - (double)u.y;
-                        const double t2 = (double)row[4 * p + 2] - (double)u.z, t3 = (double)row[4 * p + 3] - (double)u.w;
-                        t += t0 * t0;
-                        t += t1 * t1;
-                        t += t2 * t2;
-                        t += t3 * t3;
+                    s[i] = 0.f;
+#pragma unroll
+                    for (int j = 0; j < Q; ++j) s[i] += part[j][lane + kWave * i];
+                    const unsigned u = lane + kWave * i < a.K ? __float_as_uint(s[i]) & 0x7fffffffu : ~0u;
+                    next = min(next, max(best, u));
+                    at = u < best ? lane + kWave * i : at;
+                    best = min(best, u);
+                }
+                const unsigned least = wave_min_bits(best);
+                const int winner = __ffsll(__ballot(best == least)) - 1;
+                const float b0 = __uint_as_float(least), b1 = __uint_as_float(wave_min_bits(lane == winner ? next : best));
+                at = __builtin_amdgcn_readlane(at, winner);
+                // 4 P additions of squares with one rounding in the difference and two in the square, and Q more
+                constexpr float eta = (float)(4 * P + Q + 6) * 6.1e-8f;
+                if (a.K > 1 && !(b0 * (1.f + eta) < b1 * (1.f - eta) && b1 > 1e-25f && b1 < __builtin_inff())) {
+                    // every codeword that may be the nearest, in 64 bits
+                    const float limit = b0 * (1.f + 4.f * eta) + 1e-30f;
+                    const bool all = !(limit < __builtin_inff());
+                    double db = __builtin_inf();
+                    int kb = 0x7fffffff;
+#pragma unroll 1
+                    for (int i = 0; i < N; ++i) {
+                        const int k0 = lane + kWave * i;
+                        float si = s[0];
+#pragma unroll
+                        for (int j = 1; j < N; ++j) si = i == j ? s[j] : si;
+                        if (k0 >= a.K || !(all || si <= limit)) continue;
+                        double t = 0.0;
+#pragma unroll 2
+                        for (int p = 0; p < d4; ++p) {
+                            const float4 u = Th[m * SET + (size_t)p * COLS + k0], w = row[p];
+                            const double t0 = (double)w.x - (double)u.x, t1 = (double)w.y - (double)u.y, t2 = (double)w.z - (double)u.z, t3 = (double)w.w - (double)u.w;
+                            t = fma(t3, t3, fma(t2, t2, fma(t1, t1, fma(t0, t0, t))));
+                        }
+                        if (t < db) {
+                            db = t;
+                            kb = k0;
+                        }
                     }
-                    if (t < db || (t == db && kk < ka)) { db = t; ka = kk; }
-                }
 #pragma unroll
-                for (int o = 32; o > 0; o >>= 1) {
-                    const double od = __shfl_xor(db, o, kWave);
-                    const int ok = __shfl_xor(ka, o, kWave);
-                    if (od < db || (od == db && ok < ka)) { db = od; ka = ok; }
+                    for (int o = 32; o > 0; o >>= 1) {
+                        const double od = __shfl_xor(db, o, kWave);
+                        const int ok = __shfl_xor(kb, o, kWave);
+                        if (od < db || (od == db && ok < kb)) { db = od; kb = ok; }
+                    }
+                    at = kb < a.K ? kb : 0;         // beyond only where a dictionary holds no numbers
                 }
-                at = ka;
+                if (lane == 0) {
+                    chosen = at;
+                    if (slot >= 0) a.codes[(slot * a.H + h) * a.M + m] = (uint8_t)at;
+                }
             }
-            at = at < a.K ? at : 0;                 // beyond only where a dictionary holds no numbers
-            if (lane == 0) {
-                chosen[wave] = at;
-                const int64_t s0 = slot[wave];
-                if (s0 >= 0) a.codes[(s0 * a.H + h) * a.M + m] = (uint8_t)at;
-            }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            if (chosen[r] == k) {
+            __syncthreads();
+            if (chosen == k) {
 #pragma unroll
                 for (int i = 0; i < P; ++i) {
-                    const int p = q + i * Q;
-                    if (p < d4) {
-                        const float4 x = rows[r][p];
-                        rows[r][p] = make_float4(x.x - c[i].x, x.y - c[i].y, x.z - c[i].z, x.w - c[i].w);
-                    }
+                    const float4 x = row[q + i * Q];
+                    row[q + i * Q] = make_float4(x.x - c[i].x, x.y - c[i].y, x.z - c[i].z, x.w - c[i].w);
                 }
             }
+            if constexpr (AHEAD) {
+#pragma unroll
+                for (int i = 0; i < P; ++i) c[i] = ahead[i];
+            } else {
+                fetch(min(m + 1, a.M - 1), c);
+            }
+            __syncthreads();
         }
-        if (m + 1 < a.M) fetch(m + 1);
-        __syncthreads();
-    }
     }
 }
 
+// Some rows a head: a block takes sixteen rows of one head through all dictionaries, a wave sixteen codewords, its share in registers
+// as before, as operands of the fp32 matrix cores (v_mfma_f32_16x16x4_f32: lane 16 g + i holds of codeword or row i the dimension
+// that is the g-th of four).  Scores x.c - ||c||^2 / 2; a row whose two best are within what rounding can do to them,
+//   (D + 8) 2^-22 (||x|| max||c|| + max||c||^2 / 2)                 (each of D products and additions loses at most a unit or two of 2^-23),
+// is decided from all its distances by one wave (some 2 in 1000).
+constexpr int kSomeRows = 16;
+template <int COLS, int P>
+__global__ __launch_bounds__(kFewThreads) void k_cache_write_some(const CacheRowsIn a, const float4 *__restrict__ T, const float *__restrict__ halves)
+{
+    constexpr bool AHEAD = P <= 8;
+    constexpr int PITCH = 4 * P + 1;                // float4 of a row in LDS: an odd number, so that sixteen rows spread over the banks
+    __shared__ float4 rows[kSomeRows][PITCH];
+    __shared__ float4 found[kSomeRows][kWave];      // best, second, which of four; of each wave's four groups
+    __shared__ int chosen[kSomeRows];
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i16 = lane & 15, g = lane >> 4;
+    const int64_t per_head = (a.n + kSomeRows - 1) / kSomeRows, jobs = per_head * a.H;
+    const bool mine = 16 * wave < COLS;             // the wave has codewords
+    const int at = g * COLS + (mine ? 16 * wave : 0) + i16;
+    for (int64_t job = blockIdx.x; job < jobs; job += gridDim.x) {
+        const int h = (int)(job / per_head);
+        const int64_t n0 = (job - h * per_head) * kSomeRows;
+        constexpr size_t SET = (size_t)4 * P * COLS;
+        const float4 *Th = T + (size_t)h * a.M * SET;
+        const float *half = halves + (size_t)h * a.M * 256;
+        float4 c[P], ahead[AHEAD ? P : 1], hc, hahead;
+        float cmax, cmax_ahead;
+        auto piece = [&](int m, int j) { return (Th + m * SET + j * 4 * COLS)[at]; };       // 4 j + g of codeword 16 wave + i16
+        auto fetch_half = [&](int m, float4 &hm, float &most) {
+            hm = *reinterpret_cast<const float4 *>(half + (size_t)m * 256 + (mine ? 16 * wave : 0) + 4 * g);
+            most = halves[(size_t)a.H * a.M * 256 + h * a.M + m];
+        };
+#pragma unroll
+        for (int j = 0; j < P; ++j) c[j] = piece(0, j);
+        fetch_half(0, hc, cmax);
+        const int64_t slot = take_row(a, n0 + wave, h, rows[wave], 16 * P, lane);       // a wave per row
+        __syncthreads();
+        for (int m = 0; m < a.M; ++m) {
+            const int then_m = min(m + 1, a.M - 1);
+            if (mine) {
+                typedef float floatx4 __attribute__((ext_vector_type(4)));
+                floatx4 acc = {hc.x, hc.y, hc.z, hc.w};
+#pragma unroll
+                for (int j = 0; j < P; ++j) {
+                    const float4 x = rows[i16][4 * j + g];
+                    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(c[j].x, x.x, acc, 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(c[j].y, x.y, acc, 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(c[j].z, x.z, acc, 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(c[j].w, x.w, acc, 0, 0, 0);
+                    // (all loads at once would wait for each other at the head: 128 KB at 64 bytes a cycle)
+                    if constexpr (AHEAD) ahead[j] = piece(then_m, j);
+                }
+                fetch_half(then_m, hahead, cmax_ahead);
+                // lane 16 g + i: codewords 16 wave + 4 g + v of row i
+                float best = acc[0], second = -__builtin_inff();
+                int v = 0;
+#pragma unroll
+                for (int w = 1; w < 4; ++w) {
+                    second = acc[w] > best ? best : fmaxf(second, acc[w]);
+                    if (acc[w] > best) {
+                        best = acc[w];
+                        v = w;
+                    }
+                }
+                found[i16][4 * wave + g] = make_float4(best, second, __int_as_float(v), 0.f);
+            } else if (fetch_half(then_m, hahead, cmax_ahead); lane < kSomeRows) {
+#pragma unroll
+                for (int w = 0; w < 4; ++w) found[lane][4 * wave + w] = make_float4(-__builtin_inff(), -__builtin_inff(), 0.f, 0.f);
+            }
+            __syncthreads();
+            {
+                const float4 f = found[wave][lane];
+                const float4 x = 4 * lane < 16 * P ? rows[wave][lane] : make_float4(0.f, 0.f, 0.f, 0.f);
+                float xx = fmaf(x.x, x.x, fmaf(x.y, x.y, fmaf(x.z, x.z, x.w * x.w)));
+                // descending floats as ascending unsigned integers
+                auto key = [](float s) { const unsigned u = __float_as_uint(s); return (int)u < 0 ? u : ~(u | 0x80000000u); };
+                auto value = [](unsigned u) { return __uint_as_float((int)u < 0 ? u : ~u & 0x7fffffffu); };
+                const unsigned most = wave_min_bits(key(f.x));
+                const unsigned long long who = __ballot(key(f.x) == most);
+                const int winner = __ffsll(who) - 1;
+                const unsigned then = wave_min_bits(lane == winner ? key(f.y) : key(f.x));
+                xx = sum16(xx);
+                xx = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(xx), 0)) + __int_as_float(__builtin_amdgcn_readlane(__float_as_int(xx), 16)) +
+                     __int_as_float(__builtin_amdgcn_readlane(__float_as_int(xx), 32)) + __int_as_float(__builtin_amdgcn_readlane(__float_as_int(xx), 48));
+                const float err = (float)(16 * P + 8) * 2.4e-7f * (sqrtf(xx) * cmax + 0.5f * cmax * cmax) + 1e-36f;
+                int nearest = 4 * winner + __builtin_amdgcn_readlane(__float_as_int(f.z), winner);
+                const float top = value(most);
+                if (!(top - value(then) > 2.f * err)) {
+                    // the fours of codewords whose best is within the margin, sixteen lanes a codeword, in fp32
+                    const unsigned long long near = __ballot(!(f.x < top - 2.f * err));
+                    unsigned long long fours = near;
+                    float least = __builtin_inff(), next = __builtin_inff();
+                    int at = 0;
+                    while (fours) {
+                        const int k = 4 * (__ffsll(fours) - 1) + g;
+                        fours &= fours - 1ull;
+                        float d = 0.f;
+#pragma unroll
+                        for (int i = 0; i < P / 4; ++i) {
+                            const int p = i16 + 16 * i;
+                            const float4 u = Th[m * SET + (size_t)p * COLS + min(k, COLS - 1)], w = rows[wave][p];
+                            const float e0 = w.x - u.x, e1 = w.y - u.y, e2 = w.z - u.z, e3 = w.w - u.w;
+                            d = fmaf(e3, e3, fmaf(e2, e2, fmaf(e1, e1, fmaf(e0, e0, d))));
+                        }
+                        d = sum16(d);
+                        if (k >= a.K) d = __builtin_inff();
+                        next = d < least ? least : fminf(next, d);
+                        if (d < least) {
+                            least = d;
+                            at = k;
+                        }
+                    }
+                    float b0 = __builtin_inff(), b1 = __builtin_inff();
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float l = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(least), 16 * j)), t = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(next), 16 * j));
+                        b1 = l < b0 ? fminf(b0, t) : fminf(b1, l);
+                        if (l < b0) {
+                            b0 = l;
+                            nearest = __builtin_amdgcn_readlane(at, 16 * j);
+                        }
+                    }
+                    constexpr float eta = (float)(P + 10) * 6.1e-8f;
+                    if (a.K > 1 && !(b0 * (1.f + eta) < b1 * (1.f - eta) && b1 > 1e-25f)) {
+                        // the same in 64 bits, the lowest index of equals
+                        double db = __builtin_inf();
+                        int kb = 0x7fffffff;
+                        fours = near;
+#pragma unroll 1
+                        while (fours) {
+                            const int k = 4 * (__ffsll(fours) - 1) + g;
+                            fours &= fours - 1ull;
+                            double t = 0.0;
+#pragma unroll 1
+                            for (int p = i16; p < 4 * P; p += 16) {
+                                const float4 u = Th[m * SET + (size_t)p * COLS + min(k, COLS - 1)], w = rows[wave][p];
+                                const double t0 = (double)w.x - (double)u.x, t1 = (double)w.y - (double)u.y, t2 = (double)w.z - (double)u.z, t3 = (double)w.w - (double)u.w;
+                                t = fma(t3, t3, fma(t2, t2, fma(t1, t1, fma(t0, t0, t))));
+                            }
+#pragma unroll
+                            for (int o = 1; o < 16; o <<= 1) t += __shfl_xor(t, o, kWave);
+                            if (k < a.K && t < db) {                // ascending k
+                                db = t;
+                                kb = k;
+                            }
+                        }
+#pragma unroll
+                        for (int o = 16; o < kWave; o <<= 1) {
+                            const double od = __shfl_xor(db, o, kWave);
+                            const int ok = __shfl_xor(kb, o, kWave);
+                            if (od < db || (od == db && ok < kb)) { db = od; kb = ok; }
+                        }
+                        nearest = __builtin_amdgcn_readfirstlane(kb < a.K ? kb : 0);
+                    }
+                }
+                if (lane == 0) {
+                    chosen[wave] = nearest;
+                    if (slot >= 0) a.codes[(slot * a.H + h) * a.M + m] = (uint8_t)nearest;
+                }
+            }
+            __syncthreads();
+            {
+                const int all = chosen[i16];
+                unsigned hit = (unsigned)__ballot(lane < kSomeRows && (all >> 4) == wave);      // rows that leave one of the wave's codewords
+                while (hit) {
+                    const int r = __ffs(hit) - 1, k = __builtin_amdgcn_readlane(all, r);
+                    hit &= hit - 1u;
+                    if (i16 == (k & 15)) {
+#pragma unroll
+                        for (int j0 = 0; j0 < P; j0 += 4) {
+                            float4 x[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) x[j] = rows[r][4 * (j0 + j) + g];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                rows[r][4 * (j0 + j) + g] = make_float4(x[j].x - c[j0 + j].x, x[j].y - c[j0 + j].y, x[j].z - c[j0 + j].z, x[j].w - c[j0 + j].w);
+                        }
+                    }
+                }
+            }
+            if constexpr (AHEAD) {
+#pragma unroll
+                for (int j = 0; j < P; ++j) c[j] = ahead[j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < P; ++j) c[j] = piece(then_m, j);
+            }
+            hc = hahead;
+            cmax = cmax_ahead;
+            __syncthreads();
+        }
+    }
+}
 
 // Many rows a head: scores from the fp16 matrix cores, a wave per tile of 32 rows of one head, through all its dictionaries, the
 // rows staying in registers.  Scores, their bounds and the margins are those of assign_half.hpp: score k is off by at most
@@ -227,6 +427,7 @@ struct CacheTables {
     const char *parts;                              // [H M][UNITS]: what passes through LDS, as TilePart says
     const float *C;                                 // [H M][K][Dp] sorted, positions in place of coordinates, zero beyond D
     const uint8_t *order;                           // [H M][256]: the codeword at a place
+    const float *halves;                            // of k_cache_write_some (k_cache_sort)
 };
 
 // A part of a dictionary (all of it, or half of its blocks): the fp16 image, -||C||^2/2, fp16 {2^-10, w_k}, -mu, the largest w of each
@@ -252,8 +453,11 @@ __host__ __device__ constexpr int cache_chunks(int D) { return D <= 64 ? 1 : D <
 __host__ __device__ constexpr int cache_padded(int D) { return 64 * cache_chunks(D); }
 
 // Codewords in ascending order of their distance from the mean of a few, equal ones by index.  A block per dictionary.
-__global__ __launch_bounds__(256) void k_cache_sort(const float *__restrict__ C, int K, int D, float *__restrict__ sorted, uint8_t *__restrict__ order)
+// halves: [dictionaries][256] -||c||^2 / 2 of codewords as they are, -1e38 beyond K; then [dictionaries] the largest ||c|| (rounded up).
+__global__ __launch_bounds__(256) void k_cache_sort(const float *__restrict__ C, int K, int D, float *__restrict__ sorted, uint8_t *__restrict__ order,
+                                                    float *__restrict__ halves)
 {
+    __shared__ float size[256];
     __shared__ float norm[256];
     __shared__ uint8_t at[256];
     const float *Cm = C + (size_t)blockIdx.x * K * D;
@@ -270,9 +474,21 @@ __global__ __launch_bounds__(256) void k_cache_sort(const float *__restrict__ C,
         float s = 4 * lane < D ? a * a + b * b + c * c + d * d : 0.f;
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, kWave);
-        if (lane == 0) norm[k] = s;
+        const double n = wave_sum((double)v.x * v.x + (double)v.y * v.y + (double)v.z * v.z + (double)v.w * v.w);
+        if (lane == 0) {
+            norm[k] = s;
+            size[k] = (float)(0.5 * n);
+        }
     }
     __syncthreads();
+    halves[(size_t)blockIdx.x * 256 + tid] = tid < K ? -size[tid] : -1e38f;
+    if (wave == 0) {
+        float most = 0.f;
+        for (int k = lane; k < K; k += kWave) most = fmaxf(most, size[k]);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o, kWave));
+        if (lane == 0) halves[(size_t)gridDim.x * 256 + blockIdx.x] = sqrtf(2.f * most) * 1.00001f;
+    }
     if (tid < K) {
         const float mine = norm[tid];
         int rank = 0;
@@ -319,19 +535,6 @@ __global__ __launch_bounds__(256) void k_cache_pack(
 constexpr int kTileBatch = 4;                       // undecided rows of a wave at a time, sixteen lanes each
 __host__ __device__ constexpr int tile_stretch(int nc) { return nc == 4 ? 4096 : 2048; }
 __host__ __device__ constexpr int tile_lds(int kbu, int nc, int waves) { return 2 * tile_part(kbu, nc).bytes + waves * tile_stretch(nc); }
-
-typedef float floatv4 __attribute__((ext_vector_type(4)));
-
-template <int CTRL>
-__device__ __forceinline__ float dpp_plus(float v)
-{
-    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
-}
-// The sum over the sixteen lanes of a row, the same in all of them.
-__device__ __forceinline__ float sum16(float v)
-{
-    return dpp_plus<0x140>(dpp_plus<0x141>(dpp_plus<0x4E>(dpp_plus<0xB1>(v))));     // quad_perm 1 0 3 2, 2 3 0 1, row_half_mirror, row_mirror
-}
 
 // KB: blocks of 32 codewords.  NC: 64-position chunks (1, 2 or 4).  UNITS: parts in which a dictionary passes through LDS.
 template <int KB, int NC, int UNITS, int WAVES>

@@ -162,7 +162,7 @@ struct hclae_ctx {
     // coded cache: the dictionaries of its heads (hclae_cache_begin)
     int cache_H;             // 0: none yet
     float *cache_C;          // [H][M][K][D]
-    float4 *cache_T;         // [H][M][D / 4][few_columns(K)]
+    float4 *cache_T;         // [H][M][cache_padded(D) / 4][few_columns(K)]
     char *cache_buf;         // sorted, as fp16 images and tables (CacheTables)
     CacheTables cache_tab;
     // sorted rows of hclae_lookup_grad (allocated on first use)
@@ -2143,8 +2143,8 @@ static bool apart(int64_t n, int H, int D, int64_t row_stride, int64_t head_stri
     return (row_stride - D) / (H - 1) >= head_stride || (head_stride - D) / (n - 1) >= row_stride;
 }
 
-// Rows of all heads up to which k_cache_write_few takes them.
-constexpr int64_t kFewRows = 2048;
+// Rows of all heads up to which k_cache_write_one takes them, and k_cache_write_some.
+constexpr int64_t kOneRows = 256, kSomeMost = 4096;
 
 int hclae_cache_begin(hclae_ctx *ctx, const float *C, int H, int M, int K, int D)
 {
@@ -2155,20 +2155,20 @@ int hclae_cache_begin(hclae_ctx *ctx, const float *C, int H, int M, int K, int D
     if (misaligned(C)) return fail(ctx, HCLAE_EINVAL, "hclae_cache_begin: C must be 16-byte aligned");
     ON_DEVICE(ctx);
     const size_t sets = (size_t)H * M;
-    const int columns = few_columns(K), d4 = D / 4, kb = ctx->kb, nc = cache_chunks(D), kpad = 32 * kb;
+    const int columns = few_columns(K), pieces = cache_padded(D) / 4, kb = ctx->kb, nc = cache_chunks(D), kpad = 32 * kb;
     auto up = [](size_t b) { return (b + 255) / 256 * 256; };
     const int units = tile_units(kb, nc);
     const TilePart part = tile_part(kb / units, nc);
     const size_t parts_b = sets * units * part.bytes, img_b = sets * nc * kb * 4096, per_codeword_b = up(sets * kpad * sizeof(float)),
-                 mu_b = up(sets * kChunkD * nc * sizeof(float)), consts_b = up(sets * kEncodeConsts * sizeof(float)), order_b = sets * 256,
+                 mu_b = up(sets * kChunkD * nc * sizeof(float)), consts_b = up(sets * kEncodeConsts * sizeof(float)), order_b = sets * 256, halves_b = up(sets * 257 * sizeof(float)),
                  C_b = up(sets * K * D * sizeof(float)), sorted_b = up(sets * K * cache_padded(D) * sizeof(float));
     if (H > ctx->cache_H) {
         float *copy = nullptr;
         float4 *T = nullptr;
         char *buf = nullptr;
         hipError_t e = hipMalloc((void **)&copy, C_b);
-        if (e == hipSuccess) e = hipMalloc((void **)&T, sets * d4 * columns * sizeof(float4));
-        if (e == hipSuccess) e = hipMalloc((void **)&buf, parts_b + img_b + 2 * per_codeword_b + mu_b + consts_b + order_b + sorted_b + 256);
+        if (e == hipSuccess) e = hipMalloc((void **)&T, sets * pieces * columns * sizeof(float4));
+        if (e == hipSuccess) e = hipMalloc((void **)&buf, parts_b + img_b + 2 * per_codeword_b + mu_b + consts_b + order_b + sorted_b + halves_b + 256);
         if (e != hipSuccess) {
             if (copy) (void)hipFree(copy);
             if (T) (void)hipFree(T);
@@ -2191,11 +2191,12 @@ int hclae_cache_begin(hclae_ctx *ctx, const float *C, int H, int M, int K, int D
     float *consts = reinterpret_cast<float *>(p += mu_b);
     uint8_t *order = reinterpret_cast<uint8_t *>(p += consts_b);
     float *sorted = reinterpret_cast<float *>(p += order_b);
-    unsigned *unused = reinterpret_cast<unsigned *>(p += sorted_b);
-    ctx->cache_tab = {parts, sorted, order};
-    hipLaunchKernelGGL(k_cache_lay, dim3((unsigned)sets, (unsigned)((d4 + 15) / 16)), dim3(256), 0, ctx->stream, C, K, D, columns, ctx->cache_C, ctx->cache_T);
+    float *halves = reinterpret_cast<float *>(p += sorted_b);
+    unsigned *unused = reinterpret_cast<unsigned *>(p += halves_b);
+    ctx->cache_tab = {parts, sorted, order, halves};
+    hipLaunchKernelGGL(k_cache_lay, dim3((unsigned)sets, (unsigned)(pieces / 16)), dim3(256), 0, ctx->stream, C, K, D, columns, pieces, ctx->cache_C, ctx->cache_T);
     HIP_TRY(ctx, hipGetLastError());
-    hipLaunchKernelGGL(k_cache_sort, dim3((unsigned)sets), dim3(256), 0, ctx->stream, C, K, D, sorted, order);
+    hipLaunchKernelGGL(k_cache_sort, dim3((unsigned)sets), dim3(256), 0, ctx->stream, C, K, D, sorted, order, halves);
     HIP_TRY(ctx, hipGetLastError());
     hipLaunchKernelGGL(k_encode_prep<false>, dim3((unsigned)sets), dim3(kPrepThreads), 0, ctx->stream, sorted, K, cache_padded(D), kb, nc, img, hn, wtab, negmu, consts,
                        (float *)nullptr, unused);
@@ -2206,20 +2207,19 @@ int hclae_cache_begin(hclae_ctx *ctx, const float *C, int H, int M, int K, int D
 }
 
 extern "C++" {
-template <int COLS, int P, int R>
-static int launch_cache_write_few(hclae_ctx *ctx, const CacheRowsIn &a)
-{
-    const int64_t jobs = (a.n + R - 1) / R * a.H;
-    const int64_t blocks = jobs < (1 << 20) ? jobs : (1 << 20);
-    hipLaunchKernelGGL((k_cache_write_few<COLS, P, R>), dim3((unsigned)blocks), dim3(kFewThreads), 0, ctx->stream, a, ctx->cache_T);
-    HIP_TRY(ctx, hipGetLastError());
-    return HCLAE_OK;
-}
+// P: float4 pieces of a row up to which the instance goes, 16 coordinates each.
 template <int COLS, int P>
 static int launch_cache_write_rows(hclae_ctx *ctx, const CacheRowsIn &a)
 {
-    const int64_t items = a.n * a.H;
-    return items <= ctx->cus ? launch_cache_write_few<COLS, P, 1>(ctx, a) : launch_cache_write_few<COLS, P, 4>(ctx, a);
+    if (a.n * a.H <= kOneRows) {
+        hipLaunchKernelGGL((k_cache_write_one<COLS, 4 * P * COLS / kFewThreads>), dim3((unsigned)(a.n * a.H)), dim3(kFewThreads), 0, ctx->stream, a, ctx->cache_T);
+    } else {
+        const int64_t jobs = (a.n + kSomeRows - 1) / kSomeRows * a.H;
+        hipLaunchKernelGGL((k_cache_write_some<COLS, P>), dim3((unsigned)(jobs < (1 << 20) ? jobs : 1 << 20)), dim3(kFewThreads), 0, ctx->stream, a, ctx->cache_T,
+                           ctx->cache_tab.halves);
+    }
+    HIP_TRY(ctx, hipGetLastError());
+    return HCLAE_OK;
 }
 
 template <int KB, int NC>
@@ -2251,7 +2251,7 @@ int hclae_cache_write(hclae_ctx *ctx, const void *X, int type, int64_t n, int64_
     ON_DEVICE(ctx);
     const CacheRowsIn a = {X, type, row_stride, head_stride, slots, n, n_slots, codes, scale, ctx->cache_H, ctx->M, ctx->K, ctx->D};
     const int D = ctx->D;
-    if (n * a.H > kFewRows && (n / kTileVec + 1) * a.H < (int64_t)1 << 30) switch (cache_chunks(D) * 16 + ctx->kb) {
+    if (n * a.H > kSomeMost && (n / kTileVec + 1) * a.H < (int64_t)1 << 30) switch (cache_chunks(D) * 16 + ctx->kb) {
         case 16 + 1: return launch_cache_write_tiles<1, 1>(ctx, a);
         case 16 + 2: return launch_cache_write_tiles<2, 1>(ctx, a);
         case 16 + 4: return launch_cache_write_tiles<4, 1>(ctx, a);
@@ -2265,10 +2265,16 @@ int hclae_cache_write(hclae_ctx *ctx, const void *X, int type, int64_t n, int64_
         case 64 + 4: return launch_cache_write_tiles<4, 4>(ctx, a);
         default: return launch_cache_write_tiles<8, 4>(ctx, a);
         }
-    switch (few_columns(ctx->K)) {
-    case 64: return D <= 128 ? launch_cache_write_rows<64, 2>(ctx, a) : launch_cache_write_rows<64, 4>(ctx, a);
-    case 128: return D <= 128 ? launch_cache_write_rows<128, 4>(ctx, a) : launch_cache_write_rows<128, 8>(ctx, a);
-    default: return D <= 64 ? launch_cache_write_rows<256, 4>(ctx, a) : D <= 128 ? launch_cache_write_rows<256, 8>(ctx, a) : launch_cache_write_rows<256, 16>(ctx, a);
+    switch (few_columns(ctx->K) + cache_chunks(D)) {
+    case 64 + 1: return launch_cache_write_rows<64, 4>(ctx, a);
+    case 64 + 2: return launch_cache_write_rows<64, 8>(ctx, a);
+    case 64 + 4: return launch_cache_write_rows<64, 16>(ctx, a);
+    case 128 + 1: return launch_cache_write_rows<128, 4>(ctx, a);
+    case 128 + 2: return launch_cache_write_rows<128, 8>(ctx, a);
+    case 128 + 4: return launch_cache_write_rows<128, 16>(ctx, a);
+    case 256 + 1: return launch_cache_write_rows<256, 4>(ctx, a);
+    case 256 + 2: return launch_cache_write_rows<256, 8>(ctx, a);
+    default: return launch_cache_write_rows<256, 16>(ctx, a);
     }
 }
 
