@@ -2407,7 +2407,8 @@ static int launch_lookup_grad(hclae_ctx *ctx, const GradArgs &a)
         return HCLAE_OK;
     }
     const size_t M = a.M, K = a.K, N = ctx->N_max;
-    const size_t ranges_max = (N + kSortRange - 1) / kSortRange, items_max = K + 512, parts_max = 1026;
+    const size_t ranges_max = std::max<size_t>(N / sort_range(N), 512) + 1,      // fewer rows: at most 512
+                  items_max = K + 512, parts_max = 1026;
     const size_t counts_b = M * ranges_max * K * sizeof(unsigned), list_b = M * N * sizeof(int), items_b = M * items_max * sizeof(GradItem),
                  buckets_b = M * K * sizeof(GradBucket), partial_b = M * parts_max * a.D * sizeof(float);
     auto up = [](size_t b) { return (b + 255) / 256 * 256; };
@@ -2422,7 +2423,8 @@ static int launch_lookup_grad(hclae_ctx *ctx, const GradArgs &a)
     s.items = reinterpret_cast<GradItem *>(p += up(list_b));
     s.buckets = reinterpret_cast<GradBucket *>(p += up(items_b));
     s.partial = reinterpret_cast<float *>(p += up(buckets_b));
-    s.ranges = (int)((a.T + kSortRange - 1) / kSortRange);
+    s.range = sort_range(a.T);
+    s.ranges = (int)((a.T + s.range - 1) / s.range);
     s.chunk = grad_chunk(a.T);
     s.max_items = a.K + (int)(a.T / s.chunk);
     s.max_parts = 2 * (int)(a.T / s.chunk) + 2;

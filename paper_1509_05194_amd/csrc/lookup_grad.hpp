@@ -56,13 +56,6 @@ struct Piece {
             }
         }
     }
-    // the coordinates that the row has, times f
-    __device__ __forceinline__ void store(float *p, bool whole, float f) const
-    {
-        *reinterpret_cast<float4 *>(p) = make_float4(v[0] * f, v[1] * f, v[2] * f, v[3] * f);
-        if constexpr (dims == 8)
-            if (whole) *reinterpret_cast<float4 *>(p + 4) = make_float4(v[4] * f, v[5] * f, v[6] * f, v[7] * f);
-    }
 };
 
 // Code of row t in dictionary m, -1 where the row number names no row.
@@ -127,7 +120,8 @@ __global__ __launch_bounds__(kGradThreads) void k_grad_few(const GradArgs a, int
 }
 
 // Many rows: sorted by code, dictionary by dictionary (a counting sort that keeps the order of equal codes), then summed in chunks.
-constexpr int kSortRange = 1024;                    // rows of a block
+// Rows of a block: the fewer, the more blocks there are, and the more ranges k_grad_items goes through (T = 16384, 1024 rows: 13 us a pass).
+__host__ __device__ constexpr int sort_range(int64_t T) { return T <= 32768 ? 256 : T <= 131072 ? 512 : T <= 524288 ? 1024 : 2048; }
 constexpr int kSortGroup = 8;                       // dictionaries of a block, a wave each
 constexpr int kSortThreads = kSortGroup * kWave;
 
@@ -144,7 +138,7 @@ struct SortArgs {
     GradItem *items;                                // [M][max_items]
     GradBucket *buckets;                            // [M][K]
     float *partial;                                 // [M][max_parts][D]
-    int ranges, chunk, max_items, max_parts;
+    int range, ranges, chunk, max_items, max_parts;
 };
 
 // Rows of each code in each range.
@@ -152,12 +146,12 @@ __global__ __launch_bounds__(kSortThreads) void k_grad_count(const GradArgs a, c
 {
     __shared__ unsigned hist[kSortGroup][256];
     const int wave = threadIdx.x >> 6, lane = lane_id(), m = blockIdx.y * kSortGroup + wave;
-    const int64_t t0 = (int64_t)blockIdx.x * kSortRange;
+    const int64_t t0 = (int64_t)blockIdx.x * s.range;
     for (int i = lane; i < 256; i += kWave) hist[wave][i] = 0u;
     __syncthreads();
     if (m < a.M) {
 #pragma unroll 4
-        for (int i = 0; i < kSortRange; i += kWave) {
+        for (int i = 0; i < s.range; i += kWave) {
             const int64_t t = t0 + i + lane;
             const int c = t < a.T ? grad_code(a, t, m) : -1;
             if (c >= 0) atomicAdd(&hist[wave][c], 1u);
@@ -223,14 +217,14 @@ __global__ __launch_bounds__(kSortThreads) void k_grad_place(const GradArgs a, c
 {
     __shared__ unsigned next[kSortGroup][256];
     const int wave = threadIdx.x >> 6, lane = lane_id(), m = blockIdx.y * kSortGroup + wave;
-    const int64_t t0 = (int64_t)blockIdx.x * kSortRange;
+    const int64_t t0 = (int64_t)blockIdx.x * s.range;
     if (m < a.M)
         for (int k = lane; k < a.K; k += kWave) next[wave][k] = s.counts[((size_t)m * s.ranges + blockIdx.x) * a.K + k];
     __syncthreads();
     if (m >= a.M) return;
     int *list = s.list + (size_t)m * a.T;
 #pragma unroll 4
-    for (int i = 0; i < kSortRange; i += kWave) {
+    for (int i = 0; i < s.range; i += kWave) {
         const int64_t t = t0 + i + lane;
         const int c = t < a.T ? grad_code(a, t, m) : -1;
         unsigned long long same = __ballot(c >= 0);
@@ -283,13 +277,27 @@ __global__ __launch_bounds__(kGradThreads) void k_grad_sums(const GradArgs a, co
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum.add(q[j]);
     }
+    // Over the eight rows: the halves of the wave exchange half of the values each and add, then its quarters, then the eights within; lane
+    // (bits 5, 4) ends with the totals of coordinates `mine` and on
+    float t[P::dims / 2];
 #pragma unroll
-    for (int o = 8; o < kWave; o <<= 1)
+    for (int i = 0; i < P::dims / 2; ++i) {
+        const auto e = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum.v[i]), __float_as_uint(sum.v[i + P::dims / 2]), false, false);
+        t[i] = __uint_as_float(e[0]) + __uint_as_float(e[1]);
+    }
+    float r[P::dims / 4];
 #pragma unroll
-        for (int i = 0; i < P::dims; ++i) sum.v[i] += __shfl_xor(sum.v[i], o, kWave);
-    if (sub == 0 && live) {
-        float *to = item.part < 0 ? a.dC + ((size_t)m * a.K + item.k) * a.D : s.partial + ((size_t)m * s.max_parts + item.part) * a.D;
-        sum.store(to + c * P::dims, whole, item.part < 0 ? a.factor : 1.f);
+    for (int i = 0; i < P::dims / 4; ++i) {
+        const auto e = __builtin_amdgcn_permlane16_swap(__float_as_uint(t[i]), __float_as_uint(t[i + P::dims / 4]), false, false);
+        r[i] = __uint_as_float(e[0]) + __uint_as_float(e[1]);
+        r[i] += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(r[i]), 0x128, 0xf, 0xf, true));    // row_ror:8
+    }
+    const int d = c * P::dims + (lane >> 5) * (P::dims / 2) + ((lane >> 4) & 1) * (P::dims / 4);
+    if (!(lane & 8) && d < a.D) {
+        float *to = (item.part < 0 ? a.dC + ((size_t)m * a.K + item.k) * a.D : s.partial + ((size_t)m * s.max_parts + item.part) * a.D) + d;
+        const float f = item.part < 0 ? a.factor : 1.f;
+        if constexpr (P::dims == 8) *reinterpret_cast<float2 *>(to) = make_float2(r[0] * f, r[1] * f);
+        else *to = r[0] * f;
     }
 }
 
