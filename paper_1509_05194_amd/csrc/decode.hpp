@@ -53,6 +53,8 @@ struct TableRows {                                  // hclae_lookup
         const int64_t r = rows ? rows[t] : t;
         return r >= 0 && r < V ? r : kNoRow;
     }
+    __host__ __device__ constexpr int sequence(int64_t) const { return 0; }
+    __host__ __device__ constexpr int64_t at(int64_t t, int) const { return at(t); }
 };
 
 struct CacheRows {                                  // hclae_cache_read
@@ -60,15 +62,22 @@ struct CacheRows {                                  // hclae_cache_read
     int B, max_pages, page;
     int64_t pages;                                  // of the cache
     // The sequence of row t is the last one that starts at or before it; whatever `starts` holds, the search ends inside [0, B).
-    __host__ __device__ constexpr int64_t at(int64_t t) const
+    __host__ __device__ constexpr int sequence(int64_t t) const
     {
-        if (t < starts[0] || t >= starts[B]) return kSkip;
         int lo = 0, hi = B;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
             if (starts[mid] <= t) lo = mid;
             else hi = mid;
         }
+        return lo;
+    }
+    __host__ __device__ constexpr int64_t at(int64_t t) const { return at(t, sequence(t)); }
+    // The same with a sequence that the row is in or behind.
+    __host__ __device__ constexpr int64_t at(int64_t t, int lo) const
+    {
+        if (t < starts[0] || t >= starts[B]) return kSkip;
+        while (lo + 1 < B && starts[lo + 1] <= t) ++lo;
         const int64_t pos = t - starts[lo];
         if (pos < 0 || pos > 0x7fffffff) return kSkip;
         const unsigned p = (unsigned)pos / (unsigned)page, off = (unsigned)pos - p * (unsigned)page;
@@ -135,7 +144,8 @@ __global__ __launch_bounds__(kDecodeThreads) void k_decode_rows(const DecodeArgs
 // of the 64 banks twice.  The lanes of one coordinate and different dictionaries add up at the end (DPP).  G is the least that lets
 // all of it fit LDS (M = 8, K = 256: two).  A wave takes 64 rows at a time: it looks for them two rounds ahead, fetches their codes one round ahead and keeps
 // them in LDS of its own, so that no barriers are needed once the slice is there.
-constexpr int kSliceThreads = 1024;
+// Threads of a block: half as many where a row's codes take more of LDS.
+__host__ __device__ constexpr int slice_threads(int G) { return G <= 2 ? 1024 : 512; }
 constexpr int kSliceMaxM = 32;                      // codes of a row travel in eight registers
 
 struct SliceLds {
@@ -150,8 +160,8 @@ __host__ __device__ constexpr SliceLds slice_lds(int M, int K, int G)
     l.fours = (l.pairs + 1) / 2;
     l.zero = l.pairs * K * 256;
     l.codes = l.zero + 256;
-    l.factors = l.codes + kSliceThreads * G * l.fours * 8;
-    l.total = l.factors + kSliceThreads * 4;
+    l.factors = l.codes + slice_threads(G) * G * l.fours * 8;
+    l.total = l.factors + slice_threads(G) * 4;
     return l;
 }
 // The G of a shape, 0 where nothing fits `budget` bytes.  No wider slices than the rows are.
@@ -175,26 +185,29 @@ __device__ __forceinline__ float4 dpp_add(const float4 &v)
 // splits: parts of the rows; blocks with neighbouring slices of one part, which write neighbouring pieces of its rows, are on one XCD
 // (blocks go round the eight XCDs in order).  words_aligned: every row's codes are whole, aligned words.  ONE: four steps a code at most.
 template <typename T, typename Rows, int G, bool ONE>
-__global__ __launch_bounds__(kSliceThreads) void k_decode_slices(const DecodeArgs a, const Rows rows, int slices, int splits, bool words_aligned)
+__global__ __launch_bounds__(slice_threads(G)) void k_decode_slices(const DecodeArgs a, const Rows rows, int slices, int splits, bool words_aligned)
 {
     extern __shared__ float4 smem4[];
     char *lds = reinterpret_cast<char *>(smem4);
     constexpr int LQ = 8 / G, S = 4 * LQ;           // lanes and coordinates of a codeword's slice
+    constexpr int THREADS = slice_threads(G);
     constexpr int NW = ONE ? G : kSliceMaxM / 4;    // words of a row's codes
     const SliceLds L = slice_lds(a.M, a.K, G);
     const unsigned jobs = (unsigned)(a.H * slices * splits), per_xcd = (jobs + 7) / 8, job = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
     if ((blockIdx.x >> 3) >= per_xcd || job >= jobs) return;
     const int slice = (int)(job % (unsigned)slices), part = (int)(job / (unsigned)slices), h = part % a.H, split = part / a.H;
-    const int lane = lane_id(), wave = threadIdx.x >> 6;
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
     // this wave's rows: 64 at a time
     const int64_t rounds = (a.n + kWave - 1) / kWave, first = rounds * split / splits, last = rounds * (split + 1) / splits;
-    constexpr int waves = kSliceThreads / kWave;
-    int64_t round = first + wave;
+    constexpr int waves = THREADS / kWave;
+    int64_t round = first + wave;                   // the same for all lanes
     const int nw = (a.M + 3) >> 2;
-    auto find = [&](int64_t r) {
+    auto find = [&](int64_t r) -> int64_t {
         const int64_t t = r * kWave + lane;
-        return r < last && t < a.n ? rows.at(t) : kSkip;
+        if (r >= last) return kSkip;
+        const int lo = rows.sequence(r * kWave);    // the same for all lanes
+        return t < a.n ? rows.at(t, lo) : kSkip;
     };
     unsigned code[NW];
     float factor;
@@ -223,17 +236,17 @@ __global__ __launch_bounds__(kSliceThreads) void k_decode_slices(const DecodeArg
     {
         const float *C = a.C + (size_t)h * a.M * a.K * a.D;
         const int total = (L.pairs * a.K + 1) * 16, pos = threadIdx.x & 7, odd = (threadIdx.x >> 3) & 1, g = pos / LQ, d = slice * S + 4 * (pos % LQ);
-        for (int i0 = threadIdx.x; i0 < total; i0 += 8 * kSliceThreads) {
+        for (int i0 = threadIdx.x; i0 < total; i0 += 8 * THREADS) {
             float4 v[8];
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
-                const int line = (i0 + u * kSliceThreads) >> 4, i = line / a.K, k = line - i * a.K, m = (2 * i + odd) * G + g;
+                const int line = (i0 + u * THREADS) >> 4, i = line / a.K, k = line - i * a.K, m = (2 * i + odd) * G + g;
                 v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (m < a.M && i < L.pairs && d < a.D) v[u] = *reinterpret_cast<const float4 *>(C + ((size_t)m * a.K + k) * a.D + d);
             }
 #pragma unroll
             for (int u = 0; u < 8; ++u)
-                if (i0 + u * kSliceThreads < total) smem4[i0 + u * kSliceThreads] = v[u];
+                if (i0 + u * THREADS < total) smem4[i0 + u * THREADS] = v[u];
         }
     }
     __syncthreads();

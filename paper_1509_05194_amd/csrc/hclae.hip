@@ -2229,7 +2229,11 @@ static int launch_cache_write_tiles(hclae_ctx *ctx, const CacheRowsIn &a)
     constexpr size_t lds = (size_t)tile_lds(KB / UNITS, NC, WAVES);
     static_assert(lds <= (size_t)kLdsBudget, "a part and the next fit LDS");
     auto kern = &k_cache_write_tiles<KB, NC, UNITS, WAVES>;
-    HIP_TRY(ctx, hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBudget));
+    const uint64_t attr_set = 1ull << 46;       // this call site's bit in ctx->attr_done (D and K are the ctx's)
+    if (!(ctx->attr_done & attr_set)) {
+        HIP_TRY(ctx, hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBudget));
+        ctx->attr_done |= attr_set;
+    }
     const int64_t groups = (a.n + kTileVec * WAVES - 1) / (kTileVec * WAVES), per_xcd = (groups * a.H + 7) / 8, most = std::max(1, ctx->cus / 8);
     hipLaunchKernelGGL(kern, dim3((unsigned)(8 * std::min(per_xcd, most))), dim3(64 * WAVES), lds, ctx->stream, a, ctx->cache_tab, (int)groups);
     HIP_TRY(ctx, hipGetLastError());
@@ -2313,10 +2317,15 @@ template <typename T, typename Rows, int G>
 static int launch_decode_slices(hclae_ctx *ctx, const DecodeArgs &a, const Rows &rows, const SliceCut &cut)
 {
     auto kern = a.M <= 4 * G ? &k_decode_slices<T, Rows, G, true> : &k_decode_slices<T, Rows, G, false>;
-    HIP_TRY(ctx, hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBudget));
+    // this instance's bit in ctx->attr_done (M, K and D are the ctx's, and so is G)
+    const uint64_t attr_set = 1ull << (40 + 2 * (T::bytes == 4 ? 0 : __is_same(T, F16) ? 1 : 2) + (__is_same(Rows, CacheRows) ? 1 : 0));
+    if (!(ctx->attr_done & attr_set)) {
+        HIP_TRY(ctx, hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBudget));
+        ctx->attr_done |= attr_set;
+    }
     const int64_t jobs = (int64_t)a.H * cut.slices * cut.splits;
     const bool words = a.M % 4 == 0 && reinterpret_cast<uintptr_t>(a.codes) % 4 == 0;
-    hipLaunchKernelGGL(kern, dim3((unsigned)((jobs + 7) / 8 * 8)), dim3(kSliceThreads), (size_t)slice_lds(a.M, a.K, G).total, ctx->stream, a, rows, cut.slices,
+    hipLaunchKernelGGL(kern, dim3((unsigned)((jobs + 7) / 8 * 8)), dim3(slice_threads(G)), (size_t)slice_lds(a.M, a.K, G).total, ctx->stream, a, rows, cut.slices,
                        cut.splits, words);
     HIP_TRY(ctx, hipGetLastError());
     return HCLAE_OK;
@@ -2399,9 +2408,13 @@ static int launch_lookup_grad(hclae_ctx *ctx, const GradArgs &a)
 {
     const int pieces = (a.D + Piece<T>::dims - 1) / Piece<T>::dims;
     if (a.T <= kGradFew) {
-        int lanes = 1;
-        while (lanes < pieces && lanes < kWave) lanes *= 2;
-        const int parts = std::min(8, (pieces + kWave - 1) / kWave);
+        // a row as wide as the block can read it; parts of the coordinates where codewords alone are too few blocks for the CUs
+        int lanes = 1, parts = 1;
+        while (lanes < pieces && lanes < kGradThreads) lanes *= 2;
+        while (parts < 8 && a.M * a.K * parts < 4 * ctx->cus && lanes > 8) {
+            parts *= 2;
+            lanes /= 2;
+        }
         hipLaunchKernelGGL(k_grad_few<T>, dim3((unsigned)(a.M * a.K * parts)), dim3(kGradThreads), 0, ctx->stream, a, lanes, parts);
         HIP_TRY(ctx, hipGetLastError());
         return HCLAE_OK;

@@ -69,7 +69,7 @@ constexpr int kGradThreads = 256;
 constexpr int kGradFew = 4096;                      // rows up to which one launch finds and sums them
 
 // Few rows: a block per codeword of a dictionary and part of the coordinates looks at the codes of all rows, lists those that have
-// its codeword, in ascending order, and sums them: `lanes` (a power of two up to 64) lanes a row, kGradThreads / lanes rows at a
+// its codeword, in ascending order, and sums them: `lanes` (a power of two) lanes a row, kGradThreads / lanes rows at a
 // time, which are added up in ascending order at the end.
 template <typename T>
 __global__ __launch_bounds__(kGradThreads) void k_grad_few(const GradArgs a, int lanes, int parts)

@@ -164,26 +164,36 @@ def _ptr(t, dtype_name, shape=None):
     """Device pointer of a contiguous CUDA tensor of the expected dtype (None -> NULL)."""
     if t is None:
         return None
-    import torch
-    want = {"f32": torch.float32, "u8": torch.uint8, "i32": torch.int32, "f64": torch.float64, "i64": torch.int64}[dtype_name]
-    if not (t.is_cuda and t.dtype == want and t.is_contiguous()):
+    if not (t.is_cuda and t.dtype is _dtypes()[dtype_name] and t.is_contiguous()):
         raise TypeError("expected a contiguous CUDA %s tensor" % dtype_name)
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != tuple(shape):
         raise ValueError("tensor shape %s, expected %s" % (tuple(t.shape), tuple(shape)))
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr() or None
+
+
+_DTYPES = {}
+
+
+def _dtypes():
+    """The torch types behind the names, and the C ABI's number of each type of rows."""
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({"f32": torch.float32, "u8": torch.uint8, "i32": torch.int32, "f64": torch.float64, "i64": torch.int64,
+                        torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
+    return _DTYPES
 
 
 def _rows(t, shape):
     """(device pointer, type, strides in elements) of rows of float32, float16 or bfloat16 whose elements lie side by side."""
-    import torch
-    kind = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}.get(t.dtype)
+    kind = _dtypes().get(t.dtype)
     if not t.is_cuda or kind is None:
         raise TypeError("expected a CUDA float32, float16 or bfloat16 tensor")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != tuple(shape):
         raise ValueError("tensor shape %s, expected %s" % (tuple(t.shape), tuple(shape)))
-    if t.numel() and t.stride(-1) != 1:
+    strides = t.stride()
+    if strides[-1] != 1 and t.numel():
         raise ValueError("the elements of a row must lie side by side")
-    return ctypes.c_void_p(t.data_ptr()), kind, t.stride()
+    return t.data_ptr() or None, kind, strides
 
 
 class Context:
