@@ -373,7 +373,8 @@ int hclae_code_stats(hclae_ctx *ctx, const uint8_t *codes, int64_t N, int M, int
  * A cache of keys and values kept as codes: every head has M dictionaries of its own, a row of a head is M bytes
  * (and, if the caller keeps scales, one float).  hclae_cache_begin lays the dictionaries out for the calls below and
  * keeps copies of them in the ctx (at most 18 H M K D bytes, with K rounded up to 64, 128 or 256 and D to 64, 128 or 256; allocated by the
- * first call and by one with more heads than any before, which may therefore not be recorded into a HIP graph).  After a change to C it is called again.
+ * first call and by one with more heads than any before, which may therefore not be recorded into a HIP graph, and after which calls that
+ * were recorded earlier are recorded again).  After a change to C it is called again; what was written before was written with the old C.
  *   C: DEVICE float[H][M][K][D].  D <= HCLAE_CACHE_MAX_D.
  * Layout of the cache (DEVICE, caller-owned): codes uint8[n_slots][H][M], scale float[n_slots][H].
  */
@@ -389,6 +390,7 @@ int hclae_cache_begin(hclae_ctx *ctx, const float *C, int H, int M, int K, int D
  * The arithmetic is that of hclae_encode: r is held in fp32, distances are decided in their direct form in 64 bits,
  * the lowest index of equals.  A row with a NaN or an infinity is kept as a row of zeros with scale NaN, and reads back as NaN
  * (without scales as a row of zeros).  Slots that no row names are left as they are.  n <= N_max of hclae_create.  Only enqueues; uses no scratch.
+ * These calls run on the device of the ctx, whichever is current.
  */
 int hclae_cache_write(hclae_ctx *ctx, const void *X, int type, int64_t n, int64_t row_stride, int64_t head_stride,
                       const int64_t *slots, int64_t n_slots, uint8_t *codes, float *scale);

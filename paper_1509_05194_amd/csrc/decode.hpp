@@ -53,8 +53,12 @@ struct TableRows {                                  // hclae_lookup
         const int64_t r = rows ? rows[t] : t;
         return r >= 0 && r < V ? r : kNoRow;
     }
-    __host__ __device__ constexpr int sequence(int64_t) const { return 0; }
-    __host__ __device__ constexpr int64_t at(int64_t t, int) const { return at(t); }
+    // The same in two steps, a load between them that need not be waited for.
+    struct Probe {
+        int64_t r;
+    };
+    __device__ __forceinline__ Probe look(int64_t t, int64_t) const { return {rows ? rows[t] : t}; }
+    __device__ __forceinline__ int64_t at(const Probe &p) const { return p.r >= 0 && p.r < V ? p.r : kNoRow; }
 };
 
 struct CacheRows {                                  // hclae_cache_read
@@ -72,19 +76,38 @@ struct CacheRows {                                  // hclae_cache_read
         }
         return lo;
     }
-    __host__ __device__ constexpr int64_t at(int64_t t) const { return at(t, sequence(t)); }
-    // The same with a sequence that the row is in or behind.
-    __host__ __device__ constexpr int64_t at(int64_t t, int lo) const
+    // Where the row's page number is: its place in `tables`, or kNoRow or kSkip; off: its slot in the page.  lo: a sequence that the row is in or behind.
+    __host__ __device__ constexpr int64_t entry(int64_t t, int lo, unsigned &off) const
     {
         if (t < starts[0] || t >= starts[B]) return kSkip;
         while (lo + 1 < B && starts[lo + 1] <= t) ++lo;
         const int64_t pos = t - starts[lo];
         if (pos < 0 || pos > 0x7fffffff) return kSkip;
-        const unsigned p = (unsigned)pos / (unsigned)page, off = (unsigned)pos - p * (unsigned)page;
-        if (p >= (unsigned)max_pages) return kNoRow;
-        const int32_t q = tables[(int64_t)lo * max_pages + p];
-        return q >= 0 && q < pages ? (int64_t)q * page + off : kNoRow;
+        const unsigned p = (unsigned)pos / (unsigned)page;
+        off = (unsigned)pos - p * (unsigned)page;
+        return p < (unsigned)max_pages ? (int64_t)lo * max_pages + p : kNoRow;
     }
+    __host__ __device__ constexpr int64_t slot(int32_t q, unsigned off) const { return q >= 0 && q < pages ? (int64_t)q * page + off : kNoRow; }
+    __host__ __device__ constexpr int64_t at(int64_t t) const
+    {
+        unsigned off = 0;
+        const int64_t e = entry(t, sequence(t), off);
+        return e < 0 ? e : slot(tables[e], off);
+    }
+    // The same in two steps, a load between them that need not be waited for; first: a row at or before t, the same for all lanes.
+    struct Probe {
+        int64_t e;
+        int32_t q;
+        unsigned off;
+    };
+    __device__ __forceinline__ Probe look(int64_t t, int64_t first) const
+    {
+        Probe p = {0, 0, 0u};
+        p.e = entry(t, sequence(first), p.off);
+        if (p.e >= 0) p.q = tables[p.e];
+        return p;
+    }
+    __device__ __forceinline__ int64_t at(const Probe &p) const { return p.e < 0 ? p.e : slot(p.q, p.off); }
 };
 
 struct DecodeArgs {
@@ -203,12 +226,12 @@ __global__ __launch_bounds__(slice_threads(G)) void k_decode_slices(const Decode
     constexpr int waves = THREADS / kWave;
     int64_t round = first + wave;                   // the same for all lanes
     const int nw = (a.M + 3) >> 2;
-    auto find = [&](int64_t r) -> int64_t {
+    typedef typename Rows::Probe Probe;
+    auto look = [&](int64_t r) {
         const int64_t t = r * kWave + lane;
-        if (r >= last) return kSkip;
-        const int lo = rows.sequence(r * kWave);    // the same for all lanes
-        return t < a.n ? rows.at(t, lo) : kSkip;
+        return r < last && t < a.n ? rows.look(t, r * kWave) : Probe{};
     };
+    auto found = [&](int64_t r, const Probe &p) { return r < last && r * kWave + lane < a.n ? rows.at(p) : kSkip; };
     unsigned code[NW];
     float factor;
     auto fetch = [&](int64_t at) {
@@ -229,7 +252,8 @@ __global__ __launch_bounds__(slice_threads(G)) void k_decode_slices(const Decode
         }
         if (a.scale) factor = a.scale[at * a.H + h] * a.factor;
     };
-    int64_t at = find(round), next = find(round + waves);
+    int64_t at = found(round, look(round));
+    Probe probe = look(round + waves);
     fetch(at);
 
     // the slice
@@ -288,8 +312,9 @@ __global__ __launch_bounds__(slice_threads(G)) void k_decode_slices(const Decode
         const bool skips = __ballot(at == kSkip) != 0ull;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         const unsigned long long kept = __ballot(at != kSkip);
+        const int64_t next = found(round + waves, probe);
         fetch(next);
-        const int64_t after = find(round + 2 * waves);
+        probe = look(round + 2 * waves);
         char *to = static_cast<char *>(a.out) + ((round * kWave + (lane >> 3)) * a.row_stride + h * a.head_stride + d) * T::bytes;
         const int64_t step = 8 * a.row_stride * T::bytes;
         const float *factor8 = factors + (lane >> 3);
@@ -336,7 +361,6 @@ __global__ __launch_bounds__(slice_threads(G)) void k_decode_slices(const Decode
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         at = next;
-        next = after;
     }
 }
 

@@ -161,6 +161,7 @@ struct hclae_ctx {
     BeamMask *beam_mask;     // [beam_cap][beam_L]
     // coded cache: the dictionaries of its heads (hclae_cache_begin)
     int cache_H;             // 0: none yet
+    int cache_room;          // heads that the arrays have room for
     float *cache_C;          // [H][M][K][D]
     float4 *cache_T;         // [H][M][cache_padded(D) / 4][few_columns(K)]
     char *cache_buf;         // sorted, as fp16 images and tables (CacheTables)
@@ -2125,6 +2126,15 @@ struct OnDevice {
     const OnDevice device_(ctx); \
     HIP_TRY(ctx, device_.e)
 
+// Arrays of numbers of 4 and 8 bytes begin at whole numbers (null passes: checked apart).
+extern "C++" {
+template <typename... P>
+static bool odd_words(uintptr_t bytes, P... p)
+{
+    return (((reinterpret_cast<uintptr_t>(p)) | ...) & (bytes - 1)) != 0;
+}
+}  // extern "C++"
+
 // Rows of `type` in a caller's array: four elements at a time.
 static bool bad_rows(const void *p, int type, int64_t row_stride, int64_t head_stride)
 {
@@ -2162,7 +2172,7 @@ int hclae_cache_begin(hclae_ctx *ctx, const float *C, int H, int M, int K, int D
     const size_t parts_b = sets * units * part.bytes, img_b = sets * nc * kb * 4096, per_codeword_b = up(sets * kpad * sizeof(float)),
                  mu_b = up(sets * kChunkD * nc * sizeof(float)), consts_b = up(sets * kEncodeConsts * sizeof(float)), order_b = sets * 256, halves_b = up(sets * 257 * sizeof(float)),
                  C_b = up(sets * K * D * sizeof(float)), sorted_b = up(sets * K * cache_padded(D) * sizeof(float));
-    if (H > ctx->cache_H) {
+    if (H > ctx->cache_room) {
         float *copy = nullptr;
         float4 *T = nullptr;
         char *buf = nullptr;
@@ -2180,6 +2190,7 @@ int hclae_cache_begin(hclae_ctx *ctx, const float *C, int H, int M, int K, int D
         ctx->cache_C = copy;
         ctx->cache_T = T;
         ctx->cache_buf = buf;
+        ctx->cache_room = H;
     }
     ctx->cache_H = H;
     char *p = ctx->cache_buf;
@@ -2251,7 +2262,8 @@ int hclae_cache_write(hclae_ctx *ctx, const void *X, int type, int64_t n, int64_
     if (n_slots < 0 || n_slots > HCLAE_MAX_SLOTS) return fail(ctx, HCLAE_EINVAL, "hclae_cache_write: n_slots out of range");
     if (n == 0 || n_slots == 0) return HCLAE_OK;
     if (!X || !slots || !codes) return fail(ctx, HCLAE_EINVAL, "hclae_cache_write: bad argument");
-    if (bad_rows(X, type, row_stride, head_stride)) return fail(ctx, HCLAE_EINVAL, "hclae_cache_write: type, alignment or strides of X");
+    if (bad_rows(X, type, row_stride, head_stride) || odd_words(8, slots) || odd_words(4, scale))
+        return fail(ctx, HCLAE_EINVAL, "hclae_cache_write: type, alignment or strides");
     ON_DEVICE(ctx);
     const CacheRowsIn a = {X, type, row_stride, head_stride, slots, n, n_slots, codes, scale, ctx->cache_H, ctx->M, ctx->K, ctx->D};
     const int D = ctx->D;
@@ -2365,7 +2377,8 @@ int hclae_cache_read(hclae_ctx *ctx, const uint8_t *codes, const float *scale, i
         return fail(ctx, HCLAE_EINVAL, "hclae_cache_read: n_slots, B, max_pages or page out of range");
     if (n == 0 || B == 0) return HCLAE_OK;
     if (!starts || !out || (max_pages > 0 && !tables) || (n_slots > 0 && !codes)) return fail(ctx, HCLAE_EINVAL, "hclae_cache_read: bad argument");
-    if (bad_rows(out, type, row_stride, head_stride)) return fail(ctx, HCLAE_EINVAL, "hclae_cache_read: type, alignment or strides of out");
+    if (bad_rows(out, type, row_stride, head_stride) || odd_words(4, scale, tables, starts))
+        return fail(ctx, HCLAE_EINVAL, "hclae_cache_read: type, alignment or strides");
     if (!apart(n, ctx->cache_H, ctx->D, row_stride, head_stride)) return fail(ctx, HCLAE_EINVAL, "hclae_cache_read: rows of out overlap");
     ON_DEVICE(ctx);
     const DecodeArgs a = {codes, scale, 1.f, ctx->cache_C, ctx->cache_H, ctx->M, ctx->K, ctx->D, n, out, row_stride, head_stride};
@@ -2381,7 +2394,7 @@ static int check_lookup(hclae_ctx *ctx, const char *name, const int64_t *rows, i
     if (V < 0 || V > HCLAE_MAX_SLOTS || (!rows && V < T)) return fail(ctx, HCLAE_EINVAL, name);
     if (!C || misaligned(C)) return fail(ctx, HCLAE_EINVAL, name);
     if (T == 0) return HCLAE_OK;
-    if (!x || (V > 0 && !codes) || bad_rows(x, type, row_stride, 0)) return fail(ctx, HCLAE_EINVAL, name);
+    if (!x || (V > 0 && !codes) || bad_rows(x, type, row_stride, 0) || odd_words(8, rows)) return fail(ctx, HCLAE_EINVAL, name);
     return HCLAE_OK;
 }
 

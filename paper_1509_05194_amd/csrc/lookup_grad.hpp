@@ -223,7 +223,6 @@ __global__ __launch_bounds__(kSortThreads) void k_grad_place(const GradArgs a, c
     __syncthreads();
     if (m >= a.M) return;
     int *list = s.list + (size_t)m * a.T;
-#pragma unroll 4
     for (int i = 0; i < s.range; i += kWave) {
         const int64_t t = t0 + i + lane;
         const int c = t < a.T ? grad_code(a, t, m) : -1;

@@ -204,10 +204,12 @@ class Context:
         if stream is None:
             stream = torch.cuda.current_stream().cuda_stream
         self.N_max, self.D, self.M, self.K = int(N_max), int(D), int(M), int(K)
+        self._H = 0                            # heads of the cache
         self._h = ctypes.c_void_p()
         rc = lib().hclae_create(ctypes.byref(self._h), self.N_max, self.D, self.M, self.K, ctypes.c_void_p(stream))
         if rc != OK:
             raise HclaeError(rc, lib().hclae_last_error(None).decode())
+        self._device = torch.cuda.current_device()
 
     def close(self):
         if self._h:
@@ -219,6 +221,11 @@ class Context:
             self.close()
         except Exception:
             pass
+
+    def _here(self, *tensors):
+        for t in tensors:
+            if t is not None and t.get_device() not in (-1, self._device):
+                raise ValueError("a tensor on another device than the context")
 
     def _chk(self, rc):
         if rc != OK:
@@ -429,6 +436,7 @@ class Context:
     def cache_begin(self, C):
         """Lays out the dictionaries of a cache, C float32 [H][M][K][D]; called again after a change to them."""
         H = C.shape[0]
+        self._here(C)
         self._chk(lib().hclae_cache_begin(self._h, _ptr(C, "f32", (H, self.M, self.K, self.D)), H, self.M, self.K, self.D))
         self._H = H
 
@@ -436,7 +444,8 @@ class Context:
         """Quantises the rows X [n][H][D] (float32, float16 or bfloat16; rows and heads at any distance) into slots int64 [n] of
         codes uint8 [n_slots][H][M] and scale float32 [n_slots][H] (None: rows are quantised as they are); a slot outside
         [0, n_slots) keeps nothing."""
-        n, n_slots, H = X.shape[0], codes.shape[0], getattr(self, "_H", codes.shape[1])
+        n, n_slots, H = X.shape[0], codes.shape[0], self._H or codes.shape[1]
+        self._here(X, slots, codes, scale)
         p, kind, st = _rows(X, (n, H, self.D))
         self._chk(lib().hclae_cache_write(self._h, p, kind, n, st[0], st[1], _ptr(slots, "i64", (n,)), n_slots,
                                           _ptr(codes, "u8", (n_slots, H, self.M)), _ptr(scale, "f32", (n_slots, H))))
@@ -444,7 +453,8 @@ class Context:
     def cache_read(self, codes, scale, tables, starts, page, out):
         """Reads the rows of B sequences back: pages tables int32 [B][max_pages], sequence b into rows starts[b]..starts[b + 1]
         of out [n][H][D] (float32, float16 or bfloat16), starts int32 [B + 1]; other rows of out are left as they are."""
-        n, n_slots, H = out.shape[0], codes.shape[0], getattr(self, "_H", codes.shape[1])
+        n, n_slots, H = out.shape[0], codes.shape[0], self._H or codes.shape[1]
+        self._here(codes, scale, tables, starts, out)
         B, max_pages = tables.shape
         p, kind, st = _rows(out, (n, H, self.D))
         self._chk(lib().hclae_cache_read(self._h, _ptr(codes, "u8", (n_slots, H, self.M)), _ptr(scale, "f32", (n_slots, H)),
@@ -455,6 +465,7 @@ class Context:
         """out[t] = scale * sum_m C[m][codes[rows[t]][m]] for a table kept as codes uint8 [V][M]; rows int64 [T], or None: rows
         0..T-1.  out [T][D] float32, float16 or bfloat16, rows at any distance."""
         T, V = out.shape[0], codes.shape[0]
+        self._here(codes, C, out, rows)
         p, kind, st = _rows(out, (T, self.D))
         self._chk(lib().hclae_lookup(self._h, _ptr(rows, "i64", (T,)), T, _ptr(codes, "u8", (V, self.M)), V, scale,
                                      _ptr(C, "f32", (self.M, self.K, self.D)), self.M, self.K, self.D, p, kind, st[0]))
@@ -462,6 +473,7 @@ class Context:
     def lookup_grad(self, codes, grad, dC, rows=None, scale=1.0):
         """dC float32 [M][K][D], the gradient of lookup with respect to C, from that of its output, grad [T][D]."""
         T, V = grad.shape[0], codes.shape[0]
+        self._here(codes, grad, dC, rows)
         p, kind, st = _rows(grad, (T, self.D))
         self._chk(lib().hclae_lookup_grad(self._h, _ptr(rows, "i64", (T,)), T, _ptr(codes, "u8", (V, self.M)), V, scale, p, kind,
                                           st[0], self.M, self.K, self.D, _ptr(dC, "f32", (self.M, self.K, self.D))))

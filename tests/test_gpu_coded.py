@@ -487,6 +487,74 @@ def test_table_captured_and_replayed(T):
         ctx.close()
 
 
+def test_dictionaries_laid_out_again():
+    """Other dictionaries, fewer heads, then more: every call uses those of the last hclae_cache_begin."""
+    from paper_1509_05194_amd import hclae
+    n, D, M, K = 20, 64, 3, 40
+    ctx = hclae.Context(n, D, M, K)
+    for H, seed in ((3, 1), (3, 2), (1, 3), (2, 4), (7, 5)):
+        x, C = heads(n, H, D, M, K, seed)
+        ctx.cache_begin(torch.from_numpy(C).cuda())
+        codes, scale = torch.zeros((n, H, M), dtype=torch.uint8, device="cuda"), torch.zeros((n, H), device="cuda")
+        ctx.cache_write(torch.from_numpy(x).cuda(), torch.arange(n, device="cuda"), codes, scale)
+        out = torch.zeros((n, H, D), device="cuda")
+        ctx.cache_read(codes, scale, torch.arange(5, dtype=torch.int32, device="cuda")[None], torch.tensor([0, n], dtype=torch.int32, device="cuda"), 4, out)
+        for h in range(H):
+            want, g = quantise(x[:, h].copy(), C[h], True)
+            assert np.array_equal(codes[:, h].cpu().numpy(), want)
+            back, mag = decoded(want, C[h], g)
+            close_to(out[:, h], back, mag, M, torch.float32)
+    ctx.close()
+
+
+def test_large_calls_captured_on_two_streams_at_once():
+    """Two contexts on two streams, each with a prompt written, read back, and the gradient of a lookup in one graph, replayed side by side
+    with eager work in between: the bits of the same calls one after another."""
+    from paper_1509_05194_amd import hclae
+    H, D, M, K, n, page = 4, 128, 8, 256, 3000, 16
+    jobs = []
+    for seed in (1, 2):
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            x, C = heads(n, H, D, M, K, seed)
+            j = {"s": s, "X": torch.from_numpy(x).cuda().to(torch.bfloat16), "C": torch.from_numpy(C).cuda(), "ctx": hclae.Context(2 * n, D, M, K)}
+            j["slots"] = torch.randperm(n, generator=torch.Generator().manual_seed(seed)).cuda()
+            j["codes"], j["scale"] = torch.zeros((n, H, M), dtype=torch.uint8, device="cuda"), torch.zeros((n, H), device="cuda")
+            j["tables"] = torch.arange((n + page - 1) // page, dtype=torch.int32, device="cuda")[None]
+            j["starts"] = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+            j["out"], j["dC"] = torch.zeros((n, H, D), dtype=torch.bfloat16, device="cuda"), torch.zeros((M, K, D), device="cuda")
+            j["rows"] = torch.randint(-1, n * H, (2 * n,), generator=torch.Generator().manual_seed(seed)).cuda()
+            j["g"] = torch.randn((2 * n, D), generator=torch.Generator().manual_seed(seed)).cuda()
+
+            def work(j=j):
+                j["ctx"].cache_write(j["X"], j["slots"], j["codes"], j["scale"])
+                j["ctx"].cache_read(j["codes"], j["scale"], j["tables"], j["starts"], page, j["out"])
+                j["ctx"].lookup_grad(j["codes"].view(n * H, M), j["g"], j["dC"], rows=j["rows"])
+
+            j["ctx"].cache_begin(j["C"])
+            work()
+            torch.cuda.synchronize()
+            j["want"] = [j[k].clone() for k in ("codes", "scale", "out", "dC")]
+            j["graph"] = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(j["graph"], stream=s):
+                work()
+        jobs.append(j)
+    for _ in range(3):
+        for j in jobs:
+            for k in ("codes", "scale", "out", "dC"):
+                j[k].zero_()
+        torch.cuda.synchronize()
+        for j in jobs:
+            with torch.cuda.stream(j["s"]):
+                j["graph"].replay()
+        torch.cuda.synchronize()
+        for j in jobs:
+            for k, want in zip(("codes", "scale", "out", "dC"), j["want"]):
+                assert torch.equal(j[k], want), k
+    for j in jobs:
+        j["ctx"].close()
+
+
 def test_refusals():
     from paper_1509_05194_amd import hclae
     L = hclae.lib()
@@ -516,7 +584,8 @@ def test_refusals():
 
     assert write() == hclae.OK and write(n=0, X=None) == hclae.OK and write(ns=0, c=None) == hclae.OK
     for bad in (dict(X=None), dict(s=None), dict(c=None), dict(kind=3), dict(kind=-1), dict(X=x.data_ptr() + 4), dict(X=x.data_ptr() + 2, kind=1),
-                dict(rs=47), dict(hs=18), dict(rs=-48), dict(ns=-1), dict(ns=2 ** 41), dict(n=-1)):
+                dict(rs=47), dict(hs=18), dict(rs=-48), dict(ns=-1), dict(ns=2 ** 41), dict(n=-1), dict(s=slots.data_ptr() + 4),
+                dict(g=scale.data_ptr() + 2)):
         assert write(**bad) == hclae.EINVAL, bad
     assert write(n=101) == hclae.ESTATE
 
