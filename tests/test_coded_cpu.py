@@ -38,6 +38,18 @@ constexpr bool inside()
     return true;
 }
 static_assert(inside(), "any starts");
+constexpr bool quotients()
+{
+    const int pages[] = {1, 2, 3, 5, 7, 16, 24, 641, 65535, 65537, (1 << 30) - 1, 1 << 30, (1 << 30) + 1, 0x7ffffffe, 0x7fffffff};
+    for (int page : pages)
+        for (int64_t i = 0; i < 9; ++i) {
+            const int64_t q = (0x7fffffffll / page) * i / 8;        // multiples over the range, and what is next to them
+            for (int64_t x = q * page - 2; x <= q * page + 2; ++x)
+                if (x >= 0 && x <= 0x7fffffff && (int64_t)((uint64_t)x * page_mul(page) >> (31 + page_shift(page))) != x / page) return false;
+        }
+    return true;
+}
+static_assert(quotients(), "pos / page");
 // rows of a table
 constexpr int64_t rows[] = {2, -1, 7, 6, 1ll << 40, -(1ll << 62)};
 constexpr TableRows table{rows, 7};

@@ -63,12 +63,18 @@ WRITE = [
     (3, 2, 256, 3, 256, "bf16", True, "wide"), (33, 5, 80, 5, 200, "fp32", False, "heads"), (70, 3, 36, 4, 20, "fp16", True, "wide"),
     (130, 2, 132, 2, 130, "bf16", False, "tight"), (300, 1, 128, 4, 256, "bf16", True, "wide"), (65, 4, 192, 2, 64, "fp32", True, "heads"),
     (257, 2, 64, 3, 256, "fp32", False, "wide"), (515, 1, 124, 2, 100, "fp16", True, "heads"), (40, 16, 20, 2, 33, "bf16", True, "tight"),
-    # more rows, every size of dictionary and row
+    # more rows, sixteen a block
     (2100, 1, 64, 2, 20, "bf16", True, "wide"), (1101, 2, 60, 2, 60, "fp16", True, "heads"), (2200, 1, 36, 2, 100, "fp32", False, "tight"),
     (700, 3, 64, 2, 256, "bf16", True, "wide"), (2500, 1, 128, 2, 30, "fp32", True, "tight"), (1200, 2, 100, 2, 64, "bf16", True, "heads"),
     (2300, 1, 128, 2, 128, "fp16", True, "wide"), (3001, 1, 128, 3, 256, "bf16", False, "tight"), (2100, 1, 200, 2, 32, "bf16", True, "wide"),
     (1100, 2, 256, 2, 64, "fp32", False, "heads"), (2100, 1, 160, 2, 120, "fp16", True, "tight"), (700, 4, 256, 2, 256, "bf16", True, "wide"),
     (2089, 1, 196, 2, 201, "fp32", True, "heads"), (2060, 1, 4, 2, 1, "fp32", True, "tight"), (301, 9, 12, 3, 2, "fp32", False, "tight"),
+    # more than 4096 rows, in tiles: every size of dictionary (blocks of 32, 64, 128, 256) and row (64, 128, 256)
+    (4200, 1, 64, 2, 20, "bf16", True, "wide"), (1403, 3, 60, 2, 60, "fp16", True, "heads"), (4099, 1, 36, 2, 100, "fp32", False, "tight"),
+    (1400, 3, 64, 2, 256, "bf16", True, "wide"), (4130, 1, 128, 2, 30, "fp32", True, "tight"), (2103, 2, 100, 2, 64, "bf16", True, "heads"),
+    (4150, 1, 128, 2, 128, "fp16", True, "wide"), (1033, 4, 124, 3, 256, "bf16", False, "tight"), (4097, 1, 200, 2, 32, "bf16", True, "wide"),
+    (2060, 2, 256, 2, 64, "fp32", False, "heads"), (4111, 1, 160, 2, 120, "fp16", True, "tight"), (1050, 4, 256, 2, 256, "bf16", True, "wide"),
+    (4112, 1, 196, 2, 201, "fp32", True, "heads"), (4160, 1, 4, 2, 1, "fp32", True, "tight"), (601, 9, 12, 3, 2, "fp32", False, "tight"),
 ]
 
 
@@ -111,7 +117,8 @@ def test_write(n, H, D, M, K, kind, scaled, layout):
 
 
 @pytest.mark.parametrize("spread", [1e-30, 1e-18, 1e15, 1e30])
-@pytest.mark.parametrize("n,K,D", [(5, 256, 64), (200, 90, 128), (1100, 256, 128), (1200, 70, 132)])
+@pytest.mark.parametrize("n,K,D", [(5, 256, 64), (200, 90, 128), (1100, 256, 128), (1200, 70, 132), (2100, 256, 128), (2080, 70, 132),
+                                   (2090, 30, 64)])
 def test_write_unusual_magnitudes(spread, n, K, D):
     """Rows quantised as they are, whose squares leave the range of fp32."""
     from paper_1509_05194_amd import hclae
@@ -126,7 +133,8 @@ def test_write_unusual_magnitudes(spread, n, K, D):
 
 
 @pytest.mark.parametrize("n,K,D,what", [(1500, 256, 128, "far"), (1500, 256, 128, "equal"), (1100, 200, 64, "zeros"), (1100, 64, 200, "equal"),
-                                        (1300, 256, 256, "far"), (60, 256, 128, "far"), (60, 256, 128, "equal"), (60, 70, 64, "zeros")])
+                                        (1300, 256, 256, "far"), (2100, 256, 128, "far"), (2070, 256, 128, "equal"), (2100, 200, 64, "zeros"), (2060, 64, 200, "equal"),
+                                        (2200, 256, 256, "far"), (60, 256, 128, "far"), (60, 256, 128, "equal"), (60, 70, 64, "zeros")])
 def test_write_with_many_near_ties(n, K, D, what):
     """Rows far from the origin compared with what tells them apart, dictionaries of equal codewords, and of zeros."""
     from paper_1509_05194_amd import hclae
@@ -256,6 +264,31 @@ def test_read_sequences_longer_than_their_pages():
                    4, out)
     want = torch.tensor([1.0] * 8 + [0.0] * 9 + [9.0] * 3, device="cuda")
     assert torch.equal(out[:, 0], want[:, None].expand(-1, 8))
+    ctx.close()
+
+
+@pytest.mark.parametrize("n,M", [(6, 8), (5000, 8), (5000, 16)])
+def test_rows_that_are_not_there_are_zero_whatever_the_codewords_are(n, M):
+    from paper_1509_05194_amd import hclae
+    K, D = 256, 64
+    C = torch.randn((1, M, K, D), generator=torch.Generator().manual_seed(3)).cuda()
+    C[0, 0, 0, 5], C[0, M - 1, 0, 7], C[0, 1, 0, 9] = float("inf"), float("nan"), -3e38
+    codes = torch.zeros((n, 1, M), dtype=torch.uint8, device="cuda")
+    codes[3] = 1
+    ctx = hclae.Context(n, D, M, K)
+    ctx.cache_begin(C)
+    out = torch.full((n, 1, D), 9.0, device="cuda")
+    tables = torch.full((1, n), -1, dtype=torch.int32, device="cuda")
+    tables[0, 3] = 3
+    ctx.cache_read(codes, None, tables, torch.tensor([0, n - 1], dtype=torch.int32, device="cuda"), 1, out)
+    want = torch.zeros((n, 1, D), device="cuda")
+    want[3], want[n - 1] = C[0, :, 1].double().sum(0).float(), 9.0
+    assert torch.allclose(out, want, rtol=0, atol=(M + 3) * U32 * 8 * M)      # |c| < 8
+    looked = torch.full((n, D), 9.0, device="cuda")
+    rows = torch.full((n,), -1, dtype=torch.int64, device="cuda")
+    rows[4] = n
+    ctx.lookup(codes[:, 0], C[0], looked, rows=rows)
+    assert bool((looked == 0).all())
     ctx.close()
 
 
