@@ -544,6 +544,9 @@ constexpr int kTileBatch = 4;                       // undecided rows of a wave 
 __host__ __device__ constexpr int tile_stretch(int nc) { return nc == 4 ? 4096 : 2048; }
 __host__ __device__ constexpr int tile_lds(int kbu, int nc, int waves) { return 2 * tile_part(kbu, nc).bytes + waves * tile_stretch(nc); }
 
+// Waves of a block: what LDS and registers allow.  Half of them where those are enough for all tiles at once.
+__host__ __device__ constexpr int tile_waves(int nc) { return nc == 4 ? 4 : 8; }
+
 // KB: blocks of 32 codewords.  NC: 64-position chunks (1, 2 or 4).  UNITS: parts in which a dictionary passes through LDS.
 template <int KB, int NC, int UNITS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void k_cache_write_tiles(const CacheRowsIn a, const CacheTables tab, int groups)

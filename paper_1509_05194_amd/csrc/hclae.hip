@@ -2153,9 +2153,6 @@ static bool apart(int64_t n, int H, int D, int64_t row_stride, int64_t head_stri
     return (row_stride - D) / (H - 1) >= head_stride || (head_stride - D) / (n - 1) >= row_stride;
 }
 
-// Rows of all heads up to which k_cache_write_one takes them, and k_cache_write_some.
-constexpr int64_t kOneRows = 256, kSomeMost = 4096;
-
 int hclae_cache_begin(hclae_ctx *ctx, const float *C, int H, int M, int K, int D)
 {
     int rc = check_call(ctx, 0, D, M, K);
@@ -2217,30 +2214,44 @@ int hclae_cache_begin(hclae_ctx *ctx, const float *C, int H, int M, int K, int D
     return HCLAE_OK;
 }
 
+// Which kernel takes the rows of a write: the one with the least time by the rounds of blocks that the CUs go through, a round of
+// k_cache_write_one (a row a block) counting 1, of k_cache_write_some (sixteen) 2, of tiles with half of the waves 3.2 and with all of them 4.
+// Measured with M = 8, K = 256 on 256 CUs, us of one round at D = 64, 128, 256: 16, 24, 43; 29, 48, 75; 46, 78, 133; 55, 92, 150.  So at D = 128
+// and 8 heads: 256 rows 28 (one) and 44 (some), 512 rows 46 and 46, 1024 rows 89 and 48; 4096 rows 51 (some) and 78 (half),
+// 8192 rows 91 and 84; 32768 rows 82 (half) and 92 (all), 65536 rows 154 and 99.
+enum CacheWay { kWayOne, kWaySome, kWayHalf, kWayAll };
+static CacheWay cache_way(int64_t n, int H, int D, int cus)
+{
+    const int64_t waves = tile_waves(cache_chunks(D));
+    auto rounds = [&](int64_t rows) { return (double)(((n + rows - 1) / rows * H + cus - 1) / cus); };
+    const double us[4] = {rounds(1), 2.0 * rounds(kSomeRows), 3.2 * rounds(kTileVec * waves / 2), 4.0 * rounds(kTileVec * waves)};
+    int way = kWayAll;
+    for (int w = kWayHalf; w >= kWayOne; --w)
+        if (us[w] < us[way]) way = w;
+    return (CacheWay)way;
+}
+
 extern "C++" {
 // P: float4 pieces of a row up to which the instance goes, 16 coordinates each.
 template <int COLS, int P>
-static int launch_cache_write_rows(hclae_ctx *ctx, const CacheRowsIn &a)
+static int launch_cache_write_rows(hclae_ctx *ctx, const CacheRowsIn &a, CacheWay way)
 {
-    if (a.n * a.H <= kOneRows) {
-        hipLaunchKernelGGL((k_cache_write_one<COLS, 4 * P * COLS / kFewThreads>), dim3((unsigned)(a.n * a.H)), dim3(kFewThreads), 0, ctx->stream, a, ctx->cache_T);
-    } else {
-        const int64_t jobs = (a.n + kSomeRows - 1) / kSomeRows * a.H;
-        hipLaunchKernelGGL((k_cache_write_some<COLS, P>), dim3((unsigned)(jobs < (1 << 20) ? jobs : 1 << 20)), dim3(kFewThreads), 0, ctx->stream, a, ctx->cache_T,
-                           ctx->cache_tab.halves);
-    }
+    const int64_t jobs = way == kWayOne ? a.n * a.H : (a.n + kSomeRows - 1) / kSomeRows * a.H;
+    const dim3 grid((unsigned)std::min<int64_t>(jobs, 1 << 20));
+    if (way == kWayOne) hipLaunchKernelGGL((k_cache_write_one<COLS, 4 * P * COLS / kFewThreads>), grid, dim3(kFewThreads), 0, ctx->stream, a, ctx->cache_T);
+    else hipLaunchKernelGGL((k_cache_write_some<COLS, P>), grid, dim3(kFewThreads), 0, ctx->stream, a, ctx->cache_T, ctx->cache_tab.halves);
     HIP_TRY(ctx, hipGetLastError());
     return HCLAE_OK;
 }
 
-template <int KB, int NC>
-static int launch_cache_write_tiles(hclae_ctx *ctx, const CacheRowsIn &a)
+template <int KB, int NC, int WAVES>
+static int launch_cache_write_waves(hclae_ctx *ctx, const CacheRowsIn &a)
 {
-    constexpr int UNITS = tile_units(KB, NC), WAVES = NC == 4 ? 4 : 8;
+    constexpr int UNITS = tile_units(KB, NC);
     constexpr size_t lds = (size_t)tile_lds(KB / UNITS, NC, WAVES);
     static_assert(lds <= (size_t)kLdsBudget, "a part and the next fit LDS");
     auto kern = &k_cache_write_tiles<KB, NC, UNITS, WAVES>;
-    const uint64_t attr_set = 1ull << 46;       // this call site's bit in ctx->attr_done (D and K are the ctx's)
+    const uint64_t attr_set = 1ull << (WAVES == tile_waves(NC) ? 46 : 47);      // this instance's bit in ctx->attr_done (D and K are the ctx's)
     if (!(ctx->attr_done & attr_set)) {
         HIP_TRY(ctx, hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBudget));
         ctx->attr_done |= attr_set;
@@ -2249,6 +2260,11 @@ static int launch_cache_write_tiles(hclae_ctx *ctx, const CacheRowsIn &a)
     hipLaunchKernelGGL(kern, dim3((unsigned)(8 * std::min(per_xcd, most))), dim3(64 * WAVES), lds, ctx->stream, a, ctx->cache_tab, (int)groups);
     HIP_TRY(ctx, hipGetLastError());
     return HCLAE_OK;
+}
+template <int KB, int NC>
+static int launch_cache_write_tiles(hclae_ctx *ctx, const CacheRowsIn &a, CacheWay way)
+{
+    return way == kWayHalf ? launch_cache_write_waves<KB, NC, tile_waves(NC) / 2>(ctx, a) : launch_cache_write_waves<KB, NC, tile_waves(NC)>(ctx, a);
 }
 }  // extern "C++"
 
@@ -2267,30 +2283,32 @@ int hclae_cache_write(hclae_ctx *ctx, const void *X, int type, int64_t n, int64_
     ON_DEVICE(ctx);
     const CacheRowsIn a = {X, type, row_stride, head_stride, slots, n, n_slots, codes, scale, ctx->cache_H, ctx->M, ctx->K, ctx->D};
     const int D = ctx->D;
-    if (n * a.H > kSomeMost && (n / kTileVec + 1) * a.H < (int64_t)1 << 30) switch (cache_chunks(D) * 16 + ctx->kb) {
-        case 16 + 1: return launch_cache_write_tiles<1, 1>(ctx, a);
-        case 16 + 2: return launch_cache_write_tiles<2, 1>(ctx, a);
-        case 16 + 4: return launch_cache_write_tiles<4, 1>(ctx, a);
-        case 16 + 8: return launch_cache_write_tiles<8, 1>(ctx, a);
-        case 32 + 1: return launch_cache_write_tiles<1, 2>(ctx, a);
-        case 32 + 2: return launch_cache_write_tiles<2, 2>(ctx, a);
-        case 32 + 4: return launch_cache_write_tiles<4, 2>(ctx, a);
-        case 32 + 8: return launch_cache_write_tiles<8, 2>(ctx, a);
-        case 64 + 1: return launch_cache_write_tiles<1, 4>(ctx, a);
-        case 64 + 2: return launch_cache_write_tiles<2, 4>(ctx, a);
-        case 64 + 4: return launch_cache_write_tiles<4, 4>(ctx, a);
-        default: return launch_cache_write_tiles<8, 4>(ctx, a);
+    CacheWay way = cache_way(n, a.H, D, std::max(1, ctx->cus));
+    if ((n / kTileVec + 1) * a.H >= (int64_t)1 << 30) way = kWaySome;       // tiles are counted in 32 bits
+    if (way == kWayHalf || way == kWayAll) switch (cache_chunks(D) * 16 + ctx->kb) {
+        case 16 + 1: return launch_cache_write_tiles<1, 1>(ctx, a, way);
+        case 16 + 2: return launch_cache_write_tiles<2, 1>(ctx, a, way);
+        case 16 + 4: return launch_cache_write_tiles<4, 1>(ctx, a, way);
+        case 16 + 8: return launch_cache_write_tiles<8, 1>(ctx, a, way);
+        case 32 + 1: return launch_cache_write_tiles<1, 2>(ctx, a, way);
+        case 32 + 2: return launch_cache_write_tiles<2, 2>(ctx, a, way);
+        case 32 + 4: return launch_cache_write_tiles<4, 2>(ctx, a, way);
+        case 32 + 8: return launch_cache_write_tiles<8, 2>(ctx, a, way);
+        case 64 + 1: return launch_cache_write_tiles<1, 4>(ctx, a, way);
+        case 64 + 2: return launch_cache_write_tiles<2, 4>(ctx, a, way);
+        case 64 + 4: return launch_cache_write_tiles<4, 4>(ctx, a, way);
+        default: return launch_cache_write_tiles<8, 4>(ctx, a, way);
         }
     switch (few_columns(ctx->K) + cache_chunks(D)) {
-    case 64 + 1: return launch_cache_write_rows<64, 4>(ctx, a);
-    case 64 + 2: return launch_cache_write_rows<64, 8>(ctx, a);
-    case 64 + 4: return launch_cache_write_rows<64, 16>(ctx, a);
-    case 128 + 1: return launch_cache_write_rows<128, 4>(ctx, a);
-    case 128 + 2: return launch_cache_write_rows<128, 8>(ctx, a);
-    case 128 + 4: return launch_cache_write_rows<128, 16>(ctx, a);
-    case 256 + 1: return launch_cache_write_rows<256, 4>(ctx, a);
-    case 256 + 2: return launch_cache_write_rows<256, 8>(ctx, a);
-    default: return launch_cache_write_rows<256, 16>(ctx, a);
+    case 64 + 1: return launch_cache_write_rows<64, 4>(ctx, a, way);
+    case 64 + 2: return launch_cache_write_rows<64, 8>(ctx, a, way);
+    case 64 + 4: return launch_cache_write_rows<64, 16>(ctx, a, way);
+    case 128 + 1: return launch_cache_write_rows<128, 4>(ctx, a, way);
+    case 128 + 2: return launch_cache_write_rows<128, 8>(ctx, a, way);
+    case 128 + 4: return launch_cache_write_rows<128, 16>(ctx, a, way);
+    case 256 + 1: return launch_cache_write_rows<256, 4>(ctx, a, way);
+    case 256 + 2: return launch_cache_write_rows<256, 8>(ctx, a, way);
+    default: return launch_cache_write_rows<256, 16>(ctx, a, way);
     }
 }
 

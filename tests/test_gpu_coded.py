@@ -154,6 +154,33 @@ def test_write_with_many_near_ties(n, K, D, what):
     ctx.close()
 
 
+@pytest.mark.parametrize("D,K", [(64, 20), (60, 60), (36, 100), (64, 256), (128, 30), (100, 64), (128, 128), (124, 255), (200, 32), (256, 64), (160, 120),
+                                 (256, 256)])
+def test_write_of_very_many_rows_is_that_of_its_parts(D, K):
+    """Calls that fill the device with tiles; parts of 500 rows of a head, and a sample of rows in 64 bits."""
+    from paper_1509_05194_amd import hclae
+    H, M, n = 3, 3, 11333 if D <= 128 else 6007
+    x, C = heads(n, H, D, M, K, D + K)
+    x[17], x[n - 1, 1, D - 1] = 0, np.nan
+    X, slots = torch.from_numpy(x).cuda(), torch.randperm(n, generator=torch.Generator().manual_seed(1)).cuda()
+    slots[5] = n
+    ctx = hclae.Context(n, D, M, K)
+    ctx.cache_begin(torch.from_numpy(C).cuda())
+    got, want = (torch.full((n, H, M), 251, dtype=torch.uint8, device="cuda") for _ in range(2))
+    g, want_g = (torch.full((n, H), -3.0, device="cuda") for _ in range(2))
+    ctx.cache_write(X, slots, got, g)
+    for i in range(0, n, 500):
+        ctx.cache_write(X[i:i + 500], slots[i:i + 500], want, want_g)
+    assert torch.equal(got, want) and torch.equal(g.nan_to_num(-1), want_g.nan_to_num(-1))
+    at = np.concatenate([[0, 17, n - 1], np.random.default_rng(0).integers(6, n, 60)])
+    for h in range(H):
+        codes, scales = quantise(x[at, h].copy(), C[h], True)
+        where = slots.cpu().numpy()[at]
+        assert np.array_equal(got[:, h].cpu().numpy()[where], codes)
+        assert np.array_equal(g[:, h].cpu().numpy()[where], scales, equal_nan=True)
+    ctx.close()
+
+
 def test_write_gives_the_codes_of_the_encoder():
     """One head, no scales: the codes of hclae_encode, whichever kernels took the rows."""
     from paper_1509_05194_amd import hclae
