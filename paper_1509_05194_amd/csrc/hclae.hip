@@ -2218,7 +2218,7 @@ int hclae_cache_begin(hclae_ctx *ctx, const float *C, int H, int M, int K, int D
 // k_cache_write_one (a row a block) counting 1, of k_cache_write_some (sixteen) 2, of tiles with half of the waves 3.2 and with all of them 4.
 // Measured with M = 8, K = 256 on 256 CUs, us of one round at D = 64, 128, 256: 16, 24, 43; 29, 48, 75; 46, 78, 133; 55, 92, 150.  So at D = 128
 // and 8 heads: 256 rows 28 (one) and 44 (some), 512 rows 46 and 46, 1024 rows 89 and 48; 4096 rows 51 (some) and 78 (half),
-// 8192 rows 91 and 84; 32768 rows 82 (half) and 92 (all), 65536 rows 154 and 99.
+// 8192 rows 91 (some) and 82 (half); 32768 rows 82 (half) and 92 (all), 65536 rows 154 and 99.
 enum CacheWay { kWayOne, kWaySome, kWayHalf, kWayAll };
 static CacheWay cache_way(int64_t n, int H, int D, int cus)
 {
@@ -2326,7 +2326,9 @@ static int launch_decode(hclae_ctx *ctx, const DecodeArgs &a, const Rows &rows)
     return HCLAE_OK;
 }
 // How many parts the rows of a sliced decode are cut into, and what it then takes in microseconds (an estimate): every round of blocks
-// fills LDS, which costs about 6 us, and takes 64 rows in about 0.2 us.
+// fills LDS, which costs about 6 us, and takes 64 rows in about 0.2 us.  From L2 a call takes 4 us and its codewords at 12 TB/s.  Measured,
+// M = 8, K = 256, bf16, us from L2 and in slices: 8 heads of D = 128, 1024 rows 8.2 and 8.5, 2048 rows 13 and 9.4, 8192 rows 35 and 17;
+// one of D = 4096, 256 rows 7.2 and 7.3, 512 rows 11 and 8.1, 2048 rows 28 and 15, 8192 rows 93 and 30.
 struct SliceCut {
     int slices, splits;
     double us;
@@ -2366,7 +2368,6 @@ static int launch_decode_any(hclae_ctx *ctx, const DecodeArgs &a, const Rows &ro
     const int G = slice_dictionaries(a.M, a.K, a.D, kLdsBudget);
     if (G) {
         const SliceCut cut = slice_cut(ctx, a, G);
-        // codewords from L2 at about 12 TB/s
         const double direct = 4.0 + (double)a.n * a.H * a.M * a.D * 4.0 / 12e6;
         if (cut.us < direct) switch (G) {
             case 1: return launch_decode_slices<T, Rows, 1>(ctx, a, rows, cut);
@@ -2475,7 +2476,7 @@ static int launch_lookup_grad(hclae_ctx *ctx, const GradArgs &a)
     const dim3 sort_grid((unsigned)s.ranges, (unsigned)((a.M + kSortGroup - 1) / kSortGroup));
     hipLaunchKernelGGL(k_grad_count, sort_grid, dim3(kSortThreads), 0, ctx->stream, a, s);
     HIP_TRY(ctx, hipGetLastError());
-    hipLaunchKernelGGL(k_grad_items, dim3((unsigned)a.M), dim3(256), 0, ctx->stream, a, s);
+    hipLaunchKernelGGL(k_grad_items, dim3((unsigned)a.M), dim3(256 * kItemParts), 0, ctx->stream, a, s);
     HIP_TRY(ctx, hipGetLastError());
     hipLaunchKernelGGL(k_grad_place, sort_grid, dim3(kSortThreads), 0, ctx->stream, a, s);
     HIP_TRY(ctx, hipGetLastError());

@@ -66,7 +66,9 @@ __device__ __forceinline__ int grad_code(const GradArgs &a, int64_t t, int m)
 }
 
 constexpr int kGradThreads = 256;
-constexpr int kGradFew = 4096;                      // rows up to which one launch finds and sums them
+// Rows up to which one launch finds and sums them.  M = 8, K = 256, bf16, us in one launch and sorted: D = 128, T = 2048 13 and 18, T = 4096
+// 20 and 19; D = 1024, 15 and 30, 26 and 31; D = 4096, 32 and 69, 57 and 72.
+constexpr int kGradFew = 4096;
 
 // Few rows: a block per codeword of a dictionary and part of the coordinates looks at the codes of all rows, lists those that have
 // its codeword, in ascending order, and sums them: `lanes` (a power of two) lanes a row, kGradThreads / lanes rows at a
@@ -122,9 +124,9 @@ __global__ __launch_bounds__(kGradThreads) void k_grad_few(const GradArgs a, int
 }
 
 // Many rows: sorted by code, dictionary by dictionary (a counting sort that keeps the order of equal codes), then summed in chunks.
-// T = 16384, D = 4096, M = 8, K = 256 in bf16: 165 us, of which k_grad_count 5.6, k_grad_items 9.5, k_grad_place 6.7, k_grad_sums 133,
-// k_grad_join 5.9.
-// Rows of a block: the fewer, the more blocks there are, and the more ranges k_grad_items goes through (T = 16384, 1024 rows: 13 us a pass).
+// T = 16384, D = 4096, M = 8, K = 256 in bf16: 162 us, of which k_grad_count 4.7, k_grad_items 6.8, k_grad_place 6.3, k_grad_sums 135,
+// k_grad_join 4.6.
+// Rows of a block: the fewer, the more blocks there are, and the more ranges k_grad_items goes through (T = 16384: 1024 rows a block 13 us, 256 rows 6).
 __host__ __device__ constexpr int sort_range(int64_t T) { return T <= 32768 ? 256 : T <= 131072 ? 512 : T <= 524288 ? 1024 : 2048; }
 constexpr int kSortGroup = 8;                       // dictionaries of a block, a wave each
 constexpr int kSortThreads = kSortGroup * kWave;
@@ -166,54 +168,73 @@ __global__ __launch_bounds__(kSortThreads) void k_grad_count(const GradArgs a, c
         for (int k = lane; k < a.K; k += kWave) s.counts[((size_t)m * s.ranges + blockIdx.x) * a.K + k] = hist[wave][k];
 }
 
-// A block per dictionary, a thread per codeword: where the rows of a range and codeword begin in the list, and the items.
-__global__ __launch_bounds__(256) void k_grad_items(const GradArgs a, const SortArgs s)
+// A block per dictionary, four threads per codeword, each with a quarter of the ranges: where the rows of a range and codeword begin in
+// the list, and the items.  Bound by the latency of the counts, which are read twice: sixteen on their way at a time.
+constexpr int kItemParts = 4, kItemAhead = 16;
+__global__ __launch_bounds__(256 * kItemParts) void k_grad_items(const GradArgs a, const SortArgs s)
 {
     __shared__ int3 scan[256];
-    const int m = blockIdx.x, k = threadIdx.x;
+    __shared__ int quarter[kItemParts][256], begin[256];
+    const int m = blockIdx.x, k = threadIdx.x & 255, part = threadIdx.x >> 8;
+    const int r_first = (int)((int64_t)s.ranges * part / kItemParts), r_end = (int)((int64_t)s.ranges * (part + 1) / kItemParts);
     unsigned *counts = s.counts + (size_t)m * s.ranges * a.K;
-    int total = 0;
+    int mine = 0;
     if (k < a.K) {
-        for (int r0 = 0; r0 < s.ranges; r0 += 8) {
-            unsigned c[8];
+        for (int r0 = r_first; r0 < r_end; r0 += kItemAhead) {
+            unsigned c[kItemAhead];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) c[i] = r0 + i < s.ranges ? counts[(size_t)(r0 + i) * a.K + k] : 0u;
+            for (int i = 0; i < kItemAhead; ++i) c[i] = r0 + i < r_end ? counts[(size_t)(r0 + i) * a.K + k] : 0u;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) total += (int)c[i];
+            for (int i = 0; i < kItemAhead; ++i) mine += (int)c[i];
         }
     }
-    const int items = k < a.K ? max(1, (total + s.chunk - 1) / s.chunk) : 0, parts = items > 1 ? items : 0;
-    int3 mine = make_int3(total, items, parts);
-    scan[k] = mine;
+    quarter[part][k] = mine;
+    __syncthreads();
+    int total = 0, items = 0, parts = 0;
+    int3 sum = make_int3(0, 0, 0);
+    if (part == 0) {
+#pragma unroll
+        for (int q = 0; q < kItemParts; ++q) total += quarter[q][k];
+        items = k < a.K ? max(1, (total + s.chunk - 1) / s.chunk) : 0;
+        parts = items > 1 ? items : 0;
+        sum = make_int3(total, items, parts);
+        scan[k] = sum;
+    }
     __syncthreads();
     for (int o = 1; o < 256; o <<= 1) {
         int3 v = make_int3(0, 0, 0);
-        if (k >= o) v = scan[k - o];
+        if (part == 0 && k >= o) v = scan[k - o];
         __syncthreads();
-        mine = make_int3(mine.x + v.x, mine.y + v.y, mine.z + v.z);
-        scan[k] = mine;
+        sum = make_int3(sum.x + v.x, sum.y + v.y, sum.z + v.z);
+        if (part == 0) scan[k] = sum;
         __syncthreads();
     }
-    const int all = scan[255].y, first = mine.x - total, item0 = mine.y - items, part0 = mine.z - parts;
+    const int all = scan[255].y;
+    if (part == 0) begin[k] = sum.x - total;
+    __syncthreads();
     if (k < a.K) {
-        unsigned at = (unsigned)first;
-        for (int r0 = 0; r0 < s.ranges; r0 += 8) {
-            unsigned c[8];
+        unsigned at = (unsigned)begin[k];
+        for (int q = 0; q < part; ++q) at += (unsigned)quarter[q][k];
+        for (int r0 = r_first; r0 < r_end; r0 += kItemAhead) {
+            unsigned c[kItemAhead];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) c[i] = r0 + i < s.ranges ? counts[(size_t)(r0 + i) * a.K + k] : 0u;
+            for (int i = 0; i < kItemAhead; ++i) c[i] = r0 + i < r_end ? counts[(size_t)(r0 + i) * a.K + k] : 0u;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (r0 + i < s.ranges) {
+            for (int i = 0; i < kItemAhead; ++i)
+                if (r0 + i < r_end) {
                     counts[(size_t)(r0 + i) * a.K + k] = at;
                     at += c[i];
                 }
         }
-        GradItem *out = s.items + (size_t)m * s.max_items + item0;
-        for (int i = 0; i < items; ++i)
-            out[i] = {k, first + i * s.chunk, min(s.chunk, total - i * s.chunk), parts ? part0 + i : -1};
-        s.buckets[(size_t)m * a.K + k] = {part0, items};
+        if (part == 0) {
+            const int first = sum.x - total, item0 = sum.y - items, part0 = sum.z - parts;
+            GradItem *out = s.items + (size_t)m * s.max_items + item0;
+            for (int i = 0; i < items; ++i)
+                out[i] = {k, first + i * s.chunk, min(s.chunk, total - i * s.chunk), parts ? part0 + i : -1};
+            s.buckets[(size_t)m * a.K + k] = {part0, items};
+        }
     }
-    for (int i = all + k; i < s.max_items; i += 256) s.items[(size_t)m * s.max_items + i] = {0, 0, -1, -1};
+    for (int i = all + (int)threadIdx.x; i < s.max_items; i += 256 * kItemParts) s.items[(size_t)m * s.max_items + i] = {0, 0, -1, -1};
 }
 
 // The rows' places, a wave per dictionary and range: 64 rows at a time, equal codes ranked by lane.
@@ -227,22 +248,31 @@ __global__ __launch_bounds__(kSortThreads) void k_grad_place(const GradArgs a, c
     __syncthreads();
     if (m >= a.M) return;
     int *list = s.list + (size_t)m * a.T;
-    for (int i = 0; i < s.range; i += kWave) {
-        const int64_t t = t0 + i + lane;
-        const int c = t < a.T ? grad_code(a, t, m) : -1;
-        unsigned long long same = __ballot(c >= 0);
+    constexpr int AHEAD = 4;                        // codes on their way at a time; a range is 256 rows at least
+    for (int i0 = 0; i0 < s.range; i0 += AHEAD * kWave) {
+        int codes[AHEAD];
 #pragma unroll
-        for (int b = 0; b < 8; ++b) {
-            const unsigned long long bit = __ballot((c >> b) & 1);
-            same &= (c >> b) & 1 ? bit : ~bit;
+        for (int j = 0; j < AHEAD; ++j) {
+            const int64_t t = t0 + i0 + j * kWave + lane;
+            codes[j] = t < a.T ? grad_code(a, t, m) : -1;
         }
-        if (c >= 0) {
-            const unsigned at = next[wave][c], rank = (unsigned)__popcll(same & ((1ull << lane) - 1ull));
-            list[at + rank] = (int)t;
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // all lanes have read before the first of equals writes
-            if (rank == 0) next[wave][c] = at + (unsigned)__popcll(same);
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const int c = codes[j];
+            unsigned long long same = __ballot(c >= 0);
+#pragma unroll
+            for (int b = 0; b < 8; ++b) {
+                const unsigned long long bit = __ballot((c >> b) & 1);
+                same &= (c >> b) & 1 ? bit : ~bit;
+            }
+            if (c >= 0) {
+                const unsigned at = next[wave][c], rank = (unsigned)__popcll(same & ((1ull << lane) - 1ull));
+                list[at + rank] = (int)(t0 + i0 + j * kWave + lane);
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // all lanes have read before the first of equals writes
+                if (rank == 0) next[wave][c] = at + (unsigned)__popcll(same);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 

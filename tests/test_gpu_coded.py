@@ -397,6 +397,7 @@ GRAD = [
     (509, 300, 132, 3, 100, "fp16", "some", -0.5, 12), (4096, 4096, 128, 8, 256, "bf16", "all", 1.0, 0), (4097, 5000, 128, 8, 256, "bf16", "all", 1.0, 0),
     (5000, 100, 36, 11, 256, "fp16", "some", 2.0, 0), (9000, 1, 64, 2, 256, "fp32", "some", 1.0, 0), (70001, 900, 20, 3, 7, "bf16", "some", 0.25, 4),
     (6000, 3000, 1028, 2, 200, "bf16", "some", 3.0, 8), (8000, 8000, 516, 9, 256, "fp32", "all", 1.0, 0), (300, 7, 4, 2, 1, "bf16", "some", 1.0, 0),
+    (300007, 40000, 12, 2, 256, "bf16", "some", 1.0, 0), (700001, 700001, 4, 3, 90, "fp32", "all", 2.0, 4),
 ]
 
 
