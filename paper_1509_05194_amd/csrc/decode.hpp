@@ -77,6 +77,7 @@ struct CacheRows {                                  // hclae_cache_read
     int64_t pages;                                  // of the cache
     unsigned mul = page_mul(page);
     int shift = page_shift(page);
+    unsigned named = pages < 1ll << 31 ? (unsigned)pages : 1u << 31;    // pages that a table can name
     // The sequence of row t is the last one that starts at or before it; whatever `starts` holds, the search ends inside [0, B).
     __host__ __device__ constexpr int sequence(int64_t t) const
     {
@@ -95,31 +96,42 @@ struct CacheRows {                                  // hclae_cache_read
         while (lo + 1 < B && starts[lo + 1] <= t) ++lo;
         const int64_t pos = t - starts[lo];
         if (pos < 0 || pos > 0x7fffffff) return kSkip;
-        const unsigned p = (unsigned)((uint64_t)(unsigned)pos * mul >> (31 + shift));
+        const unsigned p = page_of((unsigned)pos);
         off = (unsigned)pos - p * (unsigned)page;
         return p < (unsigned)max_pages ? (int64_t)lo * max_pages + p : kNoRow;
     }
-    __host__ __device__ constexpr int64_t slot(int32_t q, unsigned off) const { return q >= 0 && q < pages ? (int64_t)q * page + off : kNoRow; }
+    __host__ __device__ constexpr unsigned page_of(unsigned pos) const { return (unsigned)((uint64_t)pos * mul >> (31 + shift)); }
+    __host__ __device__ constexpr int64_t slot(int32_t q, unsigned off) const { return (unsigned)q < named ? (int64_t)((uint64_t)(unsigned)q * (unsigned)page + off) : kNoRow; }
     __host__ __device__ constexpr int64_t at(int64_t t) const
     {
         unsigned off = 0;
         const int64_t e = entry(t, sequence(t), off);
         return e < 0 ? e : slot(tables[e], off);
     }
-    // The same in two steps, a load between them that need not be waited for; first: a row at or before t, the same for all lanes.
+    // The same in two steps, a load between them that need not be waited for; first: the row of lane 0, the others' follow it.
+    // Where all of a wave's rows are of one sequence (most often in long ones) little is done per lane.
+    static constexpr unsigned kSkipOff = ~0u;       // no slot of a page
     struct Probe {
-        int64_t e;
         int32_t q;
         unsigned off;
     };
     __device__ __forceinline__ Probe look(int64_t t, int64_t first) const
     {
-        Probe p = {0, 0, 0u};
-        p.e = entry(t, sequence(first), p.off);
-        if (p.e >= 0) p.q = tables[p.e];
+        const int lo = __builtin_amdgcn_readfirstlane(sequence(first));
+        const int begin = __builtin_amdgcn_readfirstlane(starts[lo]), end = __builtin_amdgcn_readfirstlane(starts[lo + 1]);
+        Probe p = {-1, 0u};
+        if (first >= begin && first + (kWave - 1) < end) {
+            const unsigned pos = (unsigned)(first - begin) + (unsigned)(t - first), at = page_of(pos);
+            p.off = pos - at * (unsigned)page;
+            if (at < (unsigned)max_pages) p.q = (tables + (int64_t)lo * max_pages)[at];
+            return p;
+        }
+        const int64_t e = entry(t, lo, p.off);
+        if (e == kSkip) p.off = kSkipOff;
+        if (e >= 0) p.q = tables[e];
         return p;
     }
-    __device__ __forceinline__ int64_t at(const Probe &p) const { return p.e < 0 ? p.e : slot(p.q, p.off); }
+    __device__ __forceinline__ int64_t at(const Probe &p) const { return p.off == kSkipOff ? kSkip : slot(p.q, p.off); }
 };
 
 struct DecodeArgs {
@@ -178,8 +190,8 @@ __global__ __launch_bounds__(kDecodeThreads) void k_decode_rows(const DecodeArgs
 // within the half lines; even rows read the two steps of a pair in one order, odd rows in the other.  Whatever the codes are, sixteen lanes so meet none
 // of the 64 banks twice.  The lanes of one coordinate and different dictionaries add up at the end (DPP).  G is the least that lets
 // all of it fit LDS (M = 8, K = 256: two).  A wave takes 64 rows at a time: it looks for them two rounds ahead, fetches their codes one round ahead and keeps
-// them in LDS of its own, so that no barriers are needed once the slice is there.  Bound by vector arithmetic, about 41 instructions a wave for eight
-// rows: 32768 rows of 16 heads, D = 128, M = 8, bf16 in 80 to 94 us; 16384 rows of D = 4096 in 62 us (2.2 TB/s written); a million of D = 128 in fp32
+// them in LDS of its own, so that no barriers are needed once the slice is there.  Bound by vector arithmetic, about 30 instructions a wave for eight
+// rows and as many again, spread over eight such steps, for finding rows and laying their codes out, beside reads of LDS (a third of the time alone): 32768 rows of 16 heads, D = 128, M = 8, bf16 in 70 to 85 us; 16384 rows of D = 4096 in 62 us (2.2 TB/s written); a million of D = 128 in fp32
 // in 180 us (2.8 TB/s).
 // Threads of a block: half as many where a row's codes take more of LDS.
 __host__ __device__ constexpr int slice_threads(int G) { return G <= 2 ? 1024 : 512; }
@@ -246,12 +258,14 @@ __global__ __launch_bounds__(slice_threads(G)) void k_decode_slices(const Decode
         return r < last && t < a.n ? rows.look(t, r * kWave) : Probe{};
     };
     auto found = [&](int64_t r, const Probe &p) { return r < last && r * kWave + lane < a.n ? rows.at(p) : kSkip; };
-    unsigned code[NW];
+    const uint8_t *codes_h = a.codes + h * a.M;
+    const unsigned row_codes = (unsigned)(a.H * a.M);
+    unsigned code[NW] = {};                         // of a row that is not there: any, as they are held below K and its sum is not kept
     float factor;
     auto fetch = [&](int64_t at) {
         factor = a.factor;
         if (at < 0) return;
-        const uint8_t *p = a.codes + (at * a.H + h) * a.M;
+        const uint8_t *p = codes_h + (uint64_t)at * row_codes;
         if (words_aligned) {
 #pragma unroll
             for (int j = 0; j < NW; ++j) code[j] = reinterpret_cast<const unsigned *>(p)[min(j, nw - 1)];
@@ -264,7 +278,7 @@ __global__ __launch_bounds__(slice_threads(G)) void k_decode_slices(const Decode
                 code[j] = b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24;
             }
         }
-        if (a.scale) factor = a.scale[at * a.H + h] * a.factor;
+        if (a.scale) factor = (a.scale + h)[(uint64_t)at * (unsigned)a.H] * a.factor;
     };
     int64_t at = found(round, look(round));
     Probe probe = look(round + waves);
@@ -299,7 +313,7 @@ __global__ __launch_bounds__(slice_threads(G)) void k_decode_slices(const Decode
     const bool writes = d < a.D && (G == 1 || (l8 < 4 && l8 < LQ));
     auto off_of = [&](int m) {                      // of a codeword within its lines
         const unsigned c = (code[min(m >> 2, NW - 1)] >> (8 * (m & 3))) & 255u;
-        return at >= 0 && m < a.M ? min(c, (unsigned)a.K - 1u) * 256u : 0u;
+        return m < a.M ? min(c, (unsigned)a.K - 1u) * 256u : 0u;
     };
     // four steps, those beyond the last pair being zeros
     auto four = [&](const uint2 &c, int w, float4 (&v)[4]) {

@@ -294,7 +294,7 @@ def test_read_sequences_longer_than_their_pages():
     ctx.close()
 
 
-@pytest.mark.parametrize("n,M", [(6, 8), (5000, 8), (5000, 16)])
+@pytest.mark.parametrize("n,M", [(6, 8), (40000, 8), (40000, 16)])
 def test_rows_that_are_not_there_are_zero_whatever_the_codewords_are(n, M):
     from paper_1509_05194_amd import hclae
     K, D = 256, 64
@@ -311,6 +311,10 @@ def test_rows_that_are_not_there_are_zero_whatever_the_codewords_are(n, M):
     want = torch.zeros((n, 1, D), device="cuda")
     want[3], want[n - 1] = C[0, :, 1].double().sum(0).float(), 9.0
     assert torch.allclose(out, want, rtol=0, atol=(M + 3) * U32 * 8 * M)      # |c| < 8
+    # pages of 2 rows, two of them in the table: row 3 is the last one that is there
+    out.fill_(9.0)
+    ctx.cache_read(codes, None, torch.tensor([[0, 1]], dtype=torch.int32, device="cuda"), torch.tensor([0, n - 1], dtype=torch.int32, device="cuda"), 2, out)
+    assert torch.allclose(out[3:], want[3:], rtol=0, atol=(M + 3) * U32 * 8 * M)
     looked = torch.full((n, D), 9.0, device="cuda")
     rows = torch.full((n,), -1, dtype=torch.int64, device="cuda")
     rows[4] = n
