@@ -190,9 +190,9 @@ __global__ __launch_bounds__(kDecodeThreads) void k_decode_rows(const DecodeArgs
 // within the half lines; even rows read the two steps of a pair in one order, odd rows in the other.  Whatever the codes are, sixteen lanes so meet none
 // of the 64 banks twice.  The lanes of one coordinate and different dictionaries add up at the end (DPP).  G is the least that lets
 // all of it fit LDS (M = 8, K = 256: two).  A wave takes 64 rows at a time: it looks for them two rounds ahead, fetches their codes one round ahead and keeps
-// them in LDS of its own, so that no barriers are needed once the slice is there.  Bound by vector arithmetic, about 30 instructions a wave for eight
-// rows and as many again, spread over eight such steps, for finding rows and laying their codes out, beside reads of LDS (a third of the time alone): 32768 rows of 16 heads, D = 128, M = 8, bf16 in 70 to 85 us; 16384 rows of D = 4096 in 62 us (2.2 TB/s written); a million of D = 128 in fp32
-// in 180 us (2.8 TB/s).
+// them in LDS of its own, so that no barriers are needed once the slice is there.  Bound by vector arithmetic, about 30 instructions a wave
+// for eight rows (and for 64 rows those that find them and lay their codes out), beside reads of LDS, a third of the time by themselves: 32768 rows of 16 heads,
+// D = 128, M = 8, bf16 in 70 to 85 us; 16384 rows of D = 4096 in 59 to 64 us (2.2 TB/s written); a million of D = 128 in fp32 in 180 us (2.8 TB/s).
 // Threads of a block: half as many where a row's codes take more of LDS.
 __host__ __device__ constexpr int slice_threads(int G) { return G <= 2 ? 1024 : 512; }
 constexpr int kSliceMaxM = 32;                      // codes of a row travel in eight registers
