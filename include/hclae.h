@@ -423,7 +423,8 @@ int hclae_lookup(hclae_ctx *ctx, const int64_t *rows, int64_t T, const uint8_t *
  *   dC[m][k] = factor * sum over the t with codes[rows[t]][m] == k of grad[t]          dC: DEVICE float[M][K][D]
  * Every element of dC is written, with zero where no row has the codeword.  Row numbers outside [0, V) take no part.  Sums are in
  * fp32 in an order fixed by the sizes and codes alone: equal calls give equal bits.  Beyond 4096 rows the first call allocates
- * scratch for N_max rows (4 M N_max bytes and 4 KB per row of dC at most), which the ctx keeps, and may not be recorded into a HIP graph;
+ * scratch for N_max rows (about M (4 N_max + 2 KB K + 4 KB D) bytes; N_max / 512 bytes in place of the 2 KB from a million rows on), which the ctx
+ * keeps, and may not be recorded into a HIP graph;
  * two recorded calls of one ctx share that scratch and must not run at the same time.
  */
 int hclae_lookup_grad(hclae_ctx *ctx, const int64_t *rows, int64_t T, const uint8_t *codes, int64_t V, float factor, const void *grad, int type,
