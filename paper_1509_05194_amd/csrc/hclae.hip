@@ -1542,8 +1542,7 @@ int hclae_online_chunk(hclae_ctx *ctx, const uint8_t *Xu8, int64_t n, int D, flo
 
 static void beam_release(hclae_ctx *ctx)
 {
-    void *dev[] = {ctx->beam_rows[0], ctx->beam_rows[1],
-                   ctx->beam_pre[0], ctx->beam_pre[1], ctx->beam_mask, ctx->cache_C, ctx->cache_T, ctx->cache_buf, ctx->grad_buf};
+    void *dev[] = {ctx->beam_rows[0], ctx->beam_rows[1], ctx->beam_pre[0], ctx->beam_pre[1], ctx->beam_mask};
     for (void *p : dev)
         if (p) (void)hipFree(p);
     ctx->beam_rows[0] = ctx->beam_rows[1] = nullptr;
