@@ -2430,9 +2430,6 @@ int hclae_lookup(hclae_ctx *ctx, const int64_t *rows, int64_t T, const uint8_t *
     return launch_decode_type(ctx, type, a, TableRows{rows, V});
 }
 
-// Rows of one item of a sorted gradient: 128, or so many that a dictionary has about 512 items of several-item codewords.
-static int grad_chunk(int64_t T) { return (int)std::max<int64_t>(128, (T / 512 + kWave - 1) / kWave * kWave); }
-
 extern "C++" {
 template <typename T>
 static int launch_lookup_grad(hclae_ctx *ctx, const GradArgs &a)
@@ -2451,27 +2448,22 @@ static int launch_lookup_grad(hclae_ctx *ctx, const GradArgs &a)
         return HCLAE_OK;
     }
     const size_t M = a.M, K = a.K, N = ctx->N_max;
-    const size_t ranges_max = std::max<size_t>(N / sort_range(N), 512) + 1,      // fewer rows: at most 512
-                  items_max = K + 512, parts_max = 1026;
-    const size_t counts_b = M * ranges_max * K * sizeof(unsigned), list_b = M * N * sizeof(int), items_b = M * items_max * sizeof(GradItem),
-                 buckets_b = M * K * sizeof(GradBucket), partial_b = M * parts_max * a.D * sizeof(float);
+    const GradPlan plan = grad_plan(a.T, a.K), room = grad_room(ctx->N_max, a.K);
+    if (!fits(plan, room)) return fail(ctx, HCLAE_ESTATE, "hclae_lookup_grad: more items than the scratch has room for");
+    const size_t counts_b = M * room.ranges * K * sizeof(unsigned), list_b = M * N * sizeof(int), items_b = M * room.max_items * sizeof(GradItem),
+                 buckets_b = M * K * sizeof(GradBucket), partial_b = M * room.max_parts * a.D * sizeof(float);
     auto up = [](size_t b) { return (b + 255) / 256 * 256; };
     if (!ctx->grad_buf) {
         const hipError_t e = hipMalloc((void **)&ctx->grad_buf, up(counts_b) + up(list_b) + up(items_b) + up(buckets_b) + up(partial_b));
         if (e != hipSuccess) return fail(ctx, e == hipErrorOutOfMemory ? HCLAE_ENOMEM : HCLAE_EHIP, "hipMalloc (sorted rows)", e);
     }
-    SortArgs s;
+    SortArgs s = {plan};
     char *p = ctx->grad_buf;
     s.counts = reinterpret_cast<unsigned *>(p);
     s.list = reinterpret_cast<int *>(p += up(counts_b));
     s.items = reinterpret_cast<GradItem *>(p += up(list_b));
     s.buckets = reinterpret_cast<GradBucket *>(p += up(items_b));
     s.partial = reinterpret_cast<float *>(p += up(buckets_b));
-    s.range = sort_range(a.T);
-    s.ranges = (int)((a.T + s.range - 1) / s.range);
-    s.chunk = grad_chunk(a.T);
-    s.max_items = a.K + (int)(a.T / s.chunk);
-    s.max_parts = 2 * (int)(a.T / s.chunk) + 2;
     const dim3 sort_grid((unsigned)s.ranges, (unsigned)((a.M + kSortGroup - 1) / kSortGroup));
     hipLaunchKernelGGL(k_grad_count, sort_grid, dim3(kSortThreads), 0, ctx->stream, a, s);
     HIP_TRY(ctx, hipGetLastError());

@@ -128,6 +128,34 @@ __global__ __launch_bounds__(kGradThreads) void k_grad_few(const GradArgs a, int
 // k_grad_join 4.6.
 // Rows of a block: the fewer, the more blocks there are, and the more ranges k_grad_items goes through (T = 16384: 1024 rows a block 13 us, 256 rows 6).
 __host__ __device__ constexpr int sort_range(int64_t T) { return T <= 32768 ? 256 : T <= 131072 ? 512 : T <= 524288 ? 1024 : 2048; }
+// What a sorted call of T rows needs of the scratch.  Rows of one item: 128, or so many that a dictionary's rows make at most 512 items (T / 512
+// is rounded up, then to whole waves).  A codeword of n rows has at most max(1, n / chunk + 1) of them, so a dictionary K + T / chunk; where a
+// codeword has several, at most 2 n / chunk, and their partial sums less than 2 T / chunk + 2 rows.
+constexpr int kGradItems = 512;
+struct GradPlan {
+    int range, ranges, chunk, max_items, max_parts;
+};
+__host__ __device__ constexpr GradPlan grad_plan(int64_t T, int K)
+{
+    GradPlan p = {};
+    p.range = sort_range(T);
+    p.ranges = (int)((T + p.range - 1) / p.range);
+    const int64_t most = (T + kGradItems - 1) / kGradItems, waves = (most + kWave - 1) / kWave;
+    p.chunk = waves < 2 ? 2 * kWave : (int)(waves * kWave);
+    p.max_items = K + (int)(T / p.chunk);
+    p.max_parts = 2 * (int)(T / p.chunk) + 2;
+    return p;
+}
+// The most that any call of N rows or fewer needs: one that takes a smaller range than N rows do has at most 512 of them.
+__host__ __device__ constexpr GradPlan grad_room(int64_t N, int K)
+{
+    const int64_t own = N / sort_range(N);
+    return {0, (int)(own > 512 ? own : 512) + 1, 0, K + kGradItems, 2 * kGradItems + 2};
+}
+__host__ __device__ constexpr bool fits(const GradPlan &p, const GradPlan &room)
+{
+    return p.ranges <= room.ranges && p.max_items <= room.max_items && p.max_parts <= room.max_parts;
+}
 constexpr int kSortGroup = 8;                       // dictionaries of a block, a wave each
 constexpr int kSortThreads = kSortGroup * kWave;
 
@@ -138,13 +166,12 @@ struct GradBucket {                                 // of a codeword with severa
     int part, items;                                // first row of its partial sums, how many
 };
 
-struct SortArgs {
+struct SortArgs : GradPlan {
     unsigned *counts;                               // [M][ranges][K], in the end where each range's rows begin
     int *list;                                      // [M][T]
     GradItem *items;                                // [M][max_items]
     GradBucket *buckets;                            // [M][K]
     float *partial;                                 // [M][max_parts][D]
-    int range, ranges, chunk, max_items, max_parts;
 };
 
 // Rows of each code in each range.

@@ -4,6 +4,7 @@ import pytest
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
+U32 = 2.0 ** -24
 
 
 def test_cache_and_gradient_beside_multi_path_encoding():
@@ -66,3 +67,66 @@ def test_cache_and_gradient_beside_multi_path_encoding():
         ctx.encode_beam(x, C, 10, codes, res)
         torch.cuda.synchronize()
         ctx.close()
+
+
+def codes_and_rows(T, V, M, K, seed):
+    """A table of V rows of codes, and T row numbers: a tenth of them of one row, some of none."""
+    rng = np.random.default_rng(seed)
+    ids = torch.from_numpy(rng.integers(0, K, (V, M)).astype(np.uint8)).cuda()
+    rows = torch.from_numpy(rng.integers(0, V, T)).cuda()
+    rows[5:5 + T // 10] = 3
+    rows[[0, T // 2]] = torch.tensor([-1, V], device="cuda")
+    return ids, rows
+
+
+def check_grad(dC, ids, rows, g, V, factor):
+    """A gradient is a sum of n values in fp32, in some order, times the factor: (n + 2) 2^-24 of the sum of their magnitudes."""
+    rows, ids, dC = rows.cpu(), ids.cpu(), dC.cpu().double()
+    live = (rows >= 0) & (rows < V)
+    gd, at = g.cpu().double()[live], ids[rows[live]].long()
+    M, K, D = dC.shape
+    for m in range(M):
+        c = at[:, m]
+        want = torch.zeros((K, D), dtype=torch.float64).index_add_(0, c, gd) * factor
+        mag = torch.zeros((K, D), dtype=torch.float64).index_add_(0, c, gd.abs()) * abs(factor)
+        n = torch.bincount(c, minlength=K).double()[:, None]
+        assert bool(((dC[m] - want).abs() <= (n + 2) * U32 * mag * (1 + 2.0 ** -8)).all()), m
+
+
+# Where the rows of an item grow (its last number of rows before, and the first), where the ranges of the sort do, both in contexts of
+# just that size; dictionaries from few to the most there can be.
+@pytest.mark.parametrize("T,M,K", [(65663, 8, 256), (65664, 8, 256), (66047, 8, 256), (66048, 8, 256), (66047, 64, 256), (66047, 256, 64), (98304, 8, 256),
+                                   (98305, 8, 256), (98815, 8, 256), (98815, 64, 256), (131583, 9, 256), (164351, 3, 256), (197119, 3, 255), (229887, 3, 256),
+                                   (32768, 8, 256), (32769, 8, 256), (131072, 3, 256), (131073, 3, 256), (524288, 2, 256), (524289, 2, 256),
+                                   (262143, 2, 1), (262145, 2, 1)])
+def test_gradient_where_items_and_ranges_grow(T, M, K):
+    from paper_1509_05194_amd import hclae
+    V, D = 1000, 12
+    ids, rows = codes_and_rows(T, V, M, K, T)
+    g = torch.randn((T, D), generator=torch.Generator().manual_seed(T)).cuda()
+    ctx = hclae.Context(T, D, M, K)
+    dC = torch.full((M, K, D), float("nan"), device="cuda")
+    ctx.lookup_grad(ids, g, dC, rows=rows, scale=0.5)
+    torch.cuda.synchronize()
+    check_grad(dC, ids, rows, g, V, 0.5)
+    ctx.close()
+
+
+def test_gradients_of_fewer_rows_than_a_context_has_room_for():
+    """One context for more than a million rows: the bits of contexts of just the size, whatever was summed before."""
+    from paper_1509_05194_amd import hclae
+    V, D, M, K, most = 3000, 8, 8, 256, (1 << 20) + 70001
+    ids, rows = codes_and_rows(most, V, M, K, 1)
+    g = torch.randn((most, D), generator=torch.Generator().manual_seed(2)).cuda()
+    big = hclae.Context(most, D, M, K)
+    for T in (5000, most, 66047, 4097, 32769, 524288, 98815, 131072, 700001, 4096, 229887, most - 1):
+        dC, alone = (torch.full((M, K, D), float("nan"), device="cuda") for _ in range(2))
+        big.lookup_grad(ids, g[:T], dC, rows=rows[:T])
+        ctx = hclae.Context(T, D, M, K)
+        ctx.lookup_grad(ids, g[:T], alone, rows=rows[:T])
+        torch.cuda.synchronize()
+        assert torch.equal(dC, alone), T
+        check_grad(dC, ids, rows[:T], g[:T], V, 1.0)
+        print("gradient of %d rows" % T, flush=True)
+        ctx.close()
+    big.close()
