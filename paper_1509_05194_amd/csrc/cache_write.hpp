@@ -461,7 +461,8 @@ __host__ __device__ constexpr int cache_chunks(int D) { return D <= 64 ? 1 : D <
 __host__ __device__ constexpr int cache_padded(int D) { return 64 * cache_chunks(D); }
 
 // Codewords in ascending order of their distance from the mean of a few, equal ones by index.  A block per dictionary.
-// halves: [dictionaries][256] -||c||^2 / 2 of codewords as they are, -1e38 beyond K; then [dictionaries] the largest ||c|| (rounded up).
+// halves: [dictionaries][256] -||c||^2 / 2 of codewords as they are, unscaled, and so -inf beyond K (a score may be any finite number); then
+// [dictionaries] the largest ||c|| (rounded up).
 __global__ __launch_bounds__(256) void k_cache_sort(const float *__restrict__ C, int K, int D, float *__restrict__ sorted, uint8_t *__restrict__ order,
                                                     float *__restrict__ halves)
 {
@@ -489,7 +490,7 @@ __global__ __launch_bounds__(256) void k_cache_sort(const float *__restrict__ C,
         }
     }
     __syncthreads();
-    halves[(size_t)blockIdx.x * 256 + tid] = tid < K ? -size[tid] : -1e38f;
+    halves[(size_t)blockIdx.x * 256 + tid] = tid < K ? -size[tid] : -__builtin_inff();
     if (wave == 0) {
         float most = 0.f;
         for (int k = lane; k < K; k += kWave) most = fmaxf(most, size[k]);
