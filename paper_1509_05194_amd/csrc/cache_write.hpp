@@ -622,11 +622,13 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void k_cache_write_tiles(con
 #pragma unroll
                 for (int s = 0; s < S; ++s) x[s] = make_float4(0.f, 0.f, 0.f, 0.f);
             } else if (a.scale && top) {
-                // x / g as the product with 1 / g in 64 bits, off by 2^-52 of it: a quotient of two numbers of 24 bits is no
-                // nearer than 2^-49 of it to a point between two such numbers, so the rounding is that of the quotient
-                const double f = 1.0 / (double)g;
+                // x / g in fp32 by a product.  f is above 1 / g by 2^-53 to 2^-50 of it, the product's own rounding included, and a number of 50 bits is cut off:
+                // a quotient that is a number of 50 bits comes out as it is, so one halfway between two fp32 numbers, which there is only among the
+                // subnormal ones, is rounded as a tie; any other is 2^-49 of it away from there at least, as a quotient of two numbers of 24 bits, and stays on its side.
+                const double f = 1.0 / (double)g * (1.0 + 0x1p-51);
+                auto over = [&](float v) { return (float)__longlong_as_double(__double_as_longlong(v * f) & ~7ll); };
 #pragma unroll
-                for (int s = 0; s < S; ++s) x[s] = make_float4((float)(x[s].x * f), (float)(x[s].y * f), (float)(x[s].z * f), (float)(x[s].w * f));
+                for (int s = 0; s < S; ++s) x[s] = make_float4(over(x[s].x), over(x[s].y), over(x[s].z), over(x[s].w));
             }
             if (live && hh == 0 && a.scale) a.scale[slot * a.H + h] = g;
         }

@@ -50,3 +50,31 @@ def test_write_of_codewords_whose_squares_are_near_the_largest_number(n, K, D, t
     codes, _ = written(x, C, False)
     for h in range(2):
         assert np.array_equal(codes[:, h], quantise(x[:, h], C[h], False)[0])
+
+
+@pytest.mark.parametrize("n", [40, 1100, 4200, 9001])       # a row a block, sixteen, tiles of half and of all waves
+@pytest.mark.parametrize("D", [64, 128, 200])
+def test_write_of_rows_whose_quotients_are_halfway_between_subnormal_numbers(n, D):
+    """g = 2 G and x = (2 j + 1) G 2^-149 with odd G: x / g is halfway between two numbers, and the even one is x / g in fp32.  The last
+    dictionary holds what rows leave with that rounding and with that of the product with a rounded 1 / g, side by side."""
+    rng = np.random.default_rng(D)
+    base, x, twin = 32, np.zeros((32, D), np.float32), np.zeros((32, D), np.float32)
+    for i in range(base):
+        while True:
+            G = 2 * int(rng.integers(3, 200)) + 1
+            x[i] = ((2 * rng.integers(0, 2000, D) + 1) * G * (1 - 2 * rng.integers(0, 2, D))).astype(np.float32) * np.float32(2.0 ** -149)
+            x[i, 0] = 2 * G
+            twin[i] = (x[i].astype(np.float64) * (1.0 / np.float64(2 * G))).astype(np.float32)
+            if (twin[i] != x[i] / np.float32(2 * G)).any():
+                break
+    u = x / x[:, :1]
+    assert (np.abs(u[:, 1:]) < 2.0 ** -126).all()           # zero among them, where j is 0
+    C = np.zeros((1, 2, 2 * base, D), np.float32)
+    C[0, 0, :, 0] = 1 + np.arange(2 * base)                 # the first codeword leaves zero in front
+    C[0, 1, 0::2], C[0, 1, 1::2] = twin, u
+    C[0, 1, :, 0] = 0
+    rows = x[np.arange(n) % base][:, None]
+    codes, scale = written(rows, C, True)
+    want, g = quantise(rows[:base, 0], C[0], True)
+    assert np.array_equal(want[:, 1], 2 * np.arange(base) + 1)
+    assert np.array_equal(codes[:, 0], want[np.arange(n) % base]) and np.array_equal(scale[:, 0], g[np.arange(n) % base])
