@@ -184,8 +184,12 @@ namespace {
 int fail(hclae_ctx *ctx, int code, const char *what, hipError_t e = hipSuccess)
 {
     char *dst = ctx ? ctx->err : g_create_error;
-    if (e != hipSuccess) snprintf(dst, 256, "%s: %s", what, hipGetErrorString(e));
-    else snprintf(dst, 256, "%s", what);
+    if (e != hipSuccess) {
+        (void)hipGetLastError();            // reported here: the next launch that asks, of this library or the caller's, is not to be told of it
+        snprintf(dst, 256, "%s: %s", what, hipGetErrorString(e));
+    } else {
+        snprintf(dst, 256, "%s", what);
+    }
     return code;
 }
 

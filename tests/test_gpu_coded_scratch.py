@@ -130,3 +130,24 @@ def test_gradients_of_fewer_rows_than_a_context_has_room_for():
         print("gradient of %d rows" % T, flush=True)
         ctx.close()
     big.close()
+
+
+def test_calls_after_one_that_found_no_memory():
+    """Scratch for a sorted gradient of 256 dictionaries and 330 million rows is more than a device has: the call says so, and the next
+    ones, which need none of it, are not blamed for it."""
+    from paper_1509_05194_amd import hclae
+    T, V, D, M, K = 5000, 300, 4, 256, 256
+    ids, rows = codes_and_rows(T, V, M, K, 4)
+    g, C = torch.randn((T, D), device="cuda"), torch.randn((M, K, D), device="cuda")
+    assert 330_000_000 * M * 4 > torch.cuda.get_device_properties(0).total_memory
+    ctx = hclae.Context(330_000_000, D, M, K)
+    dC, out = torch.full((M, K, D), 5.0, device="cuda"), torch.empty((T, D), device="cuda")
+    for _ in range(2):
+        with pytest.raises(hclae.HclaeError, match="HCLAE_ENOMEM"):
+            ctx.lookup_grad(ids, g, dC, rows=rows)
+        ctx.lookup(ids, C, out, rows=rows)
+    assert bool((dC == 5.0).all())
+    ctx.lookup_grad(ids, g[:4096], dC, rows=rows[:4096])
+    torch.cuda.synchronize()
+    check_grad(dC, ids, rows[:4096], g[:4096], V, 1.0)
+    ctx.close()
