@@ -78,3 +78,73 @@ def test_write_of_rows_whose_quotients_are_halfway_between_subnormal_numbers(n, 
     want, g = quantise(rows[:base, 0], C[0], True)
     assert np.array_equal(want[:, 1], 2 * np.arange(base) + 1)
     assert np.array_equal(codes[:, 0], want[np.arange(n) % base]) and np.array_equal(scale[:, 0], g[np.arange(n) % base])
+
+
+@pytest.mark.parametrize("n", [40, 1100, 4200])
+def test_write_of_rows_whose_products_are_subnormal(n):
+    """Codeword 2 has 255 products of 1.1e-38 with the row, which are 2.8e-36 together and nearer than codeword 1 by 0.8e-36 in the score; without
+    them codeword 1 would lead by more than 2e-36."""
+    D, K = 256, 40
+    x = np.full((n, 1, D), 1e-19, np.float32)
+    x[:, :, 0] = 1e-18
+    C = np.full((1, 1, K, D), 1e-17, np.float32)
+    C[0, 0, 1] = 0
+    C[0, 0, 1, 0] = 1e-18
+    C[0, 0, 2] = 1.1e-19
+    C[0, 0, 2, 0] = 0
+    want = quantise(x[:1, 0], C[0], False)[0]
+    assert want[0, 0] == 2
+    assert np.array_equal(written(x, C, False)[0][:, 0], np.repeat(want, n, 0))
+
+
+@pytest.mark.parametrize("T", [900, 9000])
+def test_gradient_of_rows_that_take_no_part_may_be_anything(T):
+    from paper_1509_05194_amd import hclae
+    V, D, M, K = 100, 20, 3, 256
+    gen = torch.Generator().manual_seed(T)
+    ids = torch.randint(0, K, (V, M), dtype=torch.uint8, generator=gen).cuda()
+    rows = torch.randint(-V, 2 * V, (T,), generator=gen).cuda()
+    g = torch.randint(-8, 9, (T, D), generator=gen).float().cuda()
+    out = (rows < 0) | (rows >= V)
+    clean = torch.where(out[:, None], 0.0, g)
+    g[out] = torch.tensor([float("nan"), float("inf"), -float("inf"), 3e38], device="cuda").repeat(D // 4)
+    ctx = hclae.Context(T, D, M, K)
+    dC, want = (torch.full((M, K, D), float("nan"), device="cuda") for _ in range(2))
+    ctx.lookup_grad(ids, g, dC, rows=rows)
+    ctx.lookup_grad(ids, clean, want, rows=rows)
+    assert torch.equal(dC, want) and bool((dC != 0).any()) and bool(dC.isfinite().all())
+    ctx.close()
+
+
+def test_dictionaries_laid_out_again_inside_a_graph():
+    """cache_begin, a write and the read of it recorded together: every replay takes what C holds by then."""
+    from paper_1509_05194_amd import hclae
+    n, H, D, M, K = 1500, 2, 64, 3, 100
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        ctx = hclae.Context(n, D, M, K)
+        C, X = torch.randn((H, M, K, D), device="cuda"), torch.randn((n, H, D), device="cuda")
+        slots, starts = torch.randperm(n, device="cuda"), torch.tensor([0, n], dtype=torch.int32, device="cuda")
+        tables = torch.arange(n // 4, dtype=torch.int32, device="cuda")[None]
+        codes, scale, out = torch.zeros((n, H, M), dtype=torch.uint8, device="cuda"), torch.zeros((n, H), device="cuda"), torch.zeros((n, H, D), device="cuda")
+
+        def work():
+            ctx.cache_begin(C)
+            ctx.cache_write(X, slots, codes, scale)
+            ctx.cache_read(codes, scale, tables, starts, 4, out)
+
+        work()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            work()
+        for i in range(3):
+            C.copy_(torch.randn((H, M, K, D), generator=torch.Generator().manual_seed(i)).cuda())
+            graph.replay()
+            torch.cuda.synchronize()
+            got = codes.clone(), scale.clone(), out.clone()
+            out.zero_()
+            work()
+            torch.cuda.synchronize()
+            assert torch.equal(codes, got[0]) and torch.equal(scale, got[1]) and torch.equal(out, got[2])
+        ctx.close()
