@@ -2351,7 +2351,10 @@ static SliceCut slice_cut(const hclae_ctx *ctx, const DecodeArgs &a, int G)
 template <typename T, typename Rows, int G>
 static int launch_decode_slices(hclae_ctx *ctx, const DecodeArgs &a, const Rows &rows, const SliceCut &cut)
 {
-    auto kern = a.M <= 4 * G ? &k_decode_slices<T, Rows, G, true> : &k_decode_slices<T, Rows, G, false>;
+    auto kern = &k_decode_slices<T, Rows, G, true>;
+    if constexpr (4 * G < kSliceMaxM) {
+        if (a.M > 4 * G) kern = &k_decode_slices<T, Rows, G, false>;
+    }
     // this instance's bit in ctx->attr_done (M, K and D are the ctx's, and so is G)
     const uint64_t attr_set = 1ull << (40 + 2 * (T::bytes == 4 ? 0 : __is_same(T, F16) ? 1 : 2) + (__is_same(Rows, CacheRows) ? 1 : 0));
     if (!(ctx->attr_done & attr_set)) {
