@@ -373,8 +373,8 @@ int hclae_code_stats(hclae_ctx *ctx, const uint8_t *codes, int64_t N, int M, int
  * A cache of keys and values kept as codes: every head has M dictionaries of its own, a row of a head is M bytes
  * (and, if the caller keeps scales, one float).  hclae_cache_begin lays the dictionaries out for the calls below and
  * keeps copies of them in the ctx (at most 18 H M K D bytes, with K rounded up to 64, 128 or 256 and D to 64, 128 or 256; allocated by the
- * first call and by one with more heads than any before, which may therefore not be recorded into a HIP graph, and after which calls that
- * were recorded earlier are recorded again).  After a change to C it is called again; what was written before was written with the old C.
+ * first call and by one with more heads than any before, which may therefore not be recorded into a HIP graph).  After a call with another H, calls
+ * that were recorded earlier are recorded again.  After a change to C it is called again; what was written before was written with the old C.
  *   C: DEVICE float[H][M][K][D].  D <= HCLAE_CACHE_MAX_D.
  * Layout of the cache (DEVICE, caller-owned): codes uint8[n_slots][H][M], scale float[n_slots][H].
  */

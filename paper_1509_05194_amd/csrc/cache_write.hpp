@@ -223,7 +223,7 @@ __global__ __launch_bounds__(kFewThreads) void k_cache_write_one(const CacheRows
 }
 
 // Some rows a head: a block takes sixteen rows of one head through all dictionaries, a wave sixteen codewords, its share in registers
-// as before, as operands of the fp32 matrix cores (v_mfma_f32_16x16x4_f32: lane 16 g + i holds of codeword or row i the dimension
+// as before (D > 64: 10 to 17 of its registers go to memory), as operands of the fp32 matrix cores (v_mfma_f32_16x16x4_f32: lane 16 g + i holds of codeword or row i the dimension
 // that is the g-th of four).  Scores x.c - ||c||^2 / 2; a row whose two best are within what rounding can do to them,
 //   (D + 8) 2^-22 (||x|| max||c|| + max||c||^2 / 2)                 (each of D products and additions loses at most a unit or two of 2^-23),
 // is decided from the distances of the codewords within that margin by one wave (some 2 in 1000).
@@ -426,7 +426,7 @@ __global__ __launch_bounds__(kFewThreads) void k_cache_write_some(const CacheRow
 // all of them).  One candidate is the nearest codeword; two or more are decided in fp32 in their direct form, or in 64 bits.
 // 131072 rows, D = 128, M = 8, K = 256: 160 us, 430 TFLOP/s of scores.  A dictionary takes a block 20000 to 28000 cycles, the products 5000 of them, the
 // rows' fp16 images 2500; the rest are the loads of candidates (2.2 rows of 32 have more than one) and of the codewords to subtract, which wait on L2
-// together in all waves of a block, as the dictionary in LDS holds them in step.  Two blocks of half the waves a CU, waves out of step by half a
+// together in all waves of a block, as the dictionary in LDS holds them in step.  (K <= 64, D from 65 to 128, eight waves: 19 vector registers go to memory.)  Two blocks of half the waves a CU, waves out of step by half a
 // dictionary and pairs of tiles a wave (registers spill) were no faster.
 //
 // Coordinates are laid out so that a lane's eight of a matrix instruction lie side by side in memory: position 16 t + 4 i .. + 3

@@ -190,9 +190,11 @@ __global__ __launch_bounds__(kDecodeThreads) void k_decode_rows(const DecodeArgs
 // within the half lines; even rows read the two steps of a pair in one order, odd rows in the other.  Whatever the codes are, sixteen lanes so meet none
 // of the 64 banks twice.  The lanes of one coordinate and different dictionaries add up at the end (DPP).  G is the least that lets
 // all of it fit LDS (M = 8, K = 256: two).  A wave takes 64 rows at a time: it looks for them two rounds ahead, fetches their codes one round ahead and keeps
-// them in LDS of its own, so that no barriers are needed once the slice is there.  Bound by vector arithmetic, about 30 instructions a wave
-// for eight rows (and for 64 rows those that find them and lay their codes out), beside reads of LDS, a third of the time by themselves: 32768 rows of 16 heads,
+// them in LDS of its own, so that no barriers are needed once the slice is there.  32768 rows of 16 heads,
 // D = 128, M = 8, bf16 in 70 to 85 us; 16384 rows of D = 4096 in 59 to 64 us (2.2 TB/s written); a million of D = 128 in fp32 in 180 us (2.8 TB/s).
+// Nothing is saturated: in these three a SIMD executes vector instructions for 53, 67 and 33 % of the time, LDS works for 30, 37 and 23 %
+// (4 % of that for bank conflicts), and a wave waits for 55, 32 and 29 % of its life on memory or LDS (in the last for 56 % on its turn to issue).
+// 290 to 360 vector instructions a wave for 64 rows and a slice; those that find the rows and lay their codes out are among them, again for every slice.
 // Threads of a block: half as many where a row's codes take more of LDS.
 __host__ __device__ constexpr int slice_threads(int G) { return G <= 2 ? 1024 : 512; }
 constexpr int kSliceMaxM = 32;                      // codes of a row travel in eight registers
@@ -232,7 +234,10 @@ __device__ __forceinline__ float4 dpp_add(const float4 &v)
 }
 
 // splits: parts of the rows; blocks with neighbouring slices of one part, which write neighbouring pieces of its rows, are on one XCD
-// (blocks go round the eight XCDs in order).  words_aligned: every row's codes are whole, aligned words.  ONE: four steps a code at most.
+// (blocks go round the eight XCDs in order).  words_aligned: every row's codes are whole, aligned words.  ONE: four steps a code at most, in
+// one go; else (M = 8 with K to 128 or so, M = 16 to 100) several, and 120 to 340 scalar registers go to lanes of vector ones, in fp32 with G = 1 or 2 also
+// 8 to 31 vector registers to memory.  32768 rows of 8 heads, D = 128, us in bf16 and fp32: M = 8, K = 64 (several, G = 1) 40 and 42, K = 256 (one, G = 2) 39 and 40;
+// M = 16, K = 64 and 100 (several, G = 2) 67 to 69 and 82 to 84, K = 256 (one, G = 4) 108 and 106.
 template <typename T, typename Rows, int G, bool ONE>
 __global__ __launch_bounds__(slice_threads(G)) void k_decode_slices(const DecodeArgs a, const Rows rows, int slices, int splits, bool words_aligned)
 {

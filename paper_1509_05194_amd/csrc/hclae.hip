@@ -2221,7 +2221,9 @@ int hclae_cache_begin(hclae_ctx *ctx, const float *C, int H, int M, int K, int D
 // k_cache_write_one (a row a block) counting 1, of k_cache_write_some (sixteen) 2, of tiles with half of the waves 3.2 and with all of them 4.
 // Measured with M = 8, K = 256 on 256 CUs, us of one round at D = 64, 128, 256: 16, 24, 43; 29, 48, 75; 46, 78, 133; 55, 92, 150.  So at D = 128
 // and 8 heads: 256 rows 28 (one) and 44 (some), 512 rows 46 and 46, 1024 rows 89 and 48; 4096 rows 51 (some) and 78 (half),
-// 8192 rows 91 (some) and 82 (half); 32768 rows 82 (half) and 92 (all), 65536 rows 154 and 99.
+// 8192 rows 91 (some) and 82 (half); 32768 rows 82 (half) and 92 (all), 65536 rows 154 and 99.  A round at D = 128, 8 heads, K = 32, 64, 128: one 10, 13, 14;
+// some 46, 41, 45; half 48, 51, 61; all 68, 70, 73 (K = 256: 28, 53, 72, 85); M = 4 and 16, K = 256: 12, 31, 45, 51 and 37, 95, 142, 176.  So with fewer
+// codewords, or few dictionaries, the weights call k_cache_write_some from one round of k_cache_write_one too early: they are those of M = 8, K = 256.
 enum CacheWay { kWayOne, kWaySome, kWayHalf, kWayAll };
 static CacheWay cache_way(int64_t n, int H, int D, int cus)
 {
@@ -2331,7 +2333,9 @@ static int launch_decode(hclae_ctx *ctx, const DecodeArgs &a, const Rows &rows)
 // How many parts the rows of a sliced decode are cut into, and what it then takes in microseconds (an estimate): every round of blocks
 // fills LDS, which costs about 6 us, and takes 64 rows in about 0.2 us.  From L2 a call takes 4 us and its codewords at 12 TB/s.  Measured,
 // M = 8, K = 256, bf16, us from L2 and in slices: 8 heads of D = 128, 1024 rows 8.2 and 8.5, 2048 rows 13 and 9.4, 8192 rows 35 and 17;
-// one of D = 4096, 256 rows 7.2 and 7.3, 512 rows 11 and 8.1, 2048 rows 28 and 15, 8192 rows 93 and 30.
+// one of D = 4096, 256 rows 7.2 and 7.3, 512 rows 11 and 8.1, 2048 rows 28 and 15, 8192 rows 93 and 30.  The constants are those of this shape; others,
+// bf16, 512 and 8192 rows of D = 4096: M = 8, K = 64 9.2 and 8.9, 66 and 29; M = 16, K = 64 16 and 9.6, 116 and 50; M = 16, K = 256 18 and 25 (the rule
+// stays with L2), 175 and 85; M = 4, K = 256 7.8 and 7.8, 52 and 21.  2048 rows of 8 heads, D = 128, M = 4 9.0 and 8.5 (the rule: L2), M = 16 24 and 19.
 struct SliceCut {
     int slices, splits;
     double us;

@@ -433,6 +433,8 @@ class Context:
         return stats.as_dict() if want_stats else None
 
     # ---- vectors of a language model as codes ---------------------------------------------
+    # Like all calls, on the context's stream: a tensor that was made or is dropped on another stream has to be ordered with it
+    # (wait_stream, record_stream) by the caller.  Outside autograd: lookup gives no gradient by itself, lookup_grad is it.
     def cache_begin(self, C):
         """Lays out the dictionaries of a cache, C float32 [H][M][K][D]; called again after a change to them."""
         H = C.shape[0]
