@@ -108,3 +108,30 @@ def test_writes_of_the_most_heads_and_of_many_dictionaries(n, H, D, M, K):
         want, mag = decoded(codes[:, h].cpu(), torch.from_numpy(C[h]), scale[:, h].cpu().double()[:, None])
         check(out[:, h].cpu(), want, mag, M, torch.float32)
     ctx.close()
+
+
+def test_rows_whose_offsets_pass_32_bits():
+    """A lookup of 600,011 rows of 4096, 4.9e9 bytes, and the gradient from as many: the last rows, the first, and some between, exactly."""
+    from paper_1509_05194_amd import hclae
+    T, V, D, M, K = 600011, 500, 4096, 2, 16
+    gen = torch.Generator().manual_seed(3)
+    C = torch.randint(-8, 9, (M, K, D), generator=gen).float().cuda()
+    ids = torch.randint(0, K, (V, M), dtype=torch.uint8, generator=gen).cuda()
+    rows = torch.randint(0, V, (T,), generator=gen).cuda()
+    at = torch.cat([torch.arange(20), torch.arange(T - 300, T), torch.randint(0, T, (500,), generator=gen)]).unique().cuda()
+    ctx = hclae.Context(T, D, M, K)
+    x = torch.full((T, D), 3.0, dtype=torch.bfloat16, device="cuda")
+    assert x.numel() * 2 > 2 ** 32
+    ctx.lookup(ids, C, x, rows=rows)
+    picked = ids[rows[at]].long()
+    assert torch.equal(x[at].float(), C[0][picked[:, 0]] + C[1][picked[:, 1]])      # whole numbers to 16
+    x.zero_()
+    g = torch.randint(-8, 9, (len(at), D), generator=gen).float().cuda()
+    x[at] = g.to(torch.bfloat16)
+    dC, want = torch.full((M, K, D), 7.0, device="cuda"), torch.zeros((M, K, D), device="cuda")
+    ctx.lookup_grad(ids, x, dC, rows=rows)
+    for m in range(M):
+        for k in range(K):
+            want[m, k] = g[picked[:, m] == k].sum(0)
+    assert torch.equal(dC, want)
+    ctx.close()

@@ -148,3 +148,16 @@ def test_dictionaries_laid_out_again_inside_a_graph():
             torch.cuda.synchronize()
             assert torch.equal(codes, got[0]) and torch.equal(scale, got[1]) and torch.equal(out, got[2])
         ctx.close()
+
+
+@pytest.mark.parametrize("n", [40, 1100, 4200])
+@pytest.mark.parametrize("spread", [1e-44, 1e-40, 2e-38, 1e37])
+def test_write_of_rows_whose_scales_are_at_the_ends_of_the_range(n, spread):
+    """Rows of subnormal numbers, and rows up to the largest ones: divided by their scale they are ordinary."""
+    rng = np.random.default_rng(n)
+    D, M, K = 100, 3, 70
+    x = np.clip(rng.standard_normal((n, 1, D)) * spread, -3.4e38, 3.4e38).astype(np.float32)
+    C = (rng.standard_normal((1, M, K, D)) * 0.5 ** np.arange(M)[None, :, None, None]).astype(np.float32)
+    codes, scale = written(x, C, True)
+    want, g = quantise(x[:, 0], C[0], True)
+    assert np.array_equal(codes[:, 0], want) and np.array_equal(scale[:, 0], g)
