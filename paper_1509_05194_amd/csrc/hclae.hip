@@ -2222,8 +2222,9 @@ int hclae_cache_begin(hclae_ctx *ctx, const float *C, int H, int M, int K, int D
 // Measured with M = 8, K = 256 on 256 CUs, us of one round at D = 64, 128, 256: 16, 24, 43; 29, 48, 75; 46, 78, 133; 55, 92, 150.  So at D = 128
 // and 8 heads: 256 rows 28 (one) and 44 (some), 512 rows 46 and 46, 1024 rows 89 and 48; 4096 rows 51 (some) and 78 (half),
 // 8192 rows 91 (some) and 82 (half); 32768 rows 82 (half) and 92 (all), 65536 rows 154 and 99.  A round at D = 128, 8 heads, K = 32, 64, 128: one 10, 13, 14;
-// some 46, 41, 45; half 48, 51, 61; all 68, 70, 73 (K = 256: 28, 53, 72, 85); M = 4 and 16, K = 256: 12, 31, 45, 51 and 37, 95, 142, 176.  So with fewer
-// codewords, or few dictionaries, the weights call k_cache_write_some from one round of k_cache_write_one too early: they are those of M = 8, K = 256.
+// some 46, 41, 45; half 48, 51, 61; all 68, 70, 73 (K = 256: 28, 53, 72, 85); M = 4 and 16, K = 256: 12, 31, 45, 51 and 37, 95, 142, 176.  The weights
+// are those of K = 256: with fewer codewords they leave k_cache_write_one too early (512, 768, 1024, 2048 rows, one and some: K = 32 21 and 45, 26 and 46, 37 and
+// 45, 69 and 46; K = 64 20 and 40, 26 and 39, 37 and 40, 69 and 40; K = 128 32 and 43, 42 and 43, 56 and 44; M = 16, K = 256 80 and 91, 114 and 91).
 enum CacheWay { kWayOne, kWaySome, kWayHalf, kWayAll };
 static CacheWay cache_way(int64_t n, int H, int D, int cus)
 {
