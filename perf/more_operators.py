@@ -57,7 +57,8 @@ def draw(rng):
     if op in ("attend", "select"):
         case.update(R=rng.choice([1, 4, 8, _between(rng, 1, 16)]), D=rng.choice([64, 128, 128, 4 * _between(rng, 8, 64)]), K=rng.choice([256, 256, _between(rng, 16, 256)]),
                     type=rng.choice(["bf16", "bf16", "fp16", "fp32"]))
-        # rows x heads x query heads a key head x dictionaries of the largest listed case
+        # products with codewords, and rows x heads x query heads a key head x dictionaries, of the largest listed cases
+        case["B"] = B = max(1, min(B, 32 * 8 * 4 * 16 * 256 * 128 // (G * case["R"] * M * case["K"] * case["D"])))
         most = (64 * 16384 * 8 * 4 * 8) // (B * G * max(case["R"], 4) * max(M, 8))
         case["n"] = _between(rng, 1, max(1, min(131072, most)))
         case["picks"] = 0
