@@ -368,6 +368,7 @@ int hclae_code_stats(hclae_ctx *ctx, const uint8_t *codes, int64_t N, int M, int
 #define HCLAE_MAX_H       1024                 /* heads of a cache                                    */
 #define HCLAE_CACHE_MAX_D 256                  /* longest row of a cache                              */
 #define HCLAE_MAX_SLOTS   ((int64_t)1 << 40)   /* rows of a code array: slots of a cache, rows of a table */
+#define HCLAE_MAX_HQ      16384                /* query heads of a call                               */
 
 /*
  * A cache of keys and values kept as codes: every head has M dictionaries of its own, a row of a head is M bytes
@@ -429,6 +430,82 @@ int hclae_lookup(hclae_ctx *ctx, const int64_t *rows, int64_t T, const uint8_t *
  */
 int hclae_lookup_grad(hclae_ctx *ctx, const int64_t *rows, int64_t T, const uint8_t *codes, int64_t V, float factor, const void *grad, int type,
                       int64_t row_stride, int M, int K, int D, float *dC);
+
+/* ---- serving from a cache of codes ----------------------------------------------------------------
+ *
+ * The sequences of a batch are rows of tables (DEVICE int32[B][max_pages]) and lengths (DEVICE int32[B]): row t of sequence b is in
+ * slot tables[b][t / page] * page + t % page of the cache, for 0 <= t < lengths[b] (a length below zero is zero, one beyond
+ * max_pages * page is that).  Entries beyond the length are not looked at.  Which pages are in use follows from tables and lengths alone:
+ *   a fork is a copied row of tables with its length; a sequence is given up by setting its length to 0; rows are taken back by
+ *   lowering it.  Pages that several sequences name are shared.
+ * A serving step is hclae_cache_extend (pages and slots for the new rows), hclae_cache_copy once per cache that goes by these tables (every
+ * layer's), hclae_cache_write into the slots, and hclae_cache_attend.
+ *
+ * These calls only enqueue.  Their scratch is in the ctx: a call that needs more than any before allocates it (what it
+ * replaces is kept until hclae_destroy, so that recorded graphs stay valid); while the stream is being captured such a call returns HCLAE_ESTATE
+ * and enqueues nothing, so a call of the same sizes is made before.  Calls of one ctx share the scratch: two recorded ones must not run at
+ * the same time.  They run on the device of the ctx, whichever is current.  Equal calls give equal bits.
+ */
+
+/*
+ * Attention of one new token of each sequence over its rows of the cache.  The cache's heads (hclae_cache_begin's H = 2 G) are G key heads
+ * and, behind them, the G value heads; query heads h R .. h R + R - 1 of Hq = G R attend to key head h.  With x(h, s) = scale[s][h] *
+ * sum_m C[h][m][codes[s][h][m]], for the rows t that take part, in slots s:
+ *   e_t = factor * q . x(h, s),   p = softmax(e),   out[b][h R + r] = sum_t p_t x(G + h, s),   lse[b][h R + r] = ln sum_t exp(e_t)
+ * Rows t that take part: begins[b] <= t < lengths[b] (begins: DEVICE int32[B], or NULL: from 0), of these with `picked` (DEVICE
+ * int32[B][G][n_picked], or NULL) the rows of the pages t / page that its head names, each as often as it is named; an entry outside [0, max_pages)
+ * names nothing.  A row whose page is not in the cache takes no part.  Where none takes part out is zero and lse -infinity.
+ * A row that takes part with a scale of NaN makes its head's outputs NaN (a value's all but lse).  Codes of K or more are read as K - 1.
+ *   Q: DEVICE, B tokens of Hq rows of `type`, row b, head hq at Q + b * q_row_stride + hq * q_head_stride (elements; strides and alignment as in
+ *   hclae_cache_write).  out: DEVICE, alike; its rows lie apart.  lse: DEVICE float[B][Hq], or NULL.  B <= N_max.
+ * Softmax statistics and sums are in 32 bits or more, out is rounded once.
+ */
+int hclae_cache_attend(hclae_ctx *ctx, const void *Q, int type, int B, int Hq, int64_t q_row_stride, int64_t q_head_stride, const uint8_t *codes,
+                       const float *scale, int64_t n_slots, const int32_t *tables, int max_pages, int page, const int32_t *begins,
+                       const int32_t *lengths, const int32_t *picked, int n_picked, float factor, void *out, int64_t out_row_stride,
+                       int64_t out_head_stride, float *lse);
+
+/*
+ * The k pages of each sequence and key head that its new token looks at most, for `picked` of hclae_cache_attend.  Every page of the cache
+ * has a stand-in, a coded row of each key head (DEVICE codes uint8[n_pages][H][M], scale float[n_pages][H] or NULL: the mean of
+ * its keys, say, written with hclae_cache_write to slot p for page p); this ctx's dictionaries (hclae_cache_begin) are those of the H key heads
+ * alone.  With R = Hq / H query heads to a key head and p = tables[b][j], j < ceil(lengths[b] / page):
+ *   score(b, h, j) = (sum_r q(h R + r)) . x(h, p)            in 64 bits; a NaN counts as -infinity
+ * picked[b][h]: DEVICE int32[B][H][k], the j of the first `first` and the last `recent` pages whatever their scores (their stand-ins are not
+ * read) and of the best others, the lower j of equals, k in all, ascending; -1 where there are no more.  Pages that are not in the cache
+ * (p outside [0, n_pages)) are not picked.  first + recent <= k.  B <= N_max.
+ */
+int hclae_cache_select(hclae_ctx *ctx, const void *Q, int type, int B, int Hq, int64_t q_row_stride, int64_t q_head_stride, const uint8_t *codes,
+                       const float *scale, int64_t n_pages, const int32_t *tables, int max_pages, int page, const int32_t *lengths, int first, int recent,
+                       int k, int32_t *picked);
+
+/*
+ * Pages and slots for the new rows of a step.  Sequence b gets rows starts[b] .. starts[b + 1] - 1 of the batch's n (DEVICE int32[B + 1],
+ * ascending): its length grows by their number, its table gets the pages they need, the lowest that no sequence uses, in the
+ * order of the sequences, and slots[i] (DEVICE int64[n], for hclae_cache_write) is where row i goes, -1 where it is not kept: rows of no
+ * sequence, and all rows of a sequence that cannot be served, whose table and length stay as they are.  These are one whose table has no
+ * entries left, and one that asks for pages when those asked for up to it (without the sequences whose tables are full) are more than are free.
+ *   A sequence that adds rows to a page that others name too gets a page of its own instead: page src[b] is to be copied to dst[b], its
+ * first rows[b] rows (DEVICE int32[B] each; -1, -1, 0 where nothing is), with hclae_cache_copy, before the rows are written.
+ *   n_pages: pages of the cache, < 2^31.  n <= N_max.  Table entries outside [0, n_pages) name no page.
+ */
+int hclae_cache_extend(hclae_ctx *ctx, int32_t *tables, int32_t *lengths, int B, int max_pages, int page, int64_t n_pages, const int32_t *starts, int64_t n,
+                       int64_t *slots, int32_t *src, int32_t *dst, int32_t *rows);
+
+/*
+ * Moves the pages in use to the front of the cache.  With u of them, the i-th lowest page in use from u on is to go to the i-th lowest
+ * free page below u: src[i], dst[i] (DEVICE int32[n_pages / 2] each, -1 behind the last move), with hclae_cache_copy; tables name the
+ * new places already.  Shared pages move once.  used: DEVICE int32[1] = u, or NULL.
+ */
+int hclae_cache_compact(hclae_ctx *ctx, int32_t *tables, const int32_t *lengths, int B, int max_pages, int page, int64_t n_pages, int32_t *src, int32_t *dst,
+                        int32_t *used);
+
+/*
+ * Copies pages of a cache (codes and, unless NULL, scale, of all heads of hclae_cache_begin): the first rows[i] rows (all, if rows is NULL) of page src[i] to page
+ * dst[i], i < n (DEVICE int32[n] each).  Pages outside the cache copy nothing, nor does a page to itself.  The destinations of a call are
+ * distinct and none is a source: else their bytes are a mixture.
+ */
+int hclae_cache_copy(hclae_ctx *ctx, uint8_t *codes, float *scale, int64_t n_slots, int page, const int32_t *src, const int32_t *dst, const int32_t *rows, int64_t n);
 
 /* ---- measurement: work done, and per-kernel durations from HIP events on the ctx's stream ------------- */
 

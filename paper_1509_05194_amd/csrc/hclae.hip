@@ -24,6 +24,7 @@
 #include "cache_write.hpp"
 #include "decode.hpp"
 #include "lookup_grad.hpp"
+#include "serve.hpp"
 #include <algorithm>
 #include <vector>
 
@@ -168,6 +169,13 @@ struct hclae_ctx {
     CacheTables cache_tab;
     // sorted rows of hclae_lookup_grad (allocated on first use)
     char *grad_buf;
+    // scratch of the calls that serve a cache: the largest any of them has asked for.  What it replaced is kept until hclae_destroy, as a
+    // recorded graph may still use it; each is at least twice as large as the one before
+    char *serve_buf;
+    size_t serve_bytes;
+    char *serve_old[48];
+    int serve_olds;
+    uint64_t serve_raised;   // kernels of serve.hip whose limit of LDS this ctx has raised
     // optional per-kernel timing (HIP events on ctx->stream)
     uint32_t t_mask;
     int t_used;
@@ -1091,9 +1099,10 @@ int hclae_destroy(hclae_ctx *ctx)
                    ctx->r16_rows, ctx->r16_norm, ctx->r16_img, ctx->r16_sums, ctx->r16_negmu, ctx->r16_consts, ctx->r16_ref, ctx->r16_words,
                    ctx->carry_u, ctx->carry_l, ctx->carry_path, ctx->carry_snap, ctx->carry_Centry, ctx->carry_T, ctx->carry_amax,
                    ctx->beam_rows[0], ctx->beam_rows[1],
-                   ctx->beam_pre[0], ctx->beam_pre[1], ctx->beam_mask, ctx->cache_C, ctx->cache_T, ctx->cache_buf, ctx->grad_buf};
+                   ctx->beam_pre[0], ctx->beam_pre[1], ctx->beam_mask, ctx->cache_C, ctx->cache_T, ctx->cache_buf, ctx->grad_buf, ctx->serve_buf};
     for (void *p : dev)
         if (p) (void)hipFree(p);
+    for (int i = 0; i < ctx->serve_olds; ++i) (void)hipFree(ctx->serve_old[i]);
     if (ctx->rec_host) (void)hipHostFree(ctx->rec_host);
     if (ctx->t_beg) {
         for (int i = 0; i < kMaxTimed; ++i) {
@@ -2503,6 +2512,149 @@ int hclae_lookup_grad(hclae_ctx *ctx, const int64_t *rows, int64_t T, const uint
     ON_DEVICE(ctx);
     const GradArgs a = {grad, row_stride, codes, {rows, V}, factor, M, K, D, T, dC};
     return type == HCLAE_F16 ? launch_lookup_grad<F16>(ctx, a) : type == HCLAE_BF16 ? launch_lookup_grad<Bf16>(ctx, a) : launch_lookup_grad<F32>(ctx, a);
+}
+
+// ---- serving from a cache of codes: attention, the choice of pages, and the pages themselves ------
+
+// Scratch of a serving call.  While a stream is being captured nothing is allocated: the call that finds too little fails, and the capture goes on.
+static int serve_room(hclae_ctx *ctx, size_t bytes, const char *name)
+{
+    if (bytes <= ctx->serve_bytes) return HCLAE_OK;
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    HIP_TRY(ctx, hipStreamIsCapturing(ctx->stream, &capture));
+    if (capture != hipStreamCaptureStatusNone) return fail(ctx, HCLAE_ESTATE, name);
+    if (ctx->serve_olds == (int)(sizeof(ctx->serve_old) / sizeof(ctx->serve_old[0]))) return fail(ctx, HCLAE_ENOMEM, name);
+    size_t want = std::max(bytes, std::max<size_t>(2 * ctx->serve_bytes, 1 << 20));
+    char *p = nullptr;
+    hipError_t e = hipMalloc((void **)&p, want);
+    if (e == hipErrorOutOfMemory && want > bytes) {
+        (void)hipGetLastError();
+        e = hipMalloc((void **)&p, want = bytes);
+    }
+    if (e != hipSuccess) return fail(ctx, e == hipErrorOutOfMemory ? HCLAE_ENOMEM : HCLAE_EHIP, "hipMalloc (scratch of a serving call)", e);
+    if (ctx->serve_buf) ctx->serve_old[ctx->serve_olds++] = ctx->serve_buf;
+    ctx->serve_buf = p;
+    ctx->serve_bytes = want;
+    return HCLAE_OK;
+}
+
+// Tables, lengths and pages of a call.
+static bool bad_pages(int B, int max_pages, int page, int64_t n_pages)
+{
+    return B < 0 || max_pages < 0 || page < 1 || n_pages < 0 || n_pages >= (int64_t)1 << 31;
+}
+
+int hclae_cache_attend(hclae_ctx *ctx, const void *Q, int type, int B, int Hq, int64_t q_row_stride, int64_t q_head_stride, const uint8_t *codes,
+                       const float *scale, int64_t n_slots, const int32_t *tables, int max_pages, int page, const int32_t *begins,
+                       const int32_t *lengths, const int32_t *picked, int n_picked, float factor, void *out, int64_t out_row_stride,
+                       int64_t out_head_stride, float *lse)
+{
+    if (!ctx) return HCLAE_EINVAL;
+    int rc = check_call(ctx, B, ctx->D, ctx->M, ctx->K);
+    if (rc != HCLAE_OK) return rc;
+    if (!ctx->cache_H) return fail(ctx, HCLAE_ESTATE, "hclae_cache_attend before hclae_cache_begin");
+    if (ctx->cache_H % 2) return fail(ctx, HCLAE_ESTATE, "hclae_cache_attend: the cache has no value head for each key head");
+    const int G = ctx->cache_H / 2;
+    if (bad_pages(B, max_pages, page, 0) || n_slots < 0 || n_slots > HCLAE_MAX_SLOTS || Hq < 1 || Hq > HCLAE_MAX_HQ || Hq % G || n_picked < 0 ||
+        (int64_t)n_picked * page >= (int64_t)1 << 31)
+        return fail(ctx, HCLAE_EINVAL, "hclae_cache_attend: B, Hq, n_slots, max_pages, page or n_picked out of range");
+    if (B == 0) return HCLAE_OK;
+    if (!Q || !lengths || !out || (max_pages > 0 && !tables) || (n_slots > 0 && !codes) || (n_picked > 0 && !picked)) return fail(ctx, HCLAE_EINVAL, "hclae_cache_attend: bad argument");
+    if (bad_rows(Q, type, q_row_stride, q_head_stride) || bad_rows(out, type, out_row_stride, out_head_stride) || odd_words(4, scale, tables, begins, lengths, picked, lse))
+        return fail(ctx, HCLAE_EINVAL, "hclae_cache_attend: type, alignment or strides");
+    if (!apart(B, Hq, ctx->D, out_row_stride, out_head_stride)) return fail(ctx, HCLAE_EINVAL, "hclae_cache_attend: rows of out overlap");
+    ON_DEVICE(ctx);
+    const AttendArgs a = {Q, q_row_stride, q_head_stride, codes, scale, {tables, lengths, B, max_pages, page, n_slots / page}, begins, picked, n_picked, factor,
+                          ctx->cache_C, G, Hq / G, ctx->M, ctx->K, ctx->D, out, out_row_stride, out_head_stride, lse};
+    rc = serve_room(ctx, attend_scratch(a, ctx->cus), "hclae_cache_attend: its scratch cannot be allocated while the stream is captured");
+    if (rc != HCLAE_OK) return rc;
+    HIP_TRY(ctx, attend_launch(a, type, ctx->cus, ctx->serve_buf, &ctx->serve_raised, ctx->stream));
+    return HCLAE_OK;
+}
+
+int hclae_cache_select(hclae_ctx *ctx, const void *Q, int type, int B, int Hq, int64_t q_row_stride, int64_t q_head_stride, const uint8_t *codes,
+                       const float *scale, int64_t n_pages, const int32_t *tables, int max_pages, int page, const int32_t *lengths, int first, int recent,
+                       int k, int32_t *picked)
+{
+    if (!ctx) return HCLAE_EINVAL;
+    int rc = check_call(ctx, B, ctx->D, ctx->M, ctx->K);
+    if (rc != HCLAE_OK) return rc;
+    if (!ctx->cache_H) return fail(ctx, HCLAE_ESTATE, "hclae_cache_select before hclae_cache_begin");
+    const int G = ctx->cache_H;
+    if (bad_pages(B, max_pages, page, n_pages) || Hq < 1 || Hq > HCLAE_MAX_HQ || Hq % G || first < 0 || recent < 0 || k < 1 || (int64_t)first + recent > k)
+        return fail(ctx, HCLAE_EINVAL, "hclae_cache_select: B, Hq, n_pages, max_pages, page, first, recent or k out of range");
+    if (B == 0) return HCLAE_OK;
+    if (!Q || !lengths || !picked || (max_pages > 0 && !tables) || (n_pages > 0 && !codes)) return fail(ctx, HCLAE_EINVAL, "hclae_cache_select: bad argument");
+    if (bad_rows(Q, type, q_row_stride, q_head_stride) || odd_words(4, scale, tables, lengths, picked))
+        return fail(ctx, HCLAE_EINVAL, "hclae_cache_select: type, alignment or strides");
+    ON_DEVICE(ctx);
+    const SelectArgs a = {Q, q_row_stride, q_head_stride, codes, scale, {tables, lengths, B, max_pages, page, n_pages}, ctx->cache_T, cache_padded(ctx->D) / 4,
+                          few_columns(ctx->K), G, Hq / G, ctx->M, ctx->K, ctx->D, first, recent, k, picked};
+    rc = serve_room(ctx, select_scratch(a), "hclae_cache_select: its scratch cannot be allocated while the stream is captured");
+    if (rc != HCLAE_OK) return rc;
+    HIP_TRY(ctx, select_launch(a, type, ctx->serve_buf, &ctx->serve_raised, ctx->stream));
+    return HCLAE_OK;
+}
+
+int hclae_cache_extend(hclae_ctx *ctx, int32_t *tables, int32_t *lengths, int B, int max_pages, int page, int64_t n_pages, const int32_t *starts, int64_t n,
+                       int64_t *slots, int32_t *src, int32_t *dst, int32_t *rows)
+{
+    if (!ctx) return HCLAE_EINVAL;
+    int rc = check_call(ctx, n, ctx->D, ctx->M, ctx->K);
+    if (rc != HCLAE_OK) return rc;
+    if (bad_pages(B, max_pages, page, n_pages)) return fail(ctx, HCLAE_EINVAL, "hclae_cache_extend: B, max_pages, page or n_pages out of range");
+    if (B == 0 && n == 0) return HCLAE_OK;
+    if (!starts || (n > 0 && !slots) || (B > 0 && (!lengths || !src || !dst || !rows)) || (B > 0 && max_pages > 0 && !tables))
+        return fail(ctx, HCLAE_EINVAL, "hclae_cache_extend: bad argument");
+    if (odd_words(4, tables, lengths, starts, src, dst, rows) || odd_words(8, slots)) return fail(ctx, HCLAE_EINVAL, "hclae_cache_extend: alignment");
+    ON_DEVICE(ctx);
+    PageArgs a = {tables, lengths, B, max_pages, page, n_pages, starts, n, slots, src, dst, rows, nullptr};
+    rc = serve_room(ctx, extend_scratch(a), "hclae_cache_extend: its scratch cannot be allocated while the stream is captured");
+    if (rc != HCLAE_OK) return rc;
+    HIP_TRY(ctx, extend_launch(a, ctx->cus, ctx->serve_buf, ctx->stream));
+    return HCLAE_OK;
+}
+
+int hclae_cache_compact(hclae_ctx *ctx, int32_t *tables, const int32_t *lengths, int B, int max_pages, int page, int64_t n_pages, int32_t *src, int32_t *dst,
+                        int32_t *used)
+{
+    if (!ctx) return HCLAE_EINVAL;
+    int rc = check_call(ctx, 0, ctx->D, ctx->M, ctx->K);
+    if (rc != HCLAE_OK) return rc;
+    if (bad_pages(B, max_pages, page, n_pages)) return fail(ctx, HCLAE_EINVAL, "hclae_cache_compact: B, max_pages, page or n_pages out of range");
+    if ((n_pages > 1 && (!src || !dst)) || (B > 0 && !lengths) || (B > 0 && max_pages > 0 && !tables)) return fail(ctx, HCLAE_EINVAL, "hclae_cache_compact: bad argument");
+    if (odd_words(4, tables, lengths, src, dst, used)) return fail(ctx, HCLAE_EINVAL, "hclae_cache_compact: alignment");
+    ON_DEVICE(ctx);
+    PageArgs a = {};
+    a.tables = tables;
+    a.lengths = const_cast<int32_t *>(lengths);             // only read
+    a.B = B;
+    a.max_pages = max_pages;
+    a.page = page;
+    a.n_pages = n_pages;
+    a.src = src;
+    a.dst = dst;
+    a.used = used;
+    rc = serve_room(ctx, compact_scratch(a), "hclae_cache_compact: its scratch cannot be allocated while the stream is captured");
+    if (rc != HCLAE_OK) return rc;
+    HIP_TRY(ctx, compact_launch(a, ctx->cus, ctx->serve_buf, ctx->stream));
+    return HCLAE_OK;
+}
+
+int hclae_cache_copy(hclae_ctx *ctx, uint8_t *codes, float *scale, int64_t n_slots, int page, const int32_t *src, const int32_t *dst, const int32_t *rows, int64_t n)
+{
+    if (!ctx) return HCLAE_EINVAL;
+    int rc = check_call(ctx, 0, ctx->D, ctx->M, ctx->K);
+    if (rc != HCLAE_OK) return rc;
+    if (!ctx->cache_H) return fail(ctx, HCLAE_ESTATE, "hclae_cache_copy before hclae_cache_begin");
+    if (page < 1 || n_slots < 0 || n_slots > HCLAE_MAX_SLOTS || n < 0 || n >= (int64_t)1 << 31) return fail(ctx, HCLAE_EINVAL, "hclae_cache_copy: n_slots, page or n out of range");
+    if (n == 0 || n_slots < page) return HCLAE_OK;
+    if (!codes || !src || !dst) return fail(ctx, HCLAE_EINVAL, "hclae_cache_copy: bad argument");
+    if (odd_words(4, scale, src, dst, rows)) return fail(ctx, HCLAE_EINVAL, "hclae_cache_copy: alignment");
+    ON_DEVICE(ctx);
+    const CopyArgs a = {codes, scale, n_slots / page, page, ctx->cache_H * ctx->M, ctx->cache_H, src, dst, rows, n};
+    HIP_TRY(ctx, copy_launch(a, ctx->cus, ctx->stream));
+    return HCLAE_OK;
 }
 
 int hclae_timing_enable(hclae_ctx *ctx, uint32_t class_mask)

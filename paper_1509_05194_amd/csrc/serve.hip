@@ -1,0 +1,228 @@
+// Launches of the kernels that serve a paged cache of codes: attention, the choice of pages, and the pages themselves.  Arguments have
+// been checked by the entry points in hclae.hip; scratch is theirs.
+#include <algorithm>
+
+#include "attend.hpp"
+#include "pages.hpp"
+#include "select.hpp"
+#include "serve.hpp"
+
+namespace hclae {
+
+namespace {
+
+constexpr int kServeLds = 156 * 1024;               // LDS that a kernel asks for at its launch; the rest of a workgroup's 160 KB is for what it declares
+
+size_t up(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+#define TRY(call)                         \
+    do {                                  \
+        const hipError_t e__ = (call);    \
+        if (e__ != hipSuccess) return e__; \
+    } while (0)
+
+template <typename K>
+hipError_t raise_lds(K kern, int bit, uint64_t *raised)
+{
+    if (*raised >> bit & 1u) return hipSuccess;
+    TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kServeLds));
+    *raised |= 1ull << bit;
+    return hipSuccess;
+}
+
+enum RaisedBit { kRaisedSelect = 0 };
+
+// ---- attention ----------------------------------------------------------------------------------
+
+int64_t direct_jobs(const AttendArgs &a, int splits)
+{
+    const int RB = heads_at_once(a.R);
+    return (int64_t)a.rows.B * a.G * ((a.R + RB - 1) / RB) * splits;
+}
+
+template <typename T, int RB>
+hipError_t launch_direct(const AttendArgs &a, int splits, char *scratch, hipStream_t stream)
+{
+    int lanes = 1;
+    while (lanes < a.D / 4) lanes *= 2;
+    const int64_t jobs = direct_jobs(a, splits);
+    PartStat *stats = reinterpret_cast<PartStat *>(scratch);
+    float *sums = reinterpret_cast<float *>(scratch + up(sizeof(PartStat) * jobs * RB));
+    hipLaunchKernelGGL((k_attend_rows<T, RB>), dim3((unsigned)jobs), dim3(kDirectThreads), 0, stream, a, splits, lanes, stats, sums);
+    TRY(hipGetLastError());
+    hipLaunchKernelGGL((k_attend_join<T, RB>), dim3((unsigned)(a.rows.B * a.G * a.R)), dim3(kWave), 0, stream, a, splits, (const PartStat *)stats, (const float *)sums);
+    return hipGetLastError();
+}
+
+// The sequences of a call are taken in rounds, which bounds its scratch and its grids.
+constexpr int64_t kAttendRound = 1 << 16;           // query heads of a round, of all its sequences
+int attend_round(const AttendArgs &a) { return (int)std::max<int64_t>(1, std::min<int64_t>(a.rows.B, kAttendRound / ((int64_t)a.G * a.R))); }
+AttendArgs round_of(const AttendArgs &a, int b0, int n, int bytes)
+{
+    AttendArgs r = a;
+    r.Q = static_cast<const char *>(a.Q) + (int64_t)b0 * a.q_row * bytes;
+    r.out = static_cast<char *>(a.out) + (int64_t)b0 * a.o_row * bytes;
+    r.rows.tables += (int64_t)b0 * a.rows.max_pages;
+    r.rows.lengths += b0;
+    r.rows.B = n;
+    if (a.begins) r.begins += b0;
+    if (a.picked) r.picked += (int64_t)b0 * a.G * a.n_picked;
+    if (a.lse) r.lse += (int64_t)b0 * a.G * a.R;
+    return r;
+}
+
+template <typename T>
+hipError_t launch_attend(const AttendArgs &a, int cus, char *scratch, uint64_t *raised, hipStream_t stream)
+{
+    const int splits = direct_splits(a, cus);
+    switch (heads_at_once(a.R)) {
+    case 1: return launch_direct<T, 1>(a, splits, scratch, stream);
+    case 2: return launch_direct<T, 2>(a, splits, scratch, stream);
+    default: return launch_direct<T, 4>(a, splits, scratch, stream);
+    }
+}
+
+// ---- the choice of pages ------------------------------------------------------------------------
+
+// As with attention, in rounds: at most 256 MB of tables and keys.
+int select_round(const SelectArgs &a)
+{
+    const int64_t each = 8ll * a.G * ((int64_t)a.M * a.K + a.rows.max_pages);
+    return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)a.rows.B, (256ll << 20) / each, (int64_t)(1 << 18) / a.G}));
+}
+SelectArgs round_of(const SelectArgs &a, int b0, int n, int bytes)
+{
+    SelectArgs r = a;
+    r.Q = static_cast<const char *>(a.Q) + (int64_t)b0 * a.q_row * bytes;
+    r.rows.tables += (int64_t)b0 * a.rows.max_pages;
+    r.rows.lengths += b0;
+    r.rows.B = n;
+    r.picked += (int64_t)b0 * a.G * a.k;
+    return r;
+}
+
+size_t table_bytes(const SelectArgs &a) { return up(sizeof(double) * (size_t)a.rows.B * a.G * a.M * a.K); }
+
+template <typename T>
+hipError_t launch_select(const SelectArgs &a, char *scratch, uint64_t *raised, hipStream_t stream)
+{
+    double *tab = reinterpret_cast<double *>(scratch);
+    uint64_t *keys = reinterpret_cast<uint64_t *>(scratch + table_bytes(a));
+    hipLaunchKernelGGL(k_select_tables<T>, dim3((unsigned)(a.G * a.M), (unsigned)((a.rows.B + kSelectSeqs - 1) / kSelectSeqs)), dim3(kSelectThreads), 0, stream, a, tab);
+    TRY(hipGetLastError());
+    const size_t lds = 8 * ((size_t)a.M * a.K + a.rows.max_pages);
+    const dim3 grid((unsigned)(a.rows.B * a.G));
+    if (lds <= (size_t)kServeLds) {
+        TRY(raise_lds(&k_select_pages<true>, kRaisedSelect, raised));
+        hipLaunchKernelGGL(k_select_pages<true>, grid, dim3(kPickThreads), lds, stream, a, (const double *)tab, keys);
+    } else {
+        hipLaunchKernelGGL(k_select_pages<false>, grid, dim3(kPickThreads), 0, stream, a, (const double *)tab, keys);
+    }
+    return hipGetLastError();
+}
+
+// ---- pages --------------------------------------------------------------------------------------
+
+size_t bitmap_bytes(const PageArgs &a) { return up(4 * (size_t)words_of(a.n_pages)); }
+
+// Bitmaps at the front of the scratch: pages named once or more, pages named twice or more.
+hipError_t launch_marks(const PageArgs &a, int cus, char *scratch, hipStream_t stream)
+{
+    const int64_t words = (int64_t)(2 * bitmap_bytes(a) / 4), entries = (int64_t)a.B * a.max_pages;
+    auto blocks = [&](int64_t items) { return dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>((items + kPageThreads - 1) / kPageThreads, 8ll * cus))); };
+    hipLaunchKernelGGL(k_pages_clear, blocks(words), dim3(kPageThreads), 0, stream, reinterpret_cast<unsigned *>(scratch), words);
+    TRY(hipGetLastError());
+    hipLaunchKernelGGL(k_pages_mark, blocks(entries), dim3(kPageThreads), 0, stream, a, reinterpret_cast<unsigned *>(scratch),
+                       reinterpret_cast<unsigned *>(scratch + bitmap_bytes(a)));
+    return hipGetLastError();
+}
+
+// Pages that the sequences of a call can ask for: each the copy of its last one, and a page begun and those that its rows fill.
+size_t extend_room(const PageArgs &a) { return (size_t)std::min<int64_t>(a.n_pages, 2ll * a.B + a.n / a.page); }
+
+}  // namespace
+
+size_t attend_scratch(const AttendArgs &a, int cus)
+{
+    size_t most = 0;
+    for (int n : {attend_round(a), a.rows.B % attend_round(a)}) {   // whole rounds, and the last one
+        if (n == 0) continue;
+        const AttendArgs r = round_of(a, 0, n, 0);
+        const int RB = heads_at_once(r.R);
+        const int64_t jobs = direct_jobs(r, direct_splits(r, cus));
+        most = std::max(most, up(sizeof(PartStat) * jobs * RB) + up(sizeof(float) * jobs * RB * r.D));
+    }
+    return most;
+}
+
+hipError_t attend_launch(const AttendArgs &a, int type, int cus, char *scratch, uint64_t *raised, hipStream_t stream)
+{
+    const int step = attend_round(a);
+    for (int b0 = 0; b0 < a.rows.B; b0 += step) {
+        const AttendArgs r = round_of(a, b0, std::min(step, a.rows.B - b0), type == kRowF32 ? 4 : 2);
+        TRY(type == kRowF32 ? launch_attend<F32>(r, cus, scratch, raised, stream) : type == kRowF16 ? launch_attend<F16>(r, cus, scratch, raised, stream)
+                                                                                                  : launch_attend<Bf16>(r, cus, scratch, raised, stream));
+    }
+    return hipSuccess;
+}
+
+size_t select_scratch(const SelectArgs &a)
+{
+    const SelectArgs r = round_of(a, 0, select_round(a), 0);
+    return table_bytes(r) + up(sizeof(uint64_t) * (size_t)r.rows.B * r.G * r.rows.max_pages);
+}
+
+hipError_t select_launch(const SelectArgs &a, int type, char *scratch, uint64_t *raised, hipStream_t stream)
+{
+    const int step = select_round(a);
+    for (int b0 = 0; b0 < a.rows.B; b0 += step) {
+        const SelectArgs r = round_of(a, b0, std::min(step, a.rows.B - b0), type == kRowF32 ? 4 : 2);
+        TRY(type == kRowF32 ? launch_select<F32>(r, scratch, raised, stream) : type == kRowF16 ? launch_select<F16>(r, scratch, raised, stream)
+                                                                                             : launch_select<Bf16>(r, scratch, raised, stream));
+    }
+    return hipSuccess;
+}
+
+size_t extend_scratch(const PageArgs &a) { return 2 * bitmap_bytes(a) + up(4 * (size_t)a.B) + up(4 * extend_room(a)) + 256; }
+
+hipError_t extend_launch(const PageArgs &a, int cus, char *scratch, hipStream_t stream)
+{
+    TRY(launch_marks(a, cus, scratch, stream));
+    ExtendScratch s;
+    char *p = scratch;
+    s.used = reinterpret_cast<unsigned *>(p);
+    s.shared = reinterpret_cast<unsigned *>(p += bitmap_bytes(a));
+    s.upto = reinterpret_cast<unsigned *>(p += bitmap_bytes(a));
+    s.free = reinterpret_cast<unsigned *>(p += up(4 * (size_t)a.B));
+    s.found = reinterpret_cast<unsigned *>(p += up(4 * extend_room(a)));
+    s.room = (unsigned)extend_room(a);
+    hipLaunchKernelGGL(k_extend_plan, dim3(1), dim3(kPlanThreads), 0, stream, a, s);
+    TRY(hipGetLastError());
+    hipLaunchKernelGGL(k_extend_rows, dim3((unsigned)std::max(1, std::min(a.B, 1 << 16))), dim3(kPageThreads), 0, stream, a, s);
+    return hipGetLastError();
+}
+
+size_t compact_scratch(const PageArgs &a) { return 2 * bitmap_bytes(a) + bitmap_bytes(a); }
+
+hipError_t compact_launch(const PageArgs &a, int cus, char *scratch, hipStream_t stream)
+{
+    TRY(launch_marks(a, cus, scratch, stream));
+    CompactScratch s = {reinterpret_cast<unsigned *>(scratch), reinterpret_cast<unsigned *>(scratch + bitmap_bytes(a)), reinterpret_cast<unsigned *>(scratch + 2 * bitmap_bytes(a))};
+    hipLaunchKernelGGL(k_compact_plan, dim3(1), dim3(kPlanThreads), 0, stream, a, s);
+    TRY(hipGetLastError());
+    const int64_t entries = (int64_t)a.B * a.max_pages;
+    if (a.n_pages == 0 || entries == 0) return hipSuccess;
+    hipLaunchKernelGGL(k_compact_tables, dim3((unsigned)std::min<int64_t>((entries + kPageThreads - 1) / kPageThreads, 8ll * cus)), dim3(kPageThreads), 0, stream, a, s);
+    return hipGetLastError();
+}
+
+hipError_t copy_launch(const CopyArgs &a, int cus, hipStream_t stream)
+{
+    // a block about 4 KB of codes
+    const int64_t bytes = (int64_t)a.page * a.row_codes;
+    const int parts = (int)std::max<int64_t>(1, std::min<int64_t>({(bytes + 4095) / 4096, (int64_t)a.page, (int64_t)64}));
+    hipLaunchKernelGGL(k_pages_copy, dim3((unsigned)std::min<int64_t>(a.n * parts, 1 << 20)), dim3(kPageThreads), 0, stream, a, parts);
+    return hipGetLastError();
+}
+
+}  // namespace hclae

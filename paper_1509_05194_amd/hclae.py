@@ -26,6 +26,7 @@ EXPORTS = (
     "hclae_reorder_by_variance", "hclae_code_stats",
     "hclae_beam_step", "hclae_encode_beam", "hclae_set_beam_width", "hclae_set_contraction", "hclae_set_pruning",
     "hclae_cache_begin", "hclae_cache_write", "hclae_cache_read", "hclae_lookup", "hclae_lookup_grad",
+    "hclae_cache_attend", "hclae_cache_select", "hclae_cache_extend", "hclae_cache_compact", "hclae_cache_copy",
 )
 
 KERNEL_CLASSES = ("heat", "cool", "assign", "refine", "accumulate", "merge", "norms", "error", "transition",
@@ -111,6 +112,11 @@ def lib():
     L.hclae_cache_read.argtypes = [vp, vp, vp, i64, vp, i32, i32, i32, vp, i64, vp, i32, i64, i64]
     L.hclae_lookup.argtypes = [vp, vp, i64, vp, i64, f32, vp, i32, i32, i32, vp, i32, i64]
     L.hclae_lookup_grad.argtypes = [vp, vp, i64, vp, i64, f32, vp, i32, i64, i32, i32, i32, vp]
+    L.hclae_cache_attend.argtypes = [vp, vp, i32, i32, i32, i64, i64, vp, vp, i64, vp, i32, i32, vp, vp, vp, i32, f32, vp, i64, i64, vp]
+    L.hclae_cache_select.argtypes = [vp, vp, i32, i32, i32, i64, i64, vp, vp, i64, vp, i32, i32, vp, i32, i32, i32, vp]
+    L.hclae_cache_extend.argtypes = [vp, vp, vp, i32, i32, i32, i64, vp, i64, vp, vp, vp, vp]
+    L.hclae_cache_compact.argtypes = [vp, vp, vp, i32, i32, i32, i64, vp, vp, vp]
+    L.hclae_cache_copy.argtypes = [vp, vp, vp, i64, i32, vp, vp, vp, i64]
     L.hclae_timing_enable.argtypes = [vp, ctypes.c_uint32]
     L.hclae_timing_read.argtypes = [vp, ctypes.POINTER(KernelTimes)]
     for name in EXPORTS:
@@ -479,6 +485,65 @@ class Context:
         p, kind, st = _rows(grad, (T, self.D))
         self._chk(lib().hclae_lookup_grad(self._h, _ptr(rows, "i64", (T,)), T, _ptr(codes, "u8", (V, self.M)), V, scale, p, kind,
                                           st[0], self.M, self.K, self.D, _ptr(dC, "f32", (self.M, self.K, self.D))))
+
+    # ---- serving from a cache of codes ------------------------------------------------------
+    # tables int32 [B][max_pages] and lengths int32 [B] say where the rows of a batch's sequences are (see include/hclae.h); a fork is a copied row of
+    # them, and a sequence is given up by setting its length to 0.
+    def cache_attend(self, Q, codes, scale, tables, lengths, page, out, factor=None, begins=None, picked=None, lse=None):
+        """Attention of one new token of each sequence, Q [B][Hq][D] (float32, float16 or bfloat16), over its rows begins..lengths of the cache,
+        of those, with picked int32 [B][G][n], the rows of the named pages: out [B][Hq][D], of Q's type, and lse float32 [B][Hq].  The cache's
+        heads are G key heads and the G value heads behind them, codes uint8 [n_slots][2 G][M].  factor: 1 / sqrt(D) unless given."""
+        B, Hq, n_slots, H = Q.shape[0], Q.shape[1], codes.shape[0], self._H or codes.shape[1]
+        self._here(Q, codes, scale, tables, lengths, out, begins, picked, lse)
+        if out.dtype is not Q.dtype:
+            raise TypeError("out is of another type than Q")
+        pq, kind, sq = _rows(Q, (B, Hq, self.D))
+        po, _, so = _rows(out, (B, Hq, self.D))
+        max_pages, n_picked = tables.shape[1], 0 if picked is None else picked.shape[2]
+        if picked is not None and n_picked == 0:
+            raise ValueError("picked names no pages")      # its pointer would be NULL, which stands for all rows
+        self._chk(lib().hclae_cache_attend(
+            self._h, pq, kind, B, Hq, sq[0], sq[1], _ptr(codes, "u8", (n_slots, H, self.M)), _ptr(scale, "f32", (n_slots, H)), n_slots,
+            _ptr(tables, "i32", (B, max_pages)), max_pages, page, _ptr(begins, "i32", (B,)), _ptr(lengths, "i32", (B,)),
+            _ptr(picked, "i32", (B, H // 2, n_picked)), n_picked, self.D ** -0.5 if factor is None else factor, po, so[0], so[1], _ptr(lse, "f32", (B, Hq))))
+
+    def cache_select(self, Q, codes, scale, tables, lengths, page, picked, first=1, recent=1):
+        """The pages that each sequence's new token looks at most, by their stand-ins codes uint8 [n_pages][H][M] and scale float32 [n_pages][H] (or
+        None), H key heads: picked int32 [B][H][k], ascending, -1 behind the last; the first `first` and last `recent` pages are always among them."""
+        B, Hq, n_pages, H = Q.shape[0], Q.shape[1], codes.shape[0], self._H or codes.shape[1]
+        self._here(Q, codes, scale, tables, lengths, picked)
+        p, kind, st = _rows(Q, (B, Hq, self.D))
+        max_pages, k = tables.shape[1], picked.shape[2]
+        self._chk(lib().hclae_cache_select(
+            self._h, p, kind, B, Hq, st[0], st[1], _ptr(codes, "u8", (n_pages, H, self.M)), _ptr(scale, "f32", (n_pages, H)), n_pages,
+            _ptr(tables, "i32", (B, max_pages)), max_pages, page, _ptr(lengths, "i32", (B,)), first, recent, k, _ptr(picked, "i32", (B, H, k))))
+
+    def cache_extend(self, tables, lengths, starts, page, n_pages, slots, src, dst, rows):
+        """Pages and slots for a step's new rows, starts[b]..starts[b + 1] of sequence b: tables and lengths grow in place, slots int64 [n] is for
+        cache_write; src, dst and rows int32 [B] are the copies to make, with cache_copy, of pages that were shared."""
+        B, max_pages = tables.shape
+        n = slots.shape[0]
+        self._here(tables, lengths, starts, slots, src, dst, rows)
+        self._chk(lib().hclae_cache_extend(
+            self._h, _ptr(tables, "i32"), _ptr(lengths, "i32", (B,)), B, max_pages, page, n_pages, _ptr(starts, "i32", (B + 1,)), n,
+            _ptr(slots, "i64", (n,)), _ptr(src, "i32", (B,)), _ptr(dst, "i32", (B,)), _ptr(rows, "i32", (B,))))
+
+    def cache_compact(self, tables, lengths, page, n_pages, src, dst, used=None):
+        """Moves the pages in use to the front: tables name their new places, src and dst int32 [n_pages // 2] are the copies to make, with
+        cache_copy (-1 behind the last), used int32 [1] their number."""
+        B, max_pages = tables.shape
+        self._here(tables, lengths, src, dst, used)
+        self._chk(lib().hclae_cache_compact(
+            self._h, _ptr(tables, "i32"), _ptr(lengths, "i32", (B,)), B, max_pages, page, n_pages, _ptr(src, "i32", (n_pages // 2,)),
+            _ptr(dst, "i32", (n_pages // 2,)), _ptr(used, "i32", (1,))))
+
+    def cache_copy(self, codes, scale, page, src, dst, rows=None):
+        """Copies the first rows[i] rows (None: all) of page src[i] of codes uint8 [n_slots][H][M] and scale float32 [n_slots][H] (or None) to page
+        dst[i]; pages outside the cache copy nothing."""
+        n, n_slots, H = src.shape[0], codes.shape[0], self._H or codes.shape[1]
+        self._here(codes, scale, src, dst, rows)
+        self._chk(lib().hclae_cache_copy(self._h, _ptr(codes, "u8", (n_slots, H, self.M)), _ptr(scale, "f32", (n_slots, H)), n_slots, page,
+                                         _ptr(src, "i32", (n,)), _ptr(dst, "i32", (n,)), _ptr(rows, "i32", (n,)), n))
 
     # ---- dictionary order and code statistics ---------------------------------------------
     def reorder_by_variance(self, C, codes):
