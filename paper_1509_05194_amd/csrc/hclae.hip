@@ -2566,7 +2566,7 @@ int hclae_cache_attend(hclae_ctx *ctx, const void *Q, int type, int B, int Hq, i
     ON_DEVICE(ctx);
     const AttendArgs a = {Q, q_row_stride, q_head_stride, codes, scale, {tables, lengths, B, max_pages, page, n_slots / page}, begins, picked, n_picked, factor,
                           ctx->cache_C, G, Hq / G, ctx->M, ctx->K, ctx->D, out, out_row_stride, out_head_stride, lse};
-    rc = serve_room(ctx, attend_scratch(a, ctx->cus), "hclae_cache_attend: its scratch cannot be allocated while the stream is captured");
+    rc = serve_room(ctx, attend_scratch(a, type, ctx->cus), "hclae_cache_attend: its scratch cannot be allocated while the stream is captured");
     if (rc != HCLAE_OK) return rc;
     HIP_TRY(ctx, attend_launch(a, type, ctx->cus, ctx->serve_buf, &ctx->serve_raised, ctx->stream));
     return HCLAE_OK;

@@ -30,7 +30,7 @@ hipError_t raise_lds(K kern, int bit, uint64_t *raised)
     return hipSuccess;
 }
 
-enum RaisedBit { kRaisedSelect = 0 };
+enum RaisedBit { kRaisedSelect = 0, kRaisedCodes = 1 };         // 15 from kRaisedCodes on
 
 // ---- attention ----------------------------------------------------------------------------------
 
@@ -55,7 +55,7 @@ hipError_t launch_direct(const AttendArgs &a, int splits, char *scratch, hipStre
 }
 
 // The sequences of a call are taken in rounds, which bounds its scratch and its grids.
-constexpr int64_t kAttendRound = 1 << 16;           // query heads of a round, of all its sequences
+constexpr int64_t kAttendRound = 1 << 14;           // query heads of a round, of all its sequences
 int attend_round(const AttendArgs &a) { return (int)std::max<int64_t>(1, std::min<int64_t>(a.rows.B, kAttendRound / ((int64_t)a.G * a.R))); }
 AttendArgs round_of(const AttendArgs &a, int b0, int n, int bytes)
 {
@@ -71,9 +71,78 @@ AttendArgs round_of(const AttendArgs &a, int b0, int n, int bytes)
     return r;
 }
 
-template <typename T>
-hipError_t launch_attend(const AttendArgs &a, int cus, char *scratch, uint64_t *raised, hipStream_t stream)
+// Whether the rows go through tables: not where a sequence can have few rows only, which are decoded before the tables are there.
+constexpr int64_t kFewRows = 512;
+CodesPlan plan_of(const AttendArgs &a, int type)
 {
+    if (attend_capacity(a) <= kFewRows) return {0, false, 0, 0};
+    return codes_plan(a.R, a.M, a.K, type == kRowF32);
+}
+
+struct CodesRoom {
+    size_t tab, stats, sums;
+};
+CodesRoom codes_room(const AttendArgs &a, const CodesPlan &plan, int splits)
+{
+    const int64_t seqs = (int64_t)a.rows.B * a.G * ((a.R + plan.RB - 1) / plan.RB), rows = seqs * splits * plan.RB;
+    return {up(sizeof(float) * seqs * plan.RB * a.M * a.K), up(sizeof(CodesStat) * rows), up(sizeof(float) * rows * sums_row(a.M, a.K))};
+}
+
+template <int RB, bool WIDE, int MW>
+hipError_t launch_codes(const AttendArgs &a, const CodesPlan &plan, int splits, const float *tab, CodesStat *stats, float *sums, uint64_t *raised, hipStream_t stream)
+{
+    constexpr int bit = kRaisedCodes + (MW == 2 ? 0 : MW == 4 ? 5 : 10) + (RB == 1 ? 0 : RB == 2 ? 1 : 3) + (RB > 1 && WIDE ? 1 : 0);
+    auto kern = &k_attend_codes<RB, WIDE, MW>;
+    TRY(raise_lds(kern, bit, raised));
+    const int64_t heads = (int64_t)a.G * ((a.R + RB - 1) / RB), units = (int64_t)a.rows.B * splits;
+    const bool grouped = units >= 32, words = a.M % 4 == 0 && reinterpret_cast<uintptr_t>(a.codes) % 4 == 0;
+    const int64_t blocks = (grouped ? (units + 7) / 8 * 8 : units) * heads;
+    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(kCodesThreads), plan.lds, stream, a, splits, grouped, words, tab, stats, sums);
+    return hipGetLastError();
+}
+
+template <typename T, int RB>
+hipError_t launch_through_tables(const AttendArgs &a, const CodesPlan &plan, int cus, char *scratch, uint64_t *raised, hipStream_t stream)
+{
+    const int splits = codes_splits(a, RB, cus);
+    const CodesRoom room = codes_room(a, plan, splits);
+    float *tab = reinterpret_cast<float *>(scratch);
+    CodesStat *stats = reinterpret_cast<CodesStat *>(scratch + room.tab);
+    float *sums = reinterpret_cast<float *>(scratch + room.tab + room.stats);
+    const int tiles = (a.rows.B * ((a.R + RB - 1) / RB) * RB + 15) / 16, groups = a.G * ((a.M * a.K + 63) / 64);
+    const dim3 grid((unsigned)groups, (unsigned)std::max(1, std::min(tiles, (4 * cus + groups - 1) / groups)));
+    auto tables = a.D <= 64 ? &k_attend_tables<T, RB, 4> : a.D <= 128 ? &k_attend_tables<T, RB, 8> : &k_attend_tables<T, RB, 16>;
+    hipLaunchKernelGGL(tables, grid, dim3(kTableThreads), 0, stream, a, tiles, tab);
+    TRY(hipGetLastError());
+    const int mw = a.M <= 8 ? 2 : a.M <= 16 ? 4 : 8;
+#define CODES(WIDE, MW) TRY((launch_codes<RB, WIDE, MW>(a, plan, splits, tab, stats, sums, raised, stream)))
+    if constexpr (RB > 1) {
+        if (!plan.wide) {
+            if (mw == 2) CODES(false, 2);
+            else if (mw == 4) CODES(false, 4);
+            else CODES(false, 8);
+        }
+    }
+    if (plan.wide) {
+        if (mw == 2) CODES(true, 2);
+        else if (mw == 4) CODES(true, 4);
+        else CODES(true, 8);
+    }
+#undef CODES
+    const int slices = (a.D + 15) / 16;
+    hipLaunchKernelGGL((k_attend_out<T, RB>), dim3((unsigned)((tiles * a.G + 7) / 8 * 8 * slices)), dim3(kOutThreads), 0, stream, a, splits, tiles, (const CodesStat *)stats, (const float *)sums);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_attend(const AttendArgs &a, int type, int cus, char *scratch, uint64_t *raised, hipStream_t stream)
+{
+    const CodesPlan plan = plan_of(a, type);
+    switch (plan.RB) {
+    case 1: return launch_through_tables<T, 1>(a, plan, cus, scratch, raised, stream);
+    case 2: return launch_through_tables<T, 2>(a, plan, cus, scratch, raised, stream);
+    case 4: return launch_through_tables<T, 4>(a, plan, cus, scratch, raised, stream);
+    }
     const int splits = direct_splits(a, cus);
     switch (heads_at_once(a.R)) {
     case 1: return launch_direct<T, 1>(a, splits, scratch, stream);
@@ -142,12 +211,18 @@ size_t extend_room(const PageArgs &a) { return (size_t)std::min<int64_t>(a.n_pag
 
 }  // namespace
 
-size_t attend_scratch(const AttendArgs &a, int cus)
+size_t attend_scratch(const AttendArgs &a, int type, int cus)
 {
     size_t most = 0;
     for (int n : {attend_round(a), a.rows.B % attend_round(a)}) {   // whole rounds, and the last one
         if (n == 0) continue;
         const AttendArgs r = round_of(a, 0, n, 0);
+        const CodesPlan plan = plan_of(r, type);
+        if (plan.RB) {
+            const CodesRoom room = codes_room(r, plan, codes_splits(r, plan.RB, cus));
+            most = std::max(most, room.tab + room.stats + room.sums);
+            continue;
+        }
         const int RB = heads_at_once(r.R);
         const int64_t jobs = direct_jobs(r, direct_splits(r, cus));
         most = std::max(most, up(sizeof(PartStat) * jobs * RB) + up(sizeof(float) * jobs * RB * r.D));
@@ -160,8 +235,8 @@ hipError_t attend_launch(const AttendArgs &a, int type, int cus, char *scratch, 
     const int step = attend_round(a);
     for (int b0 = 0; b0 < a.rows.B; b0 += step) {
         const AttendArgs r = round_of(a, b0, std::min(step, a.rows.B - b0), type == kRowF32 ? 4 : 2);
-        TRY(type == kRowF32 ? launch_attend<F32>(r, cus, scratch, raised, stream) : type == kRowF16 ? launch_attend<F16>(r, cus, scratch, raised, stream)
-                                                                                                  : launch_attend<Bf16>(r, cus, scratch, raised, stream));
+        TRY(type == kRowF32 ? launch_attend<F32>(r, type, cus, scratch, raised, stream) : type == kRowF16 ? launch_attend<F16>(r, type, cus, scratch, raised, stream)
+                                                                                                  : launch_attend<Bf16>(r, type, cus, scratch, raised, stream));
     }
     return hipSuccess;
 }

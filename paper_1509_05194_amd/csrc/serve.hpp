@@ -29,7 +29,7 @@ struct AttendArgs {                                 // hclae_cache_attend
     float *lse;                                     // [B][G R] or null
 };
 // Bytes of scratch that the call needs.
-size_t attend_scratch(const AttendArgs &a, int cus);
+size_t attend_scratch(const AttendArgs &a, int type, int cus);
 // raised: the kernels whose limit of LDS this ctx has raised, a bit each.
 hipError_t attend_launch(const AttendArgs &a, int type, int cus, char *scratch, uint64_t *raised, hipStream_t stream);
 
