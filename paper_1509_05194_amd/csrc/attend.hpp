@@ -2,7 +2,7 @@
 //   s_t = factor g_t q . (sum_m C[h][m][k_m(t)]),  p = softmax(s),  out = sum_t p_t g'_t sum_m C[G + h][m][v_m(t)]
 // Scores are kept times log2(e) and exponentials taken to the base 2; softmax statistics, weights and sums are in 32 bits or more.
 //   k_attend_rows, k_attend_join   rows decoded as they are needed: any shape, and few rows
-//   k_attend_tables, k_attend_codes, k_attend_out   many rows, never decoded: q . C[h][m][k] is tabulated once for all codewords, a row's score is
+//   k_attend_tables, k_attend_codes, k_attend_fold, k_attend_out   many rows, never decoded: q . C[h][m][k] is tabulated once for all codewords, a row's score is
 //       the sum of M entries; the weights of the rows are summed by the codes of their values, and these sums meet the codewords at the end.
 //       A row costs M reads and M adds a query head in place of M D, whatever D is.
 #pragma once
@@ -35,25 +35,32 @@ struct SeqRows {
         if (end > begin) count = picks ? (int64_t)a.n_picked * page : end - begin;
     }
     __host__ __device__ constexpr unsigned page_of(unsigned x) const { return (unsigned)((uint64_t)x * mul >> (31 + shift)); }
-    // i in [0, count)
-    __host__ __device__ constexpr int64_t slot(unsigned i) const
+    // i in [0, count): the page and where in it, the page ~0u where the row takes no part
+    __host__ __device__ constexpr unsigned where(unsigned i, unsigned &off) const
     {
-        unsigned j = 0, off = 0;
+        const bool power = page == 1u << shift;
+        unsigned j = 0;
         if (picks) {
-            const unsigned e = page_of(i);
-            off = i - e * page;
+            const unsigned e = power ? i >> shift : page_of(i);
+            off = power ? i & (page - 1u) : i - e * page;
             const int32_t at = picks[e];
-            if (at < 0 || at >= max_pages) return kNoRow;
+            if (at < 0 || at >= max_pages) return ~0u;
             const int64_t t = (int64_t)at * page + off;
-            if (t < begin || t >= end) return kNoRow;
+            if (t < begin || t >= end) return ~0u;
             j = (unsigned)at;
         } else {
             const unsigned t = (unsigned)begin + i;
-            j = page_of(t);
-            off = t - j * page;
+            j = power ? t >> shift : page_of(t);
+            off = power ? t & (page - 1u) : t - j * page;
         }
-        const int32_t q = table[j];
-        return (unsigned)q < named ? (int64_t)((uint64_t)(unsigned)q * page + off) : kNoRow;
+        const unsigned q = (unsigned)table[j];
+        return q < named ? q : ~0u;
+    }
+    __host__ __device__ constexpr int64_t slot(unsigned i) const
+    {
+        unsigned off = 0;
+        const unsigned q = where(i, off);
+        return q != ~0u ? (int64_t)((uint64_t)q * page + off) : kNoRow;
     }
 };
 
@@ -239,7 +246,12 @@ __global__ __launch_bounds__(kWave) void k_attend_join(const AttendArgs a, int s
 
 // ---- from tables --------------------------------------------------------------------------------
 
-constexpr int kCodesThreads = 1024, kCodesRows = 2, kWindow = kCodesThreads * kCodesRows, kCodesWaves = kCodesThreads / kWave;
+#ifndef ATT_T
+#define ATT_T 512
+#define ATT_R 4
+#define ATT_O 4
+#endif
+constexpr int kCodesThreads = ATT_T, kCodesRows = ATT_R, kWindow = kCodesThreads * kCodesRows, kCodesWaves = kCodesThreads / kWave;
 constexpr int kCodesMaxM = 32, kCodesSplits = 64;
 constexpr int kCodesLds = 152 * 1024;               // tables and sums; the rest is for what the kernel declares
 constexpr int kWideBits = 40, kPairBits = 19;       // steps of a fixed-point weight, as powers of two below the largest of its window
@@ -265,8 +277,8 @@ __host__ __device__ constexpr CodesPlan codes_plan(int R, int M, int K, bool wid
 // Words a thread looks after, for code rows of up to MW words.
 __host__ __device__ constexpr int codes_words(int RB, bool wide, int MW)
 {
-    const int each = wide ? RB : RB / 2, most = (kCodesLds / (wide ? 12 : 16) + kCodesThreads - 1) / kCodesThreads;
-    return MW * each < most ? MW * each : most;
+    const int all = MW * 4 * 256 * (wide ? RB : RB / 2), most = kCodesLds / (wide ? 12 : 16);
+    return ((all < most ? all : most) + kCodesThreads - 1) / kCodesThreads;
 }
 __host__ __device__ constexpr int codes_splits(const AttendArgs &a, int RB, int cus)
 {
@@ -285,88 +297,126 @@ constexpr int kTableThreads = 256;
 
 // tab[b][h][rg][codeword][RB] = factor log2(e) q . c on the fp32 matrix cores.  A wave keeps 16 codewords in registers and takes tiles of 16 queries past
 // them; queries of a head are numbered (b, rg, r).  The 4 x 4 blocks of an instruction take coordinates 16 j + 4 g + e, g the quarter of the wave: a lane so
-// loads four side by side, for both operands alike.
+// loads four side by side, for both operands alike.  Neighbouring lanes hold different rows, which the memory pipe takes one by one: the queries come
+// through LDS, the next tile's on their way.
 template <typename T, int RB, int NJ>
 __global__ __launch_bounds__(kTableThreads) void k_attend_tables(const AttendArgs a, int tiles, float *tab)
 {
-    const int MK = a.M * a.K, RG = (a.R + RB - 1) / RB, groups = (MK + 63) / 64;
+    constexpr int PITCH = 4 * NJ + 1;               // float4 of a row
+    constexpr int PER = (16 * 4 * NJ + kTableThreads - 1) / kTableThreads;
+    __shared__ float4 qs[2][16 * PITCH];
+    const int MK = a.M * a.K, RG = (a.R + RB - 1) / RB, groups = (MK + 63) / 64, d4 = a.D >> 2;
     const int h = blockIdx.x / groups, lane = lane_id(), i16 = lane & 15, g = lane >> 4;
     const int cw = (blockIdx.x - h * groups) * 64 + (threadIdx.x >> 6) * 16 + i16;
+    const int all = a.rows.B * RG * RB;
+    const float f = a.factor * kLog2e;
+    float4 q[PER];
+    auto fetch = [&](int tile) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int i = threadIdx.x + j * kTableThreads, row = i / (4 * NJ), p = i - row * (4 * NJ), n = tile * 16 + row, u = n / RB, b = u / RG, hq = (u - b * RG) * RB + (n - u * RB);
+            q[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (row < 16 && n < all && hq < a.R && p < d4) q[j] = T::load(a.Q, (int64_t)b * a.q_row + (int64_t)(h * a.R + hq) * a.q_head + 4 * p);
+        }
+    };
+    auto keep = [&](int to) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int i = threadIdx.x + j * kTableThreads, row = i / (4 * NJ), p = i - row * (4 * NJ);
+            if (row < 16) qs[to][row * PITCH + p] = make_float4(q[j].x * f, q[j].y * f, q[j].z * f, q[j].w * f);
+        }
+    };
+    int tile = blockIdx.y;
+    if (tile < tiles) fetch(tile);
     const float *C = a.C + ((size_t)h * MK + min(cw, MK - 1)) * a.D + 4 * g;
     float4 c[NJ];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) c[j] = 16 * j + 4 * g < a.D ? *reinterpret_cast<const float4 *>(C + 16 * j) : make_float4(0.f, 0.f, 0.f, 0.f);
-    const int all = a.rows.B * RG * RB;
-    const float f = a.factor * kLog2e;
-    for (int tile = blockIdx.y; tile < tiles; tile += gridDim.y) {
-        const int n = tile * 16 + i16, u = n / RB, b = u / RG, hq = (u - b * RG) * RB + (n - u * RB);
-        const bool there = n < all && hq < a.R;
-        float4 q[NJ];
-#pragma unroll
-        for (int j = 0; j < NJ; ++j)
-            q[j] = there && 16 * j + 4 * g < a.D ? T::load(a.Q, (int64_t)b * a.q_row + (int64_t)(h * a.R + hq) * a.q_head + 16 * j + 4 * g) : make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int turn = 0; tile < tiles; turn ^= 1) {
+        keep(turn);
+        const int next = tile + gridDim.y;
+        if (next < tiles) fetch(next);
+        __syncthreads();                            // the other half is free again: all have passed the barrier before this one since reading it
         floatx4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
-            s = __builtin_amdgcn_mfma_f32_16x16x4f32(q[j].x, c[j].x, s, 0, 0, 0);
-            s = __builtin_amdgcn_mfma_f32_16x16x4f32(q[j].y, c[j].y, s, 0, 0, 0);
-            s = __builtin_amdgcn_mfma_f32_16x16x4f32(q[j].z, c[j].z, s, 0, 0, 0);
-            s = __builtin_amdgcn_mfma_f32_16x16x4f32(q[j].w, c[j].w, s, 0, 0, 0);
+            const float4 v = qs[turn][i16 * PITCH + 4 * j + g];
+            s = __builtin_amdgcn_mfma_f32_16x16x4f32(v.x, c[j].x, s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_16x16x4f32(v.y, c[j].y, s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_16x16x4f32(v.z, c[j].z, s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_16x16x4f32(v.w, c[j].w, s, 0, 0, 0);
         }
-        if (cw >= MK) continue;
+        if (cw < MK)
 #pragma unroll
-        for (int e = 0; e < 4; e += RB) {           // queries tile * 16 + 4 g + e of this lane's codeword
-            const int m = tile * 16 + 4 * g + e, v = m / RB, bb = v / RG;
-            if (m >= all) break;
-            float *to = tab + ((((int64_t)bb * a.G + h) * RG + (v - bb * RG)) * MK + cw) * RB;
-            if (RB == 4) *reinterpret_cast<float4 *>(to) = make_float4(s[0] * f, s[1] * f, s[2] * f, s[3] * f);
-            else if (RB == 2) *reinterpret_cast<float2 *>(to) = make_float2(s[e] * f, s[e + 1] * f);
-            else *to = s[e] * f;
-        }
+            for (int e = 0; e < 4; e += RB) {       // queries tile * 16 + 4 g + e of this lane's codeword
+                const int m = tile * 16 + 4 * g + e, v = m / RB, bb = v / RG;
+                if (m >= all) break;
+                float *to = tab + ((((int64_t)bb * a.G + h) * RG + (v - bb * RG)) * MK + cw) * RB;
+                if (RB == 4) *reinterpret_cast<float4 *>(to) = make_float4(s[0], s[1], s[2], s[3]);
+                else if (RB == 2) *reinterpret_cast<float2 *>(to) = make_float2(s[e], s[e + 1]);
+                else *to = s[e];
+            }
+        tile = next;
     }
 }
 
-// The largest of v over the wave, in every lane (NaN are passed over).
-__device__ __forceinline__ float wave_max(float v)
+// Floats as whole numbers in the same order, and back (no NaN); the largest over the first `1 << STEPS` lanes, in every lane.
+__device__ __forceinline__ int float_key(float x)
 {
-    auto from = [](float x, auto ctrl, auto rows) {
-        return __int_as_float(__builtin_amdgcn_update_dpp((int)0xff800000, __float_as_int(x), decltype(ctrl)::value, decltype(rows)::value, 0xf, false));
-    };
-    v = fmaxf(v, from(v, std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xf>()));   // row_shr:1
-    v = fmaxf(v, from(v, std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xf>()));
-    v = fmaxf(v, from(v, std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xf>()));
-    v = fmaxf(v, from(v, std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xf>()));
-    v = fmaxf(v, from(v, std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>()));   // row_bcast:15
-    v = fmaxf(v, from(v, std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>()));   // row_bcast:31
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), kWave - 1));
+    const int i = __float_as_int(x);
+    return i ^ (int)((unsigned)(i >> 31) >> 1);
+}
+template <int STEPS>
+__device__ __forceinline__ float key_max(int v)
+{
+    const int low = (int)0x80000000;
+    v = max(v, __builtin_amdgcn_update_dpp(low, v, 0x111, 0xf, 0xf, false));   // row_shr:1
+    v = max(v, __builtin_amdgcn_update_dpp(low, v, 0x112, 0xf, 0xf, false));   // row_shr:2
+    v = max(v, __builtin_amdgcn_update_dpp(low, v, 0x114, 0xf, 0xf, false));   // row_shr:4
+    v = max(v, __builtin_amdgcn_update_dpp(low, v, 0x118, 0xf, 0xf, false));   // row_shr:8
+    if (STEPS == 6) {
+        v = max(v, __builtin_amdgcn_update_dpp(low, v, 0x142, 0xa, 0xf, false));   // row_bcast:15 into rows 1 and 3
+        v = max(v, __builtin_amdgcn_update_dpp(low, v, 0x143, 0xc, 0xf, false));   // row_bcast:31 into rows 2 and 3
+    }
+    const int i = __builtin_amdgcn_readlane(v, STEPS == 6 ? kWave - 1 : 15);
+    return __int_as_float(i ^ (int)((unsigned)(i >> 31) >> 1));
 }
 
 struct CodesStat {
     float top, sum, bad, unused;                    // bad: NaN where a value that takes part has no finite scale, else 0
 };
 
-template <int RB>
-struct Heads {
-    float v[RB];
+// What the launch knows beside the arguments.
+struct CodesArgs {
+    int splits;
+    bool grouped;                                   // blocks go round the eight XCDs: those that read the same rows to one of them
+    bool words;                                     // every row's codes are whole, aligned words
+    bool small;                                     // offsets within a page fit 32 bits, and its rows 24
+    const float *tab;
+    CodesStat *stats;
+    float *sums;
 };
 
-// A block a part of the rows of a key head and RB of its query heads.  Windows of 2048 rows, two a thread:
-//   scores from the tables in LDS; the largest score and the largest weight |p g'| of the window over the block; weights to fixed point below that weight,
-//   added up by code in LDS; these sums, times what the window's fixed point stands for, to the running sums, which threads keep in registers.
-// Where two query heads share a word, a weight is in steps of 2^-19 of the window's largest, rounded to the step below or above by a fraction that goes round
-// with the row (the golden ratio's multiples), so that many small ones add up to what they are: the error of a sum of n weights is about sqrt(n) / 4
-// steps.  bf16 and fp16 outputs have steps of 2^-8 and 2^-11.  float outputs take 64 bits a query head, steps of 2^-40.
-template <int RB, bool WIDE, int MW>
-__global__ __launch_bounds__(kCodesThreads) void k_attend_codes(const AttendArgs a, int splits, bool grouped, bool words_aligned, const float *tab, CodesStat *stats, float *sums)
+// A block a part of the rows of a key head and RB of its query heads.  Windows of 2048 rows, four a thread:
+//   scores from the tables in LDS; weights p g' to fixed point, added up by code in LDS; these sums, times what a step stands for, to the running sums,
+//   which threads keep in registers.
+// The step is 2^-19 of the largest weight so far where two query heads share a word (2048 weights of 2^19 steps fit), rounded to the step below or above
+// by a fraction that goes round with the row (the golden ratio's multiples), so that many small weights add up to what they are: the error of a sum of n is about
+// sqrt(n) / 4 steps.  bf16 and fp16 outputs have steps of 2^-8 and 2^-11.  float outputs take 64 bits a query head, steps of 2^-40.  A block looks for the largest
+// score and weight of a window only if one of them is beyond what the last ones allow for.
+// FULL: K = 256 and 4 MW dictionaries, whole aligned words: the offsets in LDS are in the instructions.
+template <int RB, bool WIDE, int MW, bool FULL>
+__global__ __launch_bounds__(kCodesThreads, ATT_O) void k_attend_codes(const AttendArgs a, const CodesArgs x)
 {
     extern __shared__ __attribute__((aligned(16))) char codes_lds[];
-    __shared__ float red[kCodesWaves][2 * RB];
-    __shared__ int any_bad;
+    __shared__ float2 red[RB][16];
+    __shared__ int any_bad, grow[2];
     constexpr int P = WIDE ? RB : RB / 2, NW = codes_words(RB, WIDE, MW);
-    const int MK = a.M * a.K, K = a.K, RG = (a.R + RB - 1) / RB, H = 2 * a.G, heads = a.G * RG;
+    constexpr float kRoom = 8.f;                    // a score may be so far above the reference
+    const int M = FULL ? 4 * MW : a.M, K = FULL ? 256 : a.K, MK = M * K, RG = (a.R + RB - 1) / RB, H = 2 * a.G, heads = a.G * RG;
     int64_t u;                                      // part of a sequence
     int hr;                                         // key head and group of its query heads
-    if (grouped) {                                  // blocks go round the eight XCDs: those that read the same rows to one of them
+    if (x.grouped) {
         const int64_t at = blockIdx.x >> 3;
         u = at / heads * 8 + (blockIdx.x & 7);
         hr = (int)(at % heads);
@@ -374,170 +424,193 @@ __global__ __launch_bounds__(kCodesThreads) void k_attend_codes(const AttendArgs
         u = blockIdx.x / heads;
         hr = (int)(blockIdx.x - u * heads);
     }
-    if (u >= (int64_t)a.rows.B * splits) return;
-    const int b = (int)(u / splits), split = (int)(u - (int64_t)b * splits), h = hr / RG;
-    const int64_t seq = (int64_t)b * heads + hr, job = seq * splits + split;
+    if (u >= (int64_t)a.rows.B * x.splits) return;
+    const int b = (int)(u / x.splits), split = (int)(u - (int64_t)b * x.splits), h = hr / RG;
+    const int64_t seq = (int64_t)b * heads + hr, job = seq * x.splits + split;
     const SeqRows rows(a, b, h);
-    const int64_t per = ((rows.count + splits - 1) / splits + 255) / 256 * 256, first = per * split, last = min(rows.count, first + per);
+    const int64_t per = ((rows.count + x.splits - 1) / x.splits + 255) / 256 * 256, first64 = per * split;
     const int lane = lane_id(), wave = threadIdx.x >> 6;
-    if (first >= last) {
-        if (threadIdx.x < RB) stats[job * RB + threadIdx.x] = {-INFINITY, 0.f, 0.f, 0.f};
+    if (first64 >= rows.count) {
+        if (threadIdx.x < RB) x.stats[job * RB + threadIdx.x] = {-INFINITY, 0.f, 0.f, 0.f};
         return;
     }
-    float *lut = reinterpret_cast<float *>(codes_lds);
-    unsigned long long *hist = reinterpret_cast<unsigned long long *>(codes_lds + (size_t)MK * RB * 4);
+    const unsigned first = (unsigned)first64, last = (unsigned)min(rows.count, first64 + per);     // rows are numbered below 2^31
     const int words = MK * P;
+    unsigned long long *hist = reinterpret_cast<unsigned long long *>(codes_lds);
+    float *lut = reinterpret_cast<float *>(codes_lds + (size_t)words * 8);
     {
-        const float *t = tab + seq * MK * RB;
+        const float *t = x.tab + seq * MK * RB;
         for (int i = threadIdx.x; i < MK * RB; i += kCodesThreads) lut[i] = t[i];
         for (int i = threadIdx.x; i < words; i += kCodesThreads) hist[i] = 0;
-        if (threadIdx.x == 0) any_bad = 0;
+        if (threadIdx.x == 0) any_bad = grow[0] = grow[1] = 0;
     }
     // which pair of query heads a word of this thread's is for, two bits each
-    unsigned pairs = 0;
+    uint64_t pairs = 0;
 #pragma unroll
-    for (int j = 0; j < NW; ++j) pairs |= (unsigned)((threadIdx.x + j * kCodesThreads) / K % P) << (2 * j);
+    for (int j = 0; j < NW; ++j) pairs |= (uint64_t)((threadIdx.x + j * kCodesThreads) / K % P) << (2 * j);
     float acc[NW][WIDE ? 1 : 2] = {};
-    Heads<RB> ref, sum;
+    float ref[RB], unit[RB], back[RB], limit[RB], sum[RB];     // reference of the scores, steps in 1 and their size, log2 of the largest weight there may be
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
-        ref.v[r] = -INFINITY;
-        sum.v[r] = 0.f;
+        ref[r] = limit[r] = -INFINITY;
+        unit[r] = back[r] = 1.f;
+        sum[r] = 0.f;
     }
     bool bad = false;
+    const unsigned page_codes = (unsigned)(a.rows.page * H * M), page_scales = (unsigned)(a.rows.page * H);
     __syncthreads();
-    for (int64_t w0 = first; w0 < last; w0 += kWindow) {
+    int turn_of = 0;
+    for (unsigned w0 = first; w0 < last; w0 += kWindow, turn_of ^= 1) {
         bool there[kCodesRows];
-        unsigned vc[kCodesRows][MW];
-        float gv[kCodesRows], s[kCodesRows][RB], top[RB], most[RB];
+        unsigned kc[kCodesRows][MW], vc[kCodesRows][MW];
+        float gk[kCodesRows], gv[kCodesRows], s[kCodesRows][RB];
+#pragma unroll
+        for (int i = 0; i < kCodesRows; ++i) {
+            const unsigned t = w0 + i * kCodesThreads + threadIdx.x;
+            unsigned off = 0, q = ~0u;
+            if (t < last) q = rows.where(t, off);
+            there[i] = q != ~0u;
+            gk[i] = gv[i] = 1.f;
+#pragma unroll
+            for (int j = 0; j < MW; ++j) kc[i][j] = vc[i][j] = 0u;
+            if (!there[i]) continue;
+            const uint64_t at = x.small ? (uint64_t)q * page_codes + __umul24(off, (unsigned)(H * M)) : ((uint64_t)q * (unsigned)a.rows.page + off) * (unsigned)(H * M);
+            const uint64_t ag = x.small ? (uint64_t)q * page_scales + __umul24(off, (unsigned)H) : ((uint64_t)q * (unsigned)a.rows.page + off) * (unsigned)H;
+            const uint8_t *kp = a.codes + at + h * M, *vp = kp + a.G * M;
+            if (FULL) {
+                typedef unsigned row_words __attribute__((ext_vector_type(MW < 4 ? MW : 4), aligned(4)));
+#pragma unroll
+                for (int j = 0; j < MW; j += 4) {
+                    const row_words k4 = *reinterpret_cast<const row_words *>(kp + 4 * j), v4 = *reinterpret_cast<const row_words *>(vp + 4 * j);
+#pragma unroll
+                    for (int e = 0; e < (MW < 4 ? MW : 4); ++e) {
+                        kc[i][j + e] = k4[e];
+                        vc[i][j + e] = v4[e];
+                    }
+                }
+            } else if (x.words) {
+#pragma unroll
+                for (int j = 0; j < MW; ++j)
+                    if (4 * j < M) {
+                        kc[i][j] = reinterpret_cast<const unsigned *>(kp)[j];
+                        vc[i][j] = reinterpret_cast<const unsigned *>(vp)[j];
+                    }
+            } else {
+#pragma unroll
+                for (int m = 0; m < 4 * MW; ++m)
+                    if (m < M) {
+                        kc[i][m >> 2] |= (unsigned)kp[m] << (8 * (m & 3));
+                        vc[i][m >> 2] |= (unsigned)vp[m] << (8 * (m & 3));
+                    }
+            }
+            if (a.scale) {
+                const float *g = a.scale + ag;
+                gk[i] = g[h];
+                gv[i] = g[a.G + h];
+            }
+        }
+        bool beyond = false;
+        float top[RB], most[RB];
 #pragma unroll
         for (int r = 0; r < RB; ++r) top[r] = most[r] = -INFINITY;
 #pragma unroll
         for (int i = 0; i < kCodesRows; ++i) {
-            const int64_t t = w0 + i * kCodesThreads + threadIdx.x;
-            const int64_t at = t < last ? rows.slot((unsigned)t) : kNoRow;
-            there[i] = at >= 0;
-            gv[i] = 0.f;
 #pragma unroll
-            for (int r = 0; r < RB; ++r) s[i][r] = -INFINITY;
-            if (at < 0) continue;
-            unsigned kc[MW];
-            float gk = 1.f;
-            auto fetch = [&](unsigned (&c)[MW], const uint8_t *p) {
-                if (words_aligned) {
-#pragma unroll
-                    for (int j = 0; j < MW; ++j) c[j] = 4 * j < a.M ? reinterpret_cast<const unsigned *>(p)[j] : 0u;
-                } else {
-#pragma unroll
-                    for (int j = 0; j < MW; ++j) {
-                        c[j] = 0u;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (4 * j + e < a.M) c[j] |= (unsigned)p[4 * j + e] << (8 * e);
-                    }
-                }
-                if (K < 256) {
-#pragma unroll
-                    for (int j = 0; j < MW; ++j) {
-                        unsigned o = 0u;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o |= min(c[j] >> (8 * e) & 255u, (unsigned)K - 1u) << (8 * e);
-                        c[j] = o;
-                    }
-                }
-            };
-            const uint8_t *row = a.codes + at * (int64_t)(H * a.M);
-            fetch(kc, row + h * a.M);
-            fetch(vc[i], row + (a.G + h) * a.M);
-            if (a.scale) {
-                const float *g = a.scale + at * H;
-                gk = g[h];
-                gv[i] = g[a.G + h];
-            } else gv[i] = 1.f;
-            bad |= !(fabsf(gv[i]) < INFINITY);
-            float x[RB] = {};
+            for (int r = 0; r < RB; ++r) s[i][r] = 0.f;
+            if (!there[i]) continue;
 #pragma unroll
             for (int m = 0; m < 4 * MW; ++m)
-                if (m < a.M) {
-                    const unsigned k = kc[m >> 2] >> (8 * (m & 3)) & 255u;
-                    const float *e = lut + (m * K + (int)k) * RB;
+                if (m < M) {
+                    unsigned k = kc[i][m >> 2] >> (8 * (m & 3)) & 255u;
+                    if (!FULL) k = min(k, (unsigned)K - 1u);
+                    const float *e = lut + m * K * RB + k * RB;
                     if (RB == 4) {
                         const float4 v = *reinterpret_cast<const float4 *>(e);
-                        x[0] += v.x;
-                        x[1] += v.y;
-                        x[RB - 2] += v.z;
-                        x[RB - 1] += v.w;
+                        s[i][0] += v.x;
+                        s[i][RB > 1 ? 1 : 0] += v.y;
+                        s[i][RB > 2 ? 2 : 0] += v.z;
+                        s[i][RB > 3 ? 3 : 0] += v.w;
                     } else if (RB == 2) {
                         const float2 v = *reinterpret_cast<const float2 *>(e);
-                        x[0] += v.x;
-                        x[RB - 1] += v.y;
-                    } else x[0] += *e;
+                        s[i][0] += v.x;
+                        s[i][RB > 1 ? 1 : 0] += v.y;
+                    } else s[i][0] += *e;
                 }
-            const float lg = log2f(fabsf(gv[i]));
+            bad |= !(fabsf(gv[i]) < INFINITY);
+            const float lg = __builtin_amdgcn_logf(fabsf(gv[i]));
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
-                s[i][r] = x[r] * gk;
+                s[i][r] *= gk[i];
                 top[r] = fmaxf(top[r], s[i][r]);
                 most[r] = fmaxf(most[r], s[i][r] + lg);
             }
         }
-        // the largest of the window, over the block
 #pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            const float x = wave_max(top[r]), y = wave_max(most[r]);
-            if (lane == 0) {
-                red[wave][2 * r] = x;
-                red[wave][2 * r + 1] = y;
+        for (int r = 0; r < RB; ++r) beyond |= top[r] > ref[r] + kRoom || most[r] > limit[r];
+        if (beyond) grow[turn_of] = 1;              // the same value from whoever writes
+        __syncthreads();
+        float fade[RB];
+#pragma unroll
+        for (int r = 0; r < RB; ++r) fade[r] = 1.f;
+        if (grow[turn_of]) {                        // the largest of the window, over the block
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                const float t = key_max<6>(float_key(top[r])), m = key_max<6>(float_key(most[r]));
+                if (lane == 0) red[r][wave] = make_float2(t, m);
+            }
+            __syncthreads();
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                const float2 v = red[r][min(lane, kCodesWaves - 1)];
+                const float t = key_max<4>(float_key(v.x)), m = fmaxf(key_max<4>(float_key(v.y)), limit[r]), now = fmaxf(ref[r], t);
+                fade[r] = ref[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref[r] - now);
+                ref[r] = now;
+                // weights up to 2^e; only zeros: any step
+                const float e = m == -INFINITY ? 0.f : fminf(fmaxf(ceilf(m - now + 0.01f), -100.f), 140.f);
+                const int n = min((WIDE ? kWideBits : kPairBits) - (int)e, 120);
+                limit[r] = m == -INFINITY ? m : now + ((WIDE ? kWideBits : kPairBits) - n) - 0.005f;
+                unit[r] = ldexpf(1.f, n);
+                back[r] = ldexpf(1.f, -n);
+                sum[r] *= fade[r];
             }
         }
-        __syncthreads();
-        float fade[RB], unit[RB], back[RB];
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            const float2 v = lane < kCodesWaves ? *reinterpret_cast<const float2 *>(&red[lane][2 * r]) : make_float2(-INFINITY, -INFINITY);
-            const float x = wave_max(v.x), y = wave_max(v.y), now = fmaxf(ref.v[r], x);
-            fade[r] = ref.v[r] == -INFINITY ? 0.f : exp2f(ref.v[r] - now);
-            ref.v[r] = now;
-            // weights below 2^e; none or only zeros: any step
-            const float e = y == -INFINITY ? 0.f : ceilf(y - now + 0.01f);
-            const int n = (WIDE ? kWideBits : kPairBits) - (int)fminf(fmaxf(e, -80.f), 140.f);
-            unit[r] = ldexpf(1.f, n > 120 ? 120 : n);
-            back[r] = ldexpf(1.f, -(n > 120 ? 120 : n));
-        }
-#pragma unroll
-        for (int r = 0; r < RB; ++r) sum.v[r] *= fade[r];
+        if (threadIdx.x == 0) grow[turn_of ^ 1] = 0;
 #pragma unroll
         for (int i = 0; i < kCodesRows; ++i) {
             if (!there[i]) continue;
-            const float turn = (float)(((unsigned)(w0 + i * kCodesThreads + threadIdx.x) * 0x9E3779B9u) >> 8) * 0x1p-24f;
+            const float turn = (float)(((w0 + i * kCodesThreads + threadIdx.x) * 0x9E3779B9u) >> 8) * 0x1p-24f;
             unsigned long long add[P];
-            long long fixed[RB];
+            long long wide[RB];
+            int fixed[RB];
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
-                const float p = exp2f(s[i][r] - ref.v[r]);
-                sum.v[r] += p;
+                const float p = __builtin_amdgcn_exp2f(s[i][r] - ref[r]);
+                sum[r] += p;
                 const float w = p * gv[i];
                 if (WIDE) {
                     const double d = (double)w * (double)unit[r];
-                    fixed[r] = d == d ? (long long)rint(d) : 0;
+                    wide[r] = d == d ? (long long)rint(d) : 0;
                 } else fixed[r] = (int)floorf(w * unit[r] + turn);
             }
 #pragma unroll
-            for (int q = 0; q < P; ++q)
-                add[q] = WIDE ? (unsigned long long)fixed[q] : ((unsigned long long)fixed[(2 * q + 1) % RB] << 32) + (unsigned long long)fixed[(2 * q) % RB];
+            for (int q = 0; q < P; ++q) {
+                if (WIDE) add[q] = (unsigned long long)wide[q];
+                else add[q] = (unsigned long long)(unsigned)(fixed[(2 * q + 1) % RB] + (fixed[(2 * q) % RB] >> 31)) << 32 | (unsigned)fixed[(2 * q) % RB];
+            }
 #pragma unroll
             for (int m = 0; m < 4 * MW; ++m)
-                if (m < a.M) {
-                    const unsigned k = vc[i][m >> 2] >> (8 * (m & 3)) & 255u;
+                if (m < M) {
+                    unsigned k = vc[i][m >> 2] >> (8 * (m & 3)) & 255u;
+                    if (!FULL) k = min(k, (unsigned)K - 1u);
 #pragma unroll
                     for (int q = 0; q < P; ++q)
-                        __hip_atomic_fetch_add(hist + (m * P + q) * K + (int)k, add[q], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                        __hip_atomic_fetch_add(hist + (m * P + q) * K + k, add[q], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
                 }
         }
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < NW; ++j) {
-            const int i = threadIdx.x + j * kCodesThreads, q = pairs >> (2 * j) & 3;
+            const int i = threadIdx.x + j * kCodesThreads, q = (int)(pairs >> (2 * j) & 3);
             if (i >= words) break;
             const unsigned long long v = hist[i];
             hist[i] = 0;
@@ -551,7 +624,7 @@ __global__ __launch_bounds__(kCodesThreads) void k_attend_codes(const AttendArgs
                     }
                 acc[j][0] = acc[j][0] * f + (float)((double)(long long)v * (double)o);
             } else {
-                const int lo = (int)(unsigned)v, hi = (int)(unsigned)((v - (unsigned long long)(long long)lo) >> 32);
+                const int lo = (int)(unsigned)v, hi = (int)((unsigned)(v >> 32) + ((unsigned)v >> 31));
                 const bool second = RB == 4 && q == 1;
                 acc[j][0] = acc[j][0] * (second ? fade[RB == 4 ? 2 : 0] : fade[0]) + (float)lo * (second ? back[RB == 4 ? 2 : 0] : back[0]);
                 acc[j][WIDE ? 0 : 1] = acc[j][WIDE ? 0 : 1] * (second ? fade[RB - 1] : fade[RB >= 2 ? 1 : 0]) + (float)hi * (second ? back[RB - 1] : back[RB >= 2 ? 1 : 0]);
@@ -559,29 +632,30 @@ __global__ __launch_bounds__(kCodesThreads) void k_attend_codes(const AttendArgs
         }
     }
     if (bad) any_bad = 1;                           // the same value from whoever writes
-    __syncthreads();
     // the exponentials' sums, in a fixed order
+    float *sums16 = reinterpret_cast<float *>(red);
+    __syncthreads();
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
-        float x = sum.v[r];
+        float v = sum[r];
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, kWave);
-        if (lane == 0) red[wave][r] = x;
+        for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
+        if (lane == 0) sums16[r * 16 + wave] = v;
     }
     __syncthreads();
     if (threadIdx.x < RB) {
-        float x = 0.f, t = 0.f;
-        for (int w = 0; w < kCodesWaves; ++w) x += red[w][threadIdx.x];
+        float v = 0.f, t = 0.f;
+        for (int w = 0; w < kCodesWaves; ++w) v += sums16[threadIdx.x * 16 + w];
 #pragma unroll
         for (int r = 0; r < RB; ++r)
-            if ((int)threadIdx.x == r) t = ref.v[r];
-        stats[job * RB + threadIdx.x] = {t, x, any_bad ? NAN : 0.f, 0.f};
+            if ((int)threadIdx.x == r) t = ref[r];
+        x.stats[job * RB + threadIdx.x] = {t, v, any_bad ? NAN : 0.f, 0.f};
     }
-    const int64_t row = sums_row(a.M, K);
-    float *to = sums + job * RB * row;
+    const int64_t row = sums_row(M, K);
+    float *to = x.sums + job * RB * row;
 #pragma unroll
     for (int j = 0; j < NW; ++j) {
-        const int i = threadIdx.x + j * kCodesThreads, q = pairs >> (2 * j) & 3;
+        const int i = threadIdx.x + j * kCodesThreads, q = (int)(pairs >> (2 * j) & 3);
         if (i >= words) break;
         const int e = i / K, mk = e / P * K + (i - e * K);
         if (WIDE) to[q * row + mk] = acc[j][0];
@@ -593,80 +667,151 @@ __global__ __launch_bounds__(kCodesThreads) void k_attend_codes(const AttendArgs
     if (threadIdx.x < RB * (int)(row - MK)) to[threadIdx.x / (int)(row - MK) * row + MK + threadIdx.x % (int)(row - MK)] = 0.f;
 }
 
-constexpr int kOutThreads = 512, kOutWaves = kOutThreads / kWave;
+constexpr int kFoldThreads = 256, kFoldFrom = 5;   // parts from which they are added up by a kernel of their own
 
-// out = sum over the parts and codewords of the sums by code, times the codewords, over the exponentials' sum: a block 16 query heads and 16 coordinates, its waves
-// a share of the codewords each, on the fp32 matrix cores.
-template <typename T, int RB>
-__global__ __launch_bounds__(kOutThreads) void k_attend_out(const AttendArgs a, int splits, int tiles, const CodesStat *stats, const float *sums)
+// What the parts of a query head amount to: their common reference, its sum, NaN where a value is; f: what each counts.  By one wave.
+__device__ __forceinline__ CodesStat join_parts(const CodesStat *st, int64_t stride, int splits, float *f)
 {
-    __shared__ float part[16][kCodesSplits], out[kOutWaves][16][17];
-    const int RG = (a.R + RB - 1) / RB, MK = a.M * a.K, slices = (a.D + 15) / 16, all = a.rows.B * RG * RB;
-    const int at = blockIdx.x >> 3, th = at / slices * 8 + (blockIdx.x & 7), slice = at % slices;    // slices of a tile on one XCD
-    if (th >= tiles * a.G) return;
-    const int tile = th / a.G, h = th - tile * a.G, lane = lane_id(), wave = threadIdx.x >> 6, i16 = lane & 15, g = lane >> 4;
-    auto job_of = [&](int n) {                      // its first part
+    static_assert(kCodesSplits <= kWave, "a part a lane");
+    const int lane = lane_id();
+    CodesStat x = {-INFINITY, 0.f, 0.f, 0.f};
+    if (lane < splits) x = st[lane * stride];
+    float top = x.top, bad = x.bad;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        top = fmaxf(top, __shfl_xor(top, o, kWave));
+        bad += __shfl_xor(bad, o, kWave);
+    }
+    const float e = x.sum != 0.f ? __builtin_amdgcn_exp2f(x.top - top) : 0.f;       // a part without rows has no sums
+    float sum = x.sum != 0.f ? e * x.sum : 0.f;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kWave);
+    if (lane < splits) f[lane] = e;
+    return {top, sum, bad, 0.f};
+}
+
+// The parts' sums by code added up, a block 1024 of a query head's; they take the place of the first part's.
+template <int RB>
+__global__ __launch_bounds__(kFoldThreads) void k_attend_fold(const AttendArgs a, int splits, const CodesStat *stats, float *sums, CodesStat *joined)
+{
+    __shared__ float f[kCodesSplits];
+    const int64_t n = blockIdx.x, seq = n / RB, row = sums_row(a.M, a.K);
+    const int r = (int)(n - seq * RB);
+    if (threadIdx.x < kWave) {
+        const CodesStat x = join_parts(stats + seq * splits * RB + r, RB, splits, f);
+        if (threadIdx.x == 0 && blockIdx.y == 0) joined[n] = x;
+    }
+    __syncthreads();
+    const int64_t i = (int64_t)(blockIdx.y * kFoldThreads + threadIdx.x) * 4;
+    if (i >= row) return;
+    float *to = sums + (seq * splits * RB + r) * row + i;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s0 = 0; s0 < splits; s0 += 8) {
+        float4 w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = *reinterpret_cast<const float4 *>(to + (int64_t)min(s0 + j, splits - 1) * RB * row);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float e = s0 + j < splits ? f[s0 + j] : 0.f;
+            if (e != 0.f) v = make_float4(v.x + e * w[j].x, v.y + e * w[j].y, v.z + e * w[j].z, v.w + e * w[j].w);
+        }
+    }
+    *reinterpret_cast<float4 *>(to) = v;
+}
+
+constexpr int kOutThreads = 512, kOutWaves = kOutThreads / kWave, kOutChunk = 128, kOutPitch = kOutChunk + 4;
+__host__ __device__ constexpr int out_lds(int CW) { return kOutWaves * 16 * kOutPitch * 4 > kOutWaves * 16 * (16 * CW + 1) * 4 ? kOutWaves * 16 * kOutPitch * 4 : kOutWaves * 16 * (16 * CW + 1) * 4; }
+
+// out = the sums by code times the codewords, over the exponentials' sum, on the fp32 matrix cores: a block 16 query heads and 16 CW coordinates (a lane CW
+// side by side), its waves every eighth 128 codewords each.  A wave lays its 128 sums of 16 query heads out in LDS of its own, the parts added up on the way.
+// Blocks of one XCD (they go round the eight) have neighbouring numbers, which is the same head most often: its codewords stay in that L2.
+// span: parts between one sequence's sums and the next; splits: parts to add up, the first of those.
+template <typename T, int RB, int CW>
+__global__ __launch_bounds__(kOutThreads) void k_attend_out(const AttendArgs a, int splits, int span, int tiles, const CodesStat *stats, const float *sums)
+{
+    extern __shared__ __attribute__((aligned(16))) float out_room[];
+    __shared__ float part[16][kCodesSplits];
+    const int RG = (a.R + RB - 1) / RB, MK = a.M * a.K, slices = (a.D + 16 * CW - 1) / (16 * CW), all = a.rows.B * RG * RB;
+    const int total = tiles * a.G * slices, per_xcd = (total + 7) / 8, job = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= per_xcd || job >= total) return;
+    const int h = job / (tiles * slices), rest = job - h * tiles * slices, tile = rest / slices, slice = rest - tile * slices;
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i16 = lane & 15, g = lane >> 4;
+    auto seq_of = [&](int n) {
         const int u = n / RB, b = u / RG;
-        return (((int64_t)b * a.G + h) * RG + (u - b * RG)) * splits;
+        return ((int64_t)b * a.G + h) * RG + (u - b * RG);
     };
-    // what a part counts: four lanes... one thread a query head
-    if (threadIdx.x < 16) {
-        const int n = tile * 16 + (int)threadIdx.x, u = n / RB, b = u / RG, hq = (u - b * RG) * RB + n % RB;
-        const bool there = n < all && hq < a.R;
-        const CodesStat *st = there ? stats + job_of(n) * RB + n % RB : stats;
-        float top = -INFINITY, sum = 0.f, bad = 0.f;
-        if (there) {
-            for (int i = 0; i < splits; ++i) top = fmaxf(top, st[(int64_t)i * RB].top);
-            for (int i = 0; i < splits; ++i) {
-                const CodesStat x = st[(int64_t)i * RB];
-                bad += x.bad;
-                float f = 0.f;
-                if (x.sum != 0.f) {
-                    f = exp2f(x.top - top);
-                    sum += f * x.sum;
-                }
-                part[threadIdx.x][i] = f;
-            }
-        } else
-            for (int i = 0; i < splits; ++i) part[threadIdx.x][i] = 0.f;
-        if (sum != 0.f)
-            for (int i = 0; i < splits; ++i) part[threadIdx.x][i] = part[threadIdx.x][i] / sum + bad;
-        if (there && slice == 0 && a.lse) a.lse[(int64_t)b * a.G * a.R + h * a.R + hq] = sum != 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+#pragma unroll
+    for (int j = 0; j < 16 / kOutWaves; ++j) {      // what a part counts, a wave two query heads
+        const int i = wave * (16 / kOutWaves) + j, n = tile * 16 + i, u = n / RB, b = u / RG, hq = (u - b * RG) * RB + (n - u * RB);
+        if (n < all && hq < a.R) {
+            const CodesStat x = join_parts(stats + seq_of(n) * splits * RB + n % RB, RB, splits, part[i]);
+            if (lane < splits) part[i][lane] = x.sum != 0.f ? part[i][lane] / x.sum + x.bad : 0.f;
+            if (slice == 0 && lane == 0 && a.lse) a.lse[(int64_t)b * a.G * a.R + h * a.R + hq] = x.sum != 0.f ? (x.top + log2f(x.sum)) * kLn2 : -INFINITY;
+        } else if (lane < splits) part[i][lane] = 0.f;
     }
     __syncthreads();
-    const int n = tile * 16 + i16, d = slice * 16 + i16;
     const int64_t row = sums_row(a.M, a.K);
-    const float *W = sums + (n < all ? job_of(n) * RB + n % RB : 0) * row + 4 * g;
-    const float *C = a.C + (size_t)(a.G + h) * MK * a.D + min(d, a.D - 1);
-    floatx4 s = {0.f, 0.f, 0.f, 0.f};
-    for (int j = 16 * wave; j < MK; j += 16 * kOutWaves) {
-        float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (j + 4 * g < MK)
-            for (int i = 0; i < splits; ++i) {
-                const float f = part[i16][i];
-                if (f == 0.f) continue;             // a part without rows has no sums
-                const float4 v = *reinterpret_cast<const float4 *>(W + (int64_t)i * RB * row + j);
-                w = make_float4(w.x + f * v.x, w.y + f * v.y, w.z + f * v.z, w.w + f * v.w);
+    const int d = (slice * 16 + i16) * CW;
+    const float *C = a.C + (size_t)(a.G + h) * MK * a.D + min(d, a.D - CW);
+    float *mine = out_room + wave * 16 * kOutPitch;
+    floatx4 s[CW];
+#pragma unroll
+    for (int c = 0; c < CW; ++c) s[c] = (floatx4){0.f, 0.f, 0.f, 0.f};
+    for (int k0 = wave * kOutChunk; k0 < MK; k0 += kOutWaves * kOutChunk) {
+        // two rows at a time, a half of the wave each
+        float4 w[8];
+        const int at = k0 + 4 * (lane & 31);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = 2 * j + (lane >> 5), n = min(tile * 16 + i, all - 1);
+            const float *from = sums + (seq_of(n) * span * RB + n % RB) * row + min((int64_t)at, row - 4);
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int p = 0; p < splits; ++p) {
+                const float f = part[i][p];
+                const float4 x = *reinterpret_cast<const float4 *>(from + (int64_t)p * RB * row);
+                if (f != 0.f) v = make_float4(v.x + f * x.x, v.y + f * x.y, v.z + f * x.z, v.w + f * x.w);
             }
-        float c[4];
+            w[j] = at < row ? v : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-        for (int e = 0; e < 4; ++e) c[e] = C[(size_t)min(j + 4 * g + e, MK - 1) * a.D];
-        s = __builtin_amdgcn_mfma_f32_16x16x4f32(w.x, c[0], s, 0, 0, 0);
-        s = __builtin_amdgcn_mfma_f32_16x16x4f32(w.y, c[1], s, 0, 0, 0);
-        s = __builtin_amdgcn_mfma_f32_16x16x4f32(w.z, c[2], s, 0, 0, 0);
-        s = __builtin_amdgcn_mfma_f32_16x16x4f32(w.w, c[3], s, 0, 0, 0);
+        for (int j = 0; j < 8; ++j) *reinterpret_cast<float4 *>(mine + (2 * j + (lane >> 5)) * kOutPitch + 4 * (lane & 31)) = w[j];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll 4
+        for (int j = 0; j < kOutChunk; j += 16) {
+            const float4 v = *reinterpret_cast<const float4 *>(mine + i16 * kOutPitch + j + 4 * g);
+            const float e[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float *from = C + (size_t)min(k0 + j + 4 * g + k, MK - 1) * a.D;
+                float c[CW];
+                if (CW == 4) {
+                    const float4 q = *reinterpret_cast<const float4 *>(from);
+                    c[0] = q.x;
+                    c[CW > 1 ? 1 : 0] = q.y;
+                    c[CW > 2 ? 2 : 0] = q.z;
+                    c[CW > 3 ? 3 : 0] = q.w;
+                } else c[0] = *from;
+#pragma unroll
+                for (int q = 0; q < CW; ++q) s[q] = __builtin_amdgcn_mfma_f32_16x16x4f32(e[k], c[q], s[q], 0, 0, 0);
+            }
+        }
     }
+    __syncthreads();                                // the sums' places are free
+    constexpr int OP = 16 * CW + 1;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) out[wave][4 * g + e][i16] = s[e];
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int c = 0; c < CW; ++c) out_room[(wave * 16 + 4 * g + e) * OP + i16 * CW + c] = s[c][e];
     __syncthreads();
-    if (threadIdx.x < 64) {
-        const int i = threadIdx.x >> 2, p = threadIdx.x & 3, m = tile * 16 + i, u = m / RB, b = u / RG, hq = (u - b * RG) * RB + m % RB;
-        if (m < all && hq < a.R && slice * 16 + 4 * p < a.D) {
+    for (int t = threadIdx.x; t < 64 * CW; t += kOutThreads) {
+        const int i = t / (4 * CW), p = t - i * 4 * CW, m = tile * 16 + i, u = m / RB, b = u / RG, hq = (u - b * RG) * RB + (m - u * RB), at = slice * 16 * CW + 4 * p;
+        if (m < all && hq < a.R && at < a.D) {
             float v[4] = {};
             for (int w = 0; w < kOutWaves; ++w)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] += out[w][i][4 * p + e];
-            T::store(a.out, (int64_t)b * a.o_row + (int64_t)(h * a.R + hq) * a.o_head + slice * 16 + 4 * p, make_float4(v[0], v[1], v[2], v[3]));
+                for (int e = 0; e < 4; ++e) v[e] += out_room[(w * 16 + i) * OP + 4 * p + e];
+            T::store(a.out, (int64_t)b * a.o_row + (int64_t)(h * a.R + hq) * a.o_head + at, make_float4(v[0], v[1], v[2], v[3]));
         }
     }
 }

@@ -30,7 +30,7 @@ hipError_t raise_lds(K kern, int bit, uint64_t *raised)
     return hipSuccess;
 }
 
-enum RaisedBit { kRaisedSelect = 0, kRaisedCodes = 1 };         // 15 from kRaisedCodes on
+enum RaisedBit { kRaisedSelect = 0, kRaisedCodes = 1, kRaisedOut = 31 };         // 30 and 18 from the last two on
 
 // ---- attention ----------------------------------------------------------------------------------
 
@@ -80,25 +80,32 @@ CodesPlan plan_of(const AttendArgs &a, int type)
 }
 
 struct CodesRoom {
-    size_t tab, stats, sums;
+    size_t tab, stats, sums, joined;
 };
 CodesRoom codes_room(const AttendArgs &a, const CodesPlan &plan, int splits)
 {
     const int64_t seqs = (int64_t)a.rows.B * a.G * ((a.R + plan.RB - 1) / plan.RB), rows = seqs * splits * plan.RB;
-    return {up(sizeof(float) * seqs * plan.RB * a.M * a.K), up(sizeof(CodesStat) * rows), up(sizeof(float) * rows * sums_row(a.M, a.K))};
+    return {up(sizeof(float) * seqs * plan.RB * a.M * a.K), up(sizeof(CodesStat) * rows), up(sizeof(float) * rows * sums_row(a.M, a.K)), up(sizeof(CodesStat) * seqs * plan.RB)};
 }
 
+template <int RB, bool WIDE, int MW, bool FULL>
+hipError_t launch_codes_as(const AttendArgs &a, const CodesPlan &plan, const CodesArgs &x, uint64_t *raised, hipStream_t stream)
+{
+    constexpr int bit = kRaisedCodes + (FULL ? 15 : 0) + (MW == 2 ? 0 : MW == 4 ? 5 : 10) + (RB == 1 ? 0 : RB == 2 ? 1 : 3) + (RB > 1 && WIDE ? 1 : 0);
+    auto kern = &k_attend_codes<RB, WIDE, MW, FULL>;
+    TRY(raise_lds(kern, bit, raised));
+    const int64_t heads = (int64_t)a.G * ((a.R + RB - 1) / RB), units = (int64_t)a.rows.B * x.splits;
+    hipLaunchKernelGGL(kern, dim3((unsigned)((x.grouped ? (units + 7) / 8 * 8 : units) * heads)), dim3(kCodesThreads), plan.lds, stream, a, x);
+    return hipGetLastError();
+}
 template <int RB, bool WIDE, int MW>
 hipError_t launch_codes(const AttendArgs &a, const CodesPlan &plan, int splits, const float *tab, CodesStat *stats, float *sums, uint64_t *raised, hipStream_t stream)
 {
-    constexpr int bit = kRaisedCodes + (MW == 2 ? 0 : MW == 4 ? 5 : 10) + (RB == 1 ? 0 : RB == 2 ? 1 : 3) + (RB > 1 && WIDE ? 1 : 0);
-    auto kern = &k_attend_codes<RB, WIDE, MW>;
-    TRY(raise_lds(kern, bit, raised));
-    const int64_t heads = (int64_t)a.G * ((a.R + RB - 1) / RB), units = (int64_t)a.rows.B * splits;
-    const bool grouped = units >= 32, words = a.M % 4 == 0 && reinterpret_cast<uintptr_t>(a.codes) % 4 == 0;
-    const int64_t blocks = (grouped ? (units + 7) / 8 * 8 : units) * heads;
-    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(kCodesThreads), plan.lds, stream, a, splits, grouped, words, tab, stats, sums);
-    return hipGetLastError();
+    const int64_t row = 2ll * a.G * a.M;
+    const CodesArgs x = {splits, (int64_t)a.rows.B * splits >= 32, a.M % 4 == 0 && reinterpret_cast<uintptr_t>(a.codes) % 4 == 0,
+                         a.rows.page < 1 << 24 && a.rows.page * row < (int64_t)1 << 32, tab, stats, sums};
+    if (MW <= 4 && a.K == 256 && a.M == 4 * MW && x.words) return launch_codes_as<RB, WIDE, MW <= 4 ? MW : 4, true>(a, plan, x, raised, stream);
+    return launch_codes_as<RB, WIDE, MW, false>(a, plan, x, raised, stream);
 }
 
 template <typename T, int RB>
@@ -129,8 +136,23 @@ hipError_t launch_through_tables(const AttendArgs &a, const CodesPlan &plan, int
         else CODES(true, 8);
     }
 #undef CODES
-    const int slices = (a.D + 15) / 16;
-    hipLaunchKernelGGL((k_attend_out<T, RB>), dim3((unsigned)((tiles * a.G + 7) / 8 * 8 * slices)), dim3(kOutThreads), 0, stream, a, splits, tiles, (const CodesStat *)stats, (const float *)sums);
+    int parts = splits;
+    if (splits >= kFoldFrom) {                      // the first parts' sums are those of all then
+        const int64_t rows = (int64_t)a.rows.B * a.G * ((a.R + RB - 1) / RB) * RB;
+        CodesStat *joined = reinterpret_cast<CodesStat *>(scratch + room.tab + room.stats + room.sums);
+        hipLaunchKernelGGL(k_attend_fold<RB>, dim3((unsigned)rows, (unsigned)((sums_row(a.M, a.K) / 4 + kFoldThreads - 1) / kFoldThreads)), dim3(kFoldThreads), 0, stream, a, splits,
+                           (const CodesStat *)stats, sums, joined);
+        TRY(hipGetLastError());
+        stats = joined;
+        parts = 1;
+    }
+    // 64 coordinates a block where that leaves enough of them
+    const bool wide = (int64_t)tiles * a.G * ((a.D + 63) / 64) >= cus / 2;
+    const int slices = (a.D + (wide ? 63 : 15)) / (wide ? 64 : 16);
+    auto out = wide ? &k_attend_out<T, RB, 4> : &k_attend_out<T, RB, 1>;
+    TRY(raise_lds(out, kRaisedOut + (wide ? 1 : 0) + 2 * (RB == 1 ? 0 : RB == 2 ? 1 : 2) + 6 * (T::bytes == 4 ? 0 : __is_same(T, F16) ? 1 : 2), raised));
+    hipLaunchKernelGGL(out, dim3((unsigned)((tiles * a.G * slices + 7) / 8 * 8)), dim3(kOutThreads), (size_t)out_lds(wide ? 4 : 1), stream, a, parts, splits, tiles, (const CodesStat *)stats,
+                       (const float *)sums);
     return hipGetLastError();
 }
 
@@ -220,7 +242,7 @@ size_t attend_scratch(const AttendArgs &a, int type, int cus)
         const CodesPlan plan = plan_of(r, type);
         if (plan.RB) {
             const CodesRoom room = codes_room(r, plan, codes_splits(r, plan.RB, cus));
-            most = std::max(most, room.tab + room.stats + room.sums);
+            most = std::max(most, room.tab + room.stats + room.sums + room.joined);
             continue;
         }
         const int RB = heads_at_once(r.R);
