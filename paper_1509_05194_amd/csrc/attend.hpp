@@ -293,70 +293,105 @@ __host__ __device__ constexpr int64_t sums_row(int M, int K) { return ((int64_t)
 
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
-constexpr int kTableThreads = 256;
-
-// tab[b][h][rg][codeword][RB] = factor log2(e) q . c on the fp32 matrix cores.  A wave keeps 16 codewords in registers and takes tiles of 16 queries past
-// them; queries of a head are numbered (b, rg, r).  The 4 x 4 blocks of an instruction take coordinates 16 j + 4 g + e, g the quarter of the wave: a lane so
-// loads four side by side, for both operands alike.  Neighbouring lanes hold different rows, which the memory pipe takes one by one: the queries come
-// through LDS, the next tile's on their way.
-template <typename T, int RB, int NJ>
-__global__ __launch_bounds__(kTableThreads) void k_attend_tables(const AttendArgs a, int tiles, float *tab)
+// Products of floats on the bf16 matrix cores: a float is the sum of three bf16 numbers, rounded one after the other, up to 2^-27 of it (of two, to 2^-18);
+// a bf16 number is one and a half number two.  Of the products of parts those beyond 2^-24 (2^-16) of the whole are left out: six for two floats of
+// three parts, 96 cycles for 16 x 16 x 32 where the fp32 matrix cores take 256.
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+template <int N>
+__device__ __forceinline__ void split_floats(const float (&x)[8], bf16x8 (&part)[N])
 {
-    constexpr int PITCH = 4 * NJ + 1;               // float4 of a row
-    constexpr int PER = (16 * 4 * NJ + kTableThreads - 1) / kTableThreads;
-    __shared__ float4 qs[2][16 * PITCH];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        float left = x[e];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            part[i][e] = (__bf16)left;
+            if (i + 1 < N) left -= (float)part[i][e];
+        }
+    }
+}
+// s += a b, the small products first; NA parts of a and NB of b.
+template <int NA, int NB>
+__device__ __forceinline__ void mfma_parts(const bf16x8 (&a)[NA], const bf16x8 (&b)[NB], floatx4 &s)
+{
+    constexpr int last = (NA > NB ? NA : NB) - 1;
+#pragma unroll
+    for (int order = last; order >= 0; --order)
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+            if (order - i >= 0 && order - i < NB) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[order - i], s, 0, 0, 0);
+}
+
+constexpr int kTableThreads = 256;
+// Queries that a block keeps in LDS at a time, for rows of 32 NJ coordinates in N parts.
+__host__ __device__ constexpr int table_queries(int N, int NJ) { return N * NJ <= 4 ? 64 : N * NJ <= 12 ? 32 : 16; }
+
+// tab[b][h][rg][codeword][RB] = factor log2(e) q . c.  A wave keeps 16 codewords in registers and takes tiles of 16 queries past them; queries of a head are numbered
+// (b, rg, r).  Of a product's 32 coordinates a lane holds 8 side by side, 8 g .. 8 g + 7 of them in the wave's quarter g, for both operands alike.  Neighbouring
+// lanes hold different rows, which the memory pipe takes one by one: the queries come through LDS.  N: parts of a query.
+template <typename T, int RB, int NJ, int N>
+__global__ __launch_bounds__(kTableThreads) void k_attend_tables(const AttendArgs a, int stages, float *tab)
+{
+    constexpr int PITCH = 32 * NJ + 8, TQ = table_queries(N, NJ);
+    __shared__ __attribute__((aligned(16))) __bf16 qs[N][TQ][PITCH];
     const int MK = a.M * a.K, RG = (a.R + RB - 1) / RB, groups = (MK + 63) / 64, d4 = a.D >> 2;
     const int h = blockIdx.x / groups, lane = lane_id(), i16 = lane & 15, g = lane >> 4;
     const int cw = (blockIdx.x - h * groups) * 64 + (threadIdx.x >> 6) * 16 + i16;
     const int all = a.rows.B * RG * RB;
     const float f = a.factor * kLog2e;
-    float4 q[PER];
-    auto fetch = [&](int tile) {
+    const float *C = a.C + ((size_t)h * MK + min(cw, MK - 1)) * a.D;
+    bf16x8 c[NJ][3];
 #pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            const int i = threadIdx.x + j * kTableThreads, row = i / (4 * NJ), p = i - row * (4 * NJ), n = tile * 16 + row, u = n / RB, b = u / RG, hq = (u - b * RG) * RB + (n - u * RB);
-            q[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (row < 16 && n < all && hq < a.R && p < d4) q[j] = T::load(a.Q, (int64_t)b * a.q_row + (int64_t)(h * a.R + hq) * a.q_head + 4 * p);
-        }
-    };
-    auto keep = [&](int to) {
+    for (int j = 0; j < NJ; ++j) {
+        const int at = 32 * j + 8 * g;              // a row is at least four long, and whole fours
+        const float4 u = *reinterpret_cast<const float4 *>(C + min(at, a.D - 4)), v = *reinterpret_cast<const float4 *>(C + min(at + 4, a.D - 4));
+        const float fu = at < a.D ? 1.f : 0.f, fv = at + 4 < a.D ? 1.f : 0.f;
+        const float w[8] = {u.x * fu, u.y * fu, u.z * fu, u.w * fu, v.x * fv, v.y * fv, v.z * fv, v.w * fv};
+        split_floats<3>(w, c[j]);
+    }
+    for (int stage = blockIdx.y; stage < stages; stage += gridDim.y) {
+        for (int i = threadIdx.x; i < TQ * 8 * NJ; i += kTableThreads) {
+            const int row = i / (8 * NJ), p = i - row * (8 * NJ), n = stage * TQ + row, u = n / RB, b = u / RG, hq = (u - b * RG) * RB + (n - u * RB);
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (n < all && hq < a.R && p < d4) v = T::load(a.Q, (int64_t)b * a.q_row + (int64_t)(h * a.R + hq) * a.q_head + 4 * p);
+            float x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            const int i = threadIdx.x + j * kTableThreads, row = i / (4 * NJ), p = i - row * (4 * NJ);
-            if (row < 16) qs[to][row * PITCH + p] = make_float4(q[j].x * f, q[j].y * f, q[j].z * f, q[j].w * f);
-        }
-    };
-    int tile = blockIdx.y;
-    if (tile < tiles) fetch(tile);
-    const float *C = a.C + ((size_t)h * MK + min(cw, MK - 1)) * a.D + 4 * g;
-    float4 c[NJ];
+            for (int k = 0; k < N; ++k) {
+                bf16x4 o;
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) c[j] = 16 * j + 4 * g < a.D ? *reinterpret_cast<const float4 *>(C + 16 * j) : make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int turn = 0; tile < tiles; turn ^= 1) {
-        keep(turn);
-        const int next = tile + gridDim.y;
-        if (next < tiles) fetch(next);
-        __syncthreads();                            // the other half is free again: all have passed the barrier before this one since reading it
-        floatx4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            const float4 v = qs[turn][i16 * PITCH + 4 * j + g];
-            s = __builtin_amdgcn_mfma_f32_16x16x4f32(v.x, c[j].x, s, 0, 0, 0);
-            s = __builtin_amdgcn_mfma_f32_16x16x4f32(v.y, c[j].y, s, 0, 0, 0);
-            s = __builtin_amdgcn_mfma_f32_16x16x4f32(v.z, c[j].z, s, 0, 0, 0);
-            s = __builtin_amdgcn_mfma_f32_16x16x4f32(v.w, c[j].w, s, 0, 0, 0);
-        }
-        if (cw < MK)
-#pragma unroll
-            for (int e = 0; e < 4; e += RB) {       // queries tile * 16 + 4 g + e of this lane's codeword
-                const int m = tile * 16 + 4 * g + e, v = m / RB, bb = v / RG;
-                if (m >= all) break;
-                float *to = tab + ((((int64_t)bb * a.G + h) * RG + (v - bb * RG)) * MK + cw) * RB;
-                if (RB == 4) *reinterpret_cast<float4 *>(to) = make_float4(s[0], s[1], s[2], s[3]);
-                else if (RB == 2) *reinterpret_cast<float2 *>(to) = make_float2(s[e], s[e + 1]);
-                else *to = s[e];
+                for (int e = 0; e < 4; ++e) {
+                    o[e] = (__bf16)x[e];
+                    x[e] -= (float)o[e];
+                }
+                *reinterpret_cast<bf16x4 *>(&qs[k][row][4 * p]) = o;
             }
-        tile = next;
+        }
+        __syncthreads();
+        const int n0 = stage * TQ;
+#pragma unroll 2
+        for (int tile = 0; tile < TQ / 16; ++tile) {
+            if (n0 + 16 * tile >= all) break;
+            floatx4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                bf16x8 q[N];
+#pragma unroll
+                for (int k = 0; k < N; ++k) q[k] = *reinterpret_cast<const bf16x8 *>(&qs[k][16 * tile + i16][32 * j + 8 * g]);
+                mfma_parts<N, 3>(q, c[j], s);
+            }
+            if (cw < MK)
+#pragma unroll
+                for (int e = 0; e < 4; e += RB) {   // queries n0 + 16 tile + 4 g + e of this lane's codeword
+                    const int m = n0 + 16 * tile + 4 * g + e, v = m / RB, bb = v / RG;
+                    if (m >= all) break;
+                    float *to = tab + ((((int64_t)bb * a.G + h) * RG + (v - bb * RG)) * MK + cw) * RB;
+                    if (RB == 4) *reinterpret_cast<float4 *>(to) = make_float4(s[0] * f, s[1] * f, s[2] * f, s[3] * f);
+                    else if (RB == 2) *reinterpret_cast<float2 *>(to) = make_float2(s[e] * f, s[e + 1] * f);
+                    else *to = s[e] * f;
+                }
+        }
+        __syncthreads();
     }
 }
 
@@ -719,15 +754,20 @@ __global__ __launch_bounds__(kFoldThreads) void k_attend_fold(const AttendArgs a
     *reinterpret_cast<float4 *>(to) = v;
 }
 
-constexpr int kOutThreads = 512, kOutWaves = kOutThreads / kWave, kOutChunk = 128, kOutPitch = kOutChunk + 4;
-__host__ __device__ constexpr int out_lds(int CW) { return kOutWaves * 16 * kOutPitch * 4 > kOutWaves * 16 * (16 * CW + 1) * 4 ? kOutWaves * 16 * kOutPitch * 4 : kOutWaves * 16 * (16 * CW + 1) * 4; }
+constexpr int kOutThreads = 512, kOutWaves = kOutThreads / kWave, kOutChunk = 64, kOutPitch = kOutChunk + 8;
+__host__ __device__ constexpr int out_lds(int N, int CW)
+{
+    const int rows = kOutWaves * N * 16 * kOutPitch * 2, sums = kOutWaves * 16 * (16 * CW + 1) * 4;
+    return rows > sums ? rows : sums;
+}
 
-// out = the sums by code times the codewords, over the exponentials' sum, on the fp32 matrix cores: a block 16 query heads and 16 CW coordinates (a lane CW
-// side by side), its waves every eighth 128 codewords each.  A wave lays its 128 sums of 16 query heads out in LDS of its own, the parts added up on the way.
+// out = the sums by code times the codewords, over the exponentials' sum: a block 16 query heads and 16 CW coordinates (a lane CW side by side), its waves
+// every eighth 64 codewords each.  A wave lays the 64 sums of 16 query heads out in LDS of its own, the parts added up on the way.
 // Blocks of one XCD (they go round the eight) have neighbouring numbers, which is the same head most often: its codewords stay in that L2.
+// N: bf16 parts of a sum and a codeword, two for outputs of 16 bits and three for floats.
 // span: parts between one sequence's sums and the next; splits: parts to add up, the first of those.
-template <typename T, int RB, int CW>
-__global__ __launch_bounds__(kOutThreads) void k_attend_out(const AttendArgs a, int splits, int span, int tiles, const CodesStat *stats, const float *sums)
+template <typename T, int RB, int CW, int N>
+__global__ __launch_bounds__(kOutThreads, 4) void k_attend_out(const AttendArgs a, int splits, int span, int tiles, const CodesStat *stats, const float *sums)
 {
     extern __shared__ __attribute__((aligned(16))) float out_room[];
     __shared__ float part[16][kCodesSplits];
@@ -740,6 +780,30 @@ __global__ __launch_bounds__(kOutThreads) void k_attend_out(const AttendArgs a, 
         const int u = n / RB, b = u / RG;
         return ((int64_t)b * a.G + h) * RG + (u - b * RG);
     };
+    const int d = (slice * 16 + i16) * CW;
+    const float *C = a.C + (size_t)(a.G + h) * MK * a.D + min(d, a.D - CW);
+    auto codewords = [&](int k0, float (&c)[8][CW]) {   // k0 + 8 g .. + 7
+        const bool whole = k0 + 32 <= MK;
+        const float *from = C + (size_t)(whole ? k0 + 8 * g : 0) * a.D;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float *at = whole ? from + e * a.D : C + (size_t)min(k0 + 8 * g + e, MK - 1) * a.D;
+            if (CW == 4) {
+                const float4 q = *reinterpret_cast<const float4 *>(at);
+                c[e][0] = q.x;
+                c[e][CW > 1 ? 1 : 0] = q.y;
+                c[e][CW > 2 ? 2 : 0] = q.z;
+                c[e][CW > 3 ? 3 : 0] = q.w;
+            } else c[e][0] = *at;
+        }
+    };
+    const int64_t row = sums_row(a.M, a.K);
+    const float *from[4];                           // a lane's four rows of sums
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int n = min(tile * 16 + 4 * j + g, all - 1);
+        from[j] = sums + (seq_of(n) * span * RB + n % RB) * row;
+    }
 #pragma unroll
     for (int j = 0; j < 16 / kOutWaves; ++j) {      // what a part counts, a wave two query heads
         const int i = wave * (16 / kOutWaves) + j, n = tile * 16 + i, u = n / RB, b = u / RG, hq = (u - b * RG) * RB + (n - u * RB);
@@ -750,59 +814,69 @@ __global__ __launch_bounds__(kOutThreads) void k_attend_out(const AttendArgs a, 
         } else if (lane < splits) part[i][lane] = 0.f;
     }
     __syncthreads();
-    const int64_t row = sums_row(a.M, a.K);
-    const int d = (slice * 16 + i16) * CW;
-    const float *C = a.C + (size_t)(a.G + h) * MK * a.D + min(d, a.D - CW);
-    float *mine = out_room + wave * 16 * kOutPitch;
+    __bf16 *mine = reinterpret_cast<__bf16 *>(out_room) + wave * N * 16 * kOutPitch;
     floatx4 s[CW];
 #pragma unroll
-    for (int c = 0; c < CW; ++c) s[c] = (floatx4){0.f, 0.f, 0.f, 0.f};
+    for (int q = 0; q < CW; ++q) s[q] = (floatx4){0.f, 0.f, 0.f, 0.f};
+    auto products = [&](int j, const float (&c)[8][CW]) {
+        bf16x8 v[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = *reinterpret_cast<const bf16x8 *>(mine + (k * 16 + i16) * kOutPitch + j + 8 * g);
+#pragma unroll
+        for (int q = 0; q < CW; ++q) {
+            float x[8];
+            bf16x8 o[N];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = c[e][q];
+            split_floats<N>(x, o);
+            mfma_parts<N, N>(v, o, s[q]);
+        }
+    };
     for (int k0 = wave * kOutChunk; k0 < MK; k0 += kOutWaves * kOutChunk) {
-        // two rows at a time, a half of the wave each
-        float4 w[8];
-        const int at = k0 + 4 * (lane & 31);
+        float c0[8][CW], c1[8][CW];
+        codewords(k0, c0);
+        // four rows at a time, a quarter of the wave each
+        float4 w[4];
+        const int at = k0 + 4 * i16;
+        const int64_t near = min((int64_t)at, row - 4);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int i = 2 * j + (lane >> 5), n = min(tile * 16 + i, all - 1);
-            const float *from = sums + (seq_of(n) * span * RB + n % RB) * row + min((int64_t)at, row - 4);
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int p = 0; p < splits; ++p) {
-                const float f = part[i][p];
-                const float4 x = *reinterpret_cast<const float4 *>(from + (int64_t)p * RB * row);
-                if (f != 0.f) v = make_float4(v.x + f * x.x, v.y + f * x.y, v.z + f * x.z, v.w + f * x.w);
-            }
-            w[j] = at < row ? v : make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        for (int j = 0; j < 4; ++j) w[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int p = 0; p < splits; ++p) {
+            float4 x[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) *reinterpret_cast<float4 *>(mine + (2 * j + (lane >> 5)) * kOutPitch + 4 * (lane & 31)) = w[j];
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll 4
-        for (int j = 0; j < kOutChunk; j += 16) {
-            const float4 v = *reinterpret_cast<const float4 *>(mine + i16 * kOutPitch + j + 4 * g);
-            const float e[4] = {v.x, v.y, v.z, v.w};
+            for (int j = 0; j < 4; ++j) x[j] = *reinterpret_cast<const float4 *>(from[j] + (int64_t)p * RB * row + near);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float *from = C + (size_t)min(k0 + j + 4 * g + k, MK - 1) * a.D;
-                float c[CW];
-                if (CW == 4) {
-                    const float4 q = *reinterpret_cast<const float4 *>(from);
-                    c[0] = q.x;
-                    c[CW > 1 ? 1 : 0] = q.y;
-                    c[CW > 2 ? 2 : 0] = q.z;
-                    c[CW > 3 ? 3 : 0] = q.w;
-                } else c[0] = *from;
-#pragma unroll
-                for (int q = 0; q < CW; ++q) s[q] = __builtin_amdgcn_mfma_f32_16x16x4f32(e[k], c[q], s[q], 0, 0, 0);
+            for (int j = 0; j < 4; ++j) {
+                const float f = part[4 * j + g][p];
+                if (f != 0.f && at < row) w[j] = make_float4(w[j].x + f * x[j].x, w[j].y + f * x[j].y, w[j].z + f * x[j].z, w[j].w + f * x[j].w);
             }
         }
+        codewords(min(k0 + 32, MK - 1), c1);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float x[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                bf16x4 o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    o[e] = (__bf16)x[e];
+                    x[e] -= (float)o[e];
+                }
+                *reinterpret_cast<bf16x4 *>(mine + (k * 16 + 4 * j + g) * kOutPitch + 4 * i16) = o;
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        products(0, c0);
+        products(32, c1);
     }
     __syncthreads();                                // the sums' places are free
     constexpr int OP = 16 * CW + 1;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
-        for (int c = 0; c < CW; ++c) out_room[(wave * 16 + 4 * g + e) * OP + i16 * CW + c] = s[c][e];
+        for (int q = 0; q < CW; ++q) out_room[(wave * 16 + 4 * g + e) * OP + i16 * CW + q] = s[q][e];
     __syncthreads();
     for (int t = threadIdx.x; t < 64 * CW; t += kOutThreads) {
         const int i = t / (4 * CW), p = t - i * 4 * CW, m = tile * 16 + i, u = m / RB, b = u / RG, hq = (u - b * RG) * RB + (m - u * RB), at = slice * 16 * CW + 4 * p;

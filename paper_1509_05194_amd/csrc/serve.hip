@@ -117,9 +117,11 @@ hipError_t launch_through_tables(const AttendArgs &a, const CodesPlan &plan, int
     CodesStat *stats = reinterpret_cast<CodesStat *>(scratch + room.tab);
     float *sums = reinterpret_cast<float *>(scratch + room.tab + room.stats);
     const int tiles = (a.rows.B * ((a.R + RB - 1) / RB) * RB + 15) / 16, groups = a.G * ((a.M * a.K + 63) / 64);
-    const dim3 grid((unsigned)groups, (unsigned)std::max(1, std::min(tiles, (4 * cus + groups - 1) / groups)));
-    auto tables = a.D <= 64 ? &k_attend_tables<T, RB, 4> : a.D <= 128 ? &k_attend_tables<T, RB, 8> : &k_attend_tables<T, RB, 16>;
-    hipLaunchKernelGGL(tables, grid, dim3(kTableThreads), 0, stream, a, tiles, tab);
+    constexpr int N = T::bytes == 4 ? 3 : __is_same(T, F16) ? 2 : 1;    // bf16 parts of a query
+    auto tables = a.D <= 64 ? &k_attend_tables<T, RB, 2, N> : a.D <= 128 ? &k_attend_tables<T, RB, 4, N> : &k_attend_tables<T, RB, 8, N>;
+    const int queries = table_queries(N, a.D <= 64 ? 2 : a.D <= 128 ? 4 : 8), stages = (a.rows.B * ((a.R + RB - 1) / RB) * RB + queries - 1) / queries;
+    const dim3 grid((unsigned)groups, (unsigned)std::max(1, std::min(stages, (4 * cus + groups - 1) / groups)));
+    hipLaunchKernelGGL(tables, grid, dim3(kTableThreads), 0, stream, a, stages, tab);
     TRY(hipGetLastError());
     const int mw = a.M <= 8 ? 2 : a.M <= 16 ? 4 : 8;
 #define CODES(WIDE, MW) TRY((launch_codes<RB, WIDE, MW>(a, plan, splits, tab, stats, sums, raised, stream)))
@@ -149,9 +151,10 @@ hipError_t launch_through_tables(const AttendArgs &a, const CodesPlan &plan, int
     // 64 coordinates a block where that leaves enough of them
     const bool wide = (int64_t)tiles * a.G * ((a.D + 63) / 64) >= cus / 2;
     const int slices = (a.D + (wide ? 63 : 15)) / (wide ? 64 : 16);
-    auto out = wide ? &k_attend_out<T, RB, 4> : &k_attend_out<T, RB, 1>;
+    constexpr int NO = T::bytes == 4 ? 3 : 2;
+    auto out = wide ? &k_attend_out<T, RB, 4, NO> : &k_attend_out<T, RB, 1, NO>;
     TRY(raise_lds(out, kRaisedOut + (wide ? 1 : 0) + 2 * (RB == 1 ? 0 : RB == 2 ? 1 : 2) + 6 * (T::bytes == 4 ? 0 : __is_same(T, F16) ? 1 : 2), raised));
-    hipLaunchKernelGGL(out, dim3((unsigned)((tiles * a.G * slices + 7) / 8 * 8)), dim3(kOutThreads), (size_t)out_lds(wide ? 4 : 1), stream, a, parts, splits, tiles, (const CodesStat *)stats,
+    hipLaunchKernelGGL(out, dim3((unsigned)((tiles * a.G * slices + 7) / 8 * 8)), dim3(kOutThreads), (size_t)out_lds(NO, wide ? 4 : 1), stream, a, parts, splits, tiles, (const CodesStat *)stats,
                        (const float *)sums);
     return hipGetLastError();
 }
