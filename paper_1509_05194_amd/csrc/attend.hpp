@@ -56,6 +56,26 @@ struct SeqRows {
         const unsigned q = (unsigned)table[j];
         return q < named ? q : ~0u;
     }
+    // The same for 64 rows from i on, a multiple of 64, in pages of multiples of 64 rows and with `begin` one too: they are in one page, from `off` on;
+    // t: the place of the first in its sequence.  Whether a row is between begin and end is the caller's to look at.
+    __host__ __device__ constexpr unsigned where_wave(unsigned i, unsigned &off, int64_t &t) const
+    {
+        unsigned j = 0;
+        if (picks) {
+            const unsigned e = page_of(i);
+            off = i - e * page;
+            const int32_t at = picks[e];
+            if (at < 0 || at >= max_pages) return ~0u;
+            j = (unsigned)at;
+        } else {
+            const unsigned at = (unsigned)begin + i;
+            j = page_of(at);
+            off = at - j * page;
+        }
+        t = (int64_t)j * page + off;
+        const unsigned q = (unsigned)table[j];
+        return q < named ? q : ~0u;
+    }
     __host__ __device__ constexpr int64_t slot(unsigned i) const
     {
         unsigned off = 0;
@@ -246,12 +266,7 @@ __global__ __launch_bounds__(kWave) void k_attend_join(const AttendArgs a, int s
 
 // ---- from tables --------------------------------------------------------------------------------
 
-#ifndef ATT_T
-#define ATT_T 512
-#define ATT_R 4
-#define ATT_O 4
-#endif
-constexpr int kCodesThreads = ATT_T, kCodesRows = ATT_R, kWindow = kCodesThreads * kCodesRows, kCodesWaves = kCodesThreads / kWave;
+constexpr int kWindow = 2048;                       // rows between two flushes of the fixed-point sums
 constexpr int kCodesMaxM = 32, kCodesSplits = 64;
 constexpr int kCodesLds = 152 * 1024;               // tables and sums; the rest is for what the kernel declares
 constexpr int kWideBits = 40, kPairBits = 19;       // steps of a fixed-point weight, as powers of two below the largest of its window
@@ -274,22 +289,28 @@ __host__ __device__ constexpr CodesPlan codes_plan(int R, int M, int K, bool wid
     }
     return {0, false, 0, 0};
 }
-// Words a thread looks after, for code rows of up to MW words.
-__host__ __device__ constexpr int codes_words(int RB, bool wide, int MW)
+// Words of LDS at most for code rows of up to MW words; threads of a block, two blocks a CU where their LDS fits; words a thread looks after.
+__host__ __device__ constexpr int codes_most(int RB, bool wide, int MW)
 {
     const int all = MW * 4 * 256 * (wide ? RB : RB / 2), most = kCodesLds / (wide ? 12 : 16);
-    return ((all < most ? all : most) + kCodesThreads - 1) / kCodesThreads;
+    return all < most ? all : most;
 }
+__host__ __device__ constexpr int codes_threads(int RB, bool wide, int MW) { return codes_most(RB, wide, MW) * (wide ? 12 : 16) <= 72 * 1024 ? 512 : 1024; }
+__host__ __device__ constexpr int codes_words(int RB, bool wide, int MW) { return (codes_most(RB, wide, MW) + codes_threads(RB, wide, MW) - 1) / codes_threads(RB, wide, MW); }
 __host__ __device__ constexpr int codes_splits(const AttendArgs &a, int RB, int cus)
 {
     const int64_t jobs = (int64_t)a.rows.B * a.G * ((a.R + RB - 1) / RB);
-    int64_t s = (2ll * cus + jobs - 1) / jobs, most = (attend_capacity(a) + 1023) / 1024;
+#ifndef ATT_S
+#define ATT_S 2
+#endif
+    int64_t s = (ATT_S * (int64_t)cus + jobs - 1) / jobs, most = (attend_capacity(a) + 1023) / 1024;
     if (s > most) s = most;
     if (s > kCodesSplits) s = kCodesSplits;
     return (int)(s < 1 ? 1 : s);
 }
-// Rows of sums: whole fours.
+// Rows of sums, and of tables of RB query heads: whole fours.
 __host__ __device__ constexpr int64_t sums_row(int M, int K) { return ((int64_t)M * K + 3) / 4 * 4; }
+__host__ __device__ constexpr int64_t tab_row(int M, int K, int RB) { return ((int64_t)M * K * RB + 3) / 4 * 4; }
 
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
@@ -385,7 +406,7 @@ __global__ __launch_bounds__(kTableThreads) void k_attend_tables(const AttendArg
                 for (int e = 0; e < 4; e += RB) {   // queries n0 + 16 tile + 4 g + e of this lane's codeword
                     const int m = n0 + 16 * tile + 4 * g + e, v = m / RB, bb = v / RG;
                     if (m >= all) break;
-                    float *to = tab + ((((int64_t)bb * a.G + h) * RG + (v - bb * RG)) * MK + cw) * RB;
+                    float *to = tab + (((int64_t)bb * a.G + h) * RG + (v - bb * RG)) * tab_row(a.M, a.K, RB) + cw * RB;
                     if (RB == 4) *reinterpret_cast<float4 *>(to) = make_float4(s[0] * f, s[1] * f, s[2] * f, s[3] * f);
                     else if (RB == 2) *reinterpret_cast<float2 *>(to) = make_float2(s[e] * f, s[e + 1] * f);
                     else *to = s[e] * f;
@@ -427,12 +448,13 @@ struct CodesArgs {
     bool grouped;                                   // blocks go round the eight XCDs: those that read the same rows to one of them
     bool words;                                     // every row's codes are whole, aligned words
     bool small;                                     // offsets within a page fit 32 bits, and its rows 24
+    bool by_wave;                                   // the 64 rows of a wave are in one page
     const float *tab;
     CodesStat *stats;
     float *sums;
 };
 
-// A block a part of the rows of a key head and RB of its query heads.  Windows of 2048 rows, four a thread:
+// A block a part of the rows of a key head and RB of its query heads.  Windows of 2048 rows, two or four a thread:
 //   scores from the tables in LDS; weights p g' to fixed point, added up by code in LDS; these sums, times what a step stands for, to the running sums,
 //   which threads keep in registers.
 // The step is 2^-19 of the largest weight so far where two query heads share a word (2048 weights of 2^19 steps fit), rounded to the step below or above
@@ -441,8 +463,9 @@ struct CodesArgs {
 // score and weight of a window only if one of them is beyond what the last ones allow for.
 // FULL: K = 256 and 4 MW dictionaries, whole aligned words: the offsets in LDS are in the instructions.
 template <int RB, bool WIDE, int MW, bool FULL>
-__global__ __launch_bounds__(kCodesThreads, ATT_O) void k_attend_codes(const AttendArgs a, const CodesArgs x)
+__global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes(const AttendArgs a, const CodesArgs x)
 {
+    constexpr int kCodesThreads = codes_threads(RB, WIDE, MW), kCodesRows = kWindow / kCodesThreads, kCodesWaves = kCodesThreads / kWave;
     extern __shared__ __attribute__((aligned(16))) char codes_lds[];
     __shared__ float2 red[RB][16];
     __shared__ int any_bad, grow[2];
@@ -474,8 +497,23 @@ __global__ __launch_bounds__(kCodesThreads, ATT_O) void k_attend_codes(const Att
     unsigned long long *hist = reinterpret_cast<unsigned long long *>(codes_lds);
     float *lut = reinterpret_cast<float *>(codes_lds + (size_t)words * 8);
     {
-        const float *t = x.tab + seq * MK * RB;
-        for (int i = threadIdx.x; i < MK * RB; i += kCodesThreads) lut[i] = t[i];
+        const float4 *t = reinterpret_cast<const float4 *>(x.tab + seq * tab_row(M, K, RB));
+        const int fours = (int)(tab_row(M, K, RB) / 4), whole = MK * RB / 4;
+        constexpr int EACH = 4;
+        for (int i0 = threadIdx.x; i0 < fours; i0 += EACH * kCodesThreads) {
+            float4 f[EACH];
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) f[j] = t[min(i0 + j * kCodesThreads, fours - 1)];
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) {
+                const int i = i0 + j * kCodesThreads;
+                if (i < whole) *reinterpret_cast<float4 *>(lut + 4 * i) = f[j];
+                else if (i < fours) {               // a last one that is not whole
+                    const float e[4] = {f[j].x, f[j].y, f[j].z, f[j].w};
+                    for (int k = 4 * i; k < MK * RB; ++k) lut[k] = e[k - 4 * i];
+                }
+            }
+        }
         for (int i = threadIdx.x; i < words; i += kCodesThreads) hist[i] = 0;
         if (threadIdx.x == 0) any_bad = grow[0] = grow[1] = 0;
     }
@@ -484,34 +522,63 @@ __global__ __launch_bounds__(kCodesThreads, ATT_O) void k_attend_codes(const Att
 #pragma unroll
     for (int j = 0; j < NW; ++j) pairs |= (uint64_t)((threadIdx.x + j * kCodesThreads) / K % P) << (2 * j);
     float acc[NW][WIDE ? 1 : 2] = {};
-    float ref[RB], unit[RB], back[RB], limit[RB], sum[RB];     // reference of the scores, steps in 1 and their size, log2 of the largest weight there may be
+    constexpr float top_step = WIDE ? 0x1p40f : 0x1p19f;
+    static_assert(kWideBits == 40 && kPairBits == 19, "the same");
+    float ref[RB], unit[RB], back[RB], largest[RB], sum[RB];   // reference of the scores, steps in 1 and their size, log2 of the largest weight
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
-        ref[r] = limit[r] = -INFINITY;
+        ref[r] = largest[r] = -INFINITY;
         unit[r] = back[r] = 1.f;
         sum[r] = 0.f;
     }
     bool bad = false;
     const unsigned page_codes = (unsigned)(a.rows.page * H * M), page_scales = (unsigned)(a.rows.page * H);
-    __syncthreads();
-    int turn_of = 0;
-    for (unsigned w0 = first; w0 < last; w0 += kWindow, turn_of ^= 1) {
-        bool there[kCodesRows];
-        unsigned kc[kCodesRows][MW], vc[kCodesRows][MW];
-        float gk[kCodesRows], gv[kCodesRows], s[kCodesRows][RB];
+    const unsigned lane_codes = (unsigned)(lane * H * M), lane_scales = (unsigned)(lane * H);
+    // Where the rows of a window are; their codes and scales, sent for while the window before is added up.
+    bool there[kCodesRows], there_next[kCodesRows];
+    unsigned page_next[kCodesRows], off_next[kCodesRows];
+    unsigned kc[kCodesRows][MW], vc[kCodesRows][MW];
+    float gk[kCodesRows], gv[kCodesRows];
+    auto locate = [&](unsigned w) {
 #pragma unroll
         for (int i = 0; i < kCodesRows; ++i) {
-            const unsigned t = w0 + i * kCodesThreads + threadIdx.x;
             unsigned off = 0, q = ~0u;
-            if (t < last) q = rows.where(t, off);
-            there[i] = q != ~0u;
+            if (x.by_wave) {
+                const unsigned t = __builtin_amdgcn_readfirstlane(w + i * kCodesThreads + wave * kWave);
+                int64_t at = 0;
+                if (t < last) q = __builtin_amdgcn_readfirstlane(rows.where_wave(t, off, at));
+                there_next[i] = q != ~0u && t + lane < last && at + lane >= rows.begin && at + lane < rows.end;
+            } else {
+                const unsigned t = w + i * kCodesThreads + threadIdx.x;
+                if (t < last) q = rows.where(t, off);
+                there_next[i] = q != ~0u;
+            }
+            page_next[i] = q;
+            off_next[i] = off;
+        }
+    };
+    auto fetch = [&](unsigned (&kc)[kCodesRows][MW], unsigned (&vc)[kCodesRows][MW], float (&gk)[kCodesRows], float (&gv)[kCodesRows]) {
+#pragma unroll
+        for (int i = 0; i < kCodesRows; ++i) {
             gk[i] = gv[i] = 1.f;
 #pragma unroll
             for (int j = 0; j < MW; ++j) kc[i][j] = vc[i][j] = 0u;
-            if (!there[i]) continue;
-            const uint64_t at = x.small ? (uint64_t)q * page_codes + __umul24(off, (unsigned)(H * M)) : ((uint64_t)q * (unsigned)a.rows.page + off) * (unsigned)(H * M);
-            const uint64_t ag = x.small ? (uint64_t)q * page_scales + __umul24(off, (unsigned)H) : ((uint64_t)q * (unsigned)a.rows.page + off) * (unsigned)H;
-            const uint8_t *kp = a.codes + at + h * M, *vp = kp + a.G * M;
+            if (!there_next[i]) continue;
+            const uint8_t *kp = a.codes + h * M;
+            const float *gp = a.scale;
+            if (x.by_wave) {
+                const uint64_t row = (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane(page_next[i]) * (unsigned)a.rows.page + (unsigned)__builtin_amdgcn_readfirstlane(off_next[i]);
+                kp += row * (unsigned)(H * M) + lane_codes;
+                gp += row * (unsigned)H + lane_scales;
+            } else if (x.small) {
+                kp += (uint64_t)page_next[i] * page_codes + __umul24(off_next[i], (unsigned)(H * M));
+                gp += (uint64_t)page_next[i] * page_scales + __umul24(off_next[i], (unsigned)H);
+            } else {
+                const uint64_t row = (uint64_t)page_next[i] * (unsigned)a.rows.page + off_next[i];
+                kp += row * (unsigned)(H * M);
+                gp += row * (unsigned)H;
+            }
+            const uint8_t *vp = kp + a.G * M;
             if (FULL) {
                 typedef unsigned row_words __attribute__((ext_vector_type(MW < 4 ? MW : 4), aligned(4)));
 #pragma unroll
@@ -539,15 +606,35 @@ __global__ __launch_bounds__(kCodesThreads, ATT_O) void k_attend_codes(const Att
                     }
             }
             if (a.scale) {
-                const float *g = a.scale + ag;
-                gk[i] = g[h];
-                gv[i] = g[a.G + h];
+                gk[i] = gp[h];
+                gv[i] = gp[a.G + h];
             }
         }
-        bool beyond = false;
-        float top[RB], most[RB];
+    };
+    locate(first);
+    fetch(kc, vc, gk, gv);
+    __syncthreads();
+    int turn_of = 0;
+    for (unsigned w0 = first; w0 < last; w0 += kWindow, turn_of ^= 1) {
 #pragma unroll
-        for (int r = 0; r < RB; ++r) top[r] = most[r] = -INFINITY;
+        for (int i = 0; i < kCodesRows; ++i) there[i] = there_next[i];
+        float s[kCodesRows][RB], v[kCodesRows][RB];
+        locate(w0 + kWindow);
+        bool beyond = false;
+        float here[RB];                             // the window's sums of exponentials
+        // weights in steps (WIDE: as they are), with the fraction that decides which way they are rounded
+        auto weigh = [&](int i) {
+            const float turn = (float)(((w0 + i * kCodesThreads + threadIdx.x) * 0x9E3779B9u) >> 8) * 0x1p-24f;
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                const float e = s[i][r] - ref[r], p = __builtin_amdgcn_exp2f(e), w = p * gv[i];
+                here[r] += p;
+                v[i][r] = WIDE ? w : w * unit[r] + turn;
+                beyond |= e > kRoom || fabsf(WIDE ? w * unit[r] : v[i][r]) > top_step;
+            }
+        };
+#pragma unroll
+        for (int r = 0; r < RB; ++r) here[r] = 0.f;
 #pragma unroll
         for (int i = 0; i < kCodesRows; ++i) {
 #pragma unroll
@@ -560,34 +647,41 @@ __global__ __launch_bounds__(kCodesThreads, ATT_O) void k_attend_codes(const Att
                     if (!FULL) k = min(k, (unsigned)K - 1u);
                     const float *e = lut + m * K * RB + k * RB;
                     if (RB == 4) {
-                        const float4 v = *reinterpret_cast<const float4 *>(e);
-                        s[i][0] += v.x;
-                        s[i][RB > 1 ? 1 : 0] += v.y;
-                        s[i][RB > 2 ? 2 : 0] += v.z;
-                        s[i][RB > 3 ? 3 : 0] += v.w;
+                        const float4 f = *reinterpret_cast<const float4 *>(e);
+                        s[i][0] += f.x;
+                        s[i][RB > 1 ? 1 : 0] += f.y;
+                        s[i][RB > 2 ? 2 : 0] += f.z;
+                        s[i][RB > 3 ? 3 : 0] += f.w;
                     } else if (RB == 2) {
-                        const float2 v = *reinterpret_cast<const float2 *>(e);
-                        s[i][0] += v.x;
-                        s[i][RB > 1 ? 1 : 0] += v.y;
+                        const float2 f = *reinterpret_cast<const float2 *>(e);
+                        s[i][0] += f.x;
+                        s[i][RB > 1 ? 1 : 0] += f.y;
                     } else s[i][0] += *e;
                 }
+#pragma unroll
+            for (int r = 0; r < RB; ++r) s[i][r] *= gk[i];
             bad |= !(fabsf(gv[i]) < INFINITY);
-            const float lg = __builtin_amdgcn_logf(fabsf(gv[i]));
-#pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                s[i][r] *= gk[i];
-                top[r] = fmaxf(top[r], s[i][r]);
-                most[r] = fmaxf(most[r], s[i][r] + lg);
-            }
+            weigh(i);
         }
-#pragma unroll
-        for (int r = 0; r < RB; ++r) beyond |= top[r] > ref[r] + kRoom || most[r] > limit[r];
         if (beyond) grow[turn_of] = 1;              // the same value from whoever writes
         __syncthreads();
         float fade[RB];
 #pragma unroll
         for (int r = 0; r < RB; ++r) fade[r] = 1.f;
         if (grow[turn_of]) {                        // the largest of the window, over the block
+            float top[RB], most[RB];
+#pragma unroll
+            for (int r = 0; r < RB; ++r) top[r] = most[r] = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < kCodesRows; ++i) {
+                if (!there[i]) continue;
+                const float lg = __builtin_amdgcn_logf(fabsf(gv[i]));
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    top[r] = fmaxf(top[r], s[i][r]);
+                    most[r] = fmaxf(most[r], s[i][r] + lg);
+                }
+            }
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
                 const float t = key_max<6>(float_key(top[r])), m = key_max<6>(float_key(most[r]));
@@ -596,41 +690,42 @@ __global__ __launch_bounds__(kCodesThreads, ATT_O) void k_attend_codes(const Att
             __syncthreads();
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
-                const float2 v = red[r][min(lane, kCodesWaves - 1)];
-                const float t = key_max<4>(float_key(v.x)), m = fmaxf(key_max<4>(float_key(v.y)), limit[r]), now = fmaxf(ref[r], t);
+                const float2 f = red[r][min(lane, kCodesWaves - 1)];
+                const float t = key_max<4>(float_key(f.x)), now = fmaxf(ref[r], t);
+                largest[r] = fmaxf(key_max<4>(float_key(f.y)), largest[r]);
                 fade[r] = ref[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref[r] - now);
                 ref[r] = now;
                 // weights up to 2^e; only zeros: any step
-                const float e = m == -INFINITY ? 0.f : fminf(fmaxf(ceilf(m - now + 0.01f), -100.f), 140.f);
+                const float e = largest[r] == -INFINITY ? 0.f : fminf(fmaxf(ceilf(largest[r] - now + 0.01f), -100.f), 140.f);
                 const int n = min((WIDE ? kWideBits : kPairBits) - (int)e, 120);
-                limit[r] = m == -INFINITY ? m : now + ((WIDE ? kWideBits : kPairBits) - n) - 0.005f;
                 unit[r] = ldexpf(1.f, n);
                 back[r] = ldexpf(1.f, -n);
                 sum[r] *= fade[r];
+                here[r] = 0.f;
             }
+#pragma unroll
+            for (int i = 0; i < kCodesRows; ++i)
+                if (there[i]) weigh(i);
         }
+#pragma unroll
+        for (int r = 0; r < RB; ++r) sum[r] += here[r];
         if (threadIdx.x == 0) grow[turn_of ^ 1] = 0;
+        unsigned kn[kCodesRows][MW], vn[kCodesRows][MW];
+        float gkn[kCodesRows], gvn[kCodesRows];
+        fetch(kn, vn, gkn, gvn);
 #pragma unroll
         for (int i = 0; i < kCodesRows; ++i) {
             if (!there[i]) continue;
-            const float turn = (float)(((w0 + i * kCodesThreads + threadIdx.x) * 0x9E3779B9u) >> 8) * 0x1p-24f;
             unsigned long long add[P];
-            long long wide[RB];
-            int fixed[RB];
-#pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                const float p = __builtin_amdgcn_exp2f(s[i][r] - ref[r]);
-                sum[r] += p;
-                const float w = p * gv[i];
-                if (WIDE) {
-                    const double d = (double)w * (double)unit[r];
-                    wide[r] = d == d ? (long long)rint(d) : 0;
-                } else fixed[r] = (int)floorf(w * unit[r] + turn);
-            }
 #pragma unroll
             for (int q = 0; q < P; ++q) {
-                if (WIDE) add[q] = (unsigned long long)wide[q];
-                else add[q] = (unsigned long long)(unsigned)(fixed[(2 * q + 1) % RB] + (fixed[(2 * q) % RB] >> 31)) << 32 | (unsigned)fixed[(2 * q) % RB];
+                if (WIDE) {
+                    const double d = (double)v[i][q] * (double)unit[q];
+                    add[q] = (unsigned long long)(d == d ? (long long)rint(d) : 0ll);
+                } else {
+                    const int lo = (int)floorf(v[i][(2 * q) % RB]), hi = (int)floorf(v[i][(2 * q + 1) % RB]);
+                    add[q] = (unsigned long long)(unsigned)(hi + (lo >> 31)) << 32 | (unsigned)lo;
+                }
             }
 #pragma unroll
             for (int m = 0; m < 4 * MW; ++m)
@@ -647,7 +742,7 @@ __global__ __launch_bounds__(kCodesThreads, ATT_O) void k_attend_codes(const Att
         for (int j = 0; j < NW; ++j) {
             const int i = threadIdx.x + j * kCodesThreads, q = (int)(pairs >> (2 * j) & 3);
             if (i >= words) break;
-            const unsigned long long v = hist[i];
+            const unsigned long long w = hist[i];
             hist[i] = 0;
             if (WIDE) {
                 float f = fade[0], o = back[0];
@@ -657,12 +752,22 @@ __global__ __launch_bounds__(kCodesThreads, ATT_O) void k_attend_codes(const Att
                         f = fade[r];
                         o = back[r];
                     }
-                acc[j][0] = acc[j][0] * f + (float)((double)(long long)v * (double)o);
+                acc[j][0] = acc[j][0] * f + (float)((double)(long long)w * (double)o);
             } else {
-                const int lo = (int)(unsigned)v, hi = (int)((unsigned)(v >> 32) + ((unsigned)v >> 31));
+                const int lo = (int)(unsigned)w, hi = (int)((unsigned)(w >> 32) + ((unsigned)w >> 31));
                 const bool second = RB == 4 && q == 1;
                 acc[j][0] = acc[j][0] * (second ? fade[RB == 4 ? 2 : 0] : fade[0]) + (float)lo * (second ? back[RB == 4 ? 2 : 0] : back[0]);
                 acc[j][WIDE ? 0 : 1] = acc[j][WIDE ? 0 : 1] * (second ? fade[RB - 1] : fade[RB >= 2 ? 1 : 0]) + (float)hi * (second ? back[RB - 1] : back[RB >= 2 ? 1 : 0]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kCodesRows; ++i) {
+            gk[i] = gkn[i];
+            gv[i] = gvn[i];
+#pragma unroll
+            for (int j = 0; j < MW; ++j) {
+                kc[i][j] = kn[i][j];
+                vc[i][j] = vn[i][j];
             }
         }
     }

@@ -85,7 +85,7 @@ struct CodesRoom {
 CodesRoom codes_room(const AttendArgs &a, const CodesPlan &plan, int splits)
 {
     const int64_t seqs = (int64_t)a.rows.B * a.G * ((a.R + plan.RB - 1) / plan.RB), rows = seqs * splits * plan.RB;
-    return {up(sizeof(float) * seqs * plan.RB * a.M * a.K), up(sizeof(CodesStat) * rows), up(sizeof(float) * rows * sums_row(a.M, a.K)), up(sizeof(CodesStat) * seqs * plan.RB)};
+    return {up(sizeof(float) * seqs * tab_row(a.M, a.K, plan.RB)), up(sizeof(CodesStat) * rows), up(sizeof(float) * rows * sums_row(a.M, a.K)), up(sizeof(CodesStat) * seqs * plan.RB)};
 }
 
 template <int RB, bool WIDE, int MW, bool FULL>
@@ -95,7 +95,7 @@ hipError_t launch_codes_as(const AttendArgs &a, const CodesPlan &plan, const Cod
     auto kern = &k_attend_codes<RB, WIDE, MW, FULL>;
     TRY(raise_lds(kern, bit, raised));
     const int64_t heads = (int64_t)a.G * ((a.R + RB - 1) / RB), units = (int64_t)a.rows.B * x.splits;
-    hipLaunchKernelGGL(kern, dim3((unsigned)((x.grouped ? (units + 7) / 8 * 8 : units) * heads)), dim3(kCodesThreads), plan.lds, stream, a, x);
+    hipLaunchKernelGGL(kern, dim3((unsigned)((x.grouped ? (units + 7) / 8 * 8 : units) * heads)), dim3(codes_threads(RB, WIDE, MW)), plan.lds, stream, a, x);
     return hipGetLastError();
 }
 template <int RB, bool WIDE, int MW>
@@ -103,7 +103,7 @@ hipError_t launch_codes(const AttendArgs &a, const CodesPlan &plan, int splits, 
 {
     const int64_t row = 2ll * a.G * a.M;
     const CodesArgs x = {splits, (int64_t)a.rows.B * splits >= 32, a.M % 4 == 0 && reinterpret_cast<uintptr_t>(a.codes) % 4 == 0,
-                         a.rows.page < 1 << 24 && a.rows.page * row < (int64_t)1 << 32, tab, stats, sums};
+                         a.rows.page < 1 << 24 && a.rows.page * row < (int64_t)1 << 32, a.rows.page % kWave == 0 && !a.begins, tab, stats, sums};
     if (MW <= 4 && a.K == 256 && a.M == 4 * MW && x.words) return launch_codes_as<RB, WIDE, MW <= 4 ? MW : 4, true>(a, plan, x, raised, stream);
     return launch_codes_as<RB, WIDE, MW, false>(a, plan, x, raised, stream);
 }
