@@ -87,7 +87,17 @@ struct SeqRows {
 // Numbers of rows at most, over all sequences.
 __host__ __device__ constexpr int64_t attend_capacity(const AttendArgs &a) { return (int64_t)(a.picked ? a.n_picked : a.rows.max_pages) * a.rows.page; }
 
-constexpr int kDirectThreads = 256, kDirectTile = 32, kDirectSplits = 256;
+constexpr int kDirectThreads = 256, kDirectSplits = 256, kDirectRows = 2, kDirectGroups = 32;
+
+// Threads that share a row, a power of two; rows that a block decodes at once, in groups of those threads.
+__host__ __device__ constexpr int direct_lanes(int D)
+{
+    int lanes = 1;
+    while (lanes < D / 4) lanes *= 2;
+    return lanes;
+}
+__host__ __device__ constexpr int direct_groups(int D) { return kDirectThreads / direct_lanes(D) < kDirectGroups ? kDirectThreads / direct_lanes(D) : kDirectGroups; }
+__host__ __device__ constexpr int direct_tile(int D) { return direct_groups(D) * kDirectRows; }
 
 // Query heads a block takes at once.
 __host__ __device__ constexpr int heads_at_once(int R) { return R >= 3 ? 4 : R; }
@@ -96,7 +106,7 @@ __host__ __device__ constexpr int heads_at_once(int R) { return R >= 3 ? 4 : R; 
 __host__ __device__ constexpr int direct_splits(const AttendArgs &a, int cus)
 {
     const int RB = heads_at_once(a.R);
-    const int64_t jobs = (int64_t)a.rows.B * a.G * ((a.R + RB - 1) / RB), tiles = (attend_capacity(a) + kDirectTile - 1) / kDirectTile;
+    const int64_t jobs = (int64_t)a.rows.B * a.G * ((a.R + RB - 1) / RB), tiles = (attend_capacity(a) + direct_tile(a.D) - 1) / direct_tile(a.D);
     int64_t s = (4ll * cus + jobs - 1) / jobs;
     if (s > tiles) s = tiles;
     if (s > kDirectSplits) s = kDirectSplits;
@@ -124,21 +134,23 @@ __device__ __forceinline__ float4 decode_piece(const float *C, const uint8_t *co
     return s;
 }
 
-// A block a part of the rows of one key head and RB of its query heads; `lanes` threads a row, the power of two from D / 4 up.
+// A block a part of the rows of one key head and RB of its query heads, in tiles of two rows a group of threads.  Keys and values are gathered
+// at the same time: a tile costs one chain of loads (table, codes, codewords), which is what few rows are bound by.
 template <typename T, int RB>
-__global__ __launch_bounds__(kDirectThreads) void k_attend_rows(const AttendArgs a, int splits, int lanes, PartStat *stats, float *sums)
+__global__ __launch_bounds__(kDirectThreads) void k_attend_rows(const AttendArgs a, int splits, PartStat *stats, float *sums)
 {
-    __shared__ float4 q[RB][64], red[kDirectThreads];
-    __shared__ float s[RB][kDirectTile], w[RB][kDirectTile], fade[RB];
-    __shared__ int64_t slots[kDirectTile];
-    const int RG = (a.R + RB - 1) / RB, d4 = a.D >> 2, H = 2 * a.G;
-    const int64_t job = blockIdx.x, head = job / splits;
-    const int split = (int)(job - head * splits), rg = (int)(head % RG), h = (int)(head / RG % a.G), b = (int)(head / RG / a.G);
+    constexpr int MOST = kDirectGroups * kDirectRows;
+    __shared__ float4 q[RB][64], red[RB][kDirectThreads];
+    __shared__ float s[RB][MOST], w[RB][MOST], fade[RB], gk[MOST], gv[MOST];
+    __shared__ int64_t slots[MOST];
+    const int RG = (a.R + RB - 1) / RB, d4 = a.D >> 2, H = 2 * a.G, lanes = direct_lanes(a.D), groups = direct_groups(a.D), tile = direct_tile(a.D);
+    const int job = blockIdx.x, head = job / splits;
+    const int split = job - head * splits, rg = head % RG, h = head / RG % a.G, b = head / RG / a.G;
     const SeqRows rows(a, b, h);
-    const int64_t per = ((rows.count + splits - 1) / splits + kDirectTile - 1) / kDirectTile * kDirectTile, first = per * split, last = min(rows.count, first + per);
-    const int lane = lane_id(), wave = threadIdx.x >> 6, g = threadIdx.x / lanes, p = threadIdx.x % lanes, groups = kDirectThreads / lanes;
+    const int64_t per = ((rows.count + splits - 1) / splits + tile - 1) / tile * tile, first = per * split, last = min(rows.count, first + per);
+    const int lane = lane_id(), wave = threadIdx.x >> 6, g = threadIdx.x / lanes, p = threadIdx.x % lanes;
     if (first >= last) {
-        if (threadIdx.x < RB) stats[job * RB + threadIdx.x] = {-INFINITY, 0.f};
+        if (threadIdx.x < RB) stats[(int64_t)job * RB + threadIdx.x] = {-INFINITY, 0.f};
         return;
     }
     for (int i = threadIdx.x; i < RB * d4; i += kDirectThreads) {
@@ -153,42 +165,50 @@ __global__ __launch_bounds__(kDirectThreads) void k_attend_rows(const AttendArgs
 #pragma unroll
     for (int r = 0; r < RB; ++r) acc[r] = make_float4(0.f, 0.f, 0.f, 0.f);
     float top = -INFINITY, sum = 0.f;               // of head `wave`, in every lane of its wave
-    for (int64_t t0 = first; t0 < last; t0 += kDirectTile) {
-        if (threadIdx.x < kDirectTile) slots[threadIdx.x] = t0 + threadIdx.x < last ? rows.slot((unsigned)(t0 + threadIdx.x)) : kNoRow;
-        __syncthreads();
-        for (int i = g; i < kDirectTile; i += groups) {
-            const int64_t at = slots[i];
-            float dot[RB] = {};
-            if (at >= 0 && p < d4) {
-                const float4 k = decode_piece(Ck, a.codes + (at * H + h) * a.M, a.M, a.K, a.D);
-#pragma unroll
-                for (int r = 0; r < RB; ++r) {
-                    const float4 v = q[r][p];
-                    dot[r] = k.x * v.x + k.y * v.y + k.z * v.z + k.w * v.w;
-                }
-            }
-            for (int o = lanes >> 1; o > 0; o >>= 1)
-#pragma unroll
-                for (int r = 0; r < RB; ++r) dot[r] += __shfl_xor(dot[r], o, kWave);
-            if (p == 0) {
-                const float f = at >= 0 && a.scale ? a.scale[at * H + h] : 1.f;
-#pragma unroll
-                for (int r = 0; r < RB; ++r) s[r][i] = dot[r] * f;
-            }
+    for (int64_t t0 = first; t0 < last; t0 += tile) {
+        if (threadIdx.x < (unsigned)tile) {
+            const int64_t at = t0 + threadIdx.x < last ? rows.slot((unsigned)(t0 + threadIdx.x)) : kNoRow;
+            slots[threadIdx.x] = at;
+            gk[threadIdx.x] = at >= 0 && a.scale ? a.scale[at * H + h] : 1.f;
+            gv[threadIdx.x] = at >= 0 && a.scale ? a.scale[at * H + a.G + h] : 1.f;
         }
         __syncthreads();
+        float4 v[kDirectRows];
+        if (g < groups)
+#pragma unroll
+            for (int u = 0; u < kDirectRows; ++u) {
+                const int i = g + u * groups;
+                const int64_t at = slots[i];
+                float4 k = make_float4(0.f, 0.f, 0.f, 0.f);
+                v[u] = k;
+                if (at >= 0 && p < d4) {
+                    const uint8_t *code = a.codes + at * H * a.M;
+                    k = decode_piece(Ck, code + h * a.M, a.M, a.K, a.D);
+                    v[u] = decode_piece(Cv, code + (a.G + h) * a.M, a.M, a.K, a.D);
+                }
+                float dot[RB];
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    const float4 x = p < d4 ? q[r][p] : make_float4(0.f, 0.f, 0.f, 0.f);
+                    dot[r] = k.x * x.x + k.y * x.y + k.z * x.z + k.w * x.w;
+                }
+                for (int o = lanes >> 1; o > 0; o >>= 1)
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) dot[r] += __shfl_xor(dot[r], o, kWave);
+                if (p == 0)
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) s[r][i] = dot[r] * gk[i];
+            }
+        __syncthreads();
         if (wave < RB) {
-            const bool there = lane < kDirectTile && slots[lane & (kDirectTile - 1)] >= 0;
+            const bool there = lane < tile && slots[lane] >= 0;
             const float x = there ? s[wave][lane] : -INFINITY;
             float m = x;
 #pragma unroll
             for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, kWave));
             const float now = fmaxf(top, m);
             float e = there ? exp2f(x - now) : 0.f;
-            if (lane < kDirectTile) {
-                const int64_t at = slots[lane];
-                w[wave][lane] = there ? (a.scale ? e * a.scale[at * H + a.G + h] : e) : 0.f;
-            }
+            w[wave][lane] = there ? e * gv[lane] : 0.f;
 #pragma unroll
             for (int o = 32; o > 0; o >>= 1) e += __shfl_xor(e, o, kWave);
             const float f = top == -INFINITY ? 0.f : exp2f(top - now);
@@ -202,32 +222,31 @@ __global__ __launch_bounds__(kDirectThreads) void k_attend_rows(const AttendArgs
             const float f = fade[r];
             acc[r] = make_float4(acc[r].x * f, acc[r].y * f, acc[r].z * f, acc[r].w * f);
         }
-        for (int i = g; i < kDirectTile; i += groups) {
-            const int64_t at = slots[i];
-            if (at < 0 || p >= d4) continue;
-            const float4 v = decode_piece(Cv, a.codes + (at * H + a.G + h) * a.M, a.M, a.K, a.D);
+        if (g < groups)
 #pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                const float f = w[r][i];
-                acc[r] = make_float4(acc[r].x + f * v.x, acc[r].y + f * v.y, acc[r].z + f * v.z, acc[r].w + f * v.w);
+            for (int u = 0; u < kDirectRows; ++u) {
+                const int i = g + u * groups;
+                if (slots[i] < 0) continue;
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    const float f = w[r][i];
+                    acc[r] = make_float4(acc[r].x + f * v[u].x, acc[r].y + f * v[u].y, acc[r].z + f * v[u].z, acc[r].w + f * v[u].w);
+                }
             }
-        }
         __syncthreads();
     }
-    if (wave < RB && lane == 0) stats[job * RB + wave] = {top, sum};
+    if (wave < RB && lane == 0) stats[(int64_t)job * RB + wave] = {top, sum};
 #pragma unroll
-    for (int r = 0; r < RB; ++r) {
-        red[threadIdx.x] = acc[r];
-        __syncthreads();
-        if (threadIdx.x < d4) {
-            float4 v = red[threadIdx.x];
-            for (int i = 1; i < groups; ++i) {
-                const float4 o = red[i * lanes + threadIdx.x];
-                v = make_float4(v.x + o.x, v.y + o.y, v.z + o.z, v.w + o.w);
-            }
-            reinterpret_cast<float4 *>(sums)[(job * RB + r) * d4 + threadIdx.x] = v;
+    for (int r = 0; r < RB; ++r) red[r][threadIdx.x] = acc[r];
+    __syncthreads();
+    for (int i = threadIdx.x; i < RB * d4; i += kDirectThreads) {
+        const int r = i / d4, e = i - r * d4;
+        float4 v = red[r][e];
+        for (int j = 1; j < groups; ++j) {
+            const float4 o = red[r][j * lanes + e];
+            v = make_float4(v.x + o.x, v.y + o.y, v.z + o.z, v.w + o.w);
         }
-        __syncthreads();
+        reinterpret_cast<float4 *>(sums)[((int64_t)job * RB + r) * d4 + e] = v;
     }
 }
 
@@ -245,15 +264,22 @@ __global__ __launch_bounds__(kWave) void k_attend_join(const AttendArgs a, int s
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     const int p = threadIdx.x;
     bool any = false;
-    for (int i = 0; i < splits; ++i) {
-        const PartStat st = stat[(int64_t)i * RB];
-        if (st.sum == 0.f) continue;                // no rows
-        any = true;
-        const float f = exp2f(st.top - top);
-        sum += f * st.sum;
-        if (p < d4) {
-            const float4 o = reinterpret_cast<const float4 *>(sums)[((job + i) * RB + r % RB) * d4 + p];
-            v = make_float4(v.x + f * o.x, v.y + f * o.y, v.z + f * o.z, v.w + f * o.w);
+    for (int i0 = 0; i0 < splits; i0 += 8) {
+        float4 o[8];
+        PartStat st[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = min(i0 + j, splits - 1);
+            st[j] = stat[(int64_t)i * RB];
+            o[j] = reinterpret_cast<const float4 *>(sums)[((job + i) * RB + r % RB) * d4 + min(p, d4 - 1)];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (i0 + j >= splits || st[j].sum == 0.f) continue;         // no rows, and no sums
+            any = true;
+            const float f = exp2f(st[j].top - top);
+            sum += f * st[j].sum;
+            v = make_float4(v.x + f * o[j].x, v.y + f * o[j].y, v.z + f * o[j].z, v.w + f * o[j].w);
         }
     }
     if (any) {
@@ -297,13 +323,11 @@ __host__ __device__ constexpr int codes_most(int RB, bool wide, int MW)
 }
 __host__ __device__ constexpr int codes_threads(int RB, bool wide, int MW) { return codes_most(RB, wide, MW) * (wide ? 12 : 16) <= 72 * 1024 ? 512 : 1024; }
 __host__ __device__ constexpr int codes_words(int RB, bool wide, int MW) { return (codes_most(RB, wide, MW) + codes_threads(RB, wide, MW) - 1) / codes_threads(RB, wide, MW); }
-__host__ __device__ constexpr int codes_splits(const AttendArgs &a, int RB, int cus)
+// Parts of a sequence's rows: as many blocks as the CUs hold at once, `blocks` each, where there are 1024 rows for each.
+__host__ __device__ constexpr int codes_splits(const AttendArgs &a, int RB, int blocks, int cus)
 {
     const int64_t jobs = (int64_t)a.rows.B * a.G * ((a.R + RB - 1) / RB);
-#ifndef ATT_S
-#define ATT_S 2
-#endif
-    int64_t s = (ATT_S * (int64_t)cus + jobs - 1) / jobs, most = (attend_capacity(a) + 1023) / 1024;
+    int64_t s = (blocks * (int64_t)cus + jobs - 1) / jobs, most = (attend_capacity(a) + 1023) / 1024;
     if (s > most) s = most;
     if (s > kCodesSplits) s = kCodesSplits;
     return (int)(s < 1 ? 1 : s);
@@ -472,38 +496,40 @@ __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes
     constexpr int P = WIDE ? RB : RB / 2, NW = codes_words(RB, WIDE, MW);
     constexpr float kRoom = 8.f;                    // a score may be so far above the reference
     const int M = FULL ? 4 * MW : a.M, K = FULL ? 256 : a.K, MK = M * K, RG = (a.R + RB - 1) / RB, H = 2 * a.G, heads = a.G * RG;
-    int64_t u;                                      // part of a sequence
+    unsigned u;                                     // part of a sequence; at most 64 each of 16384
     int hr;                                         // key head and group of its query heads
     if (x.grouped) {
-        const int64_t at = blockIdx.x >> 3;
-        u = at / heads * 8 + (blockIdx.x & 7);
-        hr = (int)(at % heads);
+        const unsigned at = blockIdx.x >> 3;
+        u = at / (unsigned)heads * 8 + (blockIdx.x & 7);
+        hr = (int)(at % (unsigned)heads);
     } else {
-        u = blockIdx.x / heads;
-        hr = (int)(blockIdx.x - u * heads);
+        u = blockIdx.x / (unsigned)heads;
+        hr = (int)(blockIdx.x - u * (unsigned)heads);
     }
-    if (u >= (int64_t)a.rows.B * x.splits) return;
-    const int b = (int)(u / x.splits), split = (int)(u - (int64_t)b * x.splits), h = hr / RG;
+    if (u >= (unsigned)a.rows.B * (unsigned)x.splits) return;
+    const int b = (int)(u / (unsigned)x.splits), split = (int)(u - (unsigned)b * (unsigned)x.splits), h = hr / RG;
     const int64_t seq = (int64_t)b * heads + hr, job = seq * x.splits + split;
     const SeqRows rows(a, b, h);
-    const int64_t per = ((rows.count + x.splits - 1) / x.splits + 255) / 256 * 256, first64 = per * split;
+    // rows are numbered below 2^31
+    const unsigned count = (unsigned)rows.count, per = ((count + (unsigned)x.splits - 1u) / (unsigned)x.splits + 255u) / 256u * 256u;
+    const uint64_t first64 = (uint64_t)per * (unsigned)split;
     const int lane = lane_id(), wave = threadIdx.x >> 6;
-    if (first64 >= rows.count) {
+    if (first64 >= count) {
         if (threadIdx.x < RB) x.stats[job * RB + threadIdx.x] = {-INFINITY, 0.f, 0.f, 0.f};
         return;
     }
-    const unsigned first = (unsigned)first64, last = (unsigned)min(rows.count, first64 + per);     // rows are numbered below 2^31
+    const unsigned first = (unsigned)first64, last = (unsigned)(first64 + per < count ? first64 + per : count);
     const int words = MK * P;
     unsigned long long *hist = reinterpret_cast<unsigned long long *>(codes_lds);
     float *lut = reinterpret_cast<float *>(codes_lds + (size_t)words * 8);
     {
-        const float4 *t = reinterpret_cast<const float4 *>(x.tab + seq * tab_row(M, K, RB));
+        const float4 *from = reinterpret_cast<const float4 *>(x.tab + seq * tab_row(M, K, RB));
         const int fours = (int)(tab_row(M, K, RB) / 4), whole = MK * RB / 4;
         constexpr int EACH = 4;
         for (int i0 = threadIdx.x; i0 < fours; i0 += EACH * kCodesThreads) {
             float4 f[EACH];
 #pragma unroll
-            for (int j = 0; j < EACH; ++j) f[j] = t[min(i0 + j * kCodesThreads, fours - 1)];
+            for (int j = 0; j < EACH; ++j) f[j] = from[min(i0 + j * kCodesThreads, fours - 1)];
 #pragma unroll
             for (int j = 0; j < EACH; ++j) {
                 const int i = i0 + j * kCodesThreads;

@@ -43,12 +43,10 @@ int64_t direct_jobs(const AttendArgs &a, int splits)
 template <typename T, int RB>
 hipError_t launch_direct(const AttendArgs &a, int splits, char *scratch, hipStream_t stream)
 {
-    int lanes = 1;
-    while (lanes < a.D / 4) lanes *= 2;
     const int64_t jobs = direct_jobs(a, splits);
     PartStat *stats = reinterpret_cast<PartStat *>(scratch);
     float *sums = reinterpret_cast<float *>(scratch + up(sizeof(PartStat) * jobs * RB));
-    hipLaunchKernelGGL((k_attend_rows<T, RB>), dim3((unsigned)jobs), dim3(kDirectThreads), 0, stream, a, splits, lanes, stats, sums);
+    hipLaunchKernelGGL((k_attend_rows<T, RB>), dim3((unsigned)jobs), dim3(kDirectThreads), 0, stream, a, splits, stats, sums);
     TRY(hipGetLastError());
     hipLaunchKernelGGL((k_attend_join<T, RB>), dim3((unsigned)(a.rows.B * a.G * a.R)), dim3(kWave), 0, stream, a, splits, (const PartStat *)stats, (const float *)sums);
     return hipGetLastError();
@@ -77,6 +75,11 @@ CodesPlan plan_of(const AttendArgs &a, int type)
 {
     if (attend_capacity(a) <= kFewRows) return {0, false, 0, 0};
     return codes_plan(a.R, a.M, a.K, type == kRowF32);
+}
+
+int splits_of(const AttendArgs &a, const CodesPlan &plan, int cus)
+{
+    return codes_splits(a, plan.RB, codes_threads(plan.RB, plan.wide, a.M <= 8 ? 2 : a.M <= 16 ? 4 : 8) == 512 ? 2 : 1, cus);
 }
 
 struct CodesRoom {
@@ -111,7 +114,7 @@ hipError_t launch_codes(const AttendArgs &a, const CodesPlan &plan, int splits, 
 template <typename T, int RB>
 hipError_t launch_through_tables(const AttendArgs &a, const CodesPlan &plan, int cus, char *scratch, uint64_t *raised, hipStream_t stream)
 {
-    const int splits = codes_splits(a, RB, cus);
+    const int splits = splits_of(a, plan, cus);
     const CodesRoom room = codes_room(a, plan, splits);
     float *tab = reinterpret_cast<float *>(scratch);
     CodesStat *stats = reinterpret_cast<CodesStat *>(scratch + room.tab);
@@ -244,7 +247,7 @@ size_t attend_scratch(const AttendArgs &a, int type, int cus)
         const AttendArgs r = round_of(a, 0, n, 0);
         const CodesPlan plan = plan_of(r, type);
         if (plan.RB) {
-            const CodesRoom room = codes_room(r, plan, codes_splits(r, plan.RB, cus));
+            const CodesRoom room = codes_room(r, plan, splits_of(r, plan, cus));
             most = std::max(most, room.tab + room.stats + room.sums + room.joined);
             continue;
         }
