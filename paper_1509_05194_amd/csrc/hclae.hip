@@ -2588,8 +2588,7 @@ int hclae_cache_select(hclae_ctx *ctx, const void *Q, int type, int B, int Hq, i
     if (bad_rows(Q, type, q_row_stride, q_head_stride) || odd_words(4, scale, tables, lengths, picked))
         return fail(ctx, HCLAE_EINVAL, "hclae_cache_select: type, alignment or strides");
     ON_DEVICE(ctx);
-    const SelectArgs a = {Q, q_row_stride, q_head_stride, codes, scale, {tables, lengths, B, max_pages, page, n_pages}, ctx->cache_T, cache_padded(ctx->D) / 4,
-                          few_columns(ctx->K), G, Hq / G, ctx->M, ctx->K, ctx->D, first, recent, k, picked};
+    const SelectArgs a = {Q, q_row_stride, q_head_stride, codes, scale, {tables, lengths, B, max_pages, page, n_pages}, ctx->cache_C, G, Hq / G, ctx->M, ctx->K, ctx->D, first, recent, k, picked};
     rc = serve_room(ctx, select_scratch(a), "hclae_cache_select: its scratch cannot be allocated while the stream is captured");
     if (rc != HCLAE_OK) return rc;
     HIP_TRY(ctx, select_launch(a, type, ctx->serve_buf, &ctx->serve_raised, ctx->stream));

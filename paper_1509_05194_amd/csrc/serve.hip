@@ -22,13 +22,15 @@ size_t up(size_t bytes) { return (bytes + 255) / 256 * 256; }
     } while (0)
 
 template <typename K>
-hipError_t raise_lds(K kern, int bit, uint64_t *raised)
+hipError_t raise_lds(K kern, int bit, uint64_t *raised, int bytes = kServeLds)
 {
     if (*raised >> bit & 1u) return hipSuccess;
-    TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kServeLds));
+    TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
     *raised |= 1ull << bit;
     return hipSuccess;
 }
+
+constexpr int kPickLds = 136 * 1024;                // as above: k_select_pages declares 20 KB
 
 enum RaisedBit { kRaisedSelect = 0, kRaisedCodes = 1, kRaisedOut = 31 };         // 30 and 18 from the last two on
 
@@ -205,12 +207,12 @@ hipError_t launch_select(const SelectArgs &a, char *scratch, uint64_t *raised, h
 {
     double *tab = reinterpret_cast<double *>(scratch);
     uint64_t *keys = reinterpret_cast<uint64_t *>(scratch + table_bytes(a));
-    hipLaunchKernelGGL(k_select_tables<T>, dim3((unsigned)(a.G * a.M), (unsigned)((a.rows.B + kSelectSeqs - 1) / kSelectSeqs)), dim3(kSelectThreads), 0, stream, a, tab);
+    hipLaunchKernelGGL(k_select_tables<T>, dim3((unsigned)(a.G * ((a.M * a.K + 63) / 64) * ((a.rows.B + kSelectSeqs - 1) / kSelectSeqs))), dim3(kSelectThreads), 0, stream, a, tab);
     TRY(hipGetLastError());
-    const size_t lds = 8 * ((size_t)a.M * a.K + a.rows.max_pages);
+    const size_t lds = pick_lds(a.M, a.K, a.rows.max_pages);
     const dim3 grid((unsigned)(a.rows.B * a.G));
-    if (lds <= (size_t)kServeLds) {
-        TRY(raise_lds(&k_select_pages<true>, kRaisedSelect, raised));
+    if (lds <= (size_t)kPickLds) {
+        TRY(raise_lds(&k_select_pages<true>, kRaisedSelect, raised, kPickLds));
         hipLaunchKernelGGL(k_select_pages<true>, grid, dim3(kPickThreads), lds, stream, a, (const double *)tab, keys);
     } else {
         hipLaunchKernelGGL(k_select_pages<false>, grid, dim3(kPickThreads), 0, stream, a, (const double *)tab, keys);

@@ -39,8 +39,7 @@ struct SelectArgs {                                 // hclae_cache_select
     const uint8_t *codes;                           // [pages][G][M]
     const float *scale;                             // [pages][G] or null
     PagedRows rows;
-    const float4 *T;                                // codewords in pieces of four coordinates: [G][M][pieces][columns]
-    int pieces, columns;
+    const float *C;                                 // [G][M][K][D]
     int G, R, M, K, D;
     int first, recent, k;
     int32_t *picked;                                // [B][G][k]
