@@ -2610,7 +2610,7 @@ int hclae_cache_extend(hclae_ctx *ctx, int32_t *tables, int32_t *lengths, int B,
     PageArgs a = {tables, lengths, B, max_pages, page, n_pages, starts, n, slots, src, dst, rows, nullptr};
     rc = serve_room(ctx, extend_scratch(a), "hclae_cache_extend: its scratch cannot be allocated while the stream is captured");
     if (rc != HCLAE_OK) return rc;
-    HIP_TRY(ctx, extend_launch(a, ctx->cus, ctx->serve_buf, ctx->stream));
+    HIP_TRY(ctx, extend_launch(a, ctx->cus, ctx->serve_buf, &ctx->serve_raised, ctx->stream));
     return HCLAE_OK;
 }
 

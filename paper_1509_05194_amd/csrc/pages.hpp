@@ -3,9 +3,11 @@
 //   k_pages_clear, k_pages_mark   bitmaps of the pages that are named once or more, and twice or more
 //   k_extend_plan, k_extend_rows  pages for new rows, in the order of the sequences, the lowest free page first
 //   k_compact_plan, k_compact_tables   the last pages in use go to the first holes
+//   k_extend_block, k_compact_block   all of it in one block, bitmaps in LDS, where tables and cache are small enough
 //   k_pages_copy                  rows of pages
+// None of it moves much memory: a call is its launches and a few chains of loads.
 #pragma once
-#include "common.hpp"
+#include "decode.hpp"
 #include "serve.hpp"
 
 namespace hclae {
@@ -44,16 +46,37 @@ __global__ __launch_bounds__(kPageThreads) void k_pages_clear(unsigned *words, i
     for (int64_t i = (int64_t)blockIdx.x * kPageThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kPageThreads) words[i] = 0u;
 }
 
+constexpr int kMarkEntries = 1024;                  // entries of one table that a block looks at at a time
+
+// The live entries of a table from j0 on, those of one thread of `threads`: f(entry's place, page).
+template <typename F>
+__device__ __forceinline__ void live_entries(const PageArgs &a, int b, int j0, int j1, int live, int thread, int threads, F f)
+{
+    const int32_t *table = a.tables + (int64_t)b * a.max_pages;
+    const int end = min(j1, live);
+    for (int j = j0 + thread; j < end; j += 4 * threads) {
+        int32_t p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = j + i * threads < end ? table[j + i * threads] : -1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (p[i] >= 0 && p[i] < a.n_pages) f(j + i * threads, p[i]);
+    }
+}
+__device__ __forceinline__ void mark_page(unsigned *used, unsigned *shared, int32_t p)
+{
+    const unsigned bit = 1u << (p & 31), old = atomicOr(&used[p >> 5], bit);
+    if (old & bit) atomicOr(&shared[p >> 5], bit);
+}
+
 __global__ __launch_bounds__(kPageThreads) void k_pages_mark(const PageArgs a, unsigned *used, unsigned *shared)
 {
-    const int64_t all = (int64_t)a.B * a.max_pages;
-    for (int64_t i = (int64_t)blockIdx.x * kPageThreads + threadIdx.x; i < all; i += (int64_t)gridDim.x * kPageThreads) {
-        const int b = (int)(i / a.max_pages), j = (int)(i - (int64_t)b * a.max_pages);
-        if (j >= pages_of(held(a.lengths[b], a.max_pages, a.page), a.page)) continue;
-        const int32_t p = a.tables[i];
-        if (p < 0 || p >= a.n_pages) continue;
-        const unsigned bit = 1u << (p & 31), old = atomicOr(&used[p >> 5], bit);
-        if (old & bit) atomicOr(&shared[p >> 5], bit);
+    const int chunks = (a.max_pages + kMarkEntries - 1) / kMarkEntries;
+    const int64_t jobs = (int64_t)a.B * chunks;
+    for (int64_t job = blockIdx.x; job < jobs; job += gridDim.x) {
+        const int b = (int)(job / chunks), j0 = (int)(job - (int64_t)b * chunks) * kMarkEntries;
+        const int live = pages_of(held(a.lengths[b], a.max_pages, a.page), a.page);
+        live_entries(a, b, j0, j0 + kMarkEntries, live, threadIdx.x, kPageThreads, [&](int, int32_t p) { mark_page(used, shared, p); });
     }
 }
 
@@ -93,10 +116,9 @@ __device__ __forceinline__ bool last_page_shared(const PageArgs &a, int b, const
     return p >= 0 && p < a.n_pages && (shared[p >> 5] >> (p & 31) & 1u);
 }
 
-// One block: how many pages the sequences up to each ask for, and that many free pages, the lowest first.
-__global__ __launch_bounds__(kPlanThreads) void k_extend_plan(const PageArgs a, const ExtendScratch s)
+// By one block: how many pages the sequences up to each ask for, and that many free pages, the lowest first.
+__device__ __forceinline__ void extend_plan(const PageArgs &a, const ExtendScratch &s, unsigned *sums)
 {
-    __shared__ unsigned sums[17];
     unsigned asked = 0;
     for (int64_t b0 = 0; b0 < a.B; b0 += kPlanThreads) {
         const int b = (int)(b0 + threadIdx.x);
@@ -130,55 +152,124 @@ __global__ __launch_bounds__(kPlanThreads) void k_extend_plan(const PageArgs a, 
     if (threadIdx.x == 0) *s.found = found;
 }
 
-// A block a sequence: its new entries, its rows' slots, its length; the rows that are of no sequence.
-__global__ __launch_bounds__(kPageThreads) void k_extend_rows(const PageArgs a, const ExtendScratch s)
+// By one thread or wave: a sequence's rows' slots, its new entries, its length.  What is read of its table is read before anything is written.
+template <int LANES>
+__device__ __forceinline__ void extend_sequence(const PageArgs &a, const ExtendScratch &s, int b, int lane)
 {
-    for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
-        const Growth g(a, b);
-        int32_t at = -1;
-        const bool split = last_page_shared(a, b, g, s.shared, &at);
-        const unsigned need = g.fits ? (unsigned)(g.new_pages - g.old_pages) + (split ? 1u : 0u) : 0u, begin = s.upto[b] - need;
-        const bool served = g.add > 0 && g.fits && (need == 0 || s.upto[b] <= *s.found);
-        int32_t *table = a.tables + (int64_t)b * a.max_pages;
-        const int64_t last = g.length / a.page;         // entry of the row that is next
-        const int32_t copy = served && split ? (int32_t)s.free[begin] : -1;
-        const int32_t tail = copy >= 0 ? copy : g.length % a.page ? at : -1;    // page of that entry, if it holds rows already
-        const unsigned *fresh = s.free + begin + (copy >= 0 ? 1 : 0);
-        for (int64_t i = threadIdx.x; i < g.add; i += kPageThreads) {
+    const Growth g(a, b);
+    int32_t at = -1;
+    const bool split = last_page_shared(a, b, g, s.shared, &at);
+    const unsigned need = g.fits ? (unsigned)(g.new_pages - g.old_pages) + (split ? 1u : 0u) : 0u, begin = s.upto[b] - need;
+    const bool served = g.add > 0 && g.fits && (need == 0 || s.upto[b] <= *s.found);
+    int32_t *table = a.tables + (int64_t)b * a.max_pages;
+    const int64_t last = g.length / a.page;             // entry of the row that is next
+    const int32_t copy = served && split ? (int32_t)s.free[begin] : -1;
+    const int32_t tail = copy >= 0 ? copy : g.length % a.page ? at : -1;    // page of that entry, if it holds rows already
+    const unsigned *fresh = s.free + begin + (copy >= 0 ? 1 : 0);
+    for (int64_t i = lane; i < g.add; i += LANES) {
+        int64_t slot = -1;
+        if (served) {
             const int64_t pos = g.length + i, e = pos / a.page, off = pos - e * a.page;
-            int64_t slot = -1;
-            if (served) {
-                const int32_t p = e < g.old_pages ? tail : (int32_t)fresh[e - g.old_pages];
-                if (p >= 0 && p < a.n_pages) slot = (int64_t)p * a.page + off;
-            }
-            a.slots[g.first + i] = slot;
+            const int32_t p = e < g.old_pages ? tail : (int32_t)fresh[e - g.old_pages];
+            if (p >= 0 && p < a.n_pages) slot = (int64_t)p * a.page + off;
         }
-        __syncthreads();                                // the entry of the next row has been read
-        if (served)
-            for (int64_t e = g.old_pages + threadIdx.x; e < g.new_pages; e += kPageThreads) table[e] = (int32_t)fresh[e - g.old_pages];
-        if (threadIdx.x == 0) {
-            if (copy >= 0) table[last] = copy;
-            if (served) a.lengths[b] = (int32_t)(g.length + g.add);
-            a.src[b] = copy >= 0 ? at : -1;
-            a.dst[b] = copy;
-            a.rows[b] = copy >= 0 ? (int32_t)(g.length % a.page) : 0;
-        }
-        __syncthreads();
+        a.slots[g.first + i] = slot;
     }
+    if (served)
+        for (int64_t e = g.old_pages + lane; e < g.new_pages; e += LANES) table[e] = (int32_t)fresh[e - g.old_pages];
+    if (lane == 0) {
+        if (copy >= 0) table[last] = copy;
+        if (served) a.lengths[b] = (int32_t)(g.length + g.add);
+        a.src[b] = copy >= 0 ? at : -1;
+        a.dst[b] = copy;
+        a.rows[b] = copy >= 0 ? (int32_t)(g.length % a.page) : 0;
+    }
+}
+// Rows that are of no sequence.
+__device__ __forceinline__ void extend_others(const PageArgs &a, int64_t at, int64_t step)
+{
     const int64_t front = a.starts[0] < 0 ? 0 : a.starts[0] > a.n ? a.n : a.starts[0], back = a.starts[a.B] < 0 ? 0 : a.starts[a.B] > a.n ? a.n : a.starts[a.B];
-    const int64_t at = (int64_t)blockIdx.x * kPageThreads + threadIdx.x, step = (int64_t)gridDim.x * kPageThreads;
     for (int64_t i = at; i < front; i += step) a.slots[i] = -1;
     for (int64_t i = back + at; i < a.n; i += step) a.slots[i] = -1;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void k_extend_plan(const PageArgs a, const ExtendScratch s)
+{
+    __shared__ unsigned sums[17];
+    extend_plan(a, s, sums);
+}
+
+__global__ __launch_bounds__(kPageThreads) void k_extend_rows(const PageArgs a, const ExtendScratch s)
+{
+    const int wave = threadIdx.x >> 6, waves = kPageThreads / kWave;
+    for (int64_t b = (int64_t)blockIdx.x * waves + wave; b < a.B; b += (int64_t)gridDim.x * waves) extend_sequence<kWave>(a, s, (int)b, lane_id());
+    extend_others(a, (int64_t)blockIdx.x * kPageThreads + threadIdx.x, (int64_t)gridDim.x * kPageThreads);
+}
+
+// All of it by one block: bitmaps, sums and the list of free pages in LDS.
+constexpr int kBlockLds = 128 * 1024, kBlockEntries = 32768, kBlockRows = 16384, kFewNew = 16;
+__host__ __device__ constexpr int64_t extend_lds(const PageArgs &a, int64_t room) { return 4 * (2 * words_of(a.n_pages) + 2 * (int64_t)a.B + room); }
+__host__ __device__ constexpr bool extend_in_block(const PageArgs &a, int64_t room)
+{
+    return (int64_t)a.B * a.max_pages <= kBlockEntries && a.B <= kBlockEntries && a.n <= kBlockRows && extend_lds(a, room) <= kBlockLds;
+}
+// f(sequence, entry, page) for all live entries of all tables: the block's threads take them one after another, eight loads on their way at a time.
+// live: how many entries of a sequence hold rows.
+template <typename F>
+__device__ __forceinline__ void all_entries(const PageArgs &a, const unsigned *live, F f)
+{
+    const unsigned total = (unsigned)(a.B * a.max_pages), mul = page_mul(max(a.max_pages, 1));
+    const int shift = page_shift(max(a.max_pages, 1));
+    for (unsigned i0 = threadIdx.x; i0 < total; i0 += 8 * kPlanThreads) {
+        int32_t p[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) p[k] = a.tables[min(i0 + k * kPlanThreads, total - 1u)];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const unsigned i = i0 + k * kPlanThreads;
+            if (i >= total || p[k] < 0 || p[k] >= a.n_pages) continue;
+            const unsigned b = (unsigned)((uint64_t)i * mul >> (31 + shift)), j = i - b * (unsigned)a.max_pages;
+            if (j < live[b]) f((int)b, (int)j, p[k]);
+        }
+    }
+}
+__device__ __forceinline__ void live_of(const PageArgs &a, unsigned *live)
+{
+    for (int b = threadIdx.x; b < a.B; b += kPlanThreads) live[b] = (unsigned)pages_of(held(a.lengths[b], a.max_pages, a.page), a.page);
+}
+__global__ __launch_bounds__(kPlanThreads) void k_extend_block(const PageArgs a, unsigned room)
+{
+    extern __shared__ unsigned page_lds[];
+    __shared__ unsigned sums[17], found;
+    const int words = (int)words_of(a.n_pages);
+    const ExtendScratch s = {page_lds, page_lds + words, page_lds + 2 * words, page_lds + 2 * words + 2 * a.B, &found, room};
+    unsigned *live = page_lds + 2 * words + a.B;
+    for (int i = threadIdx.x; i < 2 * words; i += kPlanThreads) page_lds[i] = 0u;
+    live_of(a, live);
+    __syncthreads();
+    all_entries(a, live, [&](int, int, int32_t p) { mark_page(s.used, s.shared, p); });
+    __syncthreads();
+    extend_plan(a, s, sums);
+    __syncthreads();
+    // a thread a sequence with few new rows, then a wave one with many
+    for (int b = threadIdx.x; b < a.B; b += kPlanThreads) {
+        const bool few = a.starts[b + 1] - (int64_t)a.starts[b] <= kFewNew;
+        live[b] = few ? 1u : 0u;
+        if (few) extend_sequence<1>(a, s, b, 0);
+    }
+    __syncthreads();
+    for (int b = threadIdx.x >> 6; b < a.B; b += kPlanThreads / kWave)
+        if (!live[b]) extend_sequence<kWave>(a, s, b, lane_id());
+    extend_others(a, threadIdx.x, kPlanThreads);
 }
 
 struct CompactScratch {
     unsigned *used, *unused, *before;               // before: pages in use in earlier words
 };
 
-// One block: the pages in use are counted; the i-th hole below that number takes the i-th page from that number on.
-__global__ __launch_bounds__(kPlanThreads) void k_compact_plan(const PageArgs a, const CompactScratch s)
+// By one block: the pages in use are counted; the i-th hole below that number takes the i-th page from that number on.
+__device__ __forceinline__ void compact_plan(const PageArgs &a, const CompactScratch &s, unsigned *sums)
 {
-    __shared__ unsigned sums[17];
     const int64_t words = words_of(a.n_pages);
     unsigned n = 0;
     for (int64_t w0 = 0; w0 < words; w0 += kPlanThreads) {
@@ -190,9 +281,9 @@ __global__ __launch_bounds__(kPlanThreads) void k_compact_plan(const PageArgs a,
         n += all;
     }
     if (threadIdx.x == 0 && a.used) *a.used = (int32_t)n;
-    // pages in use before page n: as many are in front of it, and the others have to move
-    const int64_t wn = n >> 5;
     __syncthreads();
+    // of the pages below n so many are in use: the others from n on have to move
+    const int64_t wn = n >> 5;
     const unsigned low = wn < words ? s.before[wn] + (unsigned)__popc(s.used[wn] & ((1u << (n & 31)) - 1u)) : n;
     const unsigned moves = n - low;
     for (int64_t w = threadIdx.x; w < words; w += kPlanThreads) {
@@ -211,21 +302,61 @@ __global__ __launch_bounds__(kPlanThreads) void k_compact_plan(const PageArgs a,
     }
     for (int64_t i = moves + threadIdx.x; i < a.n_pages / 2; i += kPlanThreads) a.src[i] = a.dst[i] = -1;
 }
+// Where a page from n on goes, `low` pages below n being in use; n and low as compact_plan has them.
+struct NewPlaces {
+    unsigned n, low;
+    __device__ __forceinline__ NewPlaces(const PageArgs &a, const CompactScratch &s)
+    {
+        const int64_t words = words_of(a.n_pages);
+        n = s.before[words - 1] + (unsigned)__popc(s.used[words - 1]);
+        const int64_t wn = n >> 5;
+        low = wn < words ? s.before[wn] + (unsigned)__popc(s.used[wn] & ((1u << (n & 31)) - 1u)) : n;
+    }
+    __device__ __forceinline__ void entry(const PageArgs &a, const CompactScratch &s, int b, int j, int32_t p) const
+    {
+        if (p >= (int64_t)n) a.tables[(int64_t)b * a.max_pages + j] = a.dst[s.before[p >> 5] + (unsigned)__popc(s.used[p >> 5] & ((1u << (p & 31)) - 1u)) - low];
+    }
+};
+
+__global__ __launch_bounds__(kPlanThreads) void k_compact_plan(const PageArgs a, const CompactScratch s)
+{
+    __shared__ unsigned sums[17];
+    compact_plan(a, s, sums);
+}
 
 __global__ __launch_bounds__(kPageThreads) void k_compact_tables(const PageArgs a, const CompactScratch s)
 {
-    const int64_t words = words_of(a.n_pages);
-    const unsigned n = s.before[words - 1] + (unsigned)__popc(s.used[words - 1]);
-    const int64_t wn = n >> 5;
-    const unsigned low = wn < words ? s.before[wn] + (unsigned)__popc(s.used[wn] & ((1u << (n & 31)) - 1u)) : n;
-    const int64_t all = (int64_t)a.B * a.max_pages;
-    for (int64_t i = (int64_t)blockIdx.x * kPageThreads + threadIdx.x; i < all; i += (int64_t)gridDim.x * kPageThreads) {
-        const int b = (int)(i / a.max_pages), j = (int)(i - (int64_t)b * a.max_pages);
-        if (j >= pages_of(held(a.lengths[b], a.max_pages, a.page), a.page)) continue;
-        const int32_t p = a.tables[i];
-        if (p < (int64_t)n || p >= a.n_pages) continue;
-        a.tables[i] = a.dst[s.before[p >> 5] + (unsigned)__popc(s.used[p >> 5] & ((1u << (p & 31)) - 1u)) - low];
+    const NewPlaces places(a, s);
+    const int chunks = (a.max_pages + kMarkEntries - 1) / kMarkEntries;
+    const int64_t jobs = (int64_t)a.B * chunks;
+    for (int64_t job = blockIdx.x; job < jobs; job += gridDim.x) {
+        const int b = (int)(job / chunks), j0 = (int)(job - (int64_t)b * chunks) * kMarkEntries;
+        const int live = pages_of(held(a.lengths[b], a.max_pages, a.page), a.page);
+        live_entries(a, b, j0, j0 + kMarkEntries, live, threadIdx.x, kPageThreads, [&](int j, int32_t p) { places.entry(a, s, b, j, p); });
     }
+}
+
+// All of it by one block, as k_extend_block.
+__host__ __device__ constexpr bool compact_in_block(const PageArgs &a)
+{
+    return (int64_t)a.B * a.max_pages <= kBlockEntries && a.B <= 8192 && a.n_pages <= 65536;
+}
+__global__ __launch_bounds__(kPlanThreads) void k_compact_block(const PageArgs a)
+{
+    extern __shared__ unsigned page_lds[];
+    __shared__ unsigned sums[17];
+    const int words = (int)words_of(a.n_pages);
+    const CompactScratch s = {page_lds, page_lds + words, page_lds + 2 * words};
+    unsigned *live = page_lds + 3 * words;
+    for (int i = threadIdx.x; i < 2 * words; i += kPlanThreads) page_lds[i] = 0u;
+    live_of(a, live);
+    __syncthreads();
+    all_entries(a, live, [&](int, int, int32_t p) { atomicOr(&s.used[p >> 5], 1u << (p & 31)); });
+    __syncthreads();
+    compact_plan(a, s, sums);
+    __syncthreads();
+    const NewPlaces places(a, s);
+    all_entries(a, live, [&](int b, int j, int32_t p) { places.entry(a, s, b, j, p); });
 }
 
 // V: bytes of a load.  Rows of a page lie side by side in both arrays, so that the rows of a copy are two stretches of memory.

@@ -32,7 +32,7 @@ hipError_t raise_lds(K kern, int bit, uint64_t *raised, int bytes = kServeLds)
 
 constexpr int kPickLds = 136 * 1024;                // as above: k_select_pages declares 20 KB
 
-enum RaisedBit { kRaisedSelect = 0, kRaisedCodes = 1, kRaisedOut = 31 };         // 30 and 18 from the last two on
+enum RaisedBit { kRaisedSelect = 0, kRaisedCodes = 1, kRaisedOut = 31, kRaisedPages = 49 };         // 30 from kRaisedCodes on, 18 from kRaisedOut on
 
 // ---- attention ----------------------------------------------------------------------------------
 
@@ -224,14 +224,20 @@ hipError_t launch_select(const SelectArgs &a, char *scratch, uint64_t *raised, h
 
 size_t bitmap_bytes(const PageArgs &a) { return up(4 * (size_t)words_of(a.n_pages)); }
 
+dim3 table_blocks(const PageArgs &a, int cus)
+{
+    const int64_t jobs = (int64_t)a.B * ((a.max_pages + kMarkEntries - 1) / kMarkEntries);
+    return dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(jobs, 8ll * cus)));
+}
+
 // Bitmaps at the front of the scratch: pages named once or more, pages named twice or more.
 hipError_t launch_marks(const PageArgs &a, int cus, char *scratch, hipStream_t stream)
 {
-    const int64_t words = (int64_t)(2 * bitmap_bytes(a) / 4), entries = (int64_t)a.B * a.max_pages;
-    auto blocks = [&](int64_t items) { return dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>((items + kPageThreads - 1) / kPageThreads, 8ll * cus))); };
-    hipLaunchKernelGGL(k_pages_clear, blocks(words), dim3(kPageThreads), 0, stream, reinterpret_cast<unsigned *>(scratch), words);
+    const int64_t words = (int64_t)(2 * bitmap_bytes(a) / 4);
+    hipLaunchKernelGGL(k_pages_clear, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>((words + kPageThreads - 1) / kPageThreads, 8ll * cus))), dim3(kPageThreads), 0, stream,
+                       reinterpret_cast<unsigned *>(scratch), words);
     TRY(hipGetLastError());
-    hipLaunchKernelGGL(k_pages_mark, blocks(entries), dim3(kPageThreads), 0, stream, a, reinterpret_cast<unsigned *>(scratch),
+    hipLaunchKernelGGL(k_pages_mark, table_blocks(a, cus), dim3(kPageThreads), 0, stream, a, reinterpret_cast<unsigned *>(scratch),
                        reinterpret_cast<unsigned *>(scratch + bitmap_bytes(a)));
     return hipGetLastError();
 }
@@ -288,10 +294,19 @@ hipError_t select_launch(const SelectArgs &a, int type, char *scratch, uint64_t 
     return hipSuccess;
 }
 
-size_t extend_scratch(const PageArgs &a) { return 2 * bitmap_bytes(a) + up(4 * (size_t)a.B) + up(4 * extend_room(a)) + 256; }
-
-hipError_t extend_launch(const PageArgs &a, int cus, char *scratch, hipStream_t stream)
+size_t extend_scratch(const PageArgs &a)
 {
+    if (extend_in_block(a, (int64_t)extend_room(a))) return 0;
+    return 2 * bitmap_bytes(a) + up(4 * (size_t)a.B) + up(4 * extend_room(a)) + 256;
+}
+
+hipError_t extend_launch(const PageArgs &a, int cus, char *scratch, uint64_t *raised, hipStream_t stream)
+{
+    if (extend_in_block(a, (int64_t)extend_room(a))) {
+        TRY(raise_lds(&k_extend_block, kRaisedPages, raised));
+        hipLaunchKernelGGL(k_extend_block, dim3(1), dim3(kPlanThreads), (size_t)extend_lds(a, (int64_t)extend_room(a)), stream, a, (unsigned)extend_room(a));
+        return hipGetLastError();
+    }
     TRY(launch_marks(a, cus, scratch, stream));
     ExtendScratch s;
     char *p = scratch;
@@ -303,21 +318,25 @@ hipError_t extend_launch(const PageArgs &a, int cus, char *scratch, hipStream_t 
     s.room = (unsigned)extend_room(a);
     hipLaunchKernelGGL(k_extend_plan, dim3(1), dim3(kPlanThreads), 0, stream, a, s);
     TRY(hipGetLastError());
-    hipLaunchKernelGGL(k_extend_rows, dim3((unsigned)std::max(1, std::min(a.B, 1 << 16))), dim3(kPageThreads), 0, stream, a, s);
+    hipLaunchKernelGGL(k_extend_rows, dim3((unsigned)std::max(1, std::min((a.B + 3) / 4, 1 << 16))), dim3(kPageThreads), 0, stream, a, s);
     return hipGetLastError();
 }
 
-size_t compact_scratch(const PageArgs &a) { return 2 * bitmap_bytes(a) + bitmap_bytes(a); }
+size_t compact_scratch(const PageArgs &a) { return a.n_pages > 0 && compact_in_block(a) ? 0 : 3 * bitmap_bytes(a); }
 
 hipError_t compact_launch(const PageArgs &a, int cus, char *scratch, hipStream_t stream)
 {
+    if (a.n_pages > 0 && compact_in_block(a)) {
+        hipLaunchKernelGGL(k_compact_block, dim3(1), dim3(kPlanThreads), (size_t)(12 * words_of(a.n_pages) + 4 * (int64_t)a.B), stream, a);
+        return hipGetLastError();
+    }
     TRY(launch_marks(a, cus, scratch, stream));
     CompactScratch s = {reinterpret_cast<unsigned *>(scratch), reinterpret_cast<unsigned *>(scratch + bitmap_bytes(a)), reinterpret_cast<unsigned *>(scratch + 2 * bitmap_bytes(a))};
     hipLaunchKernelGGL(k_compact_plan, dim3(1), dim3(kPlanThreads), 0, stream, a, s);
     TRY(hipGetLastError());
     const int64_t entries = (int64_t)a.B * a.max_pages;
     if (a.n_pages == 0 || entries == 0) return hipSuccess;
-    hipLaunchKernelGGL(k_compact_tables, dim3((unsigned)std::min<int64_t>((entries + kPageThreads - 1) / kPageThreads, 8ll * cus)), dim3(kPageThreads), 0, stream, a, s);
+    hipLaunchKernelGGL(k_compact_tables, table_blocks(a, cus), dim3(kPageThreads), 0, stream, a, s);
     return hipGetLastError();
 }
 

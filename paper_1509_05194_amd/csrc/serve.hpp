@@ -60,7 +60,7 @@ struct PageArgs {                                   // hclae_cache_extend and hc
     int32_t *used;
 };
 size_t extend_scratch(const PageArgs &a);
-hipError_t extend_launch(const PageArgs &a, int cus, char *scratch, hipStream_t stream);
+hipError_t extend_launch(const PageArgs &a, int cus, char *scratch, uint64_t *raised, hipStream_t stream);
 size_t compact_scratch(const PageArgs &a);
 hipError_t compact_launch(const PageArgs &a, int cus, char *scratch, hipStream_t stream);
 

@@ -189,6 +189,11 @@ def _dtypes():
     return _DTYPES
 
 
+def _serving_types():
+    names = _dtypes()
+    return names["u8"], names["i32"], names["f32"]
+
+
 def _rows(t, shape):
     """(device pointer, type, strides in elements) of rows of float32, float16 or bfloat16 whose elements lie side by side."""
     kind = _dtypes().get(t.dtype)
@@ -489,12 +494,25 @@ class Context:
     # ---- serving from a cache of codes ------------------------------------------------------
     # tables int32 [B][max_pages] and lengths int32 [B] say where the rows of a batch's sequences are (see include/hclae.h); a fork is a copied row of
     # them, and a sequence is given up by setting its length to 0.
+    def _arr(self, t, dtype, shape):
+        """Device pointer of a contiguous tensor of a type and shape on the context's device (None -> NULL)."""
+        if t is None:
+            return None
+        if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+            raise TypeError("expected a contiguous CUDA %s tensor" % dtype)
+        if t.shape != shape:
+            raise ValueError("tensor shape %s, expected %s" % (tuple(t.shape), shape))
+        if t.get_device() != self._device:
+            raise ValueError("a tensor on another device than the context")
+        return t.data_ptr() or None
+
     def cache_attend(self, Q, codes, scale, tables, lengths, page, out, factor=None, begins=None, picked=None, lse=None):
         """Attention of one new token of each sequence, Q [B][Hq][D] (float32, float16 or bfloat16), over its rows begins..lengths of the cache,
         of those, with picked int32 [B][G][n], the rows of the named pages: out [B][Hq][D], of Q's type, and lse float32 [B][Hq].  The cache's
         heads are G key heads and the G value heads behind them, codes uint8 [n_slots][2 G][M].  factor: 1 / sqrt(D) unless given."""
         B, Hq, n_slots, H = Q.shape[0], Q.shape[1], codes.shape[0], self._H or codes.shape[1]
-        self._here(Q, codes, scale, tables, lengths, out, begins, picked, lse)
+        self._here(Q, out)
+        u8, i32, f32 = _serving_types()
         if out.dtype is not Q.dtype:
             raise TypeError("out is of another type than Q")
         pq, kind, sq = _rows(Q, (B, Hq, self.D))
@@ -503,47 +521,48 @@ class Context:
         if picked is not None and n_picked == 0:
             raise ValueError("picked names no pages")      # its pointer would be NULL, which stands for all rows
         self._chk(lib().hclae_cache_attend(
-            self._h, pq, kind, B, Hq, sq[0], sq[1], _ptr(codes, "u8", (n_slots, H, self.M)), _ptr(scale, "f32", (n_slots, H)), n_slots,
-            _ptr(tables, "i32", (B, max_pages)), max_pages, page, _ptr(begins, "i32", (B,)), _ptr(lengths, "i32", (B,)),
-            _ptr(picked, "i32", (B, H // 2, n_picked)), n_picked, self.D ** -0.5 if factor is None else factor, po, so[0], so[1], _ptr(lse, "f32", (B, Hq))))
+            self._h, pq, kind, B, Hq, sq[0], sq[1], self._arr(codes, u8, (n_slots, H, self.M)), self._arr(scale, f32, (n_slots, H)), n_slots,
+            self._arr(tables, i32, (B, max_pages)), max_pages, page, self._arr(begins, i32, (B,)), self._arr(lengths, i32, (B,)),
+            self._arr(picked, i32, (B, H // 2, n_picked)), n_picked, self.D ** -0.5 if factor is None else factor, po, so[0], so[1], self._arr(lse, f32, (B, Hq))))
 
     def cache_select(self, Q, codes, scale, tables, lengths, page, picked, first=1, recent=1):
         """The pages that each sequence's new token looks at most, by their stand-ins codes uint8 [n_pages][H][M] and scale float32 [n_pages][H] (or
         None), H key heads: picked int32 [B][H][k], ascending, -1 behind the last; the first `first` and last `recent` pages are always among them."""
         B, Hq, n_pages, H = Q.shape[0], Q.shape[1], codes.shape[0], self._H or codes.shape[1]
-        self._here(Q, codes, scale, tables, lengths, picked)
+        self._here(Q)
+        u8, i32, f32 = _serving_types()
         p, kind, st = _rows(Q, (B, Hq, self.D))
         max_pages, k = tables.shape[1], picked.shape[2]
         self._chk(lib().hclae_cache_select(
-            self._h, p, kind, B, Hq, st[0], st[1], _ptr(codes, "u8", (n_pages, H, self.M)), _ptr(scale, "f32", (n_pages, H)), n_pages,
-            _ptr(tables, "i32", (B, max_pages)), max_pages, page, _ptr(lengths, "i32", (B,)), first, recent, k, _ptr(picked, "i32", (B, H, k))))
+            self._h, p, kind, B, Hq, st[0], st[1], self._arr(codes, u8, (n_pages, H, self.M)), self._arr(scale, f32, (n_pages, H)), n_pages,
+            self._arr(tables, i32, (B, max_pages)), max_pages, page, self._arr(lengths, i32, (B,)), first, recent, k, self._arr(picked, i32, (B, H, k))))
 
     def cache_extend(self, tables, lengths, starts, page, n_pages, slots, src, dst, rows):
         """Pages and slots for a step's new rows, starts[b]..starts[b + 1] of sequence b: tables and lengths grow in place, slots int64 [n] is for
         cache_write; src, dst and rows int32 [B] are the copies to make, with cache_copy, of pages that were shared."""
         B, max_pages = tables.shape
         n = slots.shape[0]
-        self._here(tables, lengths, starts, slots, src, dst, rows)
+        i32, i64 = _dtypes()["i32"], _dtypes()["i64"]
         self._chk(lib().hclae_cache_extend(
-            self._h, _ptr(tables, "i32"), _ptr(lengths, "i32", (B,)), B, max_pages, page, n_pages, _ptr(starts, "i32", (B + 1,)), n,
-            _ptr(slots, "i64", (n,)), _ptr(src, "i32", (B,)), _ptr(dst, "i32", (B,)), _ptr(rows, "i32", (B,))))
+            self._h, self._arr(tables, i32, (B, max_pages)), self._arr(lengths, i32, (B,)), B, max_pages, page, n_pages, self._arr(starts, i32, (B + 1,)), n,
+            self._arr(slots, i64, (n,)), self._arr(src, i32, (B,)), self._arr(dst, i32, (B,)), self._arr(rows, i32, (B,))))
 
     def cache_compact(self, tables, lengths, page, n_pages, src, dst, used=None):
         """Moves the pages in use to the front: tables name their new places, src and dst int32 [n_pages // 2] are the copies to make, with
         cache_copy (-1 behind the last), used int32 [1] their number."""
         B, max_pages = tables.shape
-        self._here(tables, lengths, src, dst, used)
+        i32 = _dtypes()["i32"]
         self._chk(lib().hclae_cache_compact(
-            self._h, _ptr(tables, "i32"), _ptr(lengths, "i32", (B,)), B, max_pages, page, n_pages, _ptr(src, "i32", (n_pages // 2,)),
-            _ptr(dst, "i32", (n_pages // 2,)), _ptr(used, "i32", (1,))))
+            self._h, self._arr(tables, i32, (B, max_pages)), self._arr(lengths, i32, (B,)), B, max_pages, page, n_pages, self._arr(src, i32, (n_pages // 2,)),
+            self._arr(dst, i32, (n_pages // 2,)), self._arr(used, i32, (1,))))
 
     def cache_copy(self, codes, scale, page, src, dst, rows=None):
         """Copies the first rows[i] rows (None: all) of page src[i] of codes uint8 [n_slots][H][M] and scale float32 [n_slots][H] (or None) to page
         dst[i]; pages outside the cache copy nothing."""
         n, n_slots, H = src.shape[0], codes.shape[0], self._H or codes.shape[1]
-        self._here(codes, scale, src, dst, rows)
-        self._chk(lib().hclae_cache_copy(self._h, _ptr(codes, "u8", (n_slots, H, self.M)), _ptr(scale, "f32", (n_slots, H)), n_slots, page,
-                                         _ptr(src, "i32", (n,)), _ptr(dst, "i32", (n,)), _ptr(rows, "i32", (n,)), n))
+        u8, i32, f32 = _serving_types()
+        self._chk(lib().hclae_cache_copy(self._h, self._arr(codes, u8, (n_slots, H, self.M)), self._arr(scale, f32, (n_slots, H)), n_slots, page,
+                                         self._arr(src, i32, (n,)), self._arr(dst, i32, (n,)), self._arr(rows, i32, (n,)), n))
 
     # ---- dictionary order and code statistics ---------------------------------------------
     def reorder_by_variance(self, C, codes):
