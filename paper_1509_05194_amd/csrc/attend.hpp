@@ -323,11 +323,15 @@ __host__ __device__ constexpr int codes_most(int RB, bool wide, int MW)
 }
 __host__ __device__ constexpr int codes_threads(int RB, bool wide, int MW) { return codes_most(RB, wide, MW) * (wide ? 12 : 16) <= 72 * 1024 ? 512 : 1024; }
 __host__ __device__ constexpr int codes_words(int RB, bool wide, int MW) { return (codes_most(RB, wide, MW) + codes_threads(RB, wide, MW) - 1) / codes_threads(RB, wide, MW); }
-// Parts of a sequence's rows: as many blocks as the CUs hold at once, `blocks` each, where there are 1024 rows for each.
+// Parts of a sequence's rows: as many blocks as the CUs hold at once, `blocks` each, with 2048 rows each at least, or 512 while there are fewer blocks than CUs.
 __host__ __device__ constexpr int codes_splits(const AttendArgs &a, int RB, int blocks, int cus)
 {
-    const int64_t jobs = (int64_t)a.rows.B * a.G * ((a.R + RB - 1) / RB);
-    int64_t s = (blocks * (int64_t)cus + jobs - 1) / jobs, most = (attend_capacity(a) + 1023) / 1024;
+    const int64_t jobs = (int64_t)a.rows.B * a.G * ((a.R + RB - 1) / RB), rows = attend_capacity(a);
+    int64_t s = (blocks * (int64_t)cus + jobs - 1) / jobs, most = (rows + 2047) / 2048;
+    if (jobs * most < cus) {
+        const int64_t more = (rows + 511) / 512, fill = (cus + jobs - 1) / jobs;
+        most = more < fill ? more : fill;
+    }
     if (s > most) s = most;
     if (s > kCodesSplits) s = kCodesSplits;
     return (int)(s < 1 ? 1 : s);
@@ -380,6 +384,7 @@ __global__ __launch_bounds__(kTableThreads) void k_attend_tables(const AttendArg
 {
     constexpr int PITCH = 32 * NJ + 8, TQ = table_queries(N, NJ);
     __shared__ __attribute__((aligned(16))) __bf16 qs[N][TQ][PITCH];
+    __shared__ int64_t q_at[TQ], tab_at[TQ];
     const int MK = a.M * a.K, RG = (a.R + RB - 1) / RB, groups = (MK + 63) / 64, d4 = a.D >> 2;
     const int h = blockIdx.x / groups, lane = lane_id(), i16 = lane & 15, g = lane >> 4;
     const int cw = (blockIdx.x - h * groups) * 64 + (threadIdx.x >> 6) * 16 + i16;
@@ -396,11 +401,27 @@ __global__ __launch_bounds__(kTableThreads) void k_attend_tables(const AttendArg
         split_floats<3>(w, c[j]);
     }
     for (int stage = blockIdx.y; stage < stages; stage += gridDim.y) {
-        for (int i = threadIdx.x; i < TQ * 8 * NJ; i += kTableThreads) {
-            const int row = i / (8 * NJ), p = i - row * (8 * NJ), n = stage * TQ + row, u = n / RB, b = u / RG, hq = (u - b * RG) * RB + (n - u * RB);
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (n < all && hq < a.R && p < d4) v = T::load(a.Q, (int64_t)b * a.q_row + (int64_t)(h * a.R + hq) * a.q_head + 4 * p);
-            float x[4] = {v.x, v.y, v.z, v.w};
+        const int n0 = stage * TQ;
+        if (threadIdx.x < TQ) {                     // where the stage's queries are, and where their tables go
+            const int n = n0 + (int)threadIdx.x, u = n / RB, b = u / RG, rg = u - b * RG, hq = rg * RB + (n - u * RB);
+            q_at[threadIdx.x] = n < all && hq < a.R ? (int64_t)b * a.q_row + (int64_t)(h * a.R + hq) * a.q_head : -1;
+            tab_at[threadIdx.x] = n < all ? (((int64_t)b * a.G + h) * RG + rg) * tab_row(a.M, a.K, RB) + (n - u * RB) : -1;
+        }
+        __syncthreads();
+        constexpr int PIECES = TQ * 8 * NJ, EACH = PIECES / kTableThreads;
+        static_assert(PIECES % kTableThreads == 0, "whole rounds");
+        float4 v[EACH];
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) {
+            const int i = threadIdx.x + j * kTableThreads, row = i / (8 * NJ), p = i - row * (8 * NJ);
+            const int64_t at = q_at[row];
+            v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (at >= 0 && p < d4) v[j] = T::load(a.Q, at + 4 * p);
+        }
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) {
+            const int i = threadIdx.x + j * kTableThreads, row = i / (8 * NJ), p = i - row * (8 * NJ);
+            float x[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
 #pragma unroll
             for (int k = 0; k < N; ++k) {
                 bf16x4 o;
@@ -413,7 +434,6 @@ __global__ __launch_bounds__(kTableThreads) void k_attend_tables(const AttendArg
             }
         }
         __syncthreads();
-        const int n0 = stage * TQ;
 #pragma unroll 2
         for (int tile = 0; tile < TQ / 16; ++tile) {
             if (n0 + 16 * tile >= all) break;
@@ -428,9 +448,9 @@ __global__ __launch_bounds__(kTableThreads) void k_attend_tables(const AttendArg
             if (cw < MK)
 #pragma unroll
                 for (int e = 0; e < 4; e += RB) {   // queries n0 + 16 tile + 4 g + e of this lane's codeword
-                    const int m = n0 + 16 * tile + 4 * g + e, v = m / RB, bb = v / RG;
-                    if (m >= all) break;
-                    float *to = tab + (((int64_t)bb * a.G + h) * RG + (v - bb * RG)) * tab_row(a.M, a.K, RB) + cw * RB;
+                    const int64_t at = tab_at[16 * tile + 4 * g + e];
+                    if (at < 0) break;
+                    float *to = tab + at + (int64_t)cw * RB;
                     if (RB == 4) *reinterpret_cast<float4 *>(to) = make_float4(s[0] * f, s[1] * f, s[2] * f, s[3] * f);
                     else if (RB == 2) *reinterpret_cast<float2 *>(to) = make_float2(s[e] * f, s[e + 1] * f);
                     else *to = s[e] * f;
