@@ -141,7 +141,7 @@ __global__ __launch_bounds__(kDirectThreads) void k_attend_rows(const AttendArgs
 {
     constexpr int MOST = kDirectGroups * kDirectRows;
     __shared__ float4 q[RB][64], red[RB][kDirectThreads];
-    __shared__ float s[RB][MOST], w[RB][MOST], fade[RB], gk[MOST], gv[MOST];
+    __shared__ float s[RB][MOST], w[RB][MOST], fade[RB], gv[MOST];
     __shared__ int64_t slots[MOST];
     const int RG = (a.R + RB - 1) / RB, d4 = a.D >> 2, H = 2 * a.G, lanes = direct_lanes(a.D), groups = direct_groups(a.D), tile = direct_tile(a.D);
     const int job = blockIdx.x, head = job / splits;
@@ -167,10 +167,7 @@ __global__ __launch_bounds__(kDirectThreads) void k_attend_rows(const AttendArgs
     float top = -INFINITY, sum = 0.f;               // of head `wave`, in every lane of its wave
     for (int64_t t0 = first; t0 < last; t0 += tile) {
         if (threadIdx.x < (unsigned)tile) {
-            const int64_t at = t0 + threadIdx.x < last ? rows.slot((unsigned)(t0 + threadIdx.x)) : kNoRow;
-            slots[threadIdx.x] = at;
-            gk[threadIdx.x] = at >= 0 && a.scale ? a.scale[at * H + h] : 1.f;
-            gv[threadIdx.x] = at >= 0 && a.scale ? a.scale[at * H + a.G + h] : 1.f;
+            slots[threadIdx.x] = t0 + threadIdx.x < last ? rows.slot((unsigned)(t0 + threadIdx.x)) : kNoRow;
         }
         __syncthreads();
         float4 v[kDirectRows];
@@ -180,7 +177,12 @@ __global__ __launch_bounds__(kDirectThreads) void k_attend_rows(const AttendArgs
                 const int i = g + u * groups;
                 const int64_t at = slots[i];
                 float4 k = make_float4(0.f, 0.f, 0.f, 0.f);
+                float g_key = 1.f, g_value = 1.f;
                 v[u] = k;
+                if (at >= 0 && a.scale) {
+                    g_key = a.scale[at * H + h];
+                    g_value = a.scale[at * H + a.G + h];
+                }
                 if (at >= 0 && p < d4) {
                     const uint8_t *code = a.codes + at * H * a.M;
                     k = decode_piece(Ck, code + h * a.M, a.M, a.K, a.D);
@@ -195,9 +197,11 @@ __global__ __launch_bounds__(kDirectThreads) void k_attend_rows(const AttendArgs
                 for (int o = lanes >> 1; o > 0; o >>= 1)
 #pragma unroll
                     for (int r = 0; r < RB; ++r) dot[r] += __shfl_xor(dot[r], o, kWave);
-                if (p == 0)
+                if (p == 0) {
+                    gv[i] = g_value;
 #pragma unroll
-                    for (int r = 0; r < RB; ++r) s[r][i] = dot[r] * gk[i];
+                    for (int r = 0; r < RB; ++r) s[r][i] = dot[r] * g_key;
+                }
             }
         __syncthreads();
         if (wave < RB) {
@@ -905,7 +909,7 @@ __global__ __launch_bounds__(kFoldThreads) void k_attend_fold(const AttendArgs a
     *reinterpret_cast<float4 *>(to) = v;
 }
 
-constexpr int kOutThreads = 512, kOutWaves = kOutThreads / kWave, kOutChunk = 64, kOutPitch = kOutChunk + 8;
+constexpr int kOutThreads = 1024, kOutWaves = kOutThreads / kWave, kOutChunk = 64, kOutPitch = kOutChunk + 8;
 __host__ __device__ constexpr int out_lds(int N, int CW)
 {
     const int rows = kOutWaves * N * 16 * kOutPitch * 2, sums = kOutWaves * 16 * (16 * CW + 1) * 4;
@@ -913,7 +917,7 @@ __host__ __device__ constexpr int out_lds(int N, int CW)
 }
 
 // out = the sums by code times the codewords, over the exponentials' sum: a block 16 query heads and 16 CW coordinates (a lane CW side by side), its waves
-// every eighth 64 codewords each.  A wave lays the 64 sums of 16 query heads out in LDS of its own, the parts added up on the way.
+// every sixteenth 64 codewords each.  A wave lays the 64 sums of 16 query heads out in LDS of its own, the parts added up on the way.
 // Blocks of one XCD (they go round the eight) have neighbouring numbers, which is the same head most often: its codewords stay in that L2.
 // N: bf16 parts of a sum and a codeword, two for outputs of 16 bits and three for floats.
 // span: parts between one sequence's sums and the next; splits: parts to add up, the first of those.
@@ -956,7 +960,7 @@ __global__ __launch_bounds__(kOutThreads, 4) void k_attend_out(const AttendArgs 
         from[j] = sums + (seq_of(n) * span * RB + n % RB) * row;
     }
 #pragma unroll
-    for (int j = 0; j < 16 / kOutWaves; ++j) {      // what a part counts, a wave two query heads
+    for (int j = 0; j < 16 / kOutWaves; ++j) {      // what a part counts, a wave a query head
         const int i = wave * (16 / kOutWaves) + j, n = tile * 16 + i, u = n / RB, b = u / RG, hq = (u - b * RG) * RB + (n - u * RB);
         if (n < all && hq < a.R) {
             const CodesStat x = join_parts(stats + seq_of(n) * splits * RB + n % RB, RB, splits, part[i]);

@@ -286,19 +286,11 @@ __device__ __forceinline__ void compact_plan(const PageArgs &a, const CompactScr
     const int64_t wn = n >> 5;
     const unsigned low = wn < words ? s.before[wn] + (unsigned)__popc(s.used[wn] & ((1u << (n & 31)) - 1u)) : n;
     const unsigned moves = n - low;
-    for (int64_t w = threadIdx.x; w < words; w += kPlanThreads) {
-        const unsigned used = s.used[w], upto = s.before[w];
-        const int64_t p0 = w * 32;
-        const unsigned front = p0 + 32 <= n ? ~0u : p0 >= n ? 0u : (1u << (n - p0)) - 1u;     // pages below n
-        for (unsigned left = ~used & front; left; left &= left - 1u) {
-            const int bit = __ffs(left) - 1;
-            const int64_t hole = p0 + bit - (upto + __popc(used & ((1u << bit) - 1u)));       // holes before this one
-            a.dst[hole] = (int32_t)(p0 + bit);
-        }
-        for (unsigned left = used & ~front; left; left &= left - 1u) {
-            const int bit = __ffs(left) - 1;
-            a.src[upto + __popc(used & ((1u << bit) - 1u)) - low] = (int32_t)(p0 + bit);
-        }
+    for (int64_t p = threadIdx.x; p < a.n_pages; p += kPlanThreads) {
+        const unsigned used = s.used[p >> 5], bit = (unsigned)(p & 31), upto = s.before[p >> 5] + (unsigned)__popc(used & ((1u << bit) - 1u));    // pages in use before it
+        if (used >> bit & 1u) {
+            if (p >= n) a.src[upto - low] = (int32_t)p;
+        } else if (p < n) a.dst[p - upto] = (int32_t)p;     // as many holes are before it
     }
     for (int64_t i = moves + threadIdx.x; i < a.n_pages / 2; i += kPlanThreads) a.src[i] = a.dst[i] = -1;
 }
