@@ -84,8 +84,12 @@ struct SeqRows {
     }
 };
 
-// Numbers of rows at most, over all sequences.
-__host__ __device__ constexpr int64_t attend_capacity(const AttendArgs &a) { return (int64_t)(a.picked ? a.n_picked : a.rows.max_pages) * a.rows.page; }
+// Numbers of rows at most, over all sequences; lengths are below 2^31.
+__host__ __device__ constexpr int64_t attend_capacity(const AttendArgs &a)
+{
+    const int64_t rows = (int64_t)(a.picked ? a.n_picked : a.rows.max_pages) * a.rows.page;
+    return rows < 1ll << 31 ? rows : 1ll << 31;
+}
 
 constexpr int kDirectThreads = 256, kDirectSplits = 256, kDirectRows = 2, kDirectGroups = 32;
 
@@ -496,7 +500,6 @@ struct CodesArgs {
     bool grouped;                                   // blocks go round the eight XCDs: those that read the same rows to one of them
     bool words;                                     // every row's codes are whole, aligned words
     bool small;                                     // offsets within a page fit 32 bits, and its rows 24
-    bool by_wave;                                   // the 64 rows of a wave are in one page
     const float *tab;
     CodesStat *stats;
     float *sums;
@@ -509,8 +512,9 @@ struct CodesArgs {
 // by a fraction that goes round with the row (the golden ratio's multiples), so that many small weights add up to what they are: the error of a sum of n is about
 // sqrt(n) / 4 steps.  bf16 and fp16 outputs have steps of 2^-8 and 2^-11.  float outputs take 64 bits a query head, steps of 2^-40.  A block looks for the largest
 // score and weight of a window only if one of them is beyond what the last ones allow for.
-// FULL: K = 256 and 4 MW dictionaries, whole aligned words: the offsets in LDS are in the instructions.
-template <int RB, bool WIDE, int MW, bool FULL>
+// FULL: K = 256 and 4 MW dictionaries, whole aligned words: the offsets in LDS are in the instructions.  BY_WAVE: pages of multiples of 64 rows: the rows of a wave are
+// in one page, found in scalar registers.
+template <int RB, bool WIDE, int MW, bool FULL, bool BY_WAVE>
 __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes(const AttendArgs a, const CodesArgs x)
 {
     constexpr int kCodesThreads = codes_threads(RB, WIDE, MW), kCodesRows = kWindow / kCodesThreads, kCodesWaves = kCodesThreads / kWave;
@@ -574,7 +578,7 @@ __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes
     float acc[NW][WIDE ? 1 : 2] = {};
     constexpr float top_step = WIDE ? 0x1p40f : 0x1p19f;
     static_assert(kWideBits == 40 && kPairBits == 19, "the same");
-    float ref[RB], unit[RB], back[RB], largest[RB], sum[RB];   // reference of the scores, steps in 1 and their size, log2 of the largest weight
+    float ref[RB], unit[RB], back[RB], largest[RB], sum[RB];   // reference of the scores, steps in 1 and their size, log2 of the largest weight so far
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
         ref[r] = largest[r] = -INFINITY;
@@ -593,7 +597,7 @@ __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes
 #pragma unroll
         for (int i = 0; i < kCodesRows; ++i) {
             unsigned off = 0, q = ~0u;
-            if (x.by_wave) {
+            if (BY_WAVE) {
                 const unsigned t = __builtin_amdgcn_readfirstlane(w + i * kCodesThreads + wave * kWave);
                 int64_t at = 0;
                 if (t < last) q = __builtin_amdgcn_readfirstlane(rows.where_wave(t, off, at));
@@ -616,7 +620,7 @@ __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes
             if (!there_next[i]) continue;
             const uint8_t *kp = a.codes + h * M;
             const float *gp = a.scale;
-            if (x.by_wave) {
+            if (BY_WAVE) {
                 const uint64_t row = (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane(page_next[i]) * (unsigned)a.rows.page + (unsigned)__builtin_amdgcn_readfirstlane(off_next[i]);
                 kp += row * (unsigned)(H * M) + lane_codes;
                 gp += row * (unsigned)H + lane_scales;
@@ -718,35 +722,37 @@ __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes
         float fade[RB];
 #pragma unroll
         for (int r = 0; r < RB; ++r) fade[r] = 1.f;
-        if (grow[turn_of]) {                        // the largest of the window, over the block
-            float top[RB], most[RB];
-#pragma unroll
-            for (int r = 0; r < RB; ++r) top[r] = most[r] = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < kCodesRows; ++i) {
-                if (!there[i]) continue;
-                const float lg = __builtin_amdgcn_logf(fabsf(gv[i]));
-#pragma unroll
-                for (int r = 0; r < RB; ++r) {
-                    top[r] = fmaxf(top[r], s[i][r]);
-                    most[r] = fmaxf(most[r], s[i][r] + lg);
-                }
-            }
+        if (grow[turn_of]) {                        // the largest score of the window over the block, then the largest weight
+            float now[RB];
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
-                const float t = key_max<6>(float_key(top[r])), m = key_max<6>(float_key(most[r]));
-                if (lane == 0) red[r][wave] = make_float2(t, m);
+                float top = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < kCodesRows; ++i)
+                    if (there[i]) top = fmaxf(top, s[i][r]);
+                top = key_max<6>(float_key(top));
+                if (lane == 0) red[r][wave].x = top;
             }
             __syncthreads();
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
-                const float2 f = red[r][min(lane, kCodesWaves - 1)];
-                const float t = key_max<4>(float_key(f.x)), now = fmaxf(ref[r], t);
-                largest[r] = fmaxf(key_max<4>(float_key(f.y)), largest[r]);
-                fade[r] = ref[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref[r] - now);
-                ref[r] = now;
+                now[r] = fmaxf(ref[r], key_max<4>(float_key(red[r][min(lane, kCodesWaves - 1)].x)));
+                float most = -INFINITY;             // log2 of the weights that the reference makes
+#pragma unroll
+                for (int i = 0; i < kCodesRows; ++i)
+                    if (there[i]) most = fmaxf(most, (s[i][r] - now[r]) + __builtin_amdgcn_logf(fabsf(gv[i])));
+                most = key_max<6>(float_key(most));
+                if (lane == 0) red[r][wave].y = most;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                const float move = ref[r] - now[r];
+                fade[r] = ref[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(move);
+                largest[r] = fmaxf(largest[r] == -INFINITY ? largest[r] : largest[r] + move, key_max<4>(float_key(red[r][min(lane, kCodesWaves - 1)].y)));
+                ref[r] = now[r];
                 // weights up to 2^e; only zeros: any step
-                const float e = largest[r] == -INFINITY ? 0.f : fminf(fmaxf(ceilf(largest[r] - now + 0.01f), -100.f), 140.f);
+                const float e = largest[r] == -INFINITY ? 0.f : fminf(fmaxf(ceilf(largest[r] + 0.01f), -100.f), 140.f);
                 const int n = min((WIDE ? kWideBits : kPairBits) - (int)e, 120);
                 unit[r] = ldexpf(1.f, n);
                 back[r] = ldexpf(1.f, -n);
@@ -777,6 +783,10 @@ __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes
                     add[q] = (unsigned long long)(unsigned)(hi + (lo >> 31)) << 32 | (unsigned)lo;
                 }
             }
+            unsigned long long any = add[0];
+#pragma unroll
+            for (int q = 1; q < P; ++q) any |= add[q];
+            if (any == 0) continue;                 // weights that are no step: rows that hardly count do not meet at banks
 #pragma unroll
             for (int m = 0; m < 4 * MW; ++m)
                 if (m < M) {

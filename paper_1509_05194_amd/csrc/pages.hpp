@@ -47,20 +47,21 @@ __global__ __launch_bounds__(kPageThreads) void k_pages_clear(unsigned *words, i
 }
 
 constexpr int kMarkEntries = 1024;                  // entries of one table that a block looks at at a time
+__host__ __device__ constexpr int table_chunks(int max_pages) { return (int)(((int64_t)max_pages + kMarkEntries - 1) / kMarkEntries); }
 
 // The live entries of a table from j0 on, those of one thread of `threads`: f(entry's place, page).
 template <typename F>
-__device__ __forceinline__ void live_entries(const PageArgs &a, int b, int j0, int j1, int live, int thread, int threads, F f)
+__device__ __forceinline__ void live_entries(const PageArgs &a, int b, int64_t j0, int64_t j1, int live, int thread, int threads, F f)
 {
     const int32_t *table = a.tables + (int64_t)b * a.max_pages;
-    const int end = min(j1, live);
-    for (int j = j0 + thread; j < end; j += 4 * threads) {
+    const int64_t end = j1 < live ? j1 : live;
+    for (int64_t j = j0 + thread; j < end; j += 4 * threads) {
         int32_t p[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) p[i] = j + i * threads < end ? table[j + i * threads] : -1;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (p[i] >= 0 && p[i] < a.n_pages) f(j + i * threads, p[i]);
+            if (p[i] >= 0 && p[i] < a.n_pages) f((int)(j + i * threads), p[i]);
     }
 }
 __device__ __forceinline__ void mark_page(unsigned *used, unsigned *shared, int32_t p)
@@ -71,28 +72,30 @@ __device__ __forceinline__ void mark_page(unsigned *used, unsigned *shared, int3
 
 __global__ __launch_bounds__(kPageThreads) void k_pages_mark(const PageArgs a, unsigned *used, unsigned *shared)
 {
-    const int chunks = (a.max_pages + kMarkEntries - 1) / kMarkEntries;
+    const int chunks = table_chunks(a.max_pages);
     const int64_t jobs = (int64_t)a.B * chunks;
     for (int64_t job = blockIdx.x; job < jobs; job += gridDim.x) {
-        const int b = (int)(job / chunks), j0 = (int)(job - (int64_t)b * chunks) * kMarkEntries;
+        const int b = (int)(job / chunks);
+        const int64_t j0 = (job - (int64_t)b * chunks) * kMarkEntries;
         const int live = pages_of(held(a.lengths[b], a.max_pages, a.page), a.page);
         live_entries(a, b, j0, j0 + kMarkEntries, live, threadIdx.x, kPageThreads, [&](int, int32_t p) { mark_page(used, shared, p); });
     }
 }
 
-// Inclusive sum over the block; *total: that of all.  sums: 17 words of LDS.
-__device__ __forceinline__ unsigned block_scan(unsigned v, unsigned *sums, unsigned *total)
+// Inclusive sum over the block; *total: that of all.  sums: 16 numbers in LDS.
+template <typename N>
+__device__ __forceinline__ N block_scan(N v, N *sums, N *total)
 {
     const int lane = lane_id(), wave = threadIdx.x >> 6;
-    unsigned x = v;
+    N x = v;
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) {
-        const unsigned y = __shfl_up(x, o, kWave);
+        const N y = __shfl_up(x, o, kWave);
         if (lane >= o) x += y;
     }
     if (lane == kWave - 1) sums[wave] = x;
     __syncthreads();
-    unsigned before = 0, all = 0;
+    N before = 0, all = 0;
     const int waves = blockDim.x >> 6;
     for (int w = 0; w < waves; ++w) {
         if (w < wave) before += sums[w];
@@ -116,40 +119,43 @@ __device__ __forceinline__ bool last_page_shared(const PageArgs &a, int b, const
     return p >= 0 && p < a.n_pages && (shared[p >> 5] >> (p & 31) & 1u);
 }
 
-// By one block: how many pages the sequences up to each ask for, and that many free pages, the lowest first.
-__device__ __forceinline__ void extend_plan(const PageArgs &a, const ExtendScratch &s, unsigned *sums)
+// By one block: how many pages the sequences up to each ask for, and that many free pages, the lowest first.  Whatever `starts` holds, no more than `room`
+// pages are given: sums are in 64 bits, and those beyond 32 are more than there are.
+__device__ __forceinline__ void extend_plan(const PageArgs &a, const ExtendScratch &s, unsigned long long *sums)
 {
-    unsigned asked = 0;
+    typedef unsigned long long u64;
+    u64 asked = 0;
     for (int64_t b0 = 0; b0 < a.B; b0 += kPlanThreads) {
         const int b = (int)(b0 + threadIdx.x);
-        unsigned need = 0, all;
+        u64 need = 0, all;
         if (b < a.B) {
             const Growth g(a, b);
             int32_t at;
-            if (g.fits) need = (unsigned)(g.new_pages - g.old_pages) + (last_page_shared(a, b, g, s.shared, &at) ? 1u : 0u);
+            if (g.fits) need = (u64)(g.new_pages - g.old_pages) + (last_page_shared(a, b, g, s.shared, &at) ? 1u : 0u);
         }
-        const unsigned upto = asked + block_scan(need, sums, &all);
-        if (b < a.B) s.upto[b] = upto;
+        const u64 upto = asked + block_scan(need, sums, &all);
+        if (b < a.B) s.upto[b] = (unsigned)min(upto, (u64)0xffffffffu);
         asked += all;
     }
-    unsigned found = 0;
+    u64 found = 0;
     const int64_t words = words_of(a.n_pages);
     for (int64_t w0 = 0; w0 < words && found < asked; w0 += kPlanThreads) {
         const int64_t w = w0 + threadIdx.x;
-        unsigned left = 0, all;
+        unsigned left = 0;
+        u64 all;
         if (w < words) {
             left = ~s.used[w];
             if (w == words - 1 && (a.n_pages & 31)) left &= (1u << (a.n_pages & 31)) - 1u;
         }
-        const unsigned here = __popc(left);
-        unsigned at = found + block_scan(here, sums, &all) - here;
+        const u64 here = (u64)__popc(left);
+        u64 at = found + block_scan(here, sums, &all) - here;
         while (left && at < asked && at < s.room) {
             s.free[at++] = (unsigned)(w * 32 + (__ffs(left) - 1));
             left &= left - 1u;
         }
         found += all;
     }
-    if (threadIdx.x == 0) *s.found = found;
+    if (threadIdx.x == 0) *s.found = (unsigned)min(found, (u64)s.room);
 }
 
 // By one thread or wave: a sequence's rows' slots, its new entries, its length.  What is read of its table is read before anything is written.
@@ -195,7 +201,7 @@ __device__ __forceinline__ void extend_others(const PageArgs &a, int64_t at, int
 
 __global__ __launch_bounds__(kPlanThreads) void k_extend_plan(const PageArgs a, const ExtendScratch s)
 {
-    __shared__ unsigned sums[17];
+    __shared__ unsigned long long sums[kPlanThreads / kWave];
     extend_plan(a, s, sums);
 }
 
@@ -240,7 +246,8 @@ __device__ __forceinline__ void live_of(const PageArgs &a, unsigned *live)
 __global__ __launch_bounds__(kPlanThreads) void k_extend_block(const PageArgs a, unsigned room)
 {
     extern __shared__ unsigned page_lds[];
-    __shared__ unsigned sums[17], found;
+    __shared__ unsigned long long sums[kPlanThreads / kWave];
+    __shared__ unsigned found;
     const int words = (int)words_of(a.n_pages);
     const ExtendScratch s = {page_lds, page_lds + words, page_lds + 2 * words, page_lds + 2 * words + 2 * a.B, &found, room};
     unsigned *live = page_lds + 2 * words + a.B;
@@ -312,17 +319,18 @@ struct NewPlaces {
 
 __global__ __launch_bounds__(kPlanThreads) void k_compact_plan(const PageArgs a, const CompactScratch s)
 {
-    __shared__ unsigned sums[17];
+    __shared__ unsigned sums[kPlanThreads / kWave];
     compact_plan(a, s, sums);
 }
 
 __global__ __launch_bounds__(kPageThreads) void k_compact_tables(const PageArgs a, const CompactScratch s)
 {
     const NewPlaces places(a, s);
-    const int chunks = (a.max_pages + kMarkEntries - 1) / kMarkEntries;
+    const int chunks = table_chunks(a.max_pages);
     const int64_t jobs = (int64_t)a.B * chunks;
     for (int64_t job = blockIdx.x; job < jobs; job += gridDim.x) {
-        const int b = (int)(job / chunks), j0 = (int)(job - (int64_t)b * chunks) * kMarkEntries;
+        const int b = (int)(job / chunks);
+        const int64_t j0 = (job - (int64_t)b * chunks) * kMarkEntries;
         const int live = pages_of(held(a.lengths[b], a.max_pages, a.page), a.page);
         live_entries(a, b, j0, j0 + kMarkEntries, live, threadIdx.x, kPageThreads, [&](int j, int32_t p) { places.entry(a, s, b, j, p); });
     }
@@ -336,7 +344,7 @@ __host__ __device__ constexpr bool compact_in_block(const PageArgs &a)
 __global__ __launch_bounds__(kPlanThreads) void k_compact_block(const PageArgs a)
 {
     extern __shared__ unsigned page_lds[];
-    __shared__ unsigned sums[17];
+    __shared__ unsigned sums[kPlanThreads / kWave];
     const int words = (int)words_of(a.n_pages);
     const CompactScratch s = {page_lds, page_lds + words, page_lds + 2 * words};
     unsigned *live = page_lds + 3 * words;

@@ -32,7 +32,7 @@ hipError_t raise_lds(K kern, int bit, uint64_t *raised, int bytes = kServeLds)
 
 constexpr int kPickLds = 136 * 1024;                // as above: k_select_pages declares 20 KB
 
-enum RaisedBit { kRaisedSelect = 0, kRaisedCodes = 1, kRaisedOut = 31, kRaisedPages = 49 };         // 30 from kRaisedCodes on, 18 from kRaisedOut on
+enum RaisedBit { kRaisedSelect = 0, kRaisedCodes = 1, kRaisedOut = 36, kRaisedPages = 54 };         // 35 from kRaisedCodes on, 18 from kRaisedOut on
 
 // ---- attention ----------------------------------------------------------------------------------
 
@@ -71,11 +71,16 @@ AttendArgs round_of(const AttendArgs &a, int b0, int n, int bytes)
     return r;
 }
 
-// Whether the rows go through tables: not where a sequence can have few rows only, which are decoded before the tables are there.
-constexpr int64_t kFewRows = 512;
+// Whether the rows go through tables: not where a sequence can have few rows only, which are decoded before the tables are there, unless there are many such
+// sequences.  G = 8, R = 4, D = 128, K = 256, bf16 in pages of 16, us decoded and through tables, in a graph: one sequence, M = 8, 64 rows 15.6 and 20.6, 128 rows 16.5 and
+// 20.7, 256 rows 18.9 and 20.8, 384 rows 23.5 and 21.6, 2048 rows 63 and 24; M = 16, 128 rows 22.9 and 29.6, 256 rows 36 and 30; R = 1, 256 rows 16.4 and 17.9, 384
+// rows 20.2 and 18.4; fp32, 256 rows 18.8 and 24.8, 384 rows 23.5 and 25.0 (the rule: tables); K = 64, 256 rows 18.7 and 18.6.  32 sequences, M = 8, 64 rows 27.8 and 36.8,
+// 128 rows 43.6 and 36.5, 2048 rows 481 and 44.
+constexpr int64_t kFewRows = 320, kFewInAll = 96 * 256;
 CodesPlan plan_of(const AttendArgs &a, int type)
 {
-    if (attend_capacity(a) <= kFewRows) return {0, false, 0, 0};
+    const int64_t rows = attend_capacity(a) * std::max(8, a.M) / 8, RB = heads_at_once(a.R);
+    if (rows <= kFewRows && rows * a.rows.B * a.G * ((a.R + RB - 1) / RB) <= kFewInAll) return {0, false, 0, 0};
     return codes_plan(a.R, a.M, a.K, type == kRowF32);
 }
 
@@ -93,11 +98,11 @@ CodesRoom codes_room(const AttendArgs &a, const CodesPlan &plan, int splits)
     return {up(sizeof(float) * seqs * tab_row(a.M, a.K, plan.RB)), up(sizeof(CodesStat) * rows), up(sizeof(float) * rows * sums_row(a.M, a.K)), up(sizeof(CodesStat) * seqs * plan.RB)};
 }
 
-template <int RB, bool WIDE, int MW, bool FULL>
+template <int RB, bool WIDE, int MW, bool FULL, bool BY_WAVE>
 hipError_t launch_codes_as(const AttendArgs &a, const CodesPlan &plan, const CodesArgs &x, uint64_t *raised, hipStream_t stream)
 {
-    constexpr int bit = kRaisedCodes + (FULL ? 15 : 0) + (MW == 2 ? 0 : MW == 4 ? 5 : 10) + (RB == 1 ? 0 : RB == 2 ? 1 : 3) + (RB > 1 && WIDE ? 1 : 0);
-    auto kern = &k_attend_codes<RB, WIDE, MW, FULL>;
+    constexpr int bit = kRaisedCodes + (BY_WAVE ? 25 : FULL ? 15 : 0) + (MW == 2 ? 0 : MW == 4 ? 5 : 10) + (RB == 1 ? 0 : RB == 2 ? 1 : 3) + (RB > 1 && WIDE ? 1 : 0);
+    auto kern = &k_attend_codes<RB, WIDE, MW, FULL, BY_WAVE>;
     TRY(raise_lds(kern, bit, raised));
     const int64_t heads = (int64_t)a.G * ((a.R + RB - 1) / RB), units = (int64_t)a.rows.B * x.splits;
     hipLaunchKernelGGL(kern, dim3((unsigned)((x.grouped ? (units + 7) / 8 * 8 : units) * heads)), dim3(codes_threads(RB, WIDE, MW)), plan.lds, stream, a, x);
@@ -108,9 +113,13 @@ hipError_t launch_codes(const AttendArgs &a, const CodesPlan &plan, int splits, 
 {
     const int64_t row = 2ll * a.G * a.M;
     const CodesArgs x = {splits, (int64_t)a.rows.B * splits >= 32, a.M % 4 == 0 && reinterpret_cast<uintptr_t>(a.codes) % 4 == 0,
-                         a.rows.page < 1 << 24 && a.rows.page * row < (int64_t)1 << 32, a.rows.page % kWave == 0 && !a.begins, tab, stats, sums};
-    if (MW <= 4 && a.K == 256 && a.M == 4 * MW && x.words) return launch_codes_as<RB, WIDE, MW <= 4 ? MW : 4, true>(a, plan, x, raised, stream);
-    return launch_codes_as<RB, WIDE, MW, false>(a, plan, x, raised, stream);
+                         a.rows.page < 1 << 24 && a.rows.page * row < (int64_t)1 << 32, tab, stats, sums};
+    if constexpr (MW <= 4) {
+        if (a.K == 256 && a.M == 4 * MW && x.words)
+            return a.rows.page % kWave == 0 && !a.begins ? launch_codes_as<RB, WIDE, MW, true, true>(a, plan, x, raised, stream)
+                                                         : launch_codes_as<RB, WIDE, MW, true, false>(a, plan, x, raised, stream);
+    }
+    return launch_codes_as<RB, WIDE, MW, false, false>(a, plan, x, raised, stream);
 }
 
 template <typename T, int RB>
@@ -226,7 +235,7 @@ size_t bitmap_bytes(const PageArgs &a) { return up(4 * (size_t)words_of(a.n_page
 
 dim3 table_blocks(const PageArgs &a, int cus)
 {
-    const int64_t jobs = (int64_t)a.B * ((a.max_pages + kMarkEntries - 1) / kMarkEntries);
+    const int64_t jobs = (int64_t)a.B * table_chunks(a.max_pages);
     return dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(jobs, 8ll * cus)));
 }
 
