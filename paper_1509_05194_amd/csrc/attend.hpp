@@ -674,8 +674,8 @@ __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes
         for (int i = 0; i < kCodesRows; ++i) there[i] = there_next[i];
         float s[kCodesRows][RB], v[kCodesRows][RB];
         locate(w0 + kWindow);
-        bool beyond = false;
         float here[RB];                             // the window's sums of exponentials
+        float highest = 0.f, heaviest = 0.f;        // score above its reference, weight in steps; NaN are passed over
         // weights in steps (WIDE: as they are), with the fraction that decides which way they are rounded
         auto weigh = [&](int i) {
             const float turn = (float)(((w0 + i * kCodesThreads + threadIdx.x) * 0x9E3779B9u) >> 8) * 0x1p-24f;
@@ -684,7 +684,8 @@ __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes
                 const float e = s[i][r] - ref[r], p = __builtin_amdgcn_exp2f(e), w = p * gv[i];
                 here[r] += p;
                 v[i][r] = WIDE ? w : w * unit[r] + turn;
-                beyond |= e > kRoom || fabsf(WIDE ? w * unit[r] : v[i][r]) > top_step;
+                highest = fmaxf(highest, e);
+                heaviest = fmaxf(heaviest, fabsf(WIDE ? w * unit[r] : v[i][r]));
             }
         };
 #pragma unroll
@@ -717,13 +718,10 @@ __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes
             bad |= !(fabsf(gv[i]) < INFINITY);
             weigh(i);
         }
-        if (beyond) grow[turn_of] = 1;              // the same value from whoever writes
+        if (highest > kRoom || heaviest > top_step) grow[turn_of] = 1;              // the same value from whoever writes
         __syncthreads();
-        float fade[RB];
-#pragma unroll
-        for (int r = 0; r < RB; ++r) fade[r] = 1.f;
         if (grow[turn_of]) {                        // the largest score of the window over the block, then the largest weight
-            float now[RB];
+            float now[RB], fade[RB];
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
                 float top = -INFINITY;
@@ -758,6 +756,21 @@ __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes
                 back[r] = ldexpf(1.f, -n);
                 sum[r] *= fade[r];
                 here[r] = 0.f;
+            }
+#pragma unroll
+            for (int j = 0; j < NW; ++j) {
+                const int q = (int)(pairs >> (2 * j) & 3);
+                if (WIDE) {
+                    float f = fade[0];
+#pragma unroll
+                    for (int r = 1; r < RB; ++r)
+                        if (q == r) f = fade[r];
+                    acc[j][0] *= f;
+                } else {
+                    const bool second = RB == 4 && q == 1;
+                    acc[j][0] *= second ? fade[RB == 4 ? 2 : 0] : fade[0];
+                    acc[j][WIDE ? 0 : 1] *= second ? fade[RB - 1] : fade[RB >= 2 ? 1 : 0];
+                }
             }
 #pragma unroll
             for (int i = 0; i < kCodesRows; ++i)
@@ -805,19 +818,16 @@ __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes
             const unsigned long long w = hist[i];
             hist[i] = 0;
             if (WIDE) {
-                float f = fade[0], o = back[0];
+                float o = back[0];
 #pragma unroll
                 for (int r = 1; r < RB; ++r)
-                    if (q == r) {
-                        f = fade[r];
-                        o = back[r];
-                    }
-                acc[j][0] = acc[j][0] * f + (float)((double)(long long)w * (double)o);
+                    if (q == r) o = back[r];
+                acc[j][0] += (float)((double)(long long)w * (double)o);
             } else {
                 const int lo = (int)(unsigned)w, hi = (int)((unsigned)(w >> 32) + ((unsigned)w >> 31));
                 const bool second = RB == 4 && q == 1;
-                acc[j][0] = acc[j][0] * (second ? fade[RB == 4 ? 2 : 0] : fade[0]) + (float)lo * (second ? back[RB == 4 ? 2 : 0] : back[0]);
-                acc[j][WIDE ? 0 : 1] = acc[j][WIDE ? 0 : 1] * (second ? fade[RB - 1] : fade[RB >= 2 ? 1 : 0]) + (float)hi * (second ? back[RB - 1] : back[RB >= 2 ? 1 : 0]);
+                acc[j][0] += (float)lo * (second ? back[RB == 4 ? 2 : 0] : back[0]);
+                acc[j][WIDE ? 0 : 1] += (float)hi * (second ? back[RB - 1] : back[RB >= 2 ? 1 : 0]);
             }
         }
 #pragma unroll
