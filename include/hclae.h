@@ -442,7 +442,9 @@ int hclae_lookup_grad(hclae_ctx *ctx, const int64_t *rows, int64_t T, const uint
  * layer's), hclae_cache_write into the slots, and hclae_cache_attend.
  *
  * These calls only enqueue.  Their scratch is in the ctx: a call that needs more than any before allocates it (what it
- * replaces is kept until hclae_destroy, so that recorded graphs stay valid); while the stream is being captured such a call returns HCLAE_ESTATE
+ * replaces is kept until hclae_destroy, so that recorded graphs stay valid): for attention 8 M K bytes a query head, of 16384 at a time, and
+ * up to 64 times half of that where few sequences are taken in many parts; for the choice of pages 8 (M K + max_pages) bytes a sequence and key head, 256 MB at most
+ * unless one sequence needs more; for pages n_pages / 4 bytes and some words a sequence; while the stream is being captured such a call returns HCLAE_ESTATE
  * and enqueues nothing, so a call of the same sizes is made before.  Calls of one ctx share the scratch: two recorded ones must not run at
  * the same time.  They run on the device of the ctx, whichever is current.  Equal calls give equal bits.
  */
@@ -483,7 +485,7 @@ int hclae_cache_select(hclae_ctx *ctx, const void *Q, int type, int B, int Hq, i
  * Pages and slots for the new rows of a step.  Sequence b gets rows starts[b] .. starts[b + 1] - 1 of the batch's n (DEVICE int32[B + 1],
  * ascending): its length grows by their number, its table gets the pages they need, the lowest that no sequence uses, in the
  * order of the sequences, and slots[i] (DEVICE int64[n], for hclae_cache_write) is where row i goes, -1 where it is not kept: rows of no
- * sequence, and all rows of a sequence that cannot be served, whose table and length stay as they are.  These are one whose table has no
+ * sequence, rows that go to an entry of the table that names no page, and all rows of a sequence that cannot be served, whose table and length stay as they are.  These are one whose table has no
  * entries left, and one that asks for pages when those asked for up to it (without the sequences whose tables are full) are more than are free.
  *   A sequence that adds rows to a page that others name too gets a page of its own instead: page src[b] is to be copied to dst[b], its
  * first rows[b] rows (DEVICE int32[B] each; -1, -1, 0 where nothing is), with hclae_cache_copy, before the rows are written.

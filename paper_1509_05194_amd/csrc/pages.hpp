@@ -212,7 +212,8 @@ __global__ __launch_bounds__(kPageThreads) void k_extend_rows(const PageArgs a, 
     extend_others(a, (int64_t)blockIdx.x * kPageThreads + threadIdx.x, (int64_t)gridDim.x * kPageThreads);
 }
 
-// All of it by one block: bitmaps, sums and the list of free pages in LDS.
+// All of it by one block: bitmaps, sums and the list of free pages in LDS.  64 sequences of 1000 to 2000 rows in pages of 16 take 10 us (the four kernels 15, and three
+// launches more), 256 of 2000 to 4000 in pages of 64 14 us; with a wave a table in place of all entries at once 17 and 50.
 constexpr int kBlockLds = 128 * 1024, kBlockEntries = 32768, kBlockRows = 16384, kFewNew = 16;
 __host__ __device__ constexpr int64_t extend_lds(const PageArgs &a, int64_t room) { return 4 * (2 * words_of(a.n_pages) + 2 * (int64_t)a.B + room); }
 __host__ __device__ constexpr bool extend_in_block(const PageArgs &a, int64_t room)
@@ -336,7 +337,7 @@ __global__ __launch_bounds__(kPageThreads) void k_compact_tables(const PageArgs 
     }
 }
 
-// All of it by one block, as k_extend_block.
+// All of it by one block, as k_extend_block: 24600 pages and 128 tables of 128 entries 18 us, 250 pages 5 us (the four kernels 19 and 10).
 __host__ __device__ constexpr bool compact_in_block(const PageArgs &a)
 {
     return (int64_t)a.B * a.max_pages <= kBlockEntries && a.B <= 8192 && a.n_pages <= 65536;
@@ -368,7 +369,7 @@ __device__ __forceinline__ void copy_stretch(char *to, const char *from, int64_t
     for (int64_t i = whole * (int64_t)sizeof(V) + threadIdx.x; i < bytes; i += kPageThreads) to[i] = from[i];
 }
 
-// parts: blocks a page, each a part of its rows.
+// parts: blocks a page, each a part of its rows.  5800 pages of 12 KB among 12300 entries, most of the others -1: 27 us, 5.2 TB/s read and written (a large copy: 5.0).
 __global__ __launch_bounds__(kPageThreads) void k_pages_copy(const CopyArgs a, int parts)
 {
     const int64_t jobs = a.n * parts;

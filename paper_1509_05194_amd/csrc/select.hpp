@@ -16,7 +16,8 @@ typedef double doublex4 __attribute__((ext_vector_type(4)));
 
 // t on the fp64 matrix cores, a wave 16 codewords of a head and 16 sequences.  The 4 x 4 blocks of an instruction take coordinates 16 j + 4 g + e, g the
 // quarter of the wave: a lane so loads four of its codeword side by side; the queries' sums come through LDS.  Of the result a lane holds codewords
-// g, 4 + g, 8 + g and 12 + g of one sequence.
+// g, 4 + g, 8 + g and 12 + g of one sequence.  8 key heads, D = 128, M = 8, K = 256: 5.8 us for one sequence, 9.8 for 32 (134 M products; a codeword a thread, eight
+// sequences at a time: 12.4 and 17).
 template <typename T>
 __global__ __launch_bounds__(kSelectThreads) void k_select_tables(const SelectArgs a, double *tab)
 {
@@ -81,7 +82,9 @@ constexpr int kDigitBits = 12, kDigits = 1 << kDigitBits, kFew = 64;
 __host__ __device__ constexpr size_t pick_lds(int M, int K, int max_pages) { return 8 * ((size_t)M * K + max_pages); }
 
 // A block a sequence and head.  IN_LDS: the tables and keys fit there.  The k-th largest key is found by digits of 12 bits (scores of one query differ in
-// their exponents and a few bits more: two digits leave a handful), the last 64 undecided are ranked one against all.
+// their exponents and a few bits more: two digits leave a handful), the last 64 undecided are ranked one against all.  Eight lists of 125 pages 10 us, 256
+// lists of 1024 to 2048 pages 24 us, 8 of it codes and scales that lie anywhere, 3 the first digit's counts (few exponents: many lanes at one word), 3 a second digit, 2 the
+// order of the pages.  Digits of 8 bits took 20 us with less spread scores and five rounds; ranking up to 256 undecided through LDS took 37.
 template <bool IN_LDS>
 __global__ __launch_bounds__(kPickThreads) void k_select_pages(const SelectArgs a, const double *tab, uint64_t *key_room)
 {
