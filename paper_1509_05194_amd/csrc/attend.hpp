@@ -472,7 +472,7 @@ __global__ __launch_bounds__(kTableThreads) void k_attend_tables(const AttendArg
     }
 }
 
-// Floats as whole numbers in the same order, and back (no NaN); the largest over the first `1 << STEPS` lanes, in every lane.
+// Floats as whole numbers in the same order, and back (no NaN); the largest over the wave (STEPS 6) or its first 16 lanes (4), in every lane.
 __device__ __forceinline__ int float_key(float x)
 {
     const int i = __float_as_int(x);
@@ -595,7 +595,7 @@ __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes
         sum[r] = 0.f;
     }
     bool bad = false;
-    const unsigned page_codes = (unsigned)(a.rows.page * H * M), page_scales = (unsigned)(a.rows.page * H);
+    const unsigned page_codes = (unsigned)a.rows.page * (unsigned)(H * M), page_scales = (unsigned)a.rows.page * (unsigned)H;   // used where they fit
     const unsigned lane_codes = (unsigned)(lane * H * M), lane_scales = (unsigned)(lane * H);
     // Where the rows of a window are; their codes and scales, sent for while the window before is added up.
     bool there[kCodesRows], there_next[kCodesRows];

@@ -170,7 +170,7 @@ struct hclae_ctx {
     // sorted rows of hclae_lookup_grad (allocated on first use)
     char *grad_buf;
     // scratch of the calls that serve a cache: the largest any of them has asked for.  What it replaced is kept until hclae_destroy, as a
-    // recorded graph may still use it; each is at least twice as large as the one before
+    // recorded graph may still use it; each is twice as large as the one before where there is memory for that
     char *serve_buf;
     size_t serve_bytes;
     char *serve_old[48];
