@@ -459,7 +459,7 @@ int hclae_lookup_grad(hclae_ctx *ctx, const int64_t *rows, int64_t T, const uint
  * names nothing.  A row whose page is not in the cache takes no part.  Where none takes part out is zero and lse -infinity.
  * A row that takes part with a scale of NaN makes its head's outputs NaN (a value's all but lse).  Codes of K or more are read as K - 1.
  *   Q: DEVICE, B tokens of Hq rows of `type`, row b, head hq at Q + b * q_row_stride + hq * q_head_stride (elements; strides and alignment as in
- *   hclae_cache_write).  out: DEVICE, alike; its rows lie apart.  lse: DEVICE float[B][Hq], or NULL.  B <= N_max.
+ *   hclae_cache_write).  out: DEVICE, alike; its rows lie apart, and it is Q itself with Q's strides or overlaps nothing that is read.  lse: DEVICE float[B][Hq], or NULL.  B <= N_max.
  * Softmax statistics and sums are in 32 bits or more, out is rounded once.
  */
 int hclae_cache_attend(hclae_ctx *ctx, const void *Q, int type, int B, int Hq, int64_t q_row_stride, int64_t q_head_stride, const uint8_t *codes,
@@ -486,7 +486,7 @@ int hclae_cache_select(hclae_ctx *ctx, const void *Q, int type, int B, int Hq, i
  * ascending): its length grows by their number, its table gets the pages they need, the lowest that no sequence uses, in the
  * order of the sequences, and slots[i] (DEVICE int64[n], for hclae_cache_write) is where row i goes, -1 where it is not kept: rows of no
  * sequence, rows that go to an entry of the table that names no page, and all rows of a sequence that cannot be served, whose table and length stay as they are.  These are one whose table has no
- * entries left, and one that asks for pages when those asked for up to it (without the sequences whose tables are full) are more than are free.
+ * entries left, one whose length would pass 2^31 - 1, and one that asks for pages when those asked for up to it (without the sequences of the first two kinds) are more than are free.
  *   A sequence that adds rows to a page that others name too gets a page of its own instead: page src[b] is to be copied to dst[b], its
  * first rows[b] rows (DEVICE int32[B] each; -1, -1, 0 where nothing is), with hclae_cache_copy, before the rows are written.
  *   n_pages: pages of the cache, < 2^31.  n <= N_max.  Table entries outside [0, n_pages) name no page.

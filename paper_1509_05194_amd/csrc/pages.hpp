@@ -28,7 +28,7 @@ struct Growth {
     int64_t length;                                 // rows it has
     int64_t first, add;                             // its new rows: of the batch, their number
     int64_t old_pages, new_pages;                   // before and after
-    bool fits;                                      // the table has entries for them
+    bool fits;                                      // the table has entries for them, and `lengths` holds their number
     __host__ __device__ constexpr Growth(const PageArgs &a, int b)
         : length(held(a.lengths[b], a.max_pages, a.page)), first(0), add(0), old_pages(0), new_pages(0), fits(false)
     {
@@ -37,7 +37,7 @@ struct Growth {
         add = to > from ? to - from : 0;
         old_pages = (length + a.page - 1) / a.page;
         new_pages = (length + add + a.page - 1) / a.page;
-        fits = new_pages <= a.max_pages;
+        fits = new_pages <= a.max_pages && length + add <= 0x7fffffff;
     }
 };
 

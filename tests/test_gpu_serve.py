@@ -435,6 +435,37 @@ def test_extend(B, most, page, spare, seed):
     ctx.close()
 
 
+@pytest.mark.parametrize("B", [4, 9000])        # one block, and several kernels
+def test_extend_up_to_the_longest(B):
+    """Lengths are 32-bit: the last row that one can count is number 2^31 - 2, and a sequence that asks for more is left as it is."""
+    from paper_1509_05194_amd import hclae
+    page, max_pages, n_pages, top = 2 ** 30, 4, 5, 2 ** 31 - 1
+    tables = np.full((B, max_pages), -1, np.int32)
+    lens, adds = np.zeros(B, np.int32), np.zeros(B, np.int64)
+    tables[0, :2], lens[0], adds[0] = (3, 1), top - 3, 3
+    tables[1, :2], lens[1], adds[1] = (0, 4), top - 3, 4
+    tables[2, :2], lens[2], adds[2] = (1, 3), top, 1
+    adds[3] = 2
+    starts = np.concatenate([[0], np.cumsum(adds)]).astype(np.int32)
+    n = int(starts[-1])
+    slots = torch.full((n,), -7, dtype=torch.int64, device="cuda")
+    moves = [torch.full((B,), -7, dtype=torch.int32, device="cuda") for _ in range(3)]
+    t, l = torch.from_numpy(tables).cuda(), torch.from_numpy(lens).cuda()
+    ctx = hclae.Context(16, 8, 2, 4)
+    ctx.cache_extend(t, l, torch.from_numpy(starts).cuda(), page, n_pages, slots, *moves)
+    torch.cuda.synchronize()
+    ctx.close()
+    # page 1 is of sequences 0 and 2: sequence 0's last page is copied to page 2, the only free one, and sequence 3 finds none
+    tables[0, 1], lens[0] = 2, top
+    first = 2 * page + (top - 3) % page
+    assert t.cpu().numpy().tolist() == tables.tolist()
+    assert l.cpu().numpy().tolist() == lens.tolist()
+    assert slots.cpu().tolist() == [first, first + 1, first + 2] + [-1] * 7
+    src, dst, rows = [m.cpu().numpy() for m in moves]
+    assert (src[0], dst[0], rows[0]) == (1, 2, (top - 3) % page)
+    assert (src[1:] == -1).all() and (dst[1:] == -1).all() and (rows[1:] == 0).all()
+
+
 def compact(tables, lens, page, n_pages):
     tables = tables.copy()
     held = [min(max(int(x), 0), tables.shape[1] * page) for x in lens]
