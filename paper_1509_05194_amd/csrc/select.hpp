@@ -243,10 +243,10 @@ __global__ __launch_bounds__(kPickThreads) void k_select_pages(const SelectArgs 
                 const uint64_t other = (uint64_t)hi << 32 | lo;
                 ahead += other > key || (other == key && __builtin_amdgcn_readlane(at, i) < at) ? 1u : 0u;
             }
-            if (lane < (int)left) keys[at] = ahead < need ? ~0ull : 0ull;       // taken, or not
+            // taken, or not; where infinite scores share the prefix of pages that are taken whatever theirs, these `need` keys are all that have it
+            if (lane < (int)left) keys[at] = ahead < need ? ~0ull : 0ull;
         }
         __syncthreads();
-        need = 0;
     }
     // in the order of the pages; of equal keys the first
     int32_t *out = a.picked + (int64_t)job * a.k;

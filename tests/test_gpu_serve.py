@@ -349,6 +349,31 @@ def test_select_all_equal():
     ctx.close()
 
 
+@pytest.mark.parametrize("P,k,first,recent", [(5, 3, 1, 1), (40, 10, 1, 1), (40, 2, 1, 1), (40, 10, 0, 0), (120, 30, 3, 2), (3000, 33, 1, 1)])
+@pytest.mark.parametrize("which", ["scales", "queries"])
+def test_select_infinite_scores(which, P, k, first, recent):
+    """Scores of both infinities, more of the greater than are asked for, beside pages that are taken whatever their scores."""
+    from paper_1509_05194_amd import hclae
+    rng = np.random.default_rng(P + k)
+    C = rng.standard_normal((2, 2, 16, 16)).astype(np.float32)
+    codes = rng.integers(0, 16, (P, 2, 2)).astype(np.uint8)
+    scale = rng.standard_normal((P, 2)).astype(np.float32)
+    Q = rng.standard_normal((2, 4, 16)).astype(np.float32)
+    if which == "scales":
+        scale[:] = np.inf
+    else:
+        Q[:, ::2, 5] = np.inf
+    tables = np.stack([rng.permutation(P) for _ in range(2)]).astype(np.int32)
+    ctx = hclae.Context(2, 16, 2, 16)
+    ctx.cache_begin(torch.from_numpy(C).cuda())
+    picked = torch.full((2, 2, k), 99, dtype=torch.int32, device="cuda")
+    ctx.cache_select(torch.from_numpy(Q).cuda(), torch.from_numpy(codes).cuda(), torch.from_numpy(scale).cuda(), torch.from_numpy(tables).cuda(),
+                     torch.tensor([P, P], dtype=torch.int32, device="cuda"), 1, picked, first=first, recent=recent)
+    want = select(Q.astype(np.float64), C, codes, scale, tables, [P, P], 1, P, k, first, recent)
+    assert np.array_equal(picked.cpu().numpy(), want)
+    ctx.close()
+
+
 # ---- pages ---------------------------------------------------------------------------------------
 
 def extend(tables, lens, starts, n, page, n_pages):
