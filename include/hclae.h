@@ -457,7 +457,8 @@ int hclae_lookup_grad(hclae_ctx *ctx, const int64_t *rows, int64_t T, const uint
  * Rows t that take part: begins[b] <= t < lengths[b] (begins: DEVICE int32[B], or NULL: from 0), of these with `picked` (DEVICE
  * int32[B][G][n_picked], or NULL) the rows of the pages t / page that its head names, each as often as it is named; an entry outside [0, max_pages)
  * names nothing.  A row whose page is not in the cache takes no part.  Where none takes part out is zero and lse -infinity.
- * A row that takes part with a scale of NaN makes its head's outputs NaN (a value's all but lse).  Codes of K or more are read as K - 1.
+ * A row that takes part with a scale of NaN makes its head's outputs NaN (a value's all but lse).  An infinite one of a value makes them NaN or infinite.
+ * A weight p times a value's scale is kept down to 2^-119; what is below may count as zero.  Codes of K or more are read as K - 1.
  *   Q: DEVICE, B tokens of Hq rows of `type`, row b, head hq at Q + b * q_row_stride + hq * q_head_stride (elements; strides and alignment as in
  *   hclae_cache_write).  out: DEVICE, alike; its rows lie apart, and it is Q itself with Q's strides or overlaps nothing that is read.  lse: DEVICE float[B][Hq], or NULL.  B <= N_max.
  * Softmax statistics and sums are in 32 bits or more, out is rounded once.
@@ -475,7 +476,7 @@ int hclae_cache_attend(hclae_ctx *ctx, const void *Q, int type, int B, int Hq, i
  *   score(b, h, j) = (sum_r q(h R + r)) . x(h, p)            in 64 bits; a NaN counts as -infinity
  * picked[b][h]: DEVICE int32[B][H][k], the j of the first `first` and the last `recent` pages whatever their scores (their stand-ins are not
  * read) and of the best others, the lower j of equals, k in all, ascending; -1 where there are no more.  Pages that are not in the cache
- * (p outside [0, n_pages)) are not picked.  first + recent <= k.  B <= N_max.
+ * (p outside [0, n_pages)) are not picked.  first + recent <= k.  max_pages, k <= 2^30.  B <= N_max.
  */
 int hclae_cache_select(hclae_ctx *ctx, const void *Q, int type, int B, int Hq, int64_t q_row_stride, int64_t q_head_stride, const uint8_t *codes,
                        const float *scale, int64_t n_pages, const int32_t *tables, int max_pages, int page, const int32_t *lengths, int first, int recent,

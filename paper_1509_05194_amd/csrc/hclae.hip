@@ -2581,7 +2581,8 @@ int hclae_cache_select(hclae_ctx *ctx, const void *Q, int type, int B, int Hq, i
     if (rc != HCLAE_OK) return rc;
     if (!ctx->cache_H) return fail(ctx, HCLAE_ESTATE, "hclae_cache_select before hclae_cache_begin");
     const int G = ctx->cache_H;
-    if (bad_pages(B, max_pages, page, n_pages) || Hq < 1 || Hq > HCLAE_MAX_HQ || Hq % G || first < 0 || recent < 0 || k < 1 || (int64_t)first + recent > k)
+    if (bad_pages(B, max_pages, page, n_pages) || Hq < 1 || Hq > HCLAE_MAX_HQ || Hq % G || first < 0 || recent < 0 || k < 1 || (int64_t)first + recent > k ||
+        max_pages > 1 << 30 || k > 1 << 30)       // its kernel counts pages in 32 bits, some thousands at a time
         return fail(ctx, HCLAE_EINVAL, "hclae_cache_select: B, Hq, n_pages, max_pages, page, first, recent or k out of range");
     if (B == 0) return HCLAE_OK;
     if (!Q || !lengths || !picked || (max_pages > 0 && !tables) || (n_pages > 0 && !codes)) return fail(ctx, HCLAE_EINVAL, "hclae_cache_select: bad argument");

@@ -712,6 +712,20 @@ def test_graph_and_streams():
     ctx.close()
 
 
+def test_select_sizes_beyond_what_it_counts():
+    """Of an empty batch, which is looked at for its sizes alone: no pointer is used."""
+    from paper_1509_05194_amd import hclae
+    ctx = hclae.Context(1, 16, 2, 4)
+    ctx.cache_begin(torch.zeros((1, 2, 4, 16), device="cuda"))
+    call = lambda max_pages, k: hclae.lib().hclae_cache_select(ctx._h, None, 0, 0, 1, 16, 16, None, None, 0, None, max_pages, 1, None, 0, 0, k, None)
+    most = 2 ** 30
+    assert call(most, most) == hclae.OK
+    assert call(most + 1, 1) == hclae.EINVAL
+    assert call(1, most + 1) == hclae.EINVAL
+    assert call(2 ** 31 - 1, 2 ** 31 - 1) == hclae.EINVAL
+    ctx.close()
+
+
 def test_refusals():
     from paper_1509_05194_amd import hclae
     c = Case([20], 2, 2, 16, 2, 4, 4, "fp32", True, seed=0)
