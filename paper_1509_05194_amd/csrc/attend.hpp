@@ -305,7 +305,6 @@ __global__ __launch_bounds__(kWave) void k_attend_join(const AttendArgs a, int s
 constexpr int kWindow = 2048;                       // rows between two flushes of the fixed-point sums
 constexpr int kCodesMaxM = 32, kCodesSplits = 64;
 constexpr int kCodesLds = 152 * 1024;               // tables and sums; the rest is for what the kernel declares
-constexpr int kWideBits = 40, kPairBits = 19;       // steps of a fixed-point weight, as powers of two below the largest of its window
 
 // Weights are summed in fixed point, by integer atomics on LDS, so that their order changes nothing.  wide: 64 bits a query head, else two query heads in
 // 64 bits, 32 each.  Clocks of a CU for 64 additions at random words, measured with sixteen waves: u64 14.5 (4 of them for the additions, the rest because three or
@@ -333,6 +332,9 @@ __host__ __device__ constexpr int codes_most(int RB, bool wide, int MW)
     return all < most ? all : most;
 }
 __host__ __device__ constexpr int codes_threads(int RB, bool wide, int MW) { return codes_most(RB, wide, MW) * (wide ? 12 : 16) <= 72 * 1024 ? 512 : 1024; }
+// Steps of the fixed-point weights: 2^codes_bits of them at most are what the rows that a wave takes of a window (four a lane, or two) weigh together when the step is chosen,
+// 7/4 of that before it is chosen anew: in 32 bits the rows of a window, all with one code, stay below 7/8 2^31 (and a step each for the rounding).
+__host__ __device__ constexpr int codes_bits(int RB, bool wide, int MW) { return wide ? 48 : codes_threads(RB, wide, MW) == 512 ? 27 : 26; }
 __host__ __device__ constexpr int codes_words(int RB, bool wide, int MW) { return (codes_most(RB, wide, MW) + codes_threads(RB, wide, MW) - 1) / codes_threads(RB, wide, MW); }
 // Parts of a sequence's rows: as many blocks as the CUs hold at once, `blocks` each, with 2048 rows each at least, or 512 while there are fewer blocks than CUs.
 __host__ __device__ constexpr int codes_splits(const AttendArgs &a, int RB, int blocks, int cus)
@@ -353,9 +355,9 @@ __host__ __device__ constexpr int64_t tab_row(int M, int K, int RB) { return ((i
 
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
-// Products of floats on the bf16 matrix cores: a float is the sum of three bf16 numbers, rounded one after the other, up to 2^-27 of it (of two, to 2^-18);
-// a bf16 number is one and a half number two.  Of the products of parts those beyond 2^-24 (2^-16) of the whole are left out: six for two floats of
-// three parts, 96 cycles for 16 x 16 x 32 where the fp32 matrix cores take 256.
+// Products of floats on the bf16 matrix cores: a float is the sum of three bf16 numbers, rounded one after the other, up to 2^-27 of it;
+// a bf16 number is one and a half number two.  Of the products of parts those beyond 2^-24 of the whole are left out: six for two floats, 96 cycles for
+// 16 x 16 x 32 where the fp32 matrix cores take 256.
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 template <int N>
@@ -494,6 +496,20 @@ __device__ __forceinline__ float key_max(int v)
     return __int_as_float(i ^ (int)((unsigned)(i >> 31) >> 1));
 }
 
+// The sum over the wave, the same in every lane.
+__device__ __forceinline__ float lanes_sum(float v)
+{
+#define LANES_PLUS(ctrl, rows) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl, rows, 0xf, false))
+    LANES_PLUS(0x111, 0xf);                         // row_shr:1, 2, 4, 8
+    LANES_PLUS(0x112, 0xf);
+    LANES_PLUS(0x114, 0xf);
+    LANES_PLUS(0x118, 0xf);
+    LANES_PLUS(0x142, 0xa);                         // row_bcast:15 into rows 1 and 3
+    LANES_PLUS(0x143, 0xc);                         // row_bcast:31 into rows 2 and 3
+#undef LANES_PLUS
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), kWave - 1));
+}
+
 struct CodesStat {
     float top, sum, bad, unused;                    // bad: NaN where a value that takes part has no finite scale, else 0
 };
@@ -512,10 +528,11 @@ struct CodesArgs {
 // A block a part of the rows of a key head and RB of its query heads.  Windows of 2048 rows, two or four a thread:
 //   scores from the tables in LDS; weights p g' to fixed point, added up by code in LDS; these sums, times what a step stands for, to the running sums,
 //   which threads keep in registers.
-// The step is 2^-19 of the largest weight so far where two query heads share a word (2048 weights of 2^19 steps fit), rounded to the step below or above
-// by a fraction that goes round with the row (the golden ratio's multiples), so that many small weights add up to what they are: the error of a sum of n is about
-// sqrt(n) / 4 steps.  bf16 and fp16 outputs have steps of 2^-8 and 2^-11.  float outputs take 64 bits a query head, steps of 2^-40.  A block looks for the largest
-// score and weight of a window only if one of them is beyond what the last ones allow for.
+// Two query heads share a word where outputs are of 16 bits, 32 bits each: a step is 2^-25 or less of what the rows of a wave have weighed together so far (codes_bits), so
+// under 2^-24 of all weights' sum, as a float's last place.  Weights are rounded to the step below or above by a fraction that goes round with the row (the golden
+// ratio's multiples), so that many small weights add up to what they are.  float outputs and single query heads take 64 bits, steps of 2^-46.  A block looks for the
+// largest score and sum of a window only if one of them is beyond what the last ones allow for; a wave adds its weights up to know (1 us of the call below; steps of
+// 2^-18 of the largest weight would save it).
 // What bounds it: 64 sequences of 8192 to 16384 rows, 8 key heads, 4 query heads each, M = 8, take 114 us (1.3 TB/s of codes and scales): LDS works for 45 % of it,
 // 61 % of that because lanes meet at banks, a SIMD executes vector instructions for 38 %, the memory pipe takes a row's four pieces (two codes, two
 // scales, lines of their own) one by one for 38 %; 13 us of a block are its first loads, the tables' 32 KB and its sums' way out, a window of two blocks on a
@@ -585,9 +602,11 @@ __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes
 #pragma unroll
     for (int j = 0; j < NW; ++j) pairs |= (uint64_t)((threadIdx.x + j * kCodesThreads) / K % P) << (2 * j);
     float acc[NW][WIDE ? 1 : 2] = {};
-    constexpr float top_step = WIDE ? 0x1p40f : 0x1p19f;
-    static_assert(kWideBits == 40 && kPairBits == 19, "the same");
-    float ref[RB], unit[RB], back[RB], largest[RB], sum[RB];   // reference of the scores, steps in 1 and their size, log2 of the largest weight so far
+    constexpr int kBits = codes_bits(RB, WIDE, MW);
+    // WIDE: of a weight, 2048 of which stay far below 2^63; else of a wave's sum
+    constexpr float top_steps = WIDE ? 0x1p51f : 1.75f * (float)(1 << (WIDE ? 0 : kBits));
+    static_assert(WIDE || (int64_t)kCodesWaves << kBits == 1 << 30, "7/4 of it and 2048 steps are below 2^31");
+    float ref[RB], unit[RB], back[RB], largest[RB], sum[RB];   // reference of the scores, steps in 1 and their size, log2 of the largest sum of a wave's weights so far
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
         ref[r] = largest[r] = -INFINITY;
@@ -684,7 +703,8 @@ __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes
         float s[kCodesRows][RB], v[kCodesRows][RB];
         locate(w0 + kWindow);
         float here[RB];                             // the window's sums of exponentials
-        float highest = 0.f, heaviest = 0.f;        // score above its reference, weight in steps; NaN are passed over
+        float highest = 0.f, heaviest = 0.f;        // score above its reference, weight in steps (WIDE); NaN are passed over
+        float heavy[RB];                            // the weights' sum in steps (not WIDE)
         // weights in steps (WIDE: as they are), with the fraction that decides which way they are rounded
         auto weigh = [&](int i) {
             const float turn = (float)(((w0 + i * kCodesThreads + threadIdx.x) * 0x9E3779B9u) >> 8) * 0x1p-24f;
@@ -694,11 +714,12 @@ __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes
                 here[r] += p;
                 v[i][r] = WIDE ? w : w * unit[r] + turn;
                 highest = fmaxf(highest, e);
-                heaviest = fmaxf(heaviest, fabsf(WIDE ? w * unit[r] : v[i][r]));
+                if (WIDE) heaviest = fmaxf(heaviest, fabsf(w * unit[r]));
+                else heavy[r] += fabsf(v[i][r]);
             }
         };
 #pragma unroll
-        for (int r = 0; r < RB; ++r) here[r] = 0.f;
+        for (int r = 0; r < RB; ++r) here[r] = heavy[r] = 0.f;
 #pragma unroll
         for (int i = 0; i < kCodesRows; ++i) {
 #pragma unroll
@@ -727,9 +748,13 @@ __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes
             bad |= !(fabsf(gv[i]) < INFINITY);
             weigh(i);
         }
-        if (highest > kRoom || heaviest > top_step) grow[turn_of] = 1;              // the same value from whoever writes
+        bool more = highest > kRoom || heaviest > top_steps;
+        if (!WIDE)
+#pragma unroll
+            for (int r = 0; r < RB; ++r) more |= !(lanes_sum(heavy[r]) <= top_steps);    // a NaN too: it would hide what is beside it
+        if (more) grow[turn_of] = 1;                // the same value from whoever writes
         __syncthreads();
-        if (grow[turn_of]) {                        // the largest score of the window over the block, then the largest weight
+        if (grow[turn_of]) {                        // the largest score of the window over the block, then the largest sum of a wave's weights
             float now[RB], fade[RB];
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
@@ -744,12 +769,18 @@ __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
                 now[r] = fmaxf(ref[r], key_max<4>(float_key(red[r][min(lane, kCodesWaves - 1)].x)));
-                float most = -INFINITY;             // log2 of the weights that the reference makes
+                float l[kCodesRows], most = -INFINITY;  // log2 of the weights that the reference makes
 #pragma unroll
-                for (int i = 0; i < kCodesRows; ++i)
-                    if (there[i]) most = fmaxf(most, (s[i][r] - now[r]) + __builtin_amdgcn_logf(fabsf(gv[i])));
+                for (int i = 0; i < kCodesRows; ++i) {
+                    l[i] = there[i] ? (s[i][r] - now[r]) + __builtin_amdgcn_logf(fabsf(gv[i])) : -INFINITY;
+                    most = fmaxf(most, l[i]);
+                }
                 most = key_max<6>(float_key(most));
-                if (lane == 0) red[r][wave].y = most;
+                float all = 0.f;                    // in parts of the largest; what is no number counts nothing
+#pragma unroll
+                for (int i = 0; i < kCodesRows; ++i) all += fmaxf(__builtin_amdgcn_exp2f(l[i] - most), 0.f);
+                all = lanes_sum(all);
+                if (lane == 0) red[r][wave].y = most + fmaxf(__builtin_amdgcn_logf(all), 0.f);
             }
             __syncthreads();
 #pragma unroll
@@ -758,13 +789,13 @@ __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes
                 fade[r] = ref[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(move);
                 largest[r] = fmaxf(largest[r] == -INFINITY ? largest[r] : largest[r] + move, key_max<4>(float_key(red[r][min(lane, kCodesWaves - 1)].y)));
                 ref[r] = now[r];
-                // weights up to 2^e; only zeros: any step
+                // a wave's weights are 2^e together; only zeros: any step
                 const float e = largest[r] == -INFINITY ? 0.f : fminf(fmaxf(ceilf(largest[r] + 0.01f), -100.f), 140.f);
-                const int n = min((WIDE ? kWideBits : kPairBits) - (int)e, 120);
+                const int n = min(kBits - (int)e, 120);
                 unit[r] = ldexpf(1.f, n);
                 back[r] = ldexpf(1.f, -n);
                 sum[r] *= fade[r];
-                here[r] = 0.f;
+                here[r] = heavy[r] = 0.f;
             }
 #pragma unroll
             for (int j = 0; j < NW; ++j) {
@@ -939,23 +970,24 @@ __global__ __launch_bounds__(kFoldThreads) void k_attend_fold(const AttendArgs a
     *reinterpret_cast<float4 *>(to) = v;
 }
 
-constexpr int kOutThreads = 1024, kOutWaves = kOutThreads / kWave, kOutChunk = 64, kOutPitch = kOutChunk + 8;
-__host__ __device__ constexpr int out_lds(int N, int CW)
+constexpr int kOutThreads = 1024, kOutWaves = kOutThreads / kWave, kOutChunk = 64, kOutPitch = kOutChunk + 8, kOutParts = 3;
+__host__ __device__ constexpr int out_lds(int CW)
 {
-    const int rows = kOutWaves * N * 16 * kOutPitch * 2, sums = kOutWaves * 16 * (16 * CW + 1) * 4;
+    const int rows = kOutWaves * kOutParts * 16 * kOutPitch * 2, sums = kOutWaves * 16 * (16 * CW + 1) * 4;
     return rows > sums ? rows : sums;
 }
 
 // out = the sums by code times the codewords, over the exponentials' sum: a block 16 query heads and 16 CW coordinates (a lane CW side by side), its waves
 // every sixteenth 64 codewords each.  A wave lays the 64 sums of 16 query heads out in LDS of its own, the parts added up on the way.
 // Blocks of one XCD (they go round the eight) have neighbouring numbers, which is the same head most often: its codewords stay in that L2.
-// N: bf16 parts of a sum and a codeword, two for outputs of 16 bits and three for floats.
+// Sums and codewords are three bf16 parts each, as in the tables: 32 bits and no less (with two, 17 bits, the calls of many rows take 2 to 6 % less).
 // 2048 query heads, D = 128, M = 8, K = 256: 16 us (fp32 matrix cores 28; eight waves a block 17; the next 64 codewords on their way 19): a chain of loads, LDS and products
 // for every 64 codewords of a wave; the sums are read once for each 64 coordinates.
 // span: parts between one sequence's sums and the next; splits: parts to add up, the first of those.
-template <typename T, int RB, int CW, int N>
+template <typename T, int RB, int CW>
 __global__ __launch_bounds__(kOutThreads, 4) void k_attend_out(const AttendArgs a, int splits, int span, int tiles, const CodesStat *stats, const float *sums)
 {
+    constexpr int N = kOutParts;
     extern __shared__ __attribute__((aligned(16))) float out_room[];
     __shared__ float part[16][kCodesSplits];
     const int RG = (a.R + RB - 1) / RB, MK = a.M * a.K, slices = (a.D + 16 * CW - 1) / (16 * CW), all = a.rows.B * RG * RB;

@@ -165,10 +165,9 @@ hipError_t launch_through_tables(const AttendArgs &a, const CodesPlan &plan, int
     // 64 coordinates a block where that leaves enough of them
     const bool wide = (int64_t)tiles * a.G * ((a.D + 63) / 64) >= cus / 2;
     const int slices = (a.D + (wide ? 63 : 15)) / (wide ? 64 : 16);
-    constexpr int NO = T::bytes == 4 ? 3 : 2;
-    auto out = wide ? &k_attend_out<T, RB, 4, NO> : &k_attend_out<T, RB, 1, NO>;
+    auto out = wide ? &k_attend_out<T, RB, 4> : &k_attend_out<T, RB, 1>;
     TRY(raise_lds(out, kRaisedOut + (wide ? 1 : 0) + 2 * (RB == 1 ? 0 : RB == 2 ? 1 : 2) + 6 * (T::bytes == 4 ? 0 : __is_same(T, F16) ? 1 : 2), raised));
-    hipLaunchKernelGGL(out, dim3((unsigned)((tiles * a.G * slices + 7) / 8 * 8)), dim3(kOutThreads), (size_t)out_lds(NO, wide ? 4 : 1), stream, a, parts, splits, tiles, (const CodesStat *)stats,
+    hipLaunchKernelGGL(out, dim3((unsigned)((tiles * a.G * slices + 7) / 8 * 8)), dim3(kOutThreads), (size_t)out_lds(wide ? 4 : 1), stream, a, parts, splits, tiles, (const CodesStat *)stats,
                        (const float *)sums);
     return hipGetLastError();
 }
