@@ -15,6 +15,8 @@
 namespace hclae {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// The reference of scores before there is one: finite, so that a score of -infinity weighs exp(-infinity) = 0 whichever rows it shares a tile or a part with.
+constexpr float kLowest = -3.402823466e38f;
 
 // The rows of a sequence that take part, numbered from 0: those from `begin` to `end`, or those of the picked pages among them.
 struct SeqRows {
@@ -118,7 +120,7 @@ __host__ __device__ constexpr int direct_splits(const AttendArgs &a, int cus)
     return (int)(s < 1 ? 1 : s);
 }
 
-// stats of a part and query head: the largest score (-inf: no rows) and the sum of exponentials below it.
+// stats of a part and query head: the largest score and the sum of exponentials below it (negative: no rows, and no sums).
 struct PartStat {
     float top, sum;
 };
@@ -156,7 +158,7 @@ __global__ __launch_bounds__(kDirectThreads) void k_attend_rows(const AttendArgs
     const int64_t per = ((rows.count + splits - 1) / splits + tile - 1) / tile * tile, first = per * split, last = min(rows.count, first + per);
     const int lane = lane_id(), wave = threadIdx.x >> 6, g = threadIdx.x / lanes, p = threadIdx.x % lanes;
     if (first >= last) {
-        if (threadIdx.x < RB) stats[(int64_t)job * RB + threadIdx.x] = {-INFINITY, 0.f};
+        if (threadIdx.x < RB) stats[(int64_t)job * RB + threadIdx.x] = {kLowest, -1.f};
         return;
     }
     for (int i = threadIdx.x; i < RB * d4; i += kDirectThreads) {
@@ -170,7 +172,7 @@ __global__ __launch_bounds__(kDirectThreads) void k_attend_rows(const AttendArgs
     float4 acc[RB];
 #pragma unroll
     for (int r = 0; r < RB; ++r) acc[r] = make_float4(0.f, 0.f, 0.f, 0.f);
-    float top = -INFINITY, sum = 0.f;               // of head `wave`, in every lane of its wave
+    float top = kLowest, sum = 0.f;                 // of head `wave`, in every lane of its wave
     for (int64_t t0 = first; t0 < last; t0 += tile) {
         if (threadIdx.x < (unsigned)tile) {
             slots[threadIdx.x] = t0 + threadIdx.x < last ? rows.slot((unsigned)(t0 + threadIdx.x)) : kNoRow;
@@ -221,7 +223,7 @@ __global__ __launch_bounds__(kDirectThreads) void k_attend_rows(const AttendArgs
             w[wave][lane] = there ? e * gv[lane] : 0.f;
 #pragma unroll
             for (int o = 32; o > 0; o >>= 1) e += __shfl_xor(e, o, kWave);
-            const float f = top == -INFINITY ? 0.f : exp2f(top - now);
+            const float f = exp2f(top - now);
             sum = sum * f + e;
             top = now;
             if (lane == 0) fade[wave] = f;
@@ -268,7 +270,7 @@ __global__ __launch_bounds__(kWave) void k_attend_join(const AttendArgs a, int s
     const int b = blockIdx.x / Hq, hq = blockIdx.x - b * Hq, h = hq / a.R, r = hq - h * a.R;
     const int64_t job = (((int64_t)b * a.G + h) * RG + r / RB) * splits;
     const PartStat *stat = stats + job * RB + r % RB;
-    float top = -INFINITY;
+    float top = kLowest;
     for (int i = 0; i < splits; ++i) top = fmaxf(top, stat[(int64_t)i * RB].top);
     float sum = 0.f;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -285,7 +287,7 @@ __global__ __launch_bounds__(kWave) void k_attend_join(const AttendArgs a, int s
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            if (i0 + j >= splits || st[j].sum == 0.f) continue;         // no rows, and no sums
+            if (i0 + j >= splits || st[j].sum < 0.f) continue;
             any = true;
             const float f = exp2f(st[j].top - top);
             sum += f * st[j].sum;
@@ -293,7 +295,7 @@ __global__ __launch_bounds__(kWave) void k_attend_join(const AttendArgs a, int s
         }
     }
     if (any) {
-        const float f = 1.f / sum;
+        const float f = sum == 0.f ? 0.f : 1.f / sum;       // no row weighs anything
         v = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
     }
     if (p < d4) T::store(a.out, (int64_t)b * a.o_row + (int64_t)hq * a.o_head + 4 * p, v);
@@ -569,7 +571,7 @@ __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes
     const uint64_t first64 = (uint64_t)per * (unsigned)split;
     const int lane = lane_id(), wave = threadIdx.x >> 6;
     if (first64 >= count) {
-        if (threadIdx.x < RB) x.stats[job * RB + threadIdx.x] = {-INFINITY, 0.f, 0.f, 0.f};
+        if (threadIdx.x < RB) x.stats[job * RB + threadIdx.x] = {kLowest, 0.f, 0.f, 0.f};
         return;
     }
     const unsigned first = (unsigned)first64, last = (unsigned)(first64 + per < count ? first64 + per : count);
@@ -609,7 +611,8 @@ __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes
     float ref[RB], unit[RB], back[RB], largest[RB], sum[RB];   // reference of the scores, steps in 1 and their size, log2 of the largest sum of a wave's weights so far
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
-        ref[r] = largest[r] = -INFINITY;
+        ref[r] = kLowest;
+        largest[r] = -INFINITY;
         unit[r] = back[r] = 1.f;
         sum[r] = 0.f;
     }
@@ -786,7 +789,7 @@ __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
                 const float move = ref[r] - now[r];
-                fade[r] = ref[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(move);
+                fade[r] = __builtin_amdgcn_exp2f(move);
                 largest[r] = fmaxf(largest[r] == -INFINITY ? largest[r] : largest[r] + move, key_max<4>(float_key(red[r][min(lane, kCodesWaves - 1)].y)));
                 ref[r] = now[r];
                 // a wave's weights are 2^e together; only zeros: any step
@@ -924,7 +927,7 @@ __device__ __forceinline__ CodesStat join_parts(const CodesStat *st, int64_t str
 {
     static_assert(kCodesSplits <= kWave, "a part a lane");
     const int lane = lane_id();
-    CodesStat x = {-INFINITY, 0.f, 0.f, 0.f};
+    CodesStat x = {kLowest, 0.f, 0.f, 0.f};
     if (lane < splits) x = st[lane * stride];
     float top = x.top, bad = x.bad;
 #pragma unroll
@@ -932,7 +935,7 @@ __device__ __forceinline__ CodesStat join_parts(const CodesStat *st, int64_t str
         top = fmaxf(top, __shfl_xor(top, o, kWave));
         bad += __shfl_xor(bad, o, kWave);
     }
-    const float e = x.sum != 0.f ? __builtin_amdgcn_exp2f(x.top - top) : 0.f;       // a part without rows has no sums
+    const float e = x.sum != 0.f ? __builtin_amdgcn_exp2f(x.top - top) : 0.f;       // a part without rows has no sums; nor need one whose rows weigh nothing be read
     float sum = x.sum != 0.f ? e * x.sum : 0.f;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kWave);
@@ -1028,7 +1031,7 @@ __global__ __launch_bounds__(kOutThreads, 4) void k_attend_out(const AttendArgs 
         const int i = wave * (16 / kOutWaves) + j, n = tile * 16 + i, u = n / RB, b = u / RG, hq = (u - b * RG) * RB + (n - u * RB);
         if (n < all && hq < a.R) {
             const CodesStat x = join_parts(stats + seq_of(n) * splits * RB + n % RB, RB, splits, part[i]);
-            if (lane < splits) part[i][lane] = x.sum != 0.f ? part[i][lane] / x.sum + x.bad : 0.f;
+            if (lane < splits) part[i][lane] = (x.sum != 0.f ? part[i][lane] / x.sum : 0.f) + x.bad;
             if (slice == 0 && lane == 0 && a.lse) a.lse[(int64_t)b * a.G * a.R + h * a.R + hq] = x.sum != 0.f ? (x.top + log2f(x.sum)) * kLn2 : -INFINITY;
         } else if (lane < splits) part[i][lane] = 0.f;
     }
