@@ -317,12 +317,14 @@ struct CodesPlan {
     int words;                                      // of 64 bits
     int lds;
 };
+// Where in LDS the tables lie behind that many words of sums: they are filled sixteen bytes at a time.
+__host__ __device__ constexpr int codes_lut(int words) { return (words + 1) / 2 * 16; }
 __host__ __device__ constexpr CodesPlan codes_plan(int R, int M, int K, bool wide)
 {
     if (M > kCodesMaxM) return {0, false, 0, 0};
     for (int RB = heads_at_once(R); RB >= 1; RB /= 2) {
         const bool w = wide || RB == 1;
-        const int words = M * K * (w ? RB : RB / 2), lds = M * K * RB * 4 + words * 8;
+        const int words = M * K * (w ? RB : RB / 2), lds = codes_lut(words) + M * K * RB * 4;
         if (lds <= kCodesLds) return {RB, w, words, lds};
     }
     return {0, false, 0, 0};
@@ -577,7 +579,7 @@ __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes
     const unsigned first = (unsigned)first64, last = (unsigned)(first64 + per < count ? first64 + per : count);
     const int words = MK * P;
     unsigned long long *hist = reinterpret_cast<unsigned long long *>(codes_lds);
-    float *lut = reinterpret_cast<float *>(codes_lds + (size_t)words * 8);
+    float *lut = reinterpret_cast<float *>(codes_lds + codes_lut(words));
     {
         const float4 *from = reinterpret_cast<const float4 *>(x.tab + seq * tab_row(M, K, RB));
         const int fours = (int)(tab_row(M, K, RB) / 4), whole = MK * RB / 4;
