@@ -459,6 +459,8 @@ int hclae_lookup_grad(hclae_ctx *ctx, const int64_t *rows, int64_t T, const uint
  * names nothing.  A row whose page is not in the cache takes no part.  Where none takes part out is zero and lse -infinity.
  * e_t is computed as factor times scale times the product of q and the sum of codewords, one beyond 2.35e38 is infinite.  Where it is -infinity the row weighs nothing, and where no row weighs anything
  * out is zero and lse -infinity; where it is +infinity or NaN its query head's outputs are NaN.
+ * Codewords that no row has count nothing, whatever they hold; one that is not finite makes its coordinates so in the heads whose rows have it and weigh something.  Where q has a NaN
+ * or an infinity out is NaN or zero.  Sums of p x are floats before they are divided by that of p.
  * A row that takes part with a scale of NaN makes its head's outputs NaN (a value's all but lse).  An infinite one of a value makes them NaN or infinite.
  * A weight p times a value's scale is kept down to 2^-119; what is below may count as zero.  Codes of K or more are read as K - 1.
  *   Q: DEVICE, B tokens of Hq rows of `type`, row b, head hq at Q + b * q_row_stride + hq * q_head_stride (elements; strides and alignment as in

@@ -1095,6 +1095,42 @@ __global__ __launch_bounds__(kOutThreads, 4) void k_attend_out(const AttendArgs 
         products(0, c0);
         products(32, c1);
     }
+    // A codeword that is not finite, or no sum of finite bf16 parts, is a NaN in every row of its column, whether its sum is zero or not.  Where a NaN is none of its query head's
+    // the wave multiplies again, one by one, and leaves out what no row has.
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int q = 0; q < CW; ++q) odd |= s[q][e] != s[q][e];
+    if (__ballot(odd)) {
+        odd = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            bool number = true;
+            for (int p = 0; p < splits; ++p) number &= part[4 * g + e][p] == part[4 * g + e][p];
+#pragma unroll
+            for (int q = 0; q < CW; ++q) odd |= number && s[q][e] != s[q][e];
+        }
+    }
+    if (__ballot(odd)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int n = min(tile * 16 + 4 * g + e, all - 1);
+            const float *sum = sums + (seq_of(n) * span * RB + n % RB) * row;
+            float v[CW] = {};
+            for (int k0 = wave * kOutChunk; k0 < MK; k0 += kOutWaves * kOutChunk)
+                for (int k = k0; k < min(k0 + kOutChunk, MK); ++k) {
+                    float w = 0.f;
+                    for (int p = 0; p < splits; ++p)
+                        if (part[4 * g + e][p] != 0.f) w += part[4 * g + e][p] * sum[(int64_t)p * RB * row + k];
+                    if (w != 0.f)
+#pragma unroll
+                        for (int q = 0; q < CW; ++q) v[q] += w * C[(size_t)k * a.D + q];
+                }
+#pragma unroll
+            for (int q = 0; q < CW; ++q) s[q][e] = v[q];
+        }
+    }
     __syncthreads();                                // the sums' places are free
     constexpr int OP = 16 * CW + 1;
 #pragma unroll
