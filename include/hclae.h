@@ -442,9 +442,10 @@ int hclae_lookup_grad(hclae_ctx *ctx, const int64_t *rows, int64_t T, const uint
  * layer's), hclae_cache_write into the slots, and hclae_cache_attend.
  *
  * These calls only enqueue.  Their scratch is in the ctx: a call that needs more than any before allocates it (what it
- * replaces is kept until hclae_destroy, so that recorded graphs stay valid): for attention 8 M K bytes a query head, of 16384 at a time, and
- * up to 64 times half of that where few sequences are taken in many parts; for the choice of pages 8 (M K + max_pages) bytes a sequence and key head, 256 MB at most
- * unless one sequence needs more; for pages n_pages / 4 bytes and some words a sequence; while the stream is being captured such a call returns HCLAE_ESTATE
+ * replaces is kept until hclae_destroy, so that recorded graphs stay valid): for attention 8 M K bytes a query head (three or more of a key head count as the next multiple
+ * of four), of 16384 at a time, and up to 64 times half of that where few sequences are taken in many parts, or where rows are decoded 4 (D + 2) bytes a query head and part, up to 256;
+ * for the choice of pages 8 (M K + max_pages) bytes a sequence and key head, 256 MB at most unless one sequence needs more; for pages n_pages / 4 bytes, and for new rows 4 a
+ * sequence and 4 for each page that they can ask for, min(n_pages, 2 B + n / page) of them; while the stream is being captured such a call returns HCLAE_ESTATE
  * and enqueues nothing, so a call of the same sizes is made before.  Calls of one ctx share the scratch: two recorded ones must not run at
  * the same time.  They run on the device of the ctx, whichever is current.  Equal calls give equal bits.
  */
@@ -466,7 +467,7 @@ int hclae_lookup_grad(hclae_ctx *ctx, const int64_t *rows, int64_t T, const uint
  *   Q: DEVICE, B tokens of Hq rows of `type`, row b, head hq at Q + b * q_row_stride + hq * q_head_stride (elements; strides and alignment as in
  *   hclae_cache_write).  out: DEVICE, alike; its rows lie apart, and it is Q itself with Q's strides or overlaps nothing that is read.  lse: DEVICE float[B][Hq], or NULL.  B <= N_max.
  * Softmax statistics and sums are in 32 bits or more, out is rounded once.  With outputs of 16 bits the weights of more than some 300 rows are added up in
- * whole steps, each below 2^-24 of the sum of all p times |scale|; codewords and sums of weights are multiplied with 24 bits.
+ * whole steps, each below 2^-24 of the sum of all p times |scale| (or 2^-119); codewords and sums of weights are multiplied with 24 bits.
  */
 int hclae_cache_attend(hclae_ctx *ctx, const void *Q, int type, int B, int Hq, int64_t q_row_stride, int64_t q_head_stride, const uint8_t *codes,
                        const float *scale, int64_t n_slots, const int32_t *tables, int max_pages, int page, const int32_t *begins,

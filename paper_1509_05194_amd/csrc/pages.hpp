@@ -64,10 +64,11 @@ __device__ __forceinline__ void live_entries(const PageArgs &a, int b, int64_t j
             if (p[i] >= 0 && p[i] < a.n_pages) f((int)(j + i * threads), p[i]);
     }
 }
+// shared: or null, where nobody asks which pages are named twice
 __device__ __forceinline__ void mark_page(unsigned *used, unsigned *shared, int32_t p)
 {
     const unsigned bit = 1u << (p & 31), old = atomicOr(&used[p >> 5], bit);
-    if (old & bit) atomicOr(&shared[p >> 5], bit);
+    if (shared && (old & bit)) atomicOr(&shared[p >> 5], bit);
 }
 
 __global__ __launch_bounds__(kPageThreads) void k_pages_mark(const PageArgs a, unsigned *used, unsigned *shared)
@@ -272,7 +273,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_extend_block(const PageArgs a,
 }
 
 struct CompactScratch {
-    unsigned *used, *unused, *before;               // before: pages in use in earlier words
+    unsigned *used, *before;                        // before: pages in use in earlier words
 };
 
 // By one block: the pages in use are counted; the i-th hole below that number takes the i-th page from that number on.
@@ -347,12 +348,12 @@ __global__ __launch_bounds__(kPlanThreads) void k_compact_block(const PageArgs a
     extern __shared__ unsigned page_lds[];
     __shared__ unsigned sums[kPlanThreads / kWave];
     const int words = (int)words_of(a.n_pages);
-    const CompactScratch s = {page_lds, page_lds + words, page_lds + 2 * words};
-    unsigned *live = page_lds + 3 * words;
-    for (int i = threadIdx.x; i < 2 * words; i += kPlanThreads) page_lds[i] = 0u;
+    const CompactScratch s = {page_lds, page_lds + words};
+    unsigned *live = page_lds + 2 * words;
+    for (int i = threadIdx.x; i < words; i += kPlanThreads) page_lds[i] = 0u;
     live_of(a, live);
     __syncthreads();
-    all_entries(a, live, [&](int, int, int32_t p) { atomicOr(&s.used[p >> 5], 1u << (p & 31)); });
+    all_entries(a, live, [&](int, int, int32_t p) { mark_page(s.used, nullptr, p); });
     __syncthreads();
     compact_plan(a, s, sums);
     __syncthreads();

@@ -238,15 +238,15 @@ dim3 table_blocks(const PageArgs &a, int cus)
     return dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(jobs, 8ll * cus)));
 }
 
-// Bitmaps at the front of the scratch: pages named once or more, pages named twice or more.
-hipError_t launch_marks(const PageArgs &a, int cus, char *scratch, hipStream_t stream)
+// Bitmaps at the front of the scratch: pages named once or more and, if twice, pages named twice or more.
+hipError_t launch_marks(const PageArgs &a, bool twice, int cus, char *scratch, hipStream_t stream)
 {
-    const int64_t words = (int64_t)(2 * bitmap_bytes(a) / 4);
+    const int64_t words = (int64_t)((twice ? 2 : 1) * bitmap_bytes(a) / 4);
     hipLaunchKernelGGL(k_pages_clear, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>((words + kPageThreads - 1) / kPageThreads, 8ll * cus))), dim3(kPageThreads), 0, stream,
                        reinterpret_cast<unsigned *>(scratch), words);
     TRY(hipGetLastError());
     hipLaunchKernelGGL(k_pages_mark, table_blocks(a, cus), dim3(kPageThreads), 0, stream, a, reinterpret_cast<unsigned *>(scratch),
-                       reinterpret_cast<unsigned *>(scratch + bitmap_bytes(a)));
+                       twice ? reinterpret_cast<unsigned *>(scratch + bitmap_bytes(a)) : nullptr);
     return hipGetLastError();
 }
 
@@ -315,7 +315,7 @@ hipError_t extend_launch(const PageArgs &a, int cus, char *scratch, uint64_t *ra
         hipLaunchKernelGGL(k_extend_block, dim3(1), dim3(kPlanThreads), (size_t)extend_lds(a, (int64_t)extend_room(a)), stream, a, (unsigned)extend_room(a));
         return hipGetLastError();
     }
-    TRY(launch_marks(a, cus, scratch, stream));
+    TRY(launch_marks(a, true, cus, scratch, stream));
     ExtendScratch s;
     char *p = scratch;
     s.used = reinterpret_cast<unsigned *>(p);
@@ -330,16 +330,16 @@ hipError_t extend_launch(const PageArgs &a, int cus, char *scratch, uint64_t *ra
     return hipGetLastError();
 }
 
-size_t compact_scratch(const PageArgs &a) { return a.n_pages > 0 && compact_in_block(a) ? 0 : 3 * bitmap_bytes(a); }
+size_t compact_scratch(const PageArgs &a) { return a.n_pages > 0 && compact_in_block(a) ? 0 : 2 * bitmap_bytes(a); }
 
 hipError_t compact_launch(const PageArgs &a, int cus, char *scratch, hipStream_t stream)
 {
     if (a.n_pages > 0 && compact_in_block(a)) {
-        hipLaunchKernelGGL(k_compact_block, dim3(1), dim3(kPlanThreads), (size_t)(12 * words_of(a.n_pages) + 4 * (int64_t)a.B), stream, a);
+        hipLaunchKernelGGL(k_compact_block, dim3(1), dim3(kPlanThreads), (size_t)(8 * words_of(a.n_pages) + 4 * (int64_t)a.B), stream, a);
         return hipGetLastError();
     }
-    TRY(launch_marks(a, cus, scratch, stream));
-    CompactScratch s = {reinterpret_cast<unsigned *>(scratch), reinterpret_cast<unsigned *>(scratch + bitmap_bytes(a)), reinterpret_cast<unsigned *>(scratch + 2 * bitmap_bytes(a))};
+    TRY(launch_marks(a, false, cus, scratch, stream));
+    CompactScratch s = {reinterpret_cast<unsigned *>(scratch), reinterpret_cast<unsigned *>(scratch + bitmap_bytes(a))};
     hipLaunchKernelGGL(k_compact_plan, dim3(1), dim3(kPlanThreads), 0, stream, a, s);
     TRY(hipGetLastError());
     const int64_t entries = (int64_t)a.B * a.max_pages;
