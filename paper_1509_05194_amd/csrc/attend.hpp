@@ -919,7 +919,8 @@ __global__ __launch_bounds__(codes_threads(RB, WIDE, MW), 4) void k_attend_codes
             to[(2 * q + 1) * row + mk] = acc[j][WIDE ? 0 : 1];
         }
     }
-    if (threadIdx.x < RB * (int)(row - MK)) to[threadIdx.x / (int)(row - MK) * row + MK + threadIdx.x % (int)(row - MK)] = 0.f;
+    if (threadIdx.x < RB)
+        for (int64_t i = MK; i < row; ++i) to[threadIdx.x * row + i] = 0.f;     // up to whole fours
 }
 
 constexpr int kFoldThreads = 256, kFoldFrom = 5;   // parts from which they are added up by a kernel of their own
