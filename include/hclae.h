@@ -466,7 +466,7 @@ int hclae_lookup_grad(hclae_ctx *ctx, const int64_t *rows, int64_t T, const uint
  * A weight p times a value's scale is kept down to 2^-119; what is below may count as zero.  Codes of K or more are read as K - 1.
  *   Q: DEVICE, B tokens of Hq rows of `type`, row b, head hq at Q + b * q_row_stride + hq * q_head_stride (elements; strides and alignment as in
  *   hclae_cache_write).  out: DEVICE, alike; its rows lie apart, and it is Q itself with Q's strides or overlaps nothing that is read.  lse: DEVICE float[B][Hq], or NULL.  B <= N_max.
- * Softmax statistics and sums are in 32 bits or more, out is rounded once.  With outputs of 16 bits the weights of more than some 300 rows are added up in
+ * Softmax statistics and sums are in 32 bits or more, out is rounded once.  With outputs of 16 bits weights may be added up in
  * whole steps, each below 2^-24 of the sum of all p times |scale| (or 2^-119); codewords and sums of weights are multiplied with 24 bits.
  */
 int hclae_cache_attend(hclae_ctx *ctx, const void *Q, int type, int B, int Hq, int64_t q_row_stride, int64_t q_head_stride, const uint8_t *codes,

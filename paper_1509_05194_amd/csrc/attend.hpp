@@ -535,8 +535,7 @@ struct CodesArgs {
 // Two query heads share a word where outputs are of 16 bits, 32 bits each: a step is 2^-25 or less of what the rows of a wave have weighed together so far (codes_bits), so
 // under 2^-24 of all weights' sum, as a float's last place.  Weights are rounded to the step below or above by a fraction that goes round with the row (the golden
 // ratio's multiples), so that many small weights add up to what they are.  float outputs and single query heads take 64 bits, steps of 2^-46.  A block looks for the
-// largest score and sum of a window only if one of them is beyond what the last ones allow for; a wave adds its weights up to know (1 us of the call below; steps of
-// 2^-18 of the largest weight would save it).
+// largest score and sum of a window only if one of them is beyond what the last ones allow for; a wave adds its weights up to know (less than 1 us of the calls below).
 // What bounds it: 64 sequences of 8192 to 16384 rows, 8 key heads, 4 query heads each, M = 8, take 114 us (1.3 TB/s of codes and scales): LDS works for 45 % of it,
 // 61 % of that because lanes meet at banks, a SIMD executes vector instructions for 38 %, the memory pipe takes a row's four pieces (two codes, two
 // scales, lines of their own) one by one for 38 %; 13 us of a block are its first loads, the tables' 32 KB and its sums' way out, a window of two blocks on a

@@ -72,11 +72,11 @@ AttendArgs round_of(const AttendArgs &a, int b0, int n, int bytes)
 }
 
 // Whether the rows go through tables: not where a sequence can have few rows only, which are decoded before the tables are there, unless there are many such
-// sequences.  G = 8, R = 4, D = 128, K = 256, bf16 in pages of 16, us decoded and through tables, in a graph: one sequence, M = 8, 64 rows 15.6 and 20.6, 128 rows 16.5 and
-// 20.7, 256 rows 18.9 and 20.8, 384 rows 23.5 and 21.6, 2048 rows 63 and 24; M = 16, 128 rows 22.9 and 29.6, 256 rows 36 and 30; R = 1, 256 rows 16.4 and 17.9, 384
-// rows 20.2 and 18.4; fp32, 256 rows 18.8 and 24.8, 384 rows 23.5 and 25.0 (the rule: tables); K = 64, 256 rows 18.7 and 18.6.  32 sequences, M = 8, 64 rows 27.8 and 36.8,
-// 128 rows 43.6 and 36.5, 2048 rows 481 and 44.
-constexpr int64_t kFewRows = 320, kFewInAll = 96 * 256;
+// sequences.  G = 8, R = 4, D = 128, K = 256, bf16 in pages of 16, us decoded and through tables, in a graph: one sequence, M = 8, 64 rows 15.8 and 22.9, 128 rows 16.6 and
+// 23.1, 256 rows 19.1 and 23.3, 384 rows 23.7 and 24.1, 512 rows 28.8 and 24.6, 2048 rows 63 and 27; M = 16, 128 rows 23.0 and 33.5, 256 rows 35.8 and 34.3; R = 1, 256 rows 16.6
+// and 19.4, 384 rows 20.2 and 20.0; fp32, 256 rows 18.9 and 25.2, 384 rows 23.6 and 25.5, 512 rows 28.9 and 26.5; K = 64, 256 rows 18.9 and 19.8, 384 rows 21.4 and 21.1.
+// 32 sequences, M = 8, 64 rows 27.9 and 42.1, 128 rows 43.2 and 41.6, 2048 rows 481 and 49.
+constexpr int64_t kFewRows = 400, kFewInAll = 96 * 256;
 CodesPlan plan_of(const AttendArgs &a, int type)
 {
     const int64_t rows = attend_capacity(a) * std::max(8, a.M) / 8, RB = heads_at_once(a.R);
