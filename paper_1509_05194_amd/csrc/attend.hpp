@@ -5,7 +5,7 @@
 //   k_attend_tables, k_attend_codes, k_attend_fold, k_attend_out   many rows, never decoded: q . C[h][m][k] is tabulated once for all codewords, a row's score is
 //       the sum of M entries; the weights of the rows are summed by the codes of their values, and these sums meet the codewords at the end.
 //       A row costs M reads and M adds a query head in place of M D, whatever D is, and is read as 2 (M + 4) bytes a head: 64 sequences of 8192 to 16384 rows,
-//       8 key heads of 4 query heads, D = 128, M = 8, take 145 us, with rows decoded 5.7 ms.
+//       8 key heads of 4 query heads, D = 128, M = 8, take 149 us of kernels, with rows decoded 5.7 ms.
 #pragma once
 #include <type_traits>
 
@@ -537,8 +537,8 @@ struct CodesArgs {
 // ratio's multiples), so that many small weights add up to what they are.  float outputs and single query heads take 64 bits, steps of 2^-46.  A block looks for the
 // largest score and sum of a window only if one of them is beyond what the last ones allow for; a wave adds its weights up to know (less than 1 us of the calls below).
 // What bounds it: 64 sequences of 8192 to 16384 rows, 8 key heads, 4 query heads each, M = 8, take 114 us (1.3 TB/s of codes and scales): LDS works for 45 % of it,
-// 61 % of that because lanes meet at banks, a SIMD executes vector instructions for 38 %, the memory pipe takes a row's four pieces (two codes, two
-// scales, lines of their own) one by one for 38 %; 13 us of a block are its first loads, the tables' 32 KB and its sums' way out, a window of two blocks on a
+// 61 % of that because lanes meet at banks, a SIMD executes vector instructions for 34 %, the memory pipe takes a row's four pieces (two codes, two
+// scales, lines of their own) one by one for 37 %; 13 us of a block are its first loads, the tables' 32 KB and its sums' way out, a window of two blocks on a
 // CU 12 us.  On the way there, us: 1024 threads with two rows each 184, 512 with one, two and four rows 221, 165 and 148; with offsets in the instructions and the
 // largest looked for only when it grows 117; with the next window's codes on their way 114.
 // FULL: K = 256 and 4 MW dictionaries, whole aligned words: the offsets in LDS are in the instructions.  BY_WAVE: pages of multiples of 64 rows: the rows of a wave are
@@ -985,8 +985,8 @@ __host__ __device__ constexpr int out_lds(int CW)
 // out = the sums by code times the codewords, over the exponentials' sum: a block 16 query heads and 16 CW coordinates (a lane CW side by side), its waves
 // every sixteenth 64 codewords each.  A wave lays the 64 sums of 16 query heads out in LDS of its own, the parts added up on the way.
 // Blocks of one XCD (they go round the eight) have neighbouring numbers, which is the same head most often: its codewords stay in that L2.
-// Sums and codewords are three bf16 parts each, as in the tables: 32 bits and no less (with two, 17 bits, the calls of many rows take 2 to 6 % less).
-// 2048 query heads, D = 128, M = 8, K = 256: 16 us (fp32 matrix cores 28; eight waves a block 17; the next 64 codewords on their way 19): a chain of loads, LDS and products
+// Sums and codewords are three bf16 parts each, as in the tables: 32 bits and no less (with two, 17 bits, calls of many rows take 1 to 7 % less).
+// 2048 query heads, D = 128, M = 8, K = 256: 21 us, with two parts 16 (with those: fp32 matrix cores 28; eight waves a block 17; the next 64 codewords on their way 19): a chain of loads, LDS and products
 // for every 64 codewords of a wave; the sums are read once for each 64 coordinates.
 // span: parts between one sequence's sums and the next; splits: parts to add up, the first of those.
 template <typename T, int RB, int CW>
