@@ -463,7 +463,7 @@ int hclae_lookup_grad(hclae_ctx *ctx, const int64_t *rows, int64_t T, const uint
  * Codewords that no row has count nothing, whatever they hold; one that is not finite makes its coordinates so in the heads whose rows have it and weigh something.  Where q has a NaN
  * or an infinity out is NaN or zero.  Sums of p x are floats before they are divided by that of p.
  * A row that takes part with a scale of NaN makes its head's outputs NaN (a value's all but lse).  An infinite one of a value makes them NaN or infinite.
- * A weight p times a value's scale is kept down to 2^-119; what is below may count as zero.  Codes of K or more are read as K - 1.
+ * A weight p is kept down to 2^-126 of the largest, p times a value's scale down to 2^-119; what is below may count as zero.  Codes of K or more are read as K - 1.
  *   Q: DEVICE, B tokens of Hq rows of `type`, row b, head hq at Q + b * q_row_stride + hq * q_head_stride (elements; strides and alignment as in
  *   hclae_cache_write).  out: DEVICE, alike; its rows lie apart, and it is Q itself with Q's strides or overlaps nothing that is read.  lse: DEVICE float[B][Hq], or NULL.  B <= N_max.
  * Softmax statistics and sums are in 32 bits or more, out is rounded once.  With outputs of 16 bits weights may be added up in

@@ -532,8 +532,8 @@ struct CodesArgs {
 // A block a part of the rows of a key head and RB of its query heads.  Windows of 2048 rows, two or four a thread:
 //   scores from the tables in LDS; weights p g' to fixed point, added up by code in LDS; these sums, times what a step stands for, to the running sums,
 //   which threads keep in registers.
-// Two query heads share a word where outputs are of 16 bits, 32 bits each: a step is 2^-25 or less of what the rows of a wave have weighed together so far (codes_bits), so
-// under 2^-24 of all weights' sum, as a float's last place.  Weights are rounded to the step below or above by a fraction that goes round with the row (the golden
+// Two query heads share a word where outputs are of 16 bits, 32 bits each: a step is under 2^-24 of the most that a wave's rows of a window have weighed together so far (codes_bits),
+// and so of all weights' sum, as a float's last place.  Weights are rounded to the step below or above by a fraction that goes round with the row (the golden
 // ratio's multiples), so that many small weights add up to what they are.  float outputs and single query heads take 64 bits, steps of 2^-46.  A block looks for the
 // largest score and sum of a window only if one of them is beyond what the last ones allow for; a wave adds its weights up to know (less than 1 us of the calls below).
 // What bounds it: 64 sequences of 8192 to 16384 rows, 8 key heads, 4 query heads each, M = 8, take 114 us (1.3 TB/s of codes and scales): LDS works for 45 % of it,
@@ -985,7 +985,7 @@ __host__ __device__ constexpr int out_lds(int CW)
 // out = the sums by code times the codewords, over the exponentials' sum: a block 16 query heads and 16 CW coordinates (a lane CW side by side), its waves
 // every sixteenth 64 codewords each.  A wave lays the 64 sums of 16 query heads out in LDS of its own, the parts added up on the way.
 // Blocks of one XCD (they go round the eight) have neighbouring numbers, which is the same head most often: its codewords stay in that L2.
-// Sums and codewords are three bf16 parts each, as in the tables: 32 bits and no less (with two, 17 bits, calls of many rows take 1 to 7 % less).
+// Sums and codewords are three bf16 parts each, as in the tables, which is what a float holds (with two, 17 bits, calls of many rows take 1 to 7 % less).
 // 2048 query heads, D = 128, M = 8, K = 256: 21 us, with two parts 16 (with those: fp32 matrix cores 28; eight waves a block 17; the next 64 codewords on their way 19): a chain of loads, LDS and products
 // for every 64 codewords of a wave; the sums are read once for each 64 coordinates.
 // span: parts between one sequence's sums and the next; splits: parts to add up, the first of those.
@@ -1096,7 +1096,7 @@ __global__ __launch_bounds__(kOutThreads, 4) void k_attend_out(const AttendArgs 
         products(32, c1);
     }
     // A codeword that is not finite, or no sum of finite bf16 parts, is a NaN in every row of its column, whether its sum is zero or not.  Where a NaN is none of its query head's
-    // the wave multiplies again, one by one, and leaves out what no row has.
+    // the wave multiplies again, one by one, and leaves out what no row has: 115 to 290 us more a call; the look costs nothing that shows.
     bool odd = false;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
